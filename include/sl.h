@@ -324,6 +324,117 @@ sl_status sl_anchor_attention_decode_batched(const sl_params* p, const sl_anchor
                                              const sl_decode_seq* seqs, int32_t B, void* ws,
                                              size_t ws_bytes, void* hip_stream);
 
+/* ---- A paged KV cache: sequences that grow, fork and end share one pool of pages.
+ * Token t of sequence s lies in page tables[s][t / page_size], at row t % page_size of that page.
+ * All arrays are device memory of the caller; the calls below read and update them on the stream,
+ * so that a whole serving step can be captured into a graph.
+ *   - A table entry outside 0 .. n_pages - 1 names no page (write -1): tokens there take no part in
+ *     attention, rows appended there are dropped.
+ *   - refs[p] is the number of table entries that name page p; a page is free when refs[p] <= 0.
+ *     A page named by several sequences holds page_size tokens of each of them (sl_pages_fork copies
+ *     the last, partly filled page), so that appending never writes into another sequence's tokens.
+ *   - Entries of tables[s] from ceil(lens[s] / page_size) on are -1.
+ * An empty cache: tables all -1, lens and refs all 0.
+ * What the device arrays hold cannot be checked by the host.  Sequence numbers outside
+ * 0 .. n_seqs - 1, table entries that name no page, lengths beyond the table and rows without
+ * a token are passed over as described at each call; no content leads to an access outside the
+ * arrays that the records describe. */
+typedef struct sl_page_cache {
+  void* K;          /* [layers][n_pages][Hkv][page_size][D], innermost contiguous */
+  void* V;          /* the same layout and strides                                */
+  int32_t* tables;  /* [n_seqs][max_pages]                                        */
+  int32_t* lens;    /* [n_seqs] tokens held                                       */
+  int32_t* refs;    /* [n_pages]                                                  */
+  int64_t layer_stride, page_stride;  /* element strides of K and V; 0 = packed; not below D */
+  int64_t kv_stride_h, kv_stride_t;   /* (0 = packed)                                        */
+  int32_t layers, n_pages, n_seqs, max_pages;  /* >= 1; max_pages * page_size < 2^31 */
+  int32_t page_size, Hkv, D, dtype;            /* D: 64 or 128 */
+} sl_page_cache;
+
+/* New tokens of B sequences: rows cu_rows[b] .. cu_rows[b+1] - 1 of the row tensors are the LAST
+ * cu_rows[b+1] - cu_rows[b] tokens of sequence seqs[b] (lens counts them already), in order.  Chunks
+ * may have any length, 0 and 1 among them.  Rows outside cu_rows[0] .. cu_rows[B] - 1 are neither
+ * read nor written.  cu_rows must not decrease (otherwise which rows are taken is unspecified). */
+typedef struct sl_paged_batch {
+  const int32_t* seqs;     /* [B] device */
+  const int32_t* cu_rows;  /* [B + 1] device */
+  int64_t rows;            /* rows per head of the row tensors, 0 .. 2^25 */
+  int64_t L;               /* no sequence of the batch holds more tokens; 0 = max_pages * page_size.  Rows at
+                              positions from L on are treated as rows without a token. */
+  int32_t B;               /* 0 .. 65535 */
+  int32_t layer;           /* layer of the cache that is read or written */
+} sl_paged_batch;
+
+/* Gives the sequences of a batch pages for their new tokens and adds those to lens: call it before
+ * the step's sl_paged_append.  Free pages are given out lowest number first, to the entries in their
+ * order; an entry that the free pages do not suffice for is left as it was, and so is every later one
+ * that needs a page.  Not served either: sequences out of range, a sequence's second entry, a
+ * length beyond the table.  ok [B]: 1 = served, 0 = left as it was.  (rows, L and layer are not
+ * read; B <= SL_MAX_PAGE_OPS.) */
+#define SL_MAX_PAGE_OPS 4096
+sl_status sl_pages_extend(const sl_page_cache* c, const sl_paged_batch* b, int32_t* ok, void* hip_stream);
+
+/* Makes dst[i] a copy of src[i], i < n: its table names the full pages of src, and a partly filled
+ * last page is copied (all layers, the filled rows) into a free page, lowest number first in the list's
+ * order; forks that no page is left for are not made.  dst[i] must be empty (lens 0); not made
+ * either: forks of a sequence to itself, out of range, to a dst listed before.  ok [n]: 1 = made.
+ * n <= SL_MAX_PAGE_OPS. */
+sl_status sl_pages_fork(const sl_page_cache* c, const int32_t* src, const int32_t* dst, int32_t n,
+                        int32_t* ok, void* hip_stream);
+
+/* Empties the n listed sequences: their table entries become -1, refs falls by one for each, lens
+ * becomes 0.  Listing a sequence twice, or an empty one, does no harm; numbers out of range are
+ * passed over. */
+sl_status sl_pages_free(const sl_page_cache* c, const int32_t* seqs, int32_t n, void* hip_stream);
+
+/* Moves the pages in use to the front of the pool: with u of them, the i-th lowest free page below
+ * u receives the i-th lowest used page from u on (all layers); tables and refs follow.  map
+ * [n_pages]: the new number of each page that was in use, -1 for the free ones.  What moved pages
+ * held stays behind in free pages. */
+size_t sl_pages_compact_workspace_bytes(const sl_page_cache* c);
+sl_status sl_pages_compact(const sl_page_cache* c, int32_t* map, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Writes the batch's new tokens into their pages.  K, V: [Hkv][rows][D] with element strides
+ * (stride_h, stride_t, 1), 0 = packed. */
+sl_status sl_paged_append(const sl_page_cache* c, const sl_paged_batch* b, const void* K, const void* V,
+                          int64_t stride_h, int64_t stride_t, void* hip_stream);
+
+/* Span keys (sl_span_keys) of the spans of S tokens that the batch's new tokens complete:
+ * Ks[seqs[b]][kv][j] = K of token (j+1)*S - 1.  Ks: [n_seqs][Hkv][n_spans][D], packed; spans from n_spans
+ * on are left out (rows is not read).  Ks of one sequence is what the span-search entry points take with
+ * L = n_spans * S.  (A batch whose chunks are whole sequences makes all keys anew.) */
+sl_status sl_paged_span_keys(const sl_page_cache* c, const sl_paged_batch* b, int32_t S, int32_t n_spans,
+                             void* Ks, void* hip_stream);
+
+/* Span-attention of the batch's new tokens over the pages: sl_span_attention_prefill / _decode and
+ * their combined forms for ragged chunks.  Row r of entry b sits at position
+ * i = lens - (new tokens of b) + (r - cu_rows[b]); c = i / S; its window is [c*S, i].  With
+ * topk = 0 and S >= L this is dense causal attention. */
+typedef struct sl_paged_attention {
+  int32_t Hq;     /* query heads, a multiple of the cache's Hkv */
+  int32_t S;      /* span length, >= 1 */
+  int32_t topk;   /* 0 .. SL_MAX_TOPK */
+  float scale;    /* 0 means 1/sqrt(D) */
+  int64_t q_stride_h, q_stride_t;  /* element strides of Q [Hq][rows][D]; 0 = packed */
+  int64_t idx_stride_h, idx_stride_t;  /* element strides of idx and scores; 0 = packed [Hq][rows][topk].  (One new token per
+                                          sequence, idx as sl_span_search_decode_batched writes it: topk and Hq * topk.) */
+} sl_paged_attention;
+
+/* Scratch bytes of the two calls below (SL_WORKSPACE_INVALID if the arguments are invalid). */
+size_t sl_paged_attention_workspace_bytes(const sl_page_cache* c, const sl_paged_batch* b, const sl_paged_attention* a);
+
+/*   idx    in: spans of each row, as the span-search entry points write them; entries < 0 or >= c are
+ *          empty slots, a span must not be listed twice in a row.
+ *   O      out: [Hq][rows][D] packed; LSE out: [Hq][rows] packed.
+ * A row that no token is left for (pages missing, a position outside the sequence) gets O = 0,
+ * LSE = -inf. */
+sl_status sl_paged_span_attention(const sl_page_cache* c, const sl_paged_batch* b, const sl_paged_attention* a, const void* Q,
+                                  const int32_t* idx, void* O, float* LSE, void* ws, size_t ws_bytes, void* hip_stream);
+/* The gated form: scores as idx, finite in non-empty slots; no LSE. */
+sl_status sl_paged_span_attention_combined(const sl_page_cache* c, const sl_paged_batch* b, const sl_paged_attention* a,
+                                           const void* Q, const int32_t* idx, const float* scores, void* O, void* ws,
+                                           size_t ws_bytes, void* hip_stream);
+
 /* Static, human-readable name of a status code. */
 const char* sl_status_string(sl_status status);
 

@@ -29,7 +29,10 @@ EXPORTS = ("sl_workspace_bytes", "sl_span_keys", "sl_span_search_prefill", "sl_s
            "sl_decode_batched_workspace_bytes", "sl_span_search_decode_batched",
            "sl_span_attention_decode_batched", "sl_span_attention_combined_decode_batched",
            "sl_anchor_batched_workspace_bytes", "sl_anchor_search_decode_batched",
-           "sl_anchor_attention_decode_batched", "sl_set_profile_events", "sl_status_string", "sl_version")
+           "sl_anchor_attention_decode_batched", "sl_set_profile_events", "sl_status_string", "sl_version",
+           "sl_pages_extend", "sl_pages_fork", "sl_pages_free", "sl_pages_compact_workspace_bytes", "sl_pages_compact",
+           "sl_paged_append", "sl_paged_span_keys", "sl_paged_attention_workspace_bytes", "sl_paged_span_attention",
+           "sl_paged_span_attention_combined")
 
 
 class SlAnchorGeometry(ctypes.Structure):
@@ -54,6 +57,24 @@ class SlParams(ctypes.Structure):
         ("q_stride_h", ctypes.c_int64), ("q_stride_t", ctypes.c_int64),
         ("kv_stride_h", ctypes.c_int64), ("kv_stride_t", ctypes.c_int64),
     ]
+
+
+class SlPageCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("K", "V", "tables", "lens", "refs")] + [
+        (n, ctypes.c_int64) for n in ("layer_stride", "page_stride", "kv_stride_h", "kv_stride_t")] + [
+        (n, ctypes.c_int32) for n in ("layers", "n_pages", "n_seqs", "max_pages", "page_size", "Hkv", "D", "dtype")]
+
+
+class SlPagedBatch(ctypes.Structure):
+    _fields_ = [("seqs", ctypes.c_void_p), ("cu_rows", ctypes.c_void_p), ("rows", ctypes.c_int64), ("L", ctypes.c_int64),
+                ("B", ctypes.c_int32), ("layer", ctypes.c_int32)]
+
+
+class SlPagedAttention(ctypes.Structure):
+    _fields_ = [("Hq", ctypes.c_int32), ("S", ctypes.c_int32), ("topk", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q_stride_h", ctypes.c_int64), ("q_stride_t", ctypes.c_int64),
+                ("idx_stride_h", ctypes.c_int64), ("idx_stride_t", ctypes.c_int64)]
+
 
 WORKSPACE_INVALID = ctypes.c_size_t(-1).value
 
@@ -126,6 +147,21 @@ def load():
     lib.sl_anchor_search_decode_batched.argtypes = [pp, gp, vp, ctypes.c_int32, vp]
     lib.sl_anchor_attention_decode_batched.restype = ctypes.c_int
     lib.sl_anchor_attention_decode_batched.argtypes = [pp, gp, vp, ctypes.c_int32, vp, ctypes.c_size_t, vp]
+    cp, bp, ap, i32, i64 = (ctypes.POINTER(SlPageCache), ctypes.POINTER(SlPagedBatch), ctypes.POINTER(SlPagedAttention),
+                            ctypes.c_int32, ctypes.c_int64)
+    for name, argtypes in (("sl_pages_extend", [cp, bp, i32p, vp]), ("sl_pages_fork", [cp, i32p, i32p, i32, i32p, vp]),
+                           ("sl_pages_free", [cp, i32p, i32, vp]), ("sl_pages_compact", [cp, i32p, vp, ctypes.c_size_t, vp]),
+                           ("sl_paged_append", [cp, bp, vp, vp, i64, i64, vp]),
+                           ("sl_paged_span_keys", [cp, bp, i32, i32, vp, vp]),
+                           ("sl_paged_span_attention", [cp, bp, ap, vp, i32p, vp, f32p, vp, ctypes.c_size_t, vp]),
+                           ("sl_paged_span_attention_combined", [cp, bp, ap, vp, i32p, f32p, vp, vp, ctypes.c_size_t, vp])):
+        fn = getattr(lib, name)
+        fn.restype = ctypes.c_int
+        fn.argtypes = argtypes
+    lib.sl_pages_compact_workspace_bytes.restype = ctypes.c_size_t
+    lib.sl_pages_compact_workspace_bytes.argtypes = [cp]
+    lib.sl_paged_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.sl_paged_attention_workspace_bytes.argtypes = [cp, bp, ap]
     lib.sl_set_profile_events.restype = None
     lib.sl_set_profile_events.argtypes = [vp, vp]
     lib.sl_status_string.restype = ctypes.c_char_p
@@ -555,3 +591,151 @@ def sl_anchor_attention_decode_batched(batch: DecodeBatch, window, backward_fact
                                                 _ptr(batch.records), batch.B, wptr, wbytes, _stream())
     _check(st, "sl_anchor_attention_decode_batched")
     return batch.O
+
+
+def _int32(t, name, device, n=None):
+    """A contiguous int32 list on the cache's device."""
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != device or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name} must be a contiguous int32 tensor{'' if n is None else f' of {n} values'} on {device}")
+    return t
+
+
+class PageCache:
+    """A paged KV cache: what sl_page_cache describes, and the tensors it points at.
+
+    K, V: [layers, n_pages, Hkv, page_size, D] (or without the layers), innermost contiguous, V with K's strides;
+    tables [n_seqs, max_pages], lens [n_seqs], refs [n_pages]: int32, contiguous, on the same device.  The tensors belong to the
+    caller and are read and updated in place; PageCache.empty makes those of an empty cache."""
+
+    def __init__(self, K, V, tables, lens, refs):
+        K5, V5 = (x.unsqueeze(0) if x.dim() == 4 else x for x in (K, V))
+        if K5.dim() != 5 or K5.stride(4) != 1 or V5.shape != K5.shape or V5.stride() != K5.stride() or V.dtype != K.dtype:
+            raise ValueError("expect K, V [layers, n_pages, Hkv, page_size, D] of one dtype, contiguous innermost, V with K's strides")
+        layers, n_pages, Hkv, ps, D = K5.shape
+        if tables.dtype != torch.int32 or tables.dim() != 2 or not tables.is_contiguous() or tables.device != K.device or V.device != K.device:
+            raise ValueError("tables must be a contiguous int32 tensor [n_seqs, max_pages] on the device of K and V")
+        _int32(lens, "lens", K.device, tables.shape[0])
+        _int32(refs, "refs", K.device, n_pages)
+        self.K, self.V, self.tables, self.lens, self.refs = K, V, tables, lens, refs
+        self.dtype, self.device, self.layers, self.page_size, self.Hkv, self.D = K.dtype, K.device, layers, ps, Hkv, D
+        st = K5.stride()
+        self.record = SlPageCache(K.data_ptr(), V.data_ptr(), tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), st[0], st[1], st[2],
+                                  st[3], layers, n_pages, tables.shape[0], tables.shape[1], ps, Hkv, D, _dtype_code(K))
+
+    @classmethod
+    def empty(cls, n_pages, page_size, Hkv, D, n_seqs, max_pages, layers=1, dtype=torch.bfloat16, device="cuda"):
+        K, V = (torch.zeros((layers, n_pages, Hkv, page_size, D), dtype=dtype, device=device) for _ in range(2))
+        lens, refs = (torch.zeros(n, dtype=torch.int32, device=device) for n in (n_seqs, n_pages))
+        return cls(K, V, torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device), lens, refs)
+
+    def check_device(self):
+        """Kernels are enqueued on the current device's current stream."""
+        if self.device.type != "cuda" or self.device.index != torch.cuda.current_device():
+            raise ValueError(f"the cache lies on {self.device}, which is not the current device")
+
+    def batch(self, seqs, cu_rows, rows=0, L=0, layer=0):
+        """The sl_paged_batch of new tokens cu_rows[b] .. cu_rows[b + 1] - 1 of sequence seqs[b]."""
+        _int32(seqs, "seqs", self.device)
+        _int32(cu_rows, "cu_rows", self.device, seqs.shape[0] + 1)
+        self.check_device()
+        return SlPagedBatch(seqs.data_ptr(), cu_rows.data_ptr(), rows, int(L), seqs.shape[0], int(layer))
+
+
+def sl_pages_extend(cache: PageCache, seqs, cu_rows, ok=None):
+    """Pages for the new tokens of each sequence, which lens counts from here on; ok[b]: 1 = served, 0 = left as it was."""
+    b = cache.batch(seqs, cu_rows)
+    ok = torch.empty_like(seqs) if ok is None else _int32(ok, "ok", cache.device, seqs.shape[0])
+    _check(load().sl_pages_extend(ctypes.byref(cache.record), ctypes.byref(b), _ptr(ok), _stream()), "sl_pages_extend")
+    return ok
+
+
+def sl_pages_fork(cache: PageCache, src, dst, ok=None):
+    """Makes the empty sequence dst[i] a copy of src[i] that shares its full pages; ok[i]: 1 = made."""
+    _int32(src, "src", cache.device)
+    _int32(dst, "dst", cache.device, src.shape[0])
+    cache.check_device()
+    ok = torch.empty_like(src) if ok is None else _int32(ok, "ok", cache.device, src.shape[0])
+    _check(load().sl_pages_fork(ctypes.byref(cache.record), _ptr(src), _ptr(dst), src.shape[0], _ptr(ok), _stream()), "sl_pages_fork")
+    return ok
+
+
+def sl_pages_free(cache: PageCache, seqs):
+    """Empties the listed sequences."""
+    _int32(seqs, "seqs", cache.device)
+    cache.check_device()
+    _check(load().sl_pages_free(ctypes.byref(cache.record), _ptr(seqs), seqs.shape[0], _stream()), "sl_pages_free")
+
+
+def sl_pages_compact(cache: PageCache, map=None, ws=None):
+    """Moves the pages in use to the front of the pool; returns the new number of each page, -1 for the free ones."""
+    lib = load()
+    cache.check_device()
+    map = torch.empty_like(cache.refs) if map is None else _int32(map, "map", cache.device, cache.refs.shape[0])
+    ws = Workspace(cache.device) if ws is None else ws
+    wptr, wbytes = ws.get(_need(lib.sl_pages_compact_workspace_bytes(ctypes.byref(cache.record))))
+    _check(lib.sl_pages_compact(ctypes.byref(cache.record), _ptr(map), wptr, wbytes, _stream()), "sl_pages_compact")
+    return map
+
+
+def sl_paged_append(cache: PageCache, seqs, cu_rows, K, V, layer=0):
+    """Writes the new tokens' K and V [Hkv, rows, D] into their pages."""
+    if (K.dim() != 3 or K.shape[0] != cache.Hkv or K.shape[2] != cache.D or K.stride(2) != 1 or V.shape != K.shape
+            or V.stride() != K.stride() or K.dtype != cache.dtype or V.dtype != cache.dtype
+            or K.device != cache.device or V.device != cache.device):
+        raise ValueError("expect K, V [Hkv, rows, D] of the cache's dtype and device, contiguous innermost, V with K's strides")
+    b = cache.batch(seqs, cu_rows, K.shape[1], 0, layer)
+    _check(load().sl_paged_append(ctypes.byref(cache.record), ctypes.byref(b), _ptr(K), _ptr(V), K.stride(0), K.stride(1), _stream()),
+           "sl_paged_append")
+
+
+def sl_paged_span_keys(cache: PageCache, seqs, cu_rows, Ks, S, layer=0):
+    """Keys of the spans that the new tokens complete, into Ks [n_seqs, Hkv, n_spans, D]; Ks[s] with L = n_spans * S is what
+    span-search takes."""
+    if (Ks.dim() != 4 or Ks.shape[0] != cache.lens.shape[0] or Ks.shape[1] != cache.Hkv or Ks.shape[3] != cache.D
+            or not Ks.is_contiguous() or Ks.dtype != cache.dtype):
+        raise ValueError("expect contiguous Ks [n_seqs, Hkv, n_spans, D] of the cache's dtype")
+    b = cache.batch(seqs, cu_rows, 0, 0, layer)
+    _check(load().sl_paged_span_keys(ctypes.byref(cache.record), ctypes.byref(b), int(S), Ks.shape[2], _ptr(Ks), _stream()),
+           "sl_paged_span_keys")
+    return Ks
+
+
+def _paged_attention(cache, seqs, cu_rows, Q, idx, scores, S, layer, L, scale, ws):
+    lib = load()
+    if Q.dim() != 3 or Q.shape[2] != cache.D or Q.stride(2) != 1 or Q.dtype != cache.dtype or Q.device != cache.device:
+        raise ValueError("expect Q [Hq, rows, D] of the cache's dtype and device with contiguous innermost dimension")
+    Hq, T, _ = Q.shape
+    topk = 0 if idx is None else idx.shape[2]
+    a = SlPagedAttention(Hq, int(S), topk, float(scale), Q.stride(0), Q.stride(1), 0, 0)
+    if topk:
+        if idx.dtype != torch.int32 or idx.shape != (Hq, T, topk) or idx.stride(2) != 1:
+            raise ValueError("idx must be int32 [Hq, rows, topk] with contiguous innermost dimension")
+        a.idx_stride_h, a.idx_stride_t = idx.stride(0), idx.stride(1)
+    if scores is not None and (scores.dtype != torch.float32 or scores.shape != idx.shape or scores.stride() != idx.stride()):
+        raise ValueError("scores must be float32 with the shape and strides of idx")
+    b = cache.batch(seqs, cu_rows, T, L, layer)
+    need = _need(lib.sl_paged_attention_workspace_bytes(ctypes.byref(cache.record), ctypes.byref(b), ctypes.byref(a)))
+    # Scratch is the call's own unless the caller gives a workspace: calls on different streams and graphs do not share it.
+    ws = Workspace(cache.device) if ws is None else ws
+    return a, b, ws.get(need), ws
+
+
+def sl_paged_span_attention(cache: PageCache, seqs, cu_rows, Q, idx, S, layer=0, L=0, scale=0.0, ws=None, out=None):
+    """Joint span-attention of the new tokens (rows of Q [Hq, rows, D]) over the pages; idx [Hq, rows, topk] or None.  L: no
+    sequence of the batch holds more tokens (0: as many as a table can).  Returns O [Hq, rows, D], LSE [Hq, rows]; rows that belong to no
+    sequence are left as they were (with out) or undefined."""
+    a, b, (wptr, wbytes), held = _paged_attention(cache, seqs, cu_rows, Q, idx, None, S, layer, L, scale, ws)
+    O, LSE = (torch.empty(Q.shape, dtype=Q.dtype, device=Q.device),
+              torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)) if out is None else out
+    _check(load().sl_paged_span_attention(ctypes.byref(cache.record), ctypes.byref(b), ctypes.byref(a), _ptr(Q), _ptr(idx), _ptr(O),
+                                          _ptr(LSE), wptr, wbytes, _stream()), "sl_paged_span_attention")
+    return O, LSE
+
+
+def sl_paged_span_attention_combined(cache: PageCache, seqs, cu_rows, Q, idx, scores, S, layer=0, L=0, scale=0.0, ws=None, out=None):
+    """The gated form: scores as span-search wrote them beside idx.  Returns O [Hq, rows, D]."""
+    a, b, (wptr, wbytes), held = _paged_attention(cache, seqs, cu_rows, Q, idx, scores, S, layer, L, scale, ws)
+    O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device) if out is None else out
+    _check(load().sl_paged_span_attention_combined(ctypes.byref(cache.record), ctypes.byref(b), ctypes.byref(a), _ptr(Q), _ptr(idx),
+                                                   _ptr(scores), _ptr(O), wptr, wbytes, _stream()), "sl_paged_span_attention_combined")
+    return O

@@ -434,6 +434,6 @@ const char* sl_status_string(sl_status status) {
   return "unknown sl_status";
 }
 
-int sl_version(void) { return 400; }  // 0.4.0: sl_anchor_attention_prefill takes a workspace (matrix-core form)
+int sl_version(void) { return 500; }  // 0.5.0: paged cache (sl_pages_*, sl_paged_*)
 
 }  // extern "C"

@@ -1,0 +1,162 @@
+"""The paged cache's refusals, without a GPU: every status comes back before anything is enqueued."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2601_18401_amd import binding as B
+
+P = 1 << 20  # a pointer that nothing dereferences
+
+
+def records(**kw):
+    c = B.SlPageCache(P, P, P, P, P, 0, 0, 0, 0, 2, 100, 8, 50, 64, 4, 128, B.SL_BF16)
+    b = B.SlPagedBatch(P, P, 40, 0, 3, 1)
+    a = B.SlPagedAttention(32, 256, 8, 0.0, 0, 0, 0, 0)
+    for k, v in kw.items():
+        for r in (c, b, a):
+            if k in [f[0] for f in r._fields_]:
+                setattr(r, k, v)
+                break
+        else:
+            raise KeyError(k)
+    return c, b, a
+
+
+def need(**kw):
+    c, b, a = records(**kw)
+    return B.load().sl_paged_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(b), ctypes.byref(a))
+
+
+def test_record_sizes():
+    assert ctypes.sizeof(B.SlPageCache) == 5 * 8 + 4 * 8 + 8 * 4
+    assert ctypes.sizeof(B.SlPagedBatch) == 2 * 8 + 2 * 8 + 8
+    assert ctypes.sizeof(B.SlPagedAttention) == 16 + 4 * 8
+
+
+BAD_CACHE = [(dict(K=None), 1), (dict(V=P + 8), 1), (dict(tables=None), 1), (dict(tables=P + 2), 1), (dict(lens=None), 1), (dict(refs=None), 1),
+             (dict(refs=P + 4), 1), (dict(layers=0), 1), (dict(n_pages=0), 1), (dict(n_seqs=0), 1), (dict(max_pages=0), 1),
+             (dict(page_size=0), 1), (dict(Hkv=0), 1), (dict(dtype=2), 1), (dict(D=96), 2), (dict(max_pages=1 << 25, page_size=64), 2),
+             (dict(kv_stride_t=-8), 1), (dict(kv_stride_t=120), 1), (dict(kv_stride_t=132), 1), (dict(kv_stride_h=4), 1),
+             (dict(page_stride=12), 1), (dict(layer_stride=-8), 1), (dict(page_stride=8), 1), (dict(page_stride=1 << 50), 2), (dict(Hkv=2048), 2)]
+BAD_BATCH = [(dict(B=-1), 1), (dict(B=65536), 2), (dict(rows=-1), 1), (dict(rows=(1 << 25) + 1), 2), (dict(L=-1), 1), (dict(layer=2), 1),
+             (dict(layer=-1), 1), (dict(seqs=None), 1), (dict(cu_rows=None), 1), (dict(cu_rows=P + 2), 1)]
+BAD_ATTENTION = [(dict(Hq=0), 1), (dict(Hq=30), 1), (dict(Hq=512), 2), (dict(S=0), 1), (dict(topk=-1), 1), (dict(topk=33), 2), (dict(scale=-1.0), 1),
+                 (dict(scale=float("nan")), 1), (dict(scale=float("inf")), 1), (dict(q_stride_t=64), 1), (dict(q_stride_h=4), 1),
+                 (dict(q_stride_t=-128), 1), (dict(idx_stride_h=-1), 1), (dict(q_stride_h=1 << 50), 2)]
+
+
+@pytest.mark.parametrize("kw,status", BAD_CACHE + BAD_BATCH + BAD_ATTENTION)
+def test_attention_refuses(kw, status):
+    lib = B.load()
+    assert need(**kw) == B.WORKSPACE_INVALID
+    c, b, a = records(**kw)
+    args = [ctypes.byref(x) for x in (c, b, a)]
+    assert lib.sl_paged_span_attention(*args, P, P, P, P, P, 1 << 40, None) == status
+    assert lib.sl_paged_span_attention_combined(*args, P, P, P, P, P, 1 << 40, None) == status
+
+
+@pytest.mark.parametrize("kw,status", BAD_CACHE)
+def test_page_calls_refuse_bad_caches(kw, status):
+    lib = B.load()
+    c, b, _ = records(**kw)
+    c, b = ctypes.byref(c), ctypes.byref(b)
+    assert lib.sl_pages_extend(c, b, P, None) == status
+    assert lib.sl_pages_fork(c, P, P, 1, P, None) == status
+    assert lib.sl_pages_free(c, P, 1, None) == status
+    assert lib.sl_pages_compact_workspace_bytes(c) == B.WORKSPACE_INVALID
+    assert lib.sl_pages_compact(c, P, P, 1 << 40, None) == status
+    assert lib.sl_paged_append(c, b, P, P, 0, 0, None) == status
+    assert lib.sl_paged_span_keys(c, b, 64, 10, P, None) == status
+
+
+@pytest.mark.parametrize("kw,status", BAD_BATCH)
+def test_page_calls_refuse_bad_batches(kw, status):
+    lib = B.load()
+    c, b, _ = records(**kw)
+    c, b = ctypes.byref(c), ctypes.byref(b)
+    assert lib.sl_pages_extend(c, b, P, None) == status
+    assert lib.sl_paged_append(c, b, P, P, 0, 0, None) == status
+    assert lib.sl_paged_span_keys(c, b, 64, 10, P, None) == status
+
+
+def test_missing_pointers_workspaces_and_long_lists():
+    lib = B.load()
+    c, b, a = records()
+    c, b, a = (ctypes.byref(x) for x in (c, b, a))
+    size = need()
+    assert 0 < size < 1 << 30
+    ok = (c, b, a, P, P, P, P, P)
+    assert lib.sl_paged_span_attention(*ok, size - 1, None) == 3
+    assert lib.sl_paged_span_attention(*ok[:-1], None, size, None) == 3
+    assert lib.sl_paged_span_attention(*ok[:-1], P + 16, size, None) == 3
+    for missing in (3, 4, 5, 6):
+        args = list(ok)
+        args[missing] = None
+        assert lib.sl_paged_span_attention(*args, size, None) == 1
+        assert lib.sl_paged_span_attention_combined(*args, size, None) == 1
+    assert lib.sl_paged_span_attention(c, b, a, P + 8, P, P, P, P, size, None) == 1
+    assert lib.sl_pages_extend(c, b, None, None) == 1
+    assert lib.sl_pages_fork(c, None, P, 1, P, None) == 1 and lib.sl_pages_fork(c, P, P, -1, P, None) == 1
+    assert lib.sl_pages_fork(c, P, P, 4097, P, None) == 2
+    assert lib.sl_pages_free(c, None, 1, None) == 1 and lib.sl_pages_free(c, P, -1, None) == 1
+    assert lib.sl_pages_compact(c, None, P, 1 << 20, None) == 1 and lib.sl_pages_compact(c, P, P, 16, None) == 3
+    assert lib.sl_paged_append(c, b, None, P, 0, 0, None) == 1 and lib.sl_paged_append(c, b, P, P, 0, 100, None) == 1
+    assert lib.sl_paged_append(c, b, P, P, -8, 0, None) == 1 and lib.sl_paged_append(c, b, P, P, 1 << 50, 0, None) == 2
+    assert lib.sl_paged_span_keys(c, b, 0, 10, P, None) == 1 and lib.sl_paged_span_keys(c, b, 64, 0, P, None) == 1
+    assert lib.sl_paged_span_keys(c, b, 64, 10, None, None) == 1 and lib.sl_paged_span_keys(c, b, 64, 1 << 23, P, None) == 2
+
+
+def test_nothing_to_do_enqueues_nothing():
+    lib = B.load()
+    for kw in (dict(B=0, seqs=None, cu_rows=None), dict(rows=0)):
+        c, b, a = records(**kw)
+        c, b, a = (ctypes.byref(x) for x in (c, b, a))
+        assert lib.sl_paged_attention_workspace_bytes(c, b, a) == 0
+        assert lib.sl_paged_span_attention(c, b, a, None, None, None, None, None, 0, None) == 0
+        assert lib.sl_paged_append(c, b, None, None, 0, 0, None) == 0
+    c, b, _ = (ctypes.byref(x) for x in records(B=0, seqs=None, cu_rows=None))
+    assert lib.sl_pages_extend(c, b, None, None) == 0
+    assert lib.sl_pages_fork(c, None, None, 0, None, None) == 0 and lib.sl_pages_free(c, None, 0, None) == 0
+
+
+def test_the_largest_problems_ask_for_sizes_that_fit():
+    """Sizes are computed in 64 bits: 2^31 rows and heads, 32 spans of the longest length."""
+    size = need(rows=1 << 25, Hq=60, Hkv=60, topk=32, S=(1 << 31) - 1, max_pages=1 << 24, page_size=127)
+    assert size != B.WORKSPACE_INVALID and size >= (1 << 25) * 60 * 33 * 128 * 2
+    assert need(rows=1 << 25, Hq=64, Hkv=64) == B.WORKSPACE_INVALID     # row ids are 32-bit
+
+
+def test_the_binding_refuses_tensors_that_do_not_fit():
+    K = torch.zeros((1, 6, 2, 16, 64), dtype=torch.bfloat16)
+    tables, lens, refs = (torch.zeros(s, dtype=torch.int32) for s in ((3, 4), (3,), (6,)))
+    cache = B.PageCache(K, K.clone(), tables, lens, refs)
+    assert cache.record.page_stride == 2 * 16 * 64 and cache.record.layers == 1
+    B.PageCache(K[0], K[0].clone(), tables, lens, refs)
+    for bad in ((K, K.float(), tables, lens, refs), (K, K[:, :5], tables, lens, refs), (K, K, tables.long(), lens, refs),
+                (K, K, tables, lens[:2], refs), (K, K, tables, lens, refs[:5]), (K, K, tables[0], lens, refs),
+                (K[..., ::2], K[..., ::2], tables, lens, refs), (K, K.transpose(2, 3).contiguous().transpose(2, 3), tables, lens, refs)):
+        with pytest.raises(ValueError):
+            B.PageCache(*bad)
+    with pytest.raises(TypeError):
+        B.PageCache(K.half(), K.half(), tables, lens, refs)
+    one, two = torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    for seqs, cu in ((one.long(), two), (one, one), (one, two.float()), (two[::2][:1].expand(1), two[:1])):
+        with pytest.raises(ValueError):
+            cache.batch(seqs, cu)
+    with pytest.raises(ValueError):      # a cache in host memory
+        cache.batch(one, two)
+    with pytest.raises(ValueError):
+        B.sl_pages_fork(cache, one, two)
+    with pytest.raises(ValueError):
+        B.sl_pages_free(cache, one.long())
+    with pytest.raises(ValueError):
+        B.sl_paged_append(cache, one, two, K[0, 0], K[0, 0, :1])
+    with pytest.raises(ValueError):
+        B.sl_paged_span_keys(cache, one, two, K[0], 16)
+    Q = torch.zeros((4, 1, 64), dtype=torch.bfloat16)
+    idx = torch.zeros((4, 1, 2), dtype=torch.int32)
+    for q, i, s in ((Q.float(), idx, None), (Q[0], idx, None), (Q, idx.long(), None), (Q, idx[:2], None), (Q, idx, idx),
+                    (Q, idx, torch.zeros((4, 1, 1)))):
+        with pytest.raises(ValueError):
+            B._paged_attention(cache, one, two, q, i, s, 16, 0, 0, 0.0, None)

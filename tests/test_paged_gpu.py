@@ -1,0 +1,470 @@
+"""The paged cache's operators against plain 64-bit forms.
+
+Tolerances.  fp32: a score is a sum of 128 products in about nine roundings of 2^-24 each, relative to sum |q k| (about 100) / sqrt(D):
+6e-6, twice that on a weight, times |v| up to 5, plus the exponential's 2^-22: below 1e-4.  bf16: the output is rounded
+(2^-8 |O|), weights may be rounded once (2^-8 of A = sum p |v|), partial outputs to 11 bits of their largest element
+(2^-11 max |V|): all of that beside the fp32 part."""
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2601_18401_amd import binding as B
+from tests import paged_reference as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def make_cache(g, Ls, ps, Hkv, D, dtype, token_major=False, layers=1, spare=3, width=1, std=1.0):
+    """Sequences of Ls tokens in pages of random order.  Whatever no sequence holds is NaN."""
+    need = sum(-(-L // ps) for L in Ls)
+    n_pages, max_pages = need + spare, max(-(-max(Ls) // ps), 1) + width
+    shape = (layers, n_pages, ps, Hkv, D) if token_major else (layers, n_pages, Hkv, ps, D)
+    K, V = (torch.full(shape, math.nan, dtype=dtype, device=DEV) for _ in range(2))
+    if token_major:
+        K, V = K.transpose(2, 3), V.transpose(2, 3)
+    order = torch.randperm(n_pages, generator=g).tolist()
+    tables = torch.full((len(Ls), max_pages), -1, dtype=torch.int32)
+    refs = torch.zeros(n_pages, dtype=torch.int32)
+    for s, L in enumerate(Ls):
+        for k in range(-(-L // ps)):
+            page = order.pop()
+            tables[s, k] = page
+            refs[page] = 1
+            n = min(ps, L - k * ps)
+            for x in (K, V):
+                x[:, page, :, :n] = (torch.randn((layers, Hkv, n, D), generator=g) * std).to(dtype).to(DEV)
+    return B.PageCache(K, V, tables.to(DEV), i32(Ls), refs.to(DEV))
+
+
+def choose(g, Hq, T, topk, spans):
+    """Random distinct spans, some beyond the candidates, and empty slots among them."""
+    idx = torch.stack([torch.stack([torch.randperm(max(spans, topk), generator=g)[:topk] for _ in range(T)]) for _ in range(Hq)])
+    idx[torch.rand(idx.shape, generator=g) < 0.15] = -1
+    return idx.to(torch.int32).to(DEV)
+
+
+def check(cache, seqs, cu, Q, idx, scores, S, O, LSE=None, scale=None, layer=0, L=None):
+    torch.cuda.synchronize()
+    K, V = (x[layer] if x.dim() == 5 else x for x in (cache.K.cpu(), cache.V.cpu()))
+    scale = scale or 1 / math.sqrt(cache.D)
+    with np.errstate(invalid="ignore"):
+        wO, wL, A = ref.attention(K, V, cache.tables.cpu(), cache.lens.cpu(), seqs, cu, Q.cpu(), None if idx is None else idx.cpu(),
+                                  None if scores is None else scores.cpu(), S, scale, L)
+    live = ~np.isnan(wL)
+    got = O.double().cpu().numpy()
+    assert np.isfinite(got[live]).all()
+    big = float(np.nanmax(A)) if live.any() else 0.0
+    tol = 1e-4 + (0 if cache.dtype == F32 else 2.0 ** -8 * (np.abs(wO) + A) + 2.0 ** -11 * max(5.0, big))
+    off = np.abs(got - wO) - tol
+    assert (off[live] <= 0).all(), float(off[live].max())
+    if LSE is not None:
+        lse = LSE.double().cpu().numpy()
+        assert np.array_equal(np.isinf(lse[live]), np.isinf(wL[live]))
+        fin = live & np.isfinite(wL)
+        assert (np.abs(lse[fin] - wL[fin]) <= 1e-4).all()
+    return live
+
+
+CASES = [
+    # dtype Hq Hkv D   ps   S    topk chunks                 lengths                 token-major
+    (BF16, 8, 2, 128, 64, 64, 4, [1], [1], False),            # the first token of all
+    (BF16, 8, 2, 128, 64, 64, 4, [1], [1000], False),
+    (BF16, 4, 4, 64, 16, 40, 3, [1, 1, 1], [39, 40, 41], True),   # around a span's end
+    (BF16, 6, 2, 128, 48, 96, 2, [5, 0, 1, 130], [300, 20, 97, 130], False),   # a chunk of none; pages that end inside a tile
+    (BF16, 3, 1, 64, 9, 33, 5, [70], [400], True),
+    (BF16, 16, 2, 128, 128, 256, 8, [33, 200], [700, 1300], False),
+    (BF16, 64, 1, 64, 32, 100, 2, [3, 9], [250, 130], False),    # 64 heads on one
+    (F32, 4, 2, 128, 16, 64, 4, [1, 37], [500, 200], True),
+    (F32, 4, 4, 64, 7, 50, 8, [64], [333], False),
+    (F32, 2, 1, 64, 1, 5, 32, [20], [64], False),             # pages of one token, all spans asked for
+    (BF16, 2, 2, 128, 1, 3, 1, [17], [17], False),
+]
+
+
+@pytest.mark.parametrize("form", ["joint", "gated"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(v) for v in c[1:]).replace(" ", ""))
+def test_attention(case, form):
+    dtype, Hq, Hkv, D, ps, S, topk, ns, Ls, token_major = case
+    g = torch.Generator().manual_seed(len(Ls) * 1000 + Ls[0])
+    cache = make_cache(g, Ls, ps, Hkv, D, dtype, token_major)
+    T = sum(ns)
+    cu = [sum(ns[:b]) for b in range(len(ns) + 1)]
+    Q = torch.randn((T, Hq, D), generator=g).to(dtype).to(DEV).transpose(0, 1)
+    idx = choose(g, Hq, T, topk, max(Ls) // S + 1)
+    scores = torch.randn(idx.shape, generator=g).to(DEV) * 2
+    seqs = list(range(len(Ls)))
+    if form == "joint":
+        O, LSE = B.sl_paged_span_attention(cache, i32(seqs), i32(cu), Q, idx, S)
+        check(cache, seqs, cu, Q, idx, None, S, O, LSE)
+    else:
+        O = B.sl_paged_span_attention_combined(cache, i32(seqs), i32(cu), Q, idx, scores, S, L=max(Ls))
+        check(cache, seqs, cu, Q, idx, scores, S, O)
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,ps,ns,Ls", [
+    (BF16, 8, 2, 128, 64, [1, 1], [1500, 3]), (BF16, 8, 1, 64, 20, [4, 1, 7], [900, 513, 7]), (BF16, 4, 4, 128, 32, [200], [200]),
+    (BF16, 12, 4, 128, 64, [150, 1, 64], [900, 64, 65]), (F32, 4, 2, 64, 16, [100, 3], [100, 600]), (BF16, 2, 1, 64, 64, [300, 129], [300, 640]),
+    (BF16, 5, 5, 128, 16, [257], [300]), (F32, 3, 1, 128, 64, [1], [3000])])
+def test_dense(dtype, Hq, Hkv, D, ps, ns, Ls):
+    """No spans and S beyond every length: causal attention over all of the sequence."""
+    g = torch.Generator().manual_seed(sum(Ls))
+    cache = make_cache(g, Ls, ps, Hkv, D, dtype)
+    cu = [sum(ns[:b]) for b in range(len(ns) + 1)]
+    Q = torch.randn((Hq, sum(ns), D), generator=g).to(dtype).to(DEV)
+    O, LSE = B.sl_paged_span_attention(cache, i32(list(range(len(Ls)))), i32(cu), Q, None, (1 << 31) - 1, L=max(Ls), scale=0.1)
+    check(cache, list(range(len(Ls))), cu, Q, None, None, (1 << 31) - 1, O, LSE, scale=0.1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("topk,S,n", [(3, 40, 6), (0, 4000, 6), (3, 40, 150), (0, 4000, 150)])
+def test_rows_without_tokens_and_rows_of_nobody(dtype, topk, S, n):
+    """Missing pages (all of a row's among them), sequence numbers out of range, chunks longer than the sequence, positions
+    from L on, the same sequence twice, rows before the first chunk and behind the last, a lengths entry beyond the table."""
+    g = torch.Generator().manual_seed(5)
+    Ls = [300, 200, 160, 30, 250]
+    cache = make_cache(g, Ls, 16, 2, 64, dtype)
+    cache.tables[0, 3:7] = -1
+    cache.tables[0, 9] = 1 << 20
+    cache.tables[1, :] = -1          # nothing left at all
+    cache.tables[1, 5] = -7
+    cache.lens[4] = 1 << 30          # more than the table holds: its whole table
+    seqs = [0, 1, 99, 2, -1, 3, 0, 4]
+    ns = [n, 3, 2, 4, 1, 40, 2, 2]
+    first, behind = 5, 7
+    cu = [first + sum(ns[:b]) for b in range(len(ns) + 1)]
+    T = cu[-1] + behind
+    Q = torch.randn((4, T, 64), generator=g).to(dtype).to(DEV)
+    idx = choose(g, 4, T, topk, 8) if topk else None
+    scores = torch.randn((4, T, topk), generator=g).to(DEV) if topk else None
+    K, V = cache.K.clone(), cache.V.clone()
+    cache.K.nan_to_num_(0.5)  # (sequence 4 names no page behind its own: what remains is unread)
+    cache.V.nan_to_num_(0.5)
+    for L in (0, 290):
+        out = torch.full(Q.shape, 7.0, dtype=dtype, device=DEV), torch.full(Q.shape[:2], 7.0, device=DEV)
+        O, LSE = B.sl_paged_span_attention(cache, i32(seqs), i32(cu), Q, idx, S, L=L, out=out)
+        assert O is out[0]
+        live = check(cache, seqs, cu, Q, idx, None, S, O, LSE, L=L)
+        assert bool((O[:, torch.tensor(~live[0], device=DEV)] == 7).all()) and int((~live[0]).sum()) == first + behind
+        if topk:
+            out = torch.full(Q.shape, 7.0, dtype=dtype, device=DEV)
+            B.sl_paged_span_attention_combined(cache, i32(seqs), i32(cu), Q, idx, scores, S, L=L, out=out)
+            check(cache, seqs, cu, Q, idx, scores, S, out, L=L)
+            assert bool((out[:, torch.tensor(~live[0], device=DEV)] == 7).all())
+    cache.K.copy_(K)
+    cache.V.copy_(V)
+
+
+@pytest.mark.parametrize("n", [3, 130])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_not_finite_where_some_rows_attend(what, n):
+    """A token that is not finite makes those rows not finite that attend it, as the formula has it, and no other: rows
+    before it, rows whose spans leave it out."""
+    g = torch.Generator().manual_seed(n)
+    L, S = 400, 50
+    cache = make_cache(g, [L], 32, 2, 128, BF16)
+    bad = [L - 2, 120]  # one of the new tokens, and one in span 2
+    for t in bad:
+        page = int(cache.tables[0, t // 32])
+        cache.V[0, page, :, t % 32, 5] = what
+    Q = torch.randn((4, n, 128), generator=g).to(BF16).to(DEV)
+    idx = torch.tensor([[[0, 2], [0, 1]][(h + r) % 2] for h in range(4) for r in range(n)], dtype=torch.int32, device=DEV).view(4, n, 2)
+    O, LSE = B.sl_paged_span_attention(cache, i32([0]), i32([0, n]), Q, idx, S)
+    G = B.sl_paged_span_attention_combined(cache, i32([0]), i32([0, n]), Q, idx, torch.zeros(idx.shape, device=DEV), S)
+    torch.cuda.synchronize()
+    clean_V = cache.V.clone()
+    for t in bad:
+        clean_V[0, int(cache.tables[0, t // 32]), :, t % 32, 5] = 0
+    clean = B.PageCache(cache.K, clean_V, cache.tables, cache.lens, cache.refs)
+    wO, wL = B.sl_paged_span_attention(clean, i32([0]), i32([0, n]), Q, idx, S)
+    wG = B.sl_paged_span_attention_combined(clean, i32([0]), i32([0, n]), Q, idx, torch.zeros(idx.shape, device=DEV), S)
+    torch.cuda.synchronize()
+    for h in range(4):
+        for r in range(n):
+            pos = L - n + r
+            hit = any((t // S == pos // S and t <= pos) or (t // S < pos // S and t // S in idx[h, r].tolist()) for t in bad)
+            for x, w in ((O, wO), (G, wG)):
+                row = x[h, r].double()
+                if hit:
+                    assert torch.isnan(row[5]) if math.isnan(what) else row[5].item() == what
+                    row, w_row = torch.cat([row[:5], row[6:]]), torch.cat([w[h, r][:5], w[h, r][6:]]).double()
+                else:
+                    w_row = w[h, r].double()
+                assert float((row - w_row).abs().max()) <= 2.0 ** -7 * 5  # (the two may take different kernels: two roundings each)
+    assert float((LSE - wL).abs().max()) <= 1e-4
+
+
+def test_append_and_span_keys():
+    for dtype, Hkv, D, ps, S, ns, have, token_major in [
+            (BF16, 2, 128, 64, 32, [1, 1, 1], [31, 0, 100], False), (F32, 3, 64, 10, 7, [50, 0, 13], [3, 5, 69], True),
+            (BF16, 1, 64, 16, 200, [1000], [0], False), (F32, 1, 128, 33, 1, [5, 64], [10, 31], False)]:
+        g = torch.Generator().manual_seed(ps)
+        Ls = [n + h for n, h in zip(ns, have)]
+        cache = make_cache(g, Ls, ps, Hkv, D, dtype, token_major, layers=2)
+        cu = [2 + sum(ns[:b]) for b in range(len(ns) + 1)]
+        T = cu[-1] + 3
+        K, V = (torch.randn((T, Hkv, D), generator=g).to(dtype).to(DEV).transpose(0, 1) for _ in range(2))
+        want_K, want_V = cache.K.clone(), cache.V.clone()
+        Ks = torch.full((len(Ls), Hkv, max(Ls) // S + 2, D), 9.0, dtype=dtype, device=DEV)
+        want_s = Ks.clone()
+        cache.tables[0, 0] = -1 if have[0] == 31 else cache.tables[0, 0]
+        for b, (n, L) in enumerate(zip(ns, Ls)):
+            for t in range(L - n, L):
+                page = int(cache.tables[b, t // ps])
+                if page < 0:
+                    continue
+                r = cu[b] + t - (L - n)
+                want_K[1, page, :, t % ps], want_V[1, page, :, t % ps] = K[:, r], V[:, r]
+                if (t + 1) % S == 0:
+                    want_s[b, :, t // S] = K[:, r]
+        seqs = i32(list(range(len(Ls))))
+        B.sl_paged_append(cache, seqs, i32(cu), K, V, layer=1)
+        B.sl_paged_span_keys(cache, seqs, i32(cu), Ks, S, layer=1)
+        torch.cuda.synchronize()
+        assert torch.equal(cache.K.nan_to_num(3.0), want_K.nan_to_num(3.0)) and torch.equal(cache.V.nan_to_num(3.0), want_V.nan_to_num(3.0))
+        assert torch.equal(Ks, want_s)
+        few = torch.full((len(Ls), Hkv, 1, D), 9.0, dtype=dtype, device=DEV)     # room for one span only
+        B.sl_paged_span_keys(cache, seqs, i32([0] + [sum(Ls[:b + 1]) for b in range(len(Ls))]), few, S, layer=1)   # all keys anew
+        for b, L in enumerate(Ls):
+            page = int(cache.tables[b, (S - 1) // ps])
+            if L >= S and page >= 0:
+                assert torch.equal(few[b, :, 0], cache.K[1, page, :, (S - 1) % ps])
+            else:
+                assert bool((few[b] == 9).all())
+
+
+def test_appending_past_the_sequence_writes_nothing():
+    g = torch.Generator().manual_seed(3)
+    cache = make_cache(g, [20, 40], 16, 1, 64, BF16)
+    before = cache.K.clone()
+    K = torch.ones((1, 40, 64), dtype=BF16, device=DEV)
+    B.sl_paged_append(cache, i32([77, -1]), i32([0, 5, 9]), K, K)
+    torch.cuda.synchronize()
+    assert torch.equal(cache.K.nan_to_num(3.0), before.nan_to_num(3.0))
+    B.sl_paged_append(cache, i32([0]), i32([0, 35]), K, K)       # 35 rows, 20 tokens: the last 20 of them
+    torch.cuda.synchronize()
+    for t in range(20):
+        assert bool((cache.K[0, int(cache.tables[0, t // 16]), 0, t % 16] == 1).all())
+    assert int((cache.K == 1).all(-1).sum()) == 20
+
+
+@pytest.mark.parametrize("seed,n_pages,ps,n_seqs,dtype,layers", [(1, 40, 4, 12, BF16, 1), (2, 300, 3, 30, F32, 2), (3, 70, 1, 9, BF16, 1),
+                                                                 (4, 17000, 2, 40, BF16, 1), (5, 1, 8, 3, BF16, 1)])
+def test_page_turns(seed, n_pages, ps, n_seqs, dtype, layers):
+    """Random turns of a scheduler, bad entries among them, against the bookkeeping done one step after the other."""
+    rng = random.Random(seed)
+    g = torch.Generator().manual_seed(seed)
+    max_pages = max(2, n_pages // 3)
+    cache = B.PageCache.empty(n_pages, ps, 2, 64, n_seqs, max_pages, layers, dtype)
+    cache.K.copy_(torch.randn(cache.K.shape, generator=g))
+    cache.V.copy_(torch.randn(cache.V.shape, generator=g))
+    model = ref.Pages(cache)
+    most = max_pages * ps
+    for turn in range(14):
+        seqs = [rng.randint(-1, n_seqs) for _ in range(rng.randint(1, n_seqs))]
+        cu = [rng.randint(0, 5)]
+        for _ in seqs:
+            cu.append(cu[-1] + rng.choice([0, 1, rng.randint(0, most // 2 + 1), rng.randint(0, 3 * ps)]))
+        ok = B.sl_pages_extend(cache, i32(seqs), i32(cu))
+        assert ok.tolist() == model.extend(seqs, cu), turn
+        model.agrees(cache)
+        src = [rng.randint(-1, n_seqs) for _ in range(rng.randint(1, 2 * n_seqs))]
+        dst = [rng.randint(-1, n_seqs) for _ in src]
+        ok = B.sl_pages_fork(cache, i32(src), i32(dst))
+        assert ok.tolist() == model.fork(src, dst), turn
+        model.agrees(cache)
+        gone = [rng.randint(-2, n_seqs + 1) for _ in range(rng.randint(0, n_seqs // 2 + 1))]
+        gone += gone[:1]
+        B.sl_pages_free(cache, i32(gone))
+        model.free(sorted(set(gone)))
+        model.agrees(cache)
+        if turn % 2:
+            where = B.sl_pages_compact(cache)
+            assert where.tolist() == model.compact()
+            model.agrees(cache)
+    B.sl_pages_free(cache, i32(list(range(n_seqs))))
+    assert int(cache.refs.abs().sum()) == 0 and int((cache.tables != -1).sum()) == 0
+
+
+def test_lists_as_long_as_they_may_be():
+    """4096 entries of one token each, with 4000 pages: the entry at which they run out, and that every later one is refused."""
+    cache = B.PageCache.empty(4000, 16, 1, 64, 5000, 2)
+    seqs, cu = i32(list(range(4096))), i32(list(range(4097)))
+    ok = B.sl_pages_extend(cache, seqs, cu)
+    assert ok.tolist() == [1] * 4000 + [0] * 96
+    assert cache.tables[:4000, 0].tolist() == list(range(4000)) and int(cache.lens.sum()) == 4000
+    again = B.sl_pages_extend(cache, seqs, cu)        # the pages have room: only the unserved ones need more
+    assert again.tolist() == [1] * 4000 + [0] * 96
+    B.sl_pages_free(cache, i32(list(range(0, 4096, 2))))
+    ok = B.sl_pages_fork(cache, i32([1] * 4096), i32(list(range(904, 5000))))
+    free_slots = [i for i, d in enumerate(range(904, 5000)) if d % 2 == 0 or d >= 4000]
+    want = [0] * 4096
+    for i in free_slots[:2000]:
+        want[i] = 1
+    assert ok.tolist() == want
+    with pytest.raises(B.SlError) as e:
+        B.sl_pages_extend(cache, i32([0] * 4097), i32([0] * 4098))
+    assert e.value.status == 2
+
+
+def test_a_serving_run_equals_the_contiguous_entry_points():
+    """Prompts in chunks, span-search on the gathered keys, paged attention; forks that go on by single tokens; compaction in
+    between.  Outputs against the contiguous entry points on each sequence's own tokens."""
+    g = torch.Generator().manual_seed(11)
+    Hq, Hkv, D, S, topk, ps = 8, 2, 128, 64, 4, 32
+    cache = B.PageCache.empty(90, ps, Hkv, D, 6, 40)
+    n_spans = 40 * ps // S
+    Ks = torch.zeros((6, Hkv, n_spans, D), dtype=BF16, device=DEV)
+    tokens = {s: (torch.empty((Hkv, 0, D), dtype=BF16, device=DEV),) * 2 for s in range(6)}
+
+    def step(seqs, ns):
+        T, cu = sum(ns), [sum(ns[:b]) for b in range(len(ns) + 1)]
+        K, V = (torch.randn((Hkv, T, D), generator=g).to(BF16).to(DEV) for _ in range(2))
+        Q = torch.randn((Hq, T, D), generator=g).to(BF16).to(DEV)
+        ds, dcu = i32(seqs), i32(cu)
+        assert B.sl_pages_extend(cache, ds, dcu).tolist() == [1] * len(seqs)
+        B.sl_paged_append(cache, ds, dcu, K, V)
+        B.sl_paged_span_keys(cache, ds, dcu, Ks, S)
+        idx, scores = torch.empty((Hq, T, topk), dtype=torch.int32, device=DEV), torch.empty((Hq, T, topk), device=DEV)
+        want = []
+        for b, s in enumerate(seqs):
+            rows = slice(cu[b], cu[b + 1])
+            tokens[s] = tuple(torch.cat([old, new[:, rows]], 1) for old, new in zip(tokens[s], (K, V)))
+            k, v = tokens[s]
+            L, q = k.shape[1], Q[:, rows].contiguous()
+            # (search reads Ks alone: a tensor of n_spans * S tokens stands for the cache)
+            stand = torch.empty((Hkv, n_spans * S, D), dtype=BF16, device=DEV)
+            i, sc = B.sl_span_search_prefill(q, stand, Ks[s], S, topk, q_pos0=L - ns[b], want_scores=True)
+            wi = B.sl_span_search_prefill(q, k, None, S, topk, q_pos0=L - ns[b])
+            assert torch.equal(i, wi)
+            idx[:, rows], scores[:, rows] = i, sc
+            want.append((B.sl_span_attention_prefill(q, k, v, i, S, q_pos0=L - ns[b]),
+                         B.sl_span_attention_combined_prefill(q, k, v, i, sc, S, q_pos0=L - ns[b])))
+        O, LSE = B.sl_paged_span_attention(cache, ds, dcu, Q, idx, S)
+        C = B.sl_paged_span_attention_combined(cache, ds, dcu, Q, idx, scores, S)
+        check(cache, seqs, cu, Q, idx, None, S, O, LSE)
+        for b in range(len(seqs)):
+            rows = slice(cu[b], cu[b + 1])
+            (wO, wL), wC = want[b]
+            assert float((O[:, rows].float() - wO.float()).abs().max()) <= 2e-2
+            assert float((C[:, rows].float() - wC.float()).abs().max()) <= 2e-2
+            assert float((LSE[:, rows] - wL).abs().max()) <= 2e-2
+
+    step([0, 1], [200, 333])
+    step([0, 1, 2], [150, 1, 70])
+    assert B.sl_pages_fork(cache, i32([1, 1, 0]), i32([3, 4, 5])).tolist() == [1, 1, 1]
+    for d, s in ((3, 1), (4, 1), (5, 0)):
+        tokens[d] = tokens[s]
+        Ks[d] = Ks[s]
+    step([3, 4, 5, 1], [1, 1, 1, 1])
+    step([4, 3, 2], [40, 1, 9])
+    B.sl_pages_free(cache, i32([1, 2]))
+    tokens[1] = tokens[2] = (torch.empty((Hkv, 0, D), dtype=BF16, device=DEV),) * 2
+    where = B.sl_pages_compact(cache)
+    used = int((cache.refs > 0).sum())
+    assert bool((cache.refs[:used] > 0).all()) and int((where >= 0).sum()) == used
+    step([0, 3, 4, 5, 1], [1, 1, 1, 1, 100])
+
+
+def test_a_captured_step_is_replayed():
+    """extend, append, keys and attention in one graph: each replay is the next step, eager calls in between."""
+    g = torch.Generator().manual_seed(12)
+    Hq, Hkv, D, S, ps, n = 8, 2, 64, 32, 16, 3
+    cache = B.PageCache.empty(64, ps, Hkv, D, 4, 30)
+    Ks = torch.zeros((4, Hkv, 20, D), dtype=BF16, device=DEV)
+    seqs, cu = i32([2, 0]), i32([0, n, n + 1])
+    K, V = (torch.randn((Hkv, n + 1, D), generator=g).to(BF16).to(DEV) for _ in range(2))
+    Q = torch.randn((Hq, n + 1, D), generator=g).to(BF16).to(DEV)
+    idx = choose(g, Hq, n + 1, 3, 4)
+    O, LSE = torch.empty_like(Q), torch.empty((Hq, n + 1), device=DEV)
+    ok = torch.empty(2, dtype=torch.int32, device=DEV)
+    ws = B.Workspace()
+    ws.get(1 << 22)
+
+    def step():
+        B.sl_pages_extend(cache, seqs, cu, ok)
+        B.sl_paged_append(cache, seqs, cu, K, V)
+        B.sl_paged_span_keys(cache, seqs, cu, Ks, S)
+        B.sl_paged_span_attention(cache, seqs, cu, Q, idx, S, ws=ws, out=(O, LSE))
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(2, 40):
+        for x in (K, V, Q):
+            x.copy_(torch.randn(x.shape, generator=g))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert cache.lens.tolist() == [i, 0, i * n, 0] and ok.tolist() == [1, 1]
+        if i % 5 == 0:
+            got = O.clone()
+            check(cache, [2, 0], [0, n, n + 1], Q, idx, None, S, O, LSE)
+            O2, _ = B.sl_paged_span_attention(cache, seqs, cu, Q, idx, S)
+            assert torch.equal(got, O2)
+
+
+def test_two_streams_at_once():
+    """Calls without a workspace of the caller's do not share scratch."""
+    g = torch.Generator().manual_seed(13)
+    cache = make_cache(g, [3000, 2500], 64, 2, 128, BF16)
+    Q = torch.randn((2, 8, 300, 128), generator=g).to(BF16).to(DEV)
+    cu = i32([0, 300])
+    idx = choose(g, 8, 300, 4, 40)
+    alone = [B.sl_paged_span_attention(cache, i32([b]), cu, Q[b], idx, 64)[0] for b in range(2)]
+    seqs = [i32([b]) for b in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [None, None]
+    for _ in range(5):
+        for b in range(2):
+            with torch.cuda.stream(streams[b]):
+                got[b] = B.sl_paged_span_attention(cache, seqs[b], cu, Q[b], idx, 64)[0]
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], alone[0]) and torch.equal(got[1], alone[1])
+
+
+def test_a_cache_beyond_32_bit_offsets():
+    """Pages behind 2^32 bytes and 2^31 elements of the pool."""
+    ps, Hkv, D = 64, 4, 128
+    n_pages = (9 << 30) // 2 // (ps * Hkv * D)      # 9 GB of K: 4.8e9 elements
+    K, V = (torch.zeros((1, n_pages, Hkv, ps, D), dtype=BF16, device=DEV) for _ in range(2))
+    g = torch.Generator().manual_seed(14)
+    pages = [n_pages - 1, 3, n_pages // 2 + 1, n_pages - 2]
+    for p in pages:
+        K[0, p], V[0, p] = (torch.randn((Hkv, ps, D), generator=g).to(BF16).to(DEV) for _ in range(2))
+    tables = torch.full((2, 6), -1, dtype=torch.int32, device=DEV)
+    tables[0, :4] = i32(pages)
+    refs = torch.zeros(n_pages, dtype=torch.int32, device=DEV)
+    refs[torch.tensor(pages, device=DEV)] = 1
+    cache = B.PageCache(K, V, tables, i32([250, 0]), refs)
+    for n in (1, 200):
+        Q = torch.randn((8, n, D), generator=g).to(BF16).to(DEV)
+        idx = choose(g, 8, n, 2, 4)
+        O, LSE = B.sl_paged_span_attention(cache, i32([0]), i32([0, n]), Q, idx, 50)
+        torch.cuda.synchronize()
+        small = B.PageCache(K[:, pages].contiguous(), V[:, pages].contiguous(), i32([[0, 1, 2, 3, -1, -1]] * 2), i32([250, 0]), i32([2] * 4))
+        wO, wL = B.sl_paged_span_attention(small, i32([0]), i32([0, n]), Q, idx, 50)
+        assert torch.equal(O, wO) and torch.equal(LSE, wL)
+        check(small, [0], [0, n], Q, idx, None, 50, O, LSE)
+    new = torch.ones((Hkv, 3, D), dtype=BF16, device=DEV)
+    B.sl_paged_append(cache, i32([0]), i32([0, 3]), new, new)
+    assert bool((K[0, n_pages - 2, :, 55:58] == 1).all()) and not bool((K[0, n_pages - 2, :, 54] == 1).any())
+    assert B.sl_pages_fork(cache, i32([0]), i32([1])).tolist() == [1]
+    assert torch.equal(K[0, 0, :, :58], K[0, n_pages - 2, :, :58]) and not bool(K[0, 0, :, 58:].any())
+    B.sl_pages_compact(cache)
+    assert sorted(cache.tables[0, :4].tolist()) == [0, 1, 2, 3] or int((cache.refs > 0).sum()) == 5
+    last = int(cache.tables[0, 3])
+    assert bool((K[0, last, :, 55:58] == 1).all())
