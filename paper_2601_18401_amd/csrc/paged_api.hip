@@ -20,8 +20,7 @@ sl_status make_cache(const sl_page_cache* p, PageCache* c) {
   if (p->layers < 1 || p->n_pages < 1 || p->n_seqs < 1 || p->max_pages < 1 || p->page_size < 1 || p->Hkv < 1) return SL_ERR_INVALID_ARG;
   if (p->dtype != SL_F32 && p->dtype != SL_BF16) return SL_ERR_INVALID_ARG;
   if (p->D != 64 && p->D != 128) return SL_ERR_UNSUPPORTED;
-  constexpr int64_t kInt = ((int64_t)1 << 31) - 1;
-  if ((int64_t)p->max_pages * p->page_size > kInt) return SL_ERR_UNSUPPORTED;
+  if ((int64_t)p->max_pages * p->page_size > (int64_t)1 << 30) return SL_ERR_UNSUPPORTED;
   // (grid dimensions are 16 bits wide in y)
   if (p->Hkv > 1024 || p->layers > 4096 || (int64_t)p->layers * 2 * p->Hkv + p->max_pages / 1024 > 65000 || p->max_pages > (1 << 25))
     return SL_ERR_UNSUPPORTED;

@@ -3,6 +3,8 @@
 // A row's keys are the tokens of its selected spans and of its window.  They are cut into pieces; a piece's softmax gives
 // a normalised output and a log-sum-exp (in log2 units), and a merge joins a row's pieces: exp2(lse_p - lse) of each for the
 // joint form, and for the gated one alpha_t * exp2(lse_p - lse_t) summed over the slots t that the piece belongs to.
+#include <climits>
+
 #include "paged.h"
 
 namespace sl {
@@ -28,6 +30,19 @@ struct PagedArgs {
   float* part_o;    // [Hq * rows][count][D]
   float* part_lse;  // [Hq * rows][count]
   float scale_log2e;
+  int row_pieces;  // of a row, its first ones: taken row by row
+};
+
+// Tiles of the matrix-core form.  Window tiles: entry e's start at floor(cu[e] * G / cols) + e, which leaves room for
+// ceil(new rows * G / cols) of them, since ceil(y - x) <= floor(y) - floor(x) + 1.
+struct TilePlan {
+  int tiles;             // window tiles of a kv head
+  int64_t window_units;  // tiles * pieces of a window * Hkv
+  int spans, buckets;    // spans of the longest sequence; B * Hkv * spans
+  int32_t *counts, *first_tile;  // [buckets]
+  int32_t *tile_count, *tile_bucket;
+  int32_t *ranks;  // [Hq * rows * topk] an item's place in its bucket, -1 for empty slots
+  int32_t *items;  // [tiles][cols] (row and head) * 32 + slot
 };
 
 __device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }  // NaN stays
@@ -150,39 +165,502 @@ __device__ __forceinline__ PieceRange range_of_piece(const PagedArgs& x, int pos
   return {(int)min(t0, (int64_t)pos + 1), (int)min(t0 + x.p.window_tokens, (int64_t)pos + 1)};
 }
 
-// Wavefront u takes piece u % count of row-and-head u / count.
+// One piece of a row and head by one wavefront, to its record.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void rows_kernel(const PagedArgs x) {
+__device__ __forceinline__ void take_piece(const PagedArgs& x, int s, int h, int row, const PieceRange& r, int64_t rec, int lane) {
   using RS = RowState<T, D>;
-  const int lane = threadIdx.x & 63;
-  const int64_t u = workgroup() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (u >= (int64_t)x.a.Hq * x.b.rows * x.p.count) return;
-  const int rh = (int)(u / x.p.count), part = (int)(u - (int64_t)rh * x.p.count);
-  const int h = rh / x.b.rows, row = rh - h * x.b.rows;
-  if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
-  const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, row), row);
   RS st;
   st.clear();
-  if (at.pos >= 0) {
-    const PieceRange r = range_of_piece(x, at.pos, part, x.idx + h * x.a.ish + row * x.a.ist);
-    if (r.t0 < r.t1) {
-      float q[RS::EPL];
-      Elem<T>::unpack(load16(static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst + lane % RS::LPR * RS::EPL), q);
+  if (r.t0 < r.t1) {
+    float q[RS::EPL];
+    Elem<T>::unpack(load16(static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst + lane % RS::LPR * RS::EPL), q);
 #pragma unroll
-      for (int e = 0; e < RS::EPL; ++e) q[e] *= x.scale_log2e;
-      const int64_t base = x.b.layer * x.c.layer + h / x.a.G * x.c.head;
-      st.template attend<4>(x.c, static_cast<const T*>(x.c.K) + base, static_cast<const T*>(x.c.V) + base,
-                            x.c.tables + (int64_t)at.s * x.c.max_pages, q, r.t0, r.t1, lane);
-      st.join_groups();
-    }
+    for (int e = 0; e < RS::EPL; ++e) q[e] *= x.scale_log2e;
+    const int64_t base = x.b.layer * x.c.layer + h / x.a.G * x.c.head;
+    st.template attend<4>(x.c, static_cast<const T*>(x.c.K) + base, static_cast<const T*>(x.c.V) + base,
+                          x.c.tables + (int64_t)s * x.c.max_pages, q, r.t0, r.t1, lane);
+    st.join_groups();
   }
-  if (lane == 0) x.part_lse[u] = st.m == -INFINITY ? -INFINITY : st.m + __log2f(st.l);
+  if (lane == 0) x.part_lse[rec] = st.m == -INFINITY ? -INFINITY : st.m + __log2f(st.l);
   if (lane < RS::LPR && !(st.m == -INFINITY)) {
     const float inv = 1.f / st.l;
 #pragma unroll
     for (int e = 0; e < RS::EPL; e += 4)
-      *reinterpret_cast<float4*>(x.part_o + u * D + lane * RS::EPL + e) =
+      *reinterpret_cast<float4*>(x.part_o + rec * D + lane * RS::EPL + e) =
           make_float4(st.o[e] * inv, st.o[e + 1] * inv, st.o[e + 2] * inv, st.o[e + 3] * inv);
+  }
+}
+
+// Wavefront u takes piece u % row_pieces of row-and-head u / row_pieces.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void rows_kernel(const PagedArgs x) {
+  const int lane = threadIdx.x & 63;
+  const int64_t u = workgroup() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (u >= (int64_t)x.a.Hq * x.b.rows * x.row_pieces) return;
+  const int rh = (int)(u / x.row_pieces), part = (int)(u - (int64_t)rh * x.row_pieces);
+  const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+  if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
+  const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, row), row);
+  const PieceRange r = at.pos < 0 ? PieceRange{0, 0} : range_of_piece(x, at.pos, part, x.idx + h * x.a.ish + row * x.a.ist);
+  take_piece<T, D>(x, at.s, h, row, r, (int64_t)rh * x.p.count + part, lane);
+}
+
+// ------------------------------------------------------------------ tiles on the matrix cores (bf16)
+// A tile is up to NW * 32 * CB query columns that attend one run of the sequence's tokens, each in a range of its own: rows and heads
+// of a kv head's group on their windows, or the rows that list a span.  Both products are taken transposed, so that a lane
+// owns a column:
+//   S^T[token][column] = K . Q^T      A = K rows from LDS, B = queries in registers
+//   O^T[d][column] += V^T . P^T       A = V through transposing LDS reads, B = P^T straight from the S^T accumulators
+// (v_mfma_f32_32x32x16_bf16: lane l of the result holds column l % 32 and rows 8 (r / 4) + 4 (l / 32) + r % 4; K rows are fed with
+// bits 2 and 3 of their number swapped, which makes a lane's eight consecutive accumulators eight consecutive tokens.)
+// K and V rows come by direct global -> LDS loads, 64 tokens a step in two stages, 16-byte pieces swizzled against bank conflicts.
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+template <int D>
+__device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
+
+__device__ __forceinline__ float across_halves_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+  return max_of(__int_as_float(r[0]), __int_as_float(r[1]));
+}
+__device__ __forceinline__ float across_halves_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+  return __int_as_float(r[0]) + __int_as_float(r[1]);
+}
+
+#define SL_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+
+// Sixteen rows of a K or V stage: global -> LDS, 1 KB an instruction.  base: row 0 of the sixteen; rows from `rows` on become zeros
+// (what lies there may be anything, and zero times that need not be zero).
+template <int D, int TENSOR>
+__device__ __forceinline__ void stage_rows(bf16_t* to, int first_row, const bf16_t* base, int rows, int row_bytes, int lane) {
+  constexpr int LPR = D / 8, RPI = 64 / LPR;
+  const __amdgpu_buffer_rsrc_t from =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(base), 0, rows <= 0 ? 0 : (rows - 1) * row_bytes + D * 2, 0x00020000);
+#pragma unroll
+  for (int i = 0; i < 16 / RPI; ++i) {
+    const int row = i * RPI + lane / LPR;
+    const int piece = lane % LPR ^ (TENSOR == 0 ? k_swizzle<D>(first_row + row) : v_swizzle<D>(first_row + row));
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, SL_LDS(to + i * 512), 16, row * row_bytes + piece * 16, 0, 0, 0);
+  }
+}
+
+// An LDS address that the compiler knows nothing of: where it sees that staged rows are read, it waits for every staging load
+// in flight, the next step's among them.
+__device__ __forceinline__ uint32_t lds_address(const bf16_t* p, int offset) {
+  uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) bf16_t*)p + offset;
+  asm volatile("" : "+v"(at));
+  return at;
+}
+
+// A wavefront's CB blocks of 32 columns; it takes 32 * KB tokens at a time.
+template <int D, int CB, int KB>
+struct Tile {
+  static constexpr int KK = D / 16, DT = D / 32;
+  bf16x8 q[CB][KK];
+  f32x16 o[CB][DT];
+  float m[CB], l[CB];
+  int lo[CB], last[CB];  // tokens that the lane's column attends
+  int kbase, vbase;
+
+  __device__ __forceinline__ void clear(int lane) {
+    const int col = lane & 31, hf = lane >> 5;
+    const int krow = (col & 0x13) | ((col & 4) << 1) | ((col & 8) >> 1);
+    kbase = 2 * (krow * D + ((hf ^ k_swizzle<D>(krow)) << 3));
+    const int vrow = (lane & 15) >> 2;
+    vbase = 2 * ((8 * hf + vrow) * D + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<D>(vrow)) << 3) + 4 * (lane & 1));
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      m[cb] = -INFINITY;
+      l[cb] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[cb][dt][r] = 0.f;
+    }
+  }
+  // 32 * KB tokens from t0 on, K rows at kt, V rows at vt (LDS); live: a bit for each sixteen of them whose page there is
+  __device__ __forceinline__ void attend(const bf16_t* kt, const bf16_t* vt, int t0, bool masked, uint32_t live, float sc, int lane) {
+    f32x16 s[CB][KB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[cb][kb][r] = 0.f;
+    const uint32_t ka = lds_address(kt, kbase);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const bf16x8 a = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8*>((uintptr_t)((ka ^ (kk << 5)) + 64 * D * kb));
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) s[cb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[cb][kk], s[cb][kb], 0, 0, 0);
+      }
+    // fragment reads run four products ahead (0x100 = LDS read, 0x008 = MFMA)
+    __builtin_amdgcn_sched_group_barrier(0x100, 4 / CB, 0);
+#pragma unroll
+    for (int i = 0; i < KK * KB - 4 / CB; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, CB, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    __builtin_amdgcn_s_setprio(3);  // (few of the vector instructions fit beside another wavefront's products)
+    if (masked) {
+      const int at = t0 + 8 * (lane >> 5);
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int t = at + 32 * kb + 16 * (r >> 3) + (r & 7);
+            s[cb][kb][r] = t >= lo[cb] && t <= last[cb] && (live >> (2 * kb + (r >> 3)) & 1) ? s[cb][kb][r] : -INFINITY;
+          }
+    }
+    bool grow[CB], any = false;
+    float top[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      top[cb] = s[cb][0][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top[cb] = max_of(top[cb], s[cb][kb][r]);
+      top[cb] = across_halves_max(top[cb]) * sc;
+      grow[cb] = !(top[cb] <= m[cb]);
+      any = any || grow[cb];
+    }
+    // Weights are taken against a bound, which moves, to the maximum + 8, only when a score passes it.
+    if (__builtin_amdgcn_ballot_w64(any) != 0) {
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        const float to = grow[cb] ? top[cb] + 8.f : m[cb];
+        const float f = grow[cb] ? weight_of(m[cb], to) : 1.f;
+        m[cb] = to;
+        l[cb] *= f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[cb][dt][r] *= f;
+      }
+    }
+    bf16x8 p[CB][2 * KB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const float minus = m[cb] == -INFINITY ? 0.f : -m[cb];
+#pragma unroll
+      for (int ks = 0; ks < 2 * KB; ++ks) {
+        f32x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(s[cb][ks >> 1][8 * (ks & 1) + e], sc, minus));
+        // the unrounded weights' sum: lse is exact to fp32
+        l[cb] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        p[cb][ks] = __builtin_convertvector(w, bf16x8);
+      }
+    }
+    __builtin_amdgcn_s_setprio(0);
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* LdsPtr;
+    const uint32_t va = lds_address(vt, vbase);
+#pragma unroll
+    for (int ks = 0; ks < 2 * KB; ++ks)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint32_t at = (va ^ (dt << 6)) + 32 * ks * D;
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(uintptr_t)at);
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(uintptr_t)(at + 8 * D));
+        const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) o[cb][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[cb][ks], o[cb][dt], 0, 0, 0);
+      }
+    __builtin_amdgcn_sched_group_barrier(0x100, 8 / CB, 1);
+#pragma unroll
+    for (int i = 0; i < 2 * KB * DT - 4 / CB; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, CB, 1);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
+  }
+};
+
+// What a workgroup works on.
+struct TileWork {
+  int s, head;       // sequence and kv head
+  int begin, end;    // tokens [begin, end), begin a multiple of 16
+};
+
+template <int NW>
+__device__ __forceinline__ void stage_barrier() {  // (LDS operations and the staged loads only: a fence would wait for stores)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  if (NW > 1) __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <int D, int NW, int CB, int STEP>
+__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
+  constexpr int COLS = NW * 32 * CB;
+  __shared__ __align__(1024) bf16_t s_kv[2][2][STEP * D];
+  __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS];
+  __shared__ int s_range[2 * NW];
+  const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t unit = workgroup();
+  TileWork w;
+  int part;
+  // columns
+  if (unit < plan.window_units) {
+    // (tile, piece) of the kv heads in turn; the last tiles first, whose ranges are the longest
+    w.head = (int)(unit % x.c.Hkv);
+    const int at = (int)(unit / x.c.Hkv), tile = plan.tiles - 1 - at / x.p.window, piece = at % x.p.window;
+    part = x.a.topk * x.p.routed + piece;
+    int lo = 0, hi = x.b.B - 1;
+    while (lo < hi) {  // entry e's tiles start at cu[e] * G / COLS + e
+      const int mid = (lo + hi + 1) >> 1;
+      if ((int)((int64_t)max(x.b.cu[mid], 0) * x.a.G / COLS) + mid <= tile) lo = mid;
+      else hi = mid - 1;
+    }
+    const int e = lo, r0 = x.b.cu[e], r1 = min(x.b.cu[e + 1], x.b.rows);
+    const int u0 = (tile - ((int)((int64_t)max(r0, 0) * x.a.G / COLS) + e)) * COLS;
+    if (r0 < 0 || u0 >= (int64_t)(r1 - r0) * x.a.G) return;
+    w.s = x.b.seqs[e];
+    const int len = length_of(x.c, w.s), pos0 = len - (x.b.cu[e + 1] - r0);
+    const int first = max(pos0 + u0 / x.a.G, 0);  // position of the tile's first row that has a token
+    const int64_t origin = (int64_t)(first / x.a.S) * x.a.S / 16 * 16 + (int64_t)piece * x.p.window_tokens;
+    for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
+      const int u = u0 + c, row = r0 + u / x.a.G, pos = pos0 + u / x.a.G;
+      int rh = -1, clo = INT_MAX, clast = -1;
+      if (row < r1) {
+        rh = (w.head * x.a.G + u % x.a.G) * x.b.rows + row;
+        if (pos >= 0 && pos < len && pos < x.b.L) {
+          clo = (int)max((int64_t)(pos / x.a.S) * x.a.S, min(origin, (int64_t)INT_MAX));
+          clast = (int)min((int64_t)pos, origin + x.p.window_tokens - 1);
+          if (clo > clast) {
+            clo = INT_MAX;
+            clast = -1;
+          }
+        }
+      }
+      s_rh[c] = rh;
+      s_lo[c] = clo;
+      s_last[c] = clast;
+    }
+  } else {
+    const int64_t u = unit - plan.window_units;
+    const int tile = (int)(u / x.p.routed), piece = (int)(u - (int64_t)tile * x.p.routed);
+    if (tile >= *plan.tile_count) return;
+    const int bucket = plan.tile_bucket[tile], count = plan.counts[bucket] - (tile - plan.first_tile[bucket]) * COLS;
+    const int j = bucket % plan.spans, eh = bucket / plan.spans;
+    w.head = eh % x.c.Hkv;
+    w.s = x.b.seqs[eh / x.c.Hkv];
+    const int t0 = j * x.a.S + piece * x.p.routed_tokens, last = min(t0 + x.p.routed_tokens, (j + 1) * x.a.S) - 1;
+    for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
+      s_rh[c] = c < count ? plan.items[(int64_t)tile * COLS + c] : -1;  // (row and head) * 32 + slot
+      s_lo[c] = c < count ? t0 : INT_MAX;
+      s_last[c] = c < count ? last : -1;
+    }
+    part = piece;
+  }
+  const bool window = unit < plan.window_units;
+  __syncthreads();
+  constexpr int KB = CB == 2 || STEP == 32 ? 1 : 2;
+  Tile<D, CB, KB> tile;
+  tile.clear(lane);
+  int any_lo = INT_MAX, any_last = -1, all_lo = 0, all_last = INT_MAX;
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    const int c = wave * 32 * CB + cb * 32 + (lane & 31);
+    const int lo = s_lo[c], last = s_last[c], item = s_rh[c];
+    tile.lo[cb] = lo;
+    tile.last[cb] = last;
+    any_lo = min(any_lo, lo);
+    any_last = max(any_last, last);
+    if (item >= 0) {
+      all_lo = max(all_lo, lo);
+      all_last = min(all_last, last);
+    }
+    const int rh = max(window ? item : item >> 5, 0);  // (a column of nobody reads some row: nothing is made of it)
+    const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+    const bf16_t* const q = static_cast<const bf16_t*>(x.Q) + h * x.a.qsh + row * x.a.qst + (lane >> 5) * 8;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) tile.q[cb][kk] = *reinterpret_cast<const bf16x8*>(q + kk * 16);
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) {
+    any_lo = min(any_lo, __shfl_xor(any_lo, off, 64));
+    any_last = max(any_last, __shfl_xor(any_last, off, 64));
+    all_lo = max(all_lo, __shfl_xor(all_lo, off, 64));
+    all_last = min(all_last, __shfl_xor(all_last, off, 64));
+  }
+  any_lo = __builtin_amdgcn_readfirstlane(any_lo);
+  any_last = __builtin_amdgcn_readfirstlane(any_last);
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_last = __builtin_amdgcn_readfirstlane(all_last);
+  w.begin = any_lo;
+  w.end = any_last + 1;
+  if (NW > 1) {
+    if (lane == 0) {
+      s_range[2 * wave] = any_lo;
+      s_range[2 * wave + 1] = any_last;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      w.begin = min(w.begin, s_range[2 * k]);
+      w.end = max(w.end, s_range[2 * k + 1] + 1);
+    }
+    w.begin = __builtin_amdgcn_readfirstlane(w.begin);
+    w.end = __builtin_amdgcn_readfirstlane(w.end);
+  }
+  w.begin = w.begin / 16 * 16;
+
+  w.s = __builtin_amdgcn_readfirstlane(w.s);
+  w.head = __builtin_amdgcn_readfirstlane(w.head);
+  const int32_t* const table = x.c.tables + (int64_t)w.s * x.c.max_pages;
+  const int64_t base = x.b.layer * x.c.layer + w.head * x.c.head;
+  const int row_bytes = (int)x.c.tok * 2;
+  // The pages of a step's rows are looked up a step before its rows are asked for; lane g has that of its rows 16 g, ...
+  constexpr int GROUPS = STEP / 16;
+  int page = -1;
+  uint32_t live[2];
+  auto look_up = [&](int t0) {
+    const int t = t0 + lane % GROUPS * 16;
+    page = t < w.end ? table[(uint32_t)t / x.c.by_ps] : -1;
+  };
+  auto stage = [&](int t0, int b) {
+    live[b] = (uint32_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages) & ((1u << GROUPS) - 1);
+#pragma unroll
+    for (int i = 0; i < GROUPS / NW; ++i) {
+      const int g = NW == 1 ? i : wave, r0 = g * 16, t = t0 + r0;
+      const bool on = live[b] >> g & 1;
+      const int rows = on ? min(w.end - t, 16) : 0;
+      const int64_t at = on ? base + __builtin_amdgcn_readlane(page, g) * x.c.page +
+                                  (int64_t)((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps) * x.c.tok
+                            : 0;
+      stage_rows<D, 0>(&s_kv[b][0][r0 * D], r0, static_cast<const bf16_t*>(x.c.K) + at, rows, row_bytes, lane);
+      stage_rows<D, 1>(&s_kv[b][1][r0 * D], r0, static_cast<const bf16_t*>(x.c.V) + at, rows, row_bytes, lane);
+    }
+    look_up(t0 + STEP);
+  };
+  if (w.begin < w.end) {
+    look_up(w.begin);
+    stage(w.begin, 0);
+  }
+  int b = 0;
+  for (int t0 = w.begin; t0 < w.end; t0 += STEP, b ^= 1) {
+    stage_barrier<NW>();
+    if (t0 + STEP < w.end) stage(t0 + STEP, b ^ 1);
+#pragma unroll 1
+    for (int at = 0; at < STEP; at += 32 * KB) {
+      const int t = t0 + at, end = t + 32 * KB - 1;
+      if (end < any_lo || t > any_last) continue;
+      constexpr uint32_t kAll = (1u << 2 * KB) - 1;
+      const uint32_t there = live[b] >> (at / 16) & kAll;
+      tile.attend(&s_kv[b][0][at * D], &s_kv[b][1][at * D], t, t < all_lo || end > all_last || there != kAll, there, x.scale_log2e, lane);
+    }
+  }
+  // Partials.  A column with a value that is not finite is marked by an lse that is not a number: it may have come from a
+  // token that the column does not attend, and the merge takes such a piece again, row by row.
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    const int item = s_rh[wave * 32 * CB + cb * 32 + (lane & 31)];
+    const float sum = across_halves_sum(tile.l[cb]);
+    const float inv = 1.f / sum;
+    float check = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) check = fmaf(tile.o[cb][dt][r], 0.f, check);
+    check = across_halves_sum(check);
+    if (item < 0) continue;
+    const int64_t rec = (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
+    const bool none = tile.m[cb] == -INFINITY;
+    if (lane < 32) x.part_lse[rec] = none ? -INFINITY : check == 0.f ? tile.m[cb] + __log2f(sum) : NAN;
+    if (none) continue;
+    float* const to = x.part_o + rec * D + 4 * (lane >> 5);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(to + dt * 32 + g * 8) = make_float4(tile.o[cb][dt][4 * g] * inv, tile.o[cb][dt][4 * g + 1] * inv,
+                                                                      tile.o[cb][dt][4 * g + 2] * inv, tile.o[cb][dt][4 * g + 3] * inv);
+  }
+}
+
+// ---- the rows that list a span: buckets (entry, kv head, span), each cut into tiles of `cols` items
+__global__ __launch_bounds__(256) void zero_kernel(int32_t* __restrict__ to, int n) {
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) to[i] = 0;
+}
+
+// One thread a row and head.  Pieces of empty slots are marked here: no tile writes them.
+__global__ __launch_bounds__(256) void count_kernel(const PagedArgs x, const TilePlan plan) {
+  const int64_t rh = workgroup() * 256 + threadIdx.x;
+  if (rh >= (int64_t)x.a.Hq * x.b.rows) return;
+  const int h = (int)(rh / x.b.rows), row = (int)(rh - (int64_t)h * x.b.rows);
+  if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
+  const int e = entry_of_row(x.b.cu, x.b.B, row);
+  const RowPlace at = place_of_row(x, e, row);
+  const int c = at.pos < 0 ? 0 : at.pos / x.a.S;
+  const int32_t* const slots = x.idx + h * x.a.ish + row * x.a.ist;
+  const int first = (e * x.c.Hkv + h / x.a.G) * plan.spans;
+  for (int k = 0; k < x.a.topk; ++k) {
+    const int j = slots[k];
+    if (j >= 0 && j < c) {
+      plan.ranks[rh * x.a.topk + k] = atomicAdd(&plan.counts[first + j], 1);
+    } else {
+      plan.ranks[rh * x.a.topk + k] = -1;
+      for (int q = 0; q < x.p.routed; ++q) x.part_lse[rh * x.p.count + k * x.p.routed + q] = -INFINITY;
+    }
+  }
+}
+
+// Tiles of each bucket in the buckets' order; one workgroup.
+__global__ __launch_bounds__(1024) void tiles_kernel(const TilePlan plan, int cols_log2) {
+  __shared__ int s_wave[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0;
+  for (int base = 0; base < plan.buckets; base += 1024) {
+    const int i = base + threadIdx.x;
+    const int n = i < plan.buckets ? (plan.counts[i] + (1 << cols_log2) - 1) >> cols_log2 : 0;
+    int v = n;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int y = __shfl_up(v, off, 64);
+      if (lane >= off) v += y;
+    }
+    __syncthreads();
+    if (lane == 63) s_wave[wave] = v;
+    __syncthreads();
+    int at = before + v - n, all = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      if (k < wave) at += s_wave[k];
+      all += s_wave[k];
+    }
+    if (i < plan.buckets) {
+      plan.first_tile[i] = at;
+      for (int k = 0; k < n; ++k) plan.tile_bucket[at + k] = i;
+    }
+    before += all;
+  }
+  if (threadIdx.x == 0) *plan.tile_count = before;
+}
+
+__global__ __launch_bounds__(256) void items_kernel(const PagedArgs x, const TilePlan plan, int cols_log2) {
+  const int64_t rh = workgroup() * 256 + threadIdx.x;
+  if (rh >= (int64_t)x.a.Hq * x.b.rows) return;
+  const int h = (int)(rh / x.b.rows), row = (int)(rh - (int64_t)h * x.b.rows);
+  if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
+  const int e = entry_of_row(x.b.cu, x.b.B, row);
+  const int32_t* const slots = x.idx + h * x.a.ish + row * x.a.ist;
+  const int first = (e * x.c.Hkv + h / x.a.G) * plan.spans;
+  for (int k = 0; k < x.a.topk; ++k) {
+    const int rank = plan.ranks[rh * x.a.topk + k];
+    if (rank >= 0) plan.items[((int64_t)plan.first_tile[first + slots[k]] << cols_log2) + rank] = (int)rh * 32 + k;
   }
 }
 
@@ -200,6 +678,27 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   const int h = rh / x.b.rows, row = rh - h * x.b.rows;
   if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
   const float* const lse = x.part_lse + (int64_t)rh * P;
+  const int routed = x.a.topk * x.p.routed;
+  if (x.row_pieces < P) {
+    // Pieces that a tile marked: once more, row by row.  Of the window, whose tiles cut it where they like, all into its first record.
+    bool marked = false;
+    for (int k = x.row_pieces + tid; k < P; k += 256) marked = marked || lse[k] != lse[k];
+    if (__syncthreads_or(marked)) {
+      const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, row), row);
+      const int32_t* const slots = x.idx + h * x.a.ish + row * x.a.ist;
+      bool near = false;
+      for (int k = routed; k < P; ++k) near = near || lse[k] != lse[k];
+      __syncthreads();
+      for (int k = x.row_pieces + wave; k < routed; k += 4)
+        if (lse[k] != lse[k]) take_piece<T, D>(x, at.s, h, row, range_of_piece(x, at.pos, k, slots), (int64_t)rh * P + k, lane);
+      if (near) {
+        if (wave == 0) take_piece<T, D>(x, at.s, h, row, {at.pos / x.a.S * x.a.S, at.pos + 1}, (int64_t)rh * P + routed, lane);
+        for (int k = routed + 1 + tid; k < P; k += 256) x.part_lse[(int64_t)rh * P + k] = -INFINITY;
+      }
+      __threadfence_block();
+      __syncthreads();
+    }
+  }
   auto all_max = [&](float v) {
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) v = max_of(v, __shfl_xor(v, off, 64));
@@ -226,7 +725,6 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
     for (int k = from + tid; k < to; k += 256) l += weight_of(lse[k], m);
     return m + __log2f(all_sum(l));
   };
-  const int routed = x.a.topk * x.p.routed;
   float total = -INFINITY;
   bool any = false;  // a slot holds a span
   if (x.a.combined) {
@@ -300,30 +798,93 @@ dim3 grid_of(int64_t workgroups) {
   return workgroups <= kMost ? dim3((unsigned)workgroups) : dim3((unsigned)kMost, (unsigned)div_up(workgroups, kMost));
 }
 
-// Pieces of at least 64 tokens, enough of them for 4096 wavefronts.
-Pieces pieces_of(const PagedBatch& b, const PagedAttention& a) {
+// How a call is taken.
+struct Form {
+  Pieces p;
+  bool window_tiles, routed_tiles;
+  int cols_log2;  // columns of a tile
+  TilePlan plan;  // (pointers unset)
+  int64_t most_tiles;
+  size_t o_bytes, lse_bytes, plan_bytes;
+};
+
+Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   const int64_t rh = (int64_t)a.Hq * b.rows, window = a.S < b.L ? a.S : b.L;
-  Pieces p = {1, a.S, 1, (int)window, 0};
-  auto cut = [](int64_t tokens, int64_t units, int64_t most) {
-    int64_t n = div_up(4096, units);
+  Form f = {};
+  // Sixteen rows of a stage lie in one page, and 16 token strides within a buffer's 32-bit offsets.
+  const bool tiles = c.dtype == SL_BF16 && c.ps % 16 == 0 && c.tok < ((int64_t)1 << 26) && rh < ((int64_t)1 << 26);
+  f.window_tiles = tiles;
+  const int64_t spans = div_up(b.L, a.S), buckets = (int64_t)b.B * c.Hkv * spans, items = rh * a.topk;
+  f.routed_tiles = tiles && a.topk > 0 && items >= 4 * buckets && items < ((int64_t)1 << 30);
+  const int64_t columns = (int64_t)b.rows * a.G;  // of a kv head
+  f.cols_log2 = columns <= 32 * (int64_t)b.B && !f.routed_tiles ? 5 : 7;
+  const int cols = 1 << f.cols_log2;
+  auto cut = [](int64_t tokens, int64_t units, int64_t wanted, int64_t most) {
+    int64_t n = div_up(wanted, units);
     if (n > most) n = most;
     if (n > div_up(tokens, 64)) n = div_up(tokens, 64);
     return n < 1 ? 1 : n;
   };
-  if (a.topk > 0) {
-    p.routed_tokens = (int)div_up(a.S, cut(a.S, rh * a.topk, 64));
+  Pieces& p = f.p;
+  p = {1, a.S, 1, (int)window, 0};
+  if (a.topk > 0 && a.S <= b.L) {  // (no row has a longer span among its candidates)
+    const int64_t units = f.routed_tiles ? items / cols + 1 : items;
+    p.routed_tokens = (int)div_up(div_up(a.S, cut(a.S, units, f.routed_tiles ? 1024 : 4096, 64)), 16) * 16;
     p.routed = (int)div_up(a.S, p.routed_tokens);
   }
-  p.window_tokens = (int)div_up(window, cut(window, rh, 256));
-  p.window = (int)div_up(window, p.window_tokens);
+  if (tiles) {
+    f.plan.tiles = (int)(columns / cols) + b.B;
+    const int64_t longest = window + cols / a.G + 17;  // a tile's rows may lie in two windows; it begins at a multiple of 16
+    const int64_t n = cut(longest, (int64_t)f.plan.tiles * c.Hkv, cols == 32 ? 2048 : 1024, 256);
+    p.window_tokens = (int)div_up(div_up(longest, n), 64) * 64;
+    p.window = (int)div_up(longest, p.window_tokens);
+    f.plan.window_units = (int64_t)f.plan.tiles * p.window * c.Hkv;
+  } else {
+    p.window_tokens = (int)div_up(window, cut(window, rh, 4096, 256));
+    p.window = (int)div_up(window, p.window_tokens);
+  }
   p.count = a.topk * p.routed + p.window;
-  return p;
+  f.o_bytes = align_up((size_t)rh * p.count * c.D * sizeof(float), 256);
+  f.lse_bytes = align_up((size_t)rh * p.count * sizeof(float), 256);
+  if (f.routed_tiles) {
+    f.plan.spans = (int)spans;
+    f.plan.buckets = (int)buckets;
+    f.most_tiles = items / cols + (buckets < items ? buckets : items);
+    f.plan_bytes = align_up(sizeof(int32_t) * (2 * (size_t)buckets + 64 + (size_t)f.most_tiles + (size_t)items + (size_t)f.most_tiles * cols), 256);
+  }
+  return f;
+}
+
+template <int D, int NW, int CB, int STEP>
+void launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
+  const int64_t units = plan.window_units + (f.routed_tiles ? f.most_tiles * f.p.routed : 0);
+  tile_kernel<D, NW, CB, STEP><<<grid_of(units), 64 * NW, 0, st>>>(x, plan);
 }
 
 template <typename T, int D>
-sl_status launch(const PagedArgs& x, hipStream_t st) {
+sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
   const int64_t rh = (int64_t)x.a.Hq * x.b.rows;
-  rows_kernel<T, D><<<grid_of(div_up(rh * x.p.count, 4)), 256, 0, st>>>(x);
+  if constexpr (sizeof(T) == 2) {
+    if (f.window_tiles) {
+      TilePlan plan = f.plan;
+      if (f.routed_tiles) {
+        plan.counts = reinterpret_cast<int32_t*>(ws + f.o_bytes + f.lse_bytes);
+        plan.first_tile = plan.counts + plan.buckets;
+        plan.tile_count = plan.first_tile + plan.buckets;
+        plan.tile_bucket = plan.tile_count + 64;
+        plan.ranks = plan.tile_bucket + f.most_tiles;
+        plan.items = plan.ranks + rh * x.a.topk;
+        const int64_t blocks = div_up(plan.buckets, 1024);
+        zero_kernel<<<(unsigned)(blocks < 1024 ? blocks : 1024), 256, 0, st>>>(plan.counts, plan.buckets);
+        count_kernel<<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x, plan);
+        tiles_kernel<<<1, 1024, 0, st>>>(plan, f.cols_log2);
+        items_kernel<<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x, plan, f.cols_log2);
+      }
+      if (f.cols_log2 == 5) launch_tiles<D, 1, 1, 32>(x, f, plan, st);
+      else launch_tiles<D, 4, 1, 64>(x, f, plan, st);
+    }
+  }
+  if (x.row_pieces > 0) rows_kernel<T, D><<<grid_of(div_up(rh * x.row_pieces, 4)), 256, 0, st>>>(x);
   merge_kernel<T, D><<<grid_of(rh), 256, x.p.count * sizeof(float), st>>>(x);
   return hipGetLastError() == hipSuccess ? SL_OK : SL_ERR_LAUNCH;
 }
@@ -331,18 +892,18 @@ sl_status launch(const PagedArgs& x, hipStream_t st) {
 }  // namespace
 
 size_t paged_attention_ws_bytes(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
-  const Pieces p = pieces_of(b, a);
-  const size_t records = (size_t)a.Hq * b.rows * p.count;
-  return align_up(records * c.D * sizeof(float), 256) + align_up(records * sizeof(float), 256);
+  const Form f = form_of(c, b, a);
+  return f.o_bytes + f.lse_bytes + f.plan_bytes;
 }
 
 sl_status paged_attention(const PageCache& c, const PagedBatch& b, const PagedAttention& a, const void* Q, const int32_t* idx,
                           const float* scores, void* O, float* LSE, void* ws, hipStream_t st) {
-  PagedArgs x = {c, b, a, pieces_of(b, a), Q, idx, scores, O, LSE, static_cast<float*>(ws), nullptr, a.scale * kLog2e};
-  x.part_lse = reinterpret_cast<float*>(static_cast<char*>(ws) +
-                                        align_up((size_t)a.Hq * b.rows * x.p.count * c.D * sizeof(float), 256));
-  if (c.dtype == SL_BF16) return c.D == 128 ? launch<bf16_t, 128>(x, st) : launch<bf16_t, 64>(x, st);
-  return c.D == 128 ? launch<float, 128>(x, st) : launch<float, 64>(x, st);
+  const Form f = form_of(c, b, a);
+  char* const at = static_cast<char*>(ws);
+  PagedArgs x = {c, b, a, f.p, Q, idx, scores, O, LSE, static_cast<float*>(ws), reinterpret_cast<float*>(at + f.o_bytes), a.scale * kLog2e,
+                 f.routed_tiles ? 0 : f.window_tiles ? a.topk * f.p.routed : f.p.count};
+  if (c.dtype == SL_BF16) return c.D == 128 ? launch<bf16_t, 128>(x, f, at, st) : launch<bf16_t, 64>(x, f, at, st);
+  return c.D == 128 ? launch<float, 128>(x, f, at, st) : launch<float, 64>(x, f, at, st);
 }
 
 }  // namespace sl

@@ -122,7 +122,7 @@ def test_nothing_to_do_enqueues_nothing():
 
 def test_the_largest_problems_ask_for_sizes_that_fit():
     """Sizes are computed in 64 bits: 2^31 rows and heads, 32 spans of the longest length."""
-    size = need(rows=1 << 25, Hq=60, Hkv=60, topk=32, S=(1 << 31) - 1, max_pages=1 << 24, page_size=127)
+    size = need(rows=1 << 25, Hq=60, Hkv=60, topk=32, S=(1 << 31) - 1, max_pages=1 << 24, page_size=64)
     assert size != B.WORKSPACE_INVALID and size >= (1 << 25) * 60 * 33 * 128 * 2
     assert need(rows=1 << 25, Hq=64, Hkv=64) == B.WORKSPACE_INVALID     # row ids are 32-bit
 
