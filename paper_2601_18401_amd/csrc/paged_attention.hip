@@ -4,6 +4,7 @@
 // a normalised output and a log-sum-exp (in log2 units), and a merge joins a row's pieces: exp2(lse_p - lse) of each for the
 // joint form, and for the gated one alpha_t * exp2(lse_p - lse_t) summed over the slots t that the piece belongs to.
 #include <climits>
+#include <mutex>
 
 #include "paged.h"
 
@@ -27,14 +28,14 @@ struct PagedArgs {
   const float* scores;
   void* O;
   float* LSE;
-  float* part_o;    // [Hq * rows][count][D]
-  float* part_lse;  // [Hq * rows][count]
+  void* part_o;       // [Hq * rows][count][D], see Record
+  float* part_lse;    // [Hq * rows][count] log2-sum-exp2; -inf: no token, and no output
+  float* part_scale;  // [Hq * rows][count] of bf16 calls
   float scale_log2e;
   int row_pieces;  // of a row, its first ones: taken row by row
 };
 
-// Tiles of the matrix-core form.  Window tiles: entry e's start at floor(cu[e] * G / cols) + e, which leaves room for
-// ceil(new rows * G / cols) of them, since ceil(y - x) <= floor(y) - floor(x) + 1.
+// Tiles of the matrix-core form.
 struct TilePlan {
   int tiles;             // window tiles of a kv head
   int64_t window_units;  // tiles * pieces of a window * Hkv
@@ -51,6 +52,27 @@ __device__ __forceinline__ float weight_of(float a, float b) { return a == -INFI
 
 // Grids of more than 2^20 workgroups go on in y (a launch holds fewer than 2^32 threads in x).
 __device__ __forceinline__ int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// A piece's normalised output: fp32, or for bf16 calls fp16 beside a power of two above the row's largest value: half the
+// bytes, and 2^-12 of that value is a sixteenth of the step that rounds the result (bf16 there would be as large as that step).
+template <typename T>
+struct Record {
+  typedef float Value;
+};
+template <>
+struct Record<bf16_t> {
+  typedef _Float16 Value;
+};
+// a power of two from the largest of a row's finite values on (half of it at the end of fp32's range)
+__device__ __forceinline__ float scale_above(float largest) {
+  const int e = __builtin_amdgcn_frexp_expf(largest);
+  return largest > 0.f ? ldexpf(1.f, e < -100 ? -100 : e > 127 ? 127 : e) : 1.f;
+}
 
 struct RowPlace {
   int s, pos;  // sequence and position; pos < 0: a row without a token
@@ -165,44 +187,99 @@ __device__ __forceinline__ PieceRange range_of_piece(const PagedArgs& x, int pos
   return {(int)min(t0, (int64_t)pos + 1), (int)min(t0 + x.p.window_tokens, (int64_t)pos + 1)};
 }
 
-// One piece of a row and head by one wavefront, to its record.
-template <typename T, int D>
-__device__ __forceinline__ void take_piece(const PagedArgs& x, int s, int h, int row, const PieceRange& r, int64_t rec, int lane) {
+// One piece of a row and head by `WAVES` wavefronts of a workgroup, a run of its tokens each, to its record (or, DIRECT, to the
+// row's result).  s_o, s_ml: [WAVES][D] and [WAVES][2] of LDS.
+template <typename T, int D, int WAVES, bool DIRECT>
+__device__ __forceinline__ void take_piece(const PagedArgs& x, int s, int rh, const PieceRange& r, int64_t rec, float* s_o, float* s_ml) {
   using RS = RowState<T, D>;
+  const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
+  const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+  constexpr int RUN = 4 * RS::RPW;
+  const int run = ((r.t1 - r.t0 + WAVES - 1) / WAVES + RUN - 1) / RUN * RUN;
+  const int t0 = r.t0 + wave * run, t1 = min(t0 + run, r.t1);
   RS st;
   st.clear();
-  if (r.t0 < r.t1) {
+  if (t0 < t1) {
     float q[RS::EPL];
     Elem<T>::unpack(load16(static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst + lane % RS::LPR * RS::EPL), q);
 #pragma unroll
     for (int e = 0; e < RS::EPL; ++e) q[e] *= x.scale_log2e;
     const int64_t base = x.b.layer * x.c.layer + h / x.a.G * x.c.head;
     st.template attend<4>(x.c, static_cast<const T*>(x.c.K) + base, static_cast<const T*>(x.c.V) + base,
-                          x.c.tables + (int64_t)s * x.c.max_pages, q, r.t0, r.t1, lane);
+                          x.c.tables + (int64_t)s * x.c.max_pages, q, t0, t1, lane);
     st.join_groups();
   }
-  if (lane == 0) x.part_lse[rec] = st.m == -INFINITY ? -INFINITY : st.m + __log2f(st.l);
-  if (lane < RS::LPR && !(st.m == -INFINITY)) {
-    const float inv = 1.f / st.l;
+  float m = st.m, l = st.l;
+  if (WAVES > 1) {
+    if (lane == 0) {
+      s_ml[2 * wave] = m;
+      s_ml[2 * wave + 1] = l;
+    }
+    if (lane < RS::LPR) {
 #pragma unroll
-    for (int e = 0; e < RS::EPL; e += 4)
-      *reinterpret_cast<float4*>(x.part_o + rec * D + lane * RS::EPL + e) =
-          make_float4(st.o[e] * inv, st.o[e + 1] * inv, st.o[e + 2] * inv, st.o[e + 3] * inv);
+      for (int e = 0; e < RS::EPL; ++e) s_o[wave * D + lane * RS::EPL + e] = st.o[e];
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    m = s_ml[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) m = max_of(m, s_ml[2 * w]);
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < RS::EPL; ++e) st.o[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float f = weight_of(s_ml[2 * w], m);
+      if (s_ml[2 * w] == -INFINITY) continue;
+      l = fmaf(f, s_ml[2 * w + 1], l);
+#pragma unroll
+      for (int e = 0; e < RS::EPL; ++e) st.o[e] = fmaf(f, s_o[w * D + lane % RS::LPR * RS::EPL + e], st.o[e]);
+    }
   }
+  const bool none = m == -INFINITY;
+  const float lse = none ? m : m + __log2f(l), inv = none ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < RS::EPL; ++e) st.o[e] *= inv;
+  if (DIRECT) {
+    if (lane == 0 && x.LSE) x.LSE[rh] = lse * kLn2;
+    if (lane < RS::LPR)
+#pragma unroll
+      for (int e = 0; e < RS::EPL; ++e) Elem<T>::store1(static_cast<T*>(x.O) + (int64_t)rh * D + lane * RS::EPL + e, none ? 0.f : st.o[e]);
+    return;
+  }
+  if (lane == 0) x.part_lse[rec] = lse;
+  if (none) return;
+  typedef typename Record<T>::Value Value;
+  typedef Value Values __attribute__((ext_vector_type(RS::EPL)));
+  float by = 1.f;
+  if (sizeof(Value) == 2) {
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < RS::EPL; ++e) top = fmaxf(top, fabsf(st.o[e]) < INFINITY ? fabsf(st.o[e]) : 0.f);
+#pragma unroll
+    for (int off = 1; off < RS::LPR; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    const float scale = scale_above(top);
+    if (lane == 0) x.part_scale[rec] = scale;
+    by = 1.f / scale;
+  }
+  Values v;
+#pragma unroll
+  for (int e = 0; e < RS::EPL; ++e) v[e] = (Value)(st.o[e] * by);
+  if (lane < RS::LPR) *reinterpret_cast<Values*>(static_cast<Value*>(x.part_o) + rec * D + lane * RS::EPL) = v;
 }
 
-// Wavefront u takes piece u % row_pieces of row-and-head u / row_pieces.
+// Workgroup u takes piece u % row_pieces of row-and-head u / row_pieces.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void rows_kernel(const PagedArgs x) {
-  const int lane = threadIdx.x & 63;
-  const int64_t u = workgroup() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ float s_o[4 * D], s_ml[8];
+  const int64_t u = workgroup();
   if (u >= (int64_t)x.a.Hq * x.b.rows * x.row_pieces) return;
   const int rh = (int)(u / x.row_pieces), part = (int)(u - (int64_t)rh * x.row_pieces);
   const int h = rh / x.b.rows, row = rh - h * x.b.rows;
   if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
   const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, row), row);
   const PieceRange r = at.pos < 0 ? PieceRange{0, 0} : range_of_piece(x, at.pos, part, x.idx + h * x.a.ish + row * x.a.ist);
-  take_piece<T, D>(x, at.s, h, row, r, (int64_t)rh * x.p.count + part, lane);
+  take_piece<T, D, 4, false>(x, at.s, rh, r, (int64_t)rh * x.p.count + part, s_o, s_ml);
 }
 
 // ------------------------------------------------------------------ tiles on the matrix cores (bf16)
@@ -255,6 +332,16 @@ __device__ __forceinline__ uint32_t lds_address(const bf16_t* p, int offset) {
   uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) bf16_t*)p + offset;
   asm volatile("" : "+v"(at));
   return at;
+}
+
+// Two transposing reads: the lane's column of rows 0 .. 3 and 4 .. 7 behind p.
+template <int D>
+__device__ __forceinline__ bf16x8 transposed8(const bf16_t* __restrict__ p) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4* LdsPtr;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)p);
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(p + 4 * D));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // A wavefront's CB blocks of 32 columns; it takes 32 * KB tokens at a time.
@@ -364,17 +451,13 @@ struct Tile {
       }
     }
     __builtin_amdgcn_s_setprio(0);
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) s16x4* LdsPtr;
     const uint32_t va = lds_address(vt, vbase);
 #pragma unroll
     for (int ks = 0; ks < 2 * KB; ++ks)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const uint32_t at = (va ^ (dt << 6)) + 32 * ks * D;
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(uintptr_t)at);
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(uintptr_t)(at + 8 * D));
-        const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        const bf16x8 a = transposed8<D>((const bf16_t*)(const __attribute__((address_space(3))) bf16_t*)(uintptr_t)at);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) o[cb][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[cb][ks], o[cb][dt], 0, 0, 0);
       }
@@ -387,6 +470,30 @@ struct Tile {
     __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
   }
 };
+
+// The columns of a tile: rows and heads of one kv head's group, rows first.  Entry e's tiles start at floor(cu[e] * G / cols) + e, which
+// leaves room for ceil(new rows * G / cols) of them, since ceil(y - x) <= floor(y) - floor(x) + 1.
+struct ColumnRun {
+  int e, r0, r1;  // entry and its rows
+  int u0, n;      // columns u0 .. u0 + n - 1 of the entry: row r0 + u / G, head u % G of the group
+};
+__device__ __forceinline__ ColumnRun columns_of(const PagedArgs& x, int tile, int cols) {
+  int lo = 0, hi = x.b.B - 1;
+  auto first = [&](int e) { return (int)((int64_t)max(x.b.cu[e], 0) * x.a.G / cols) + e; };
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first(mid) <= tile) lo = mid;
+    else hi = mid - 1;
+  }
+  ColumnRun r;
+  r.e = lo;
+  r.r0 = x.b.cu[lo];
+  r.r1 = min(x.b.cu[lo + 1], x.b.rows);
+  const int64_t u0 = (int64_t)(tile - first(lo)) * cols, n = (int64_t)(r.r1 - r.r0) * x.a.G - u0;
+  r.u0 = (int)u0;
+  r.n = r.r0 < 0 || u0 < 0 || n <= 0 ? 0 : (int)min(n, (int64_t)cols);
+  return r;
+}
 
 // What a workgroup works on.
 struct TileWork {
@@ -405,7 +512,8 @@ __device__ __forceinline__ void stage_barrier() {  // (LDS operations and the st
 template <int D, int NW, int CB, int STEP>
 __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
   constexpr int COLS = NW * 32 * CB;
-  __shared__ __align__(1024) bf16_t s_kv[2][2][STEP * D];
+  extern __shared__ __align__(1024) char s_dynamic[];  // (static, the compiler would wait for staging loads at every read)
+  bf16_t(*const s_kv)[2][STEP * D] = reinterpret_cast<bf16_t(*)[2][STEP * D]>(s_dynamic);
   __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS];
   __shared__ int s_range[2 * NW];
   const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -418,23 +526,17 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
     w.head = (int)(unit % x.c.Hkv);
     const int at = (int)(unit / x.c.Hkv), tile = plan.tiles - 1 - at / x.p.window, piece = at % x.p.window;
     part = x.a.topk * x.p.routed + piece;
-    int lo = 0, hi = x.b.B - 1;
-    while (lo < hi) {  // entry e's tiles start at cu[e] * G / COLS + e
-      const int mid = (lo + hi + 1) >> 1;
-      if ((int)((int64_t)max(x.b.cu[mid], 0) * x.a.G / COLS) + mid <= tile) lo = mid;
-      else hi = mid - 1;
-    }
-    const int e = lo, r0 = x.b.cu[e], r1 = min(x.b.cu[e + 1], x.b.rows);
-    const int u0 = (tile - ((int)((int64_t)max(r0, 0) * x.a.G / COLS) + e)) * COLS;
-    if (r0 < 0 || u0 >= (int64_t)(r1 - r0) * x.a.G) return;
-    w.s = x.b.seqs[e];
-    const int len = length_of(x.c, w.s), pos0 = len - (x.b.cu[e + 1] - r0);
+    const ColumnRun run = columns_of(x, tile, COLS);
+    if (run.n <= 0) return;
+    const int r0 = run.r0, u0 = run.u0;
+    w.s = x.b.seqs[run.e];
+    const int len = length_of(x.c, w.s), pos0 = len - (x.b.cu[run.e + 1] - r0);
     const int first = max(pos0 + u0 / x.a.G, 0);  // position of the tile's first row that has a token
     const int64_t origin = (int64_t)(first / x.a.S) * x.a.S / 16 * 16 + (int64_t)piece * x.p.window_tokens;
     for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
       const int u = u0 + c, row = r0 + u / x.a.G, pos = pos0 + u / x.a.G;
       int rh = -1, clo = INT_MAX, clast = -1;
-      if (row < r1) {
+      if (c < run.n) {
         rh = (w.head * x.a.G + u % x.a.G) * x.b.rows + row;
         if (pos >= 0 && pos < len && pos < x.b.L) {
           clo = (int)max((int64_t)(pos / x.a.S) * x.a.S, min(origin, (int64_t)INT_MAX));
@@ -535,12 +637,11 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
     live[b] = (uint32_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages) & ((1u << GROUPS) - 1);
 #pragma unroll
     for (int i = 0; i < GROUPS / NW; ++i) {
-      const int g = NW == 1 ? i : wave, r0 = g * 16, t = t0 + r0;
+      const int g = NW == 1 ? i : wave, r0 = g * 16, t = __builtin_amdgcn_readfirstlane(t0 + r0);
       const bool on = live[b] >> g & 1;
       const int rows = on ? min(w.end - t, 16) : 0;
-      const int64_t at = on ? base + __builtin_amdgcn_readlane(page, g) * x.c.page +
-                                  (int64_t)((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps) * x.c.tok
-                            : 0;
+      const int in_page = __builtin_amdgcn_readfirstlane((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps);
+      const int64_t at = on ? uniform64(base + __builtin_amdgcn_readlane(page, g) * x.c.page + in_page * x.c.tok) : 0;
       stage_rows<D, 0>(&s_kv[b][0][r0 * D], r0, static_cast<const bf16_t*>(x.c.K) + at, rows, row_bytes, lane);
       stage_rows<D, 1>(&s_kv[b][1][r0 * D], r0, static_cast<const bf16_t*>(x.c.V) + at, rows, row_bytes, lane);
     }
@@ -570,24 +671,51 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
     const int item = s_rh[wave * 32 * CB + cb * 32 + (lane & 31)];
     const float sum = across_halves_sum(tile.l[cb]);
     const float inv = 1.f / sum;
-    float check = 0.f;
+    float check = 0.f, top = 0.f;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) check = fmaf(tile.o[cb][dt][r], 0.f, check);
+      for (int r = 0; r < 16; ++r) {
+        check = fmaf(tile.o[cb][dt][r], 0.f, check);
+        top = max_of(top, fabsf(tile.o[cb][dt][r]));
+      }
     check = across_halves_sum(check);
+    top = across_halves_max(top);
     if (item < 0) continue;
-    const int64_t rec = (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
     const bool none = tile.m[cb] == -INFINITY;
-    if (lane < 32) x.part_lse[rec] = none ? -INFINITY : check == 0.f ? tile.m[cb] + __log2f(sum) : NAN;
+    const float lse = none ? -INFINITY : check == 0.f ? tile.m[cb] + __log2f(sum) : NAN;
+    typedef _Float16 Half4 __attribute__((ext_vector_type(4)));
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    const int64_t rec = (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
+    if (lane < 32) x.part_lse[rec] = lse;
+    if (x.p.count == 1) {  // the row's result
+      if (lane < 32 && x.LSE) x.LSE[rec] = lse * kLn2;
+      bf16_t* const to = static_cast<bf16_t*>(x.O) + rec * D + 4 * (lane >> 5);
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : tile.o[cb][dt][4 * g + e] * inv;
+          *reinterpret_cast<bf16x4*>(to + dt * 32 + g * 8) = __builtin_convertvector(v, bf16x4);
+        }
+      continue;
+    }
     if (none) continue;
-    float* const to = x.part_o + rec * D + 4 * (lane >> 5);
+    const float scale = scale_above(top * inv), by = inv / scale;
+    if (lane < 32) x.part_scale[rec] = scale;
+    _Float16* const to = static_cast<_Float16*>(x.part_o) + rec * D + 4 * (lane >> 5);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4*>(to + dt * 32 + g * 8) = make_float4(tile.o[cb][dt][4 * g] * inv, tile.o[cb][dt][4 * g + 1] * inv,
-                                                                      tile.o[cb][dt][4 * g + 2] * inv, tile.o[cb][dt][4 * g + 3] * inv);
+      for (int g = 0; g < 4; ++g) {
+        Half4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (_Float16)(tile.o[cb][dt][4 * g + e] * by);
+        *reinterpret_cast<Half4*>(to + dt * 32 + g * 8) = v;
+      }
   }
 }
 
@@ -596,24 +724,44 @@ __global__ __launch_bounds__(256) void zero_kernel(int32_t* __restrict__ to, int
   for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) to[i] = 0;
 }
 
-// One thread a row and head.  Pieces of empty slots are marked here: no tile writes them.
+// An item's place in its bucket.  A workgroup takes kCountCols columns (rows and heads of an entry's kv head, as a window tile does): it
+// counts them in LDS, adds its counts to the buckets', and hands out the places that it got; their order among workgroups
+// may differ from run to run, which no result depends on.  Atomics on the buckets alone took 188 us for 512000 items of 512 buckets.
+// Pieces of empty slots are marked here: no tile writes them.
+constexpr int kCountCols = 1024, kCountSpans = 12288;
 __global__ __launch_bounds__(256) void count_kernel(const PagedArgs x, const TilePlan plan) {
-  const int64_t rh = workgroup() * 256 + threadIdx.x;
-  if (rh >= (int64_t)x.a.Hq * x.b.rows) return;
-  const int h = (int)(rh / x.b.rows), row = (int)(rh - (int64_t)h * x.b.rows);
-  if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
-  const int e = entry_of_row(x.b.cu, x.b.B, row);
-  const RowPlace at = place_of_row(x, e, row);
-  const int c = at.pos < 0 ? 0 : at.pos / x.a.S;
-  const int32_t* const slots = x.idx + h * x.a.ish + row * x.a.ist;
-  const int first = (e * x.c.Hkv + h / x.a.G) * plan.spans;
-  for (int k = 0; k < x.a.topk; ++k) {
-    const int j = slots[k];
-    if (j >= 0 && j < c) {
-      plan.ranks[rh * x.a.topk + k] = atomicAdd(&plan.counts[first + j], 1);
-    } else {
-      plan.ranks[rh * x.a.topk + k] = -1;
-      for (int q = 0; q < x.p.routed; ++q) x.part_lse[rh * x.p.count + k * x.p.routed + q] = -INFINITY;
+  extern __shared__ int32_t s_count[];  // [spans], if they fit
+  const int head = blockIdx.y;
+  const ColumnRun run = columns_of(x, blockIdx.x, kCountCols);
+  if (run.n <= 0) return;
+  const bool local = plan.spans <= kCountSpans;
+  if (local)
+    for (int j = threadIdx.x; j < plan.spans; j += 256) s_count[j] = 0;
+  __syncthreads();
+  int32_t* const counts = plan.counts + ((int64_t)run.e * x.c.Hkv + head) * plan.spans;
+  const int s = x.b.seqs[run.e], len = length_of(x.c, s), end = x.b.cu[run.e + 1];
+  for (int pass = local ? 0 : 1; pass < 2; ++pass) {
+    for (int u = threadIdx.x; u < run.n; u += 256) {
+      const int row = run.r0 + (run.u0 + u) / x.a.G, h = head * x.a.G + (run.u0 + u) % x.a.G;
+      const int pos = len - (end - row), c = pos >= 0 && pos < len && pos < x.b.L ? pos / x.a.S : 0;
+      const int64_t rh = (int64_t)h * x.b.rows + row;
+      const int32_t* const slots = x.idx + h * x.a.ish + row * x.a.ist;
+      for (int k = 0; k < x.a.topk; ++k) {
+        const int j = slots[k];
+        if (j >= 0 && j < c) {
+          if (pass == 0) atomicAdd(&s_count[j], 1);
+          else plan.ranks[rh * x.a.topk + k] = local ? atomicAdd(&s_count[j], 1) : atomicAdd(&counts[j], 1);
+        } else if (pass == 1) {
+          plan.ranks[rh * x.a.topk + k] = -1;
+          for (int q = 0; q < x.p.routed; ++q) x.part_lse[rh * x.p.count + k * x.p.routed + q] = -INFINITY;
+        }
+      }
+    }
+    if (pass == 0) {
+      __syncthreads();
+      for (int j = threadIdx.x; j < plan.spans; j += 256)
+        if (s_count[j]) s_count[j] = atomicAdd(&counts[j], s_count[j]);
+      __syncthreads();
     }
   }
 }
@@ -665,43 +813,88 @@ __global__ __launch_bounds__(256) void items_kernel(const PagedArgs x, const Til
 }
 
 // ------------------------------------------------------------------ merge
-// A workgroup joins the pieces of one row and head: weights to LDS, then D / 4 lanes a piece.
+// Pieces that a tile marked, once more, row by row: of the window, whose tiles cut it where they like, all into its first record.
+// By one wavefront.
 template <typename T, int D>
+__device__ __forceinline__ void take_marked(const PagedArgs& x, int rh, int h, int row) {
+  const float* const lse = x.part_lse + (int64_t)rh * x.p.count;
+  const int routed = x.a.topk * x.p.routed, lane = threadIdx.x & 63;
+  const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, row), row);
+  bool near = false;
+  for (int k = x.row_pieces; k < x.p.count; ++k) {
+    if (lse[k] == lse[k]) continue;
+    if (k < routed)
+      take_piece<T, D, 1, false>(x, at.s, rh, range_of_piece(x, at.pos, k, x.idx + h * x.a.ish + row * x.a.ist), (int64_t)rh * x.p.count + k,
+                                 nullptr, nullptr);
+    else near = true;
+  }
+  if (near) {
+    take_piece<T, D, 1, false>(x, at.s, rh, {at.pos / x.a.S * x.a.S, at.pos + 1}, (int64_t)rh * x.p.count + routed, nullptr, nullptr);
+    for (int k = routed + 1 + lane; k < x.p.count; k += 64) x.part_lse[(int64_t)rh * x.p.count + k] = -INFINITY;
+  }
+  __threadfence_block();
+}
+
+// One piece a row: the tiles wrote the results themselves.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void mend_kernel(const PagedArgs x) {
+  const int64_t n = (int64_t)x.a.Hq * x.b.rows;
+  const int lane = threadIdx.x & 63;
+  const int64_t first = (workgroup() * 4 + (threadIdx.x >> 6)) * 64, mine = first + lane;
+  const int at_row = (int)(mine % x.b.rows);
+  const bool on = mine < n && at_row >= x.b.cu[0] && at_row < x.b.cu[x.b.B];
+  const float lse = on ? x.part_lse[mine] : 0.f;
+  uint64_t marked = __builtin_amdgcn_ballot_w64(lse != lse);
+  while (marked) {
+    const int rh = (int)first + __builtin_ctzll(marked);
+    marked &= marked - 1;
+    const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, rh % x.b.rows), rh % x.b.rows);
+    take_piece<T, D, 1, true>(x, at.s, rh, {at.pos / x.a.S * x.a.S, at.pos + 1}, 0, nullptr, nullptr);
+  }
+}
+
+// WAVES wavefronts (of a workgroup's four) join the pieces of one row and head: weights to LDS, then D / 8 (fp32: D / 4) lanes
+// a piece.
+template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
-  extern __shared__ float s_w[];  // [count]
-  __shared__ float s_red[8];
-  __shared__ float s_gate[SL_MAX_TOPK], s_lse[SL_MAX_TOPK];
-  constexpr int LANES = D / 4, GROUPS = 256 / LANES;
-  __shared__ float4 s_o[GROUPS][LANES];
-  if (workgroup() >= (int64_t)x.a.Hq * x.b.rows) return;
-  const int rh = (int)workgroup(), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, P = x.p.count;
+  typedef typename Record<T>::Value Value;
+  constexpr int EPL = 16 / sizeof(Value), LANES = D / EPL, GROUPS = 64 * WAVES / LANES;
+  typedef Value Values __attribute__((ext_vector_type(EPL)));
+  extern __shared__ float s_dyn[];  // [4 / WAVES][count] weights
+  __shared__ float s_red[4];
+  __shared__ float s_gates[4 / WAVES][SL_MAX_TOPK], s_lses[4 / WAVES][SL_MAX_TOPK];
+  __shared__ float s_out[WAVES == 1 ? 1 : GROUPS * D];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = WAVES == 1 ? lane : threadIdx.x, P = x.p.count;
+  const int64_t unit = WAVES == 1 ? workgroup() * 4 + wave : workgroup();
+  if (unit >= (int64_t)x.a.Hq * x.b.rows) return;
+  const int rh = (int)unit, sub = WAVES == 1 ? wave : 0;
   const int h = rh / x.b.rows, row = rh - h * x.b.rows;
   if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
+  float* const s_w = s_dyn + sub * P;
+  float *const s_gate = s_gates[sub], *const s_lse = s_lses[sub];
   const float* const lse = x.part_lse + (int64_t)rh * P;
-  const int routed = x.a.topk * x.p.routed;
+  auto barrier = [] {
+    if (WAVES > 1) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  };
+  constexpr int N = 64 * WAVES;
   if (x.row_pieces < P) {
-    // Pieces that a tile marked: once more, row by row.  Of the window, whose tiles cut it where they like, all into its first record.
     bool marked = false;
-    for (int k = x.row_pieces + tid; k < P; k += 256) marked = marked || lse[k] != lse[k];
-    if (__syncthreads_or(marked)) {
-      const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, row), row);
-      const int32_t* const slots = x.idx + h * x.a.ish + row * x.a.ist;
-      bool near = false;
-      for (int k = routed; k < P; ++k) near = near || lse[k] != lse[k];
-      __syncthreads();
-      for (int k = x.row_pieces + wave; k < routed; k += 4)
-        if (lse[k] != lse[k]) take_piece<T, D>(x, at.s, h, row, range_of_piece(x, at.pos, k, slots), (int64_t)rh * P + k, lane);
-      if (near) {
-        if (wave == 0) take_piece<T, D>(x, at.s, h, row, {at.pos / x.a.S * x.a.S, at.pos + 1}, (int64_t)rh * P + routed, lane);
-        for (int k = routed + 1 + tid; k < P; k += 256) x.part_lse[(int64_t)rh * P + k] = -INFINITY;
-      }
-      __threadfence_block();
-      __syncthreads();
+    for (int k = x.row_pieces + tid; k < P; k += N) marked = marked || lse[k] != lse[k];
+    const bool any = WAVES > 1 ? __syncthreads_or(marked) : __builtin_amdgcn_ballot_w64(marked) != 0;
+    if (any) {
+      if (WAVES == 1 || wave == 0) take_marked<T, D>(x, rh, h, row);
+      barrier();
     }
   }
   auto all_max = [&](float v) {
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) v = max_of(v, __shfl_xor(v, off, 64));
+    if (WAVES == 1) return v;
     __syncthreads();
     if (lane == 0) s_red[wave] = v;
     __syncthreads();
@@ -710,6 +903,7 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   auto all_sum = [&](float v) {
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+    if (WAVES == 1) return v;
     __syncthreads();
     if (lane == 0) s_red[wave] = v;
     __syncthreads();
@@ -718,14 +912,14 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   // log2-sum-exp2 of pieces [from, to)
   auto lse_of = [&](int from, int to) {
     float v = -INFINITY;
-    for (int k = from + tid; k < to; k += 256) v = max_of(v, lse[k]);
+    for (int k = from + tid; k < to; k += N) v = max_of(v, lse[k]);
     const float m = all_max(v);
     if (m == -INFINITY) return m;
     float l = 0.f;
-    for (int k = from + tid; k < to; k += 256) l += weight_of(lse[k], m);
+    for (int k = from + tid; k < to; k += N) l += weight_of(lse[k], m);
     return m + __log2f(all_sum(l));
   };
-  float total = -INFINITY;
+  const int routed = x.a.topk * x.p.routed;
   bool any = false;  // a slot holds a span
   if (x.a.combined) {
     const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, row), row);
@@ -743,14 +937,14 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
       for (int k = 0; k < x.p.routed; ++k) l += weight_of(lse[tid * x.p.routed + k], m);
       s_lse[tid] = m == -INFINITY ? m : m + __log2f(l);
     }
-    any = __syncthreads_or(mine);
+    any = WAVES > 1 ? __syncthreads_or(mine) : __builtin_amdgcn_ballot_w64(mine) != 0;
     if (any) {
       const float top = all_max(score);
       const float e = mine ? fast_exp2((score - top) * kLog2e) : 0.f;
       const float sum = all_sum(e);
       if (tid < x.a.topk) s_gate[tid] = e / sum;
-      __syncthreads();
-      for (int k = tid; k < P; k += 256) {
+      barrier();
+      for (int k = tid; k < P; k += N) {
         float w = 0.f;
         if (k < routed) {
           const int t = k / x.p.routed;
@@ -764,30 +958,65 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
     }
   }
   if (!any) {
-    total = lse_of(x.a.combined ? routed : 0, P);
-    for (int k = tid; k < P; k += 256) s_w[k] = x.a.combined && k < routed ? 0.f : weight_of(lse[k], total);
+    const float total = lse_of(x.a.combined ? routed : 0, P);
+    for (int k = tid; k < P; k += N) s_w[k] = x.a.combined && k < routed ? 0.f : weight_of(lse[k], total);
     if (tid == 0 && x.LSE) x.LSE[rh] = total * kLn2;
   }
-  __syncthreads();
-  const int g = tid / LANES, c = tid % LANES;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  const float4* const po = reinterpret_cast<const float4*>(x.part_o + (int64_t)rh * P * D) + c;
-  for (int k = g; k < P; k += GROUPS) {
-    const float w = s_w[k];
-    if (w == 0.f) continue;  // (a piece without tokens has written no output)
-    const float4 v = po[(int64_t)k * LANES];
-    acc.x = fmaf(w, v.x, acc.x);
-    acc.y = fmaf(w, v.y, acc.y);
-    acc.z = fmaf(w, v.z, acc.z);
-    acc.w = fmaf(w, v.w, acc.w);
+  barrier();
+  if (sizeof(Value) == 2) {  // (a piece without tokens has written neither output nor scale)
+    for (int k = tid; k < P; k += N)
+      if (s_w[k] != 0.f) s_w[k] *= x.part_scale[(int64_t)rh * P + k];
+    barrier();
   }
-  s_o[g][c] = acc;
-  __syncthreads();
-  if (tid < D) {
-    float v = 0.f;
+  const int g = tid / LANES, c = tid % LANES;
+  float acc[EPL];
 #pragma unroll
-    for (int k = 0; k < GROUPS; ++k) v += reinterpret_cast<const float*>(s_o[k])[tid];
-    Elem<T>::store1(static_cast<T*>(x.O) + (int64_t)rh * D + tid, v);
+  for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
+  const Values* const po = reinterpret_cast<const Values*>(static_cast<const Value*>(x.part_o) + (int64_t)rh * P * D) + c;
+  constexpr int U = 4;  // pieces asked for at once
+  for (int k0 = g; k0 < P; k0 += U * GROUPS) {
+    Values v[U];
+    float w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u * GROUPS;
+      w[u] = k < P ? s_w[k] : 0.f;
+      if (w[u] != 0.f) v[u] = __builtin_nontemporal_load(po + (int64_t)k * LANES);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (w[u] != 0.f) {
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) acc[e] = fmaf(w[u], (float)v[u][e], acc[e]);
+      }
+  }
+  if (WAVES == 1) {
+#pragma unroll
+    for (int off = LANES; off < 64; off <<= 1)
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) acc[e] += __shfl_xor(acc[e], off, 64);
+    if (g == 0) {
+      T* const to = static_cast<T*>(x.O) + (int64_t)rh * D + c * EPL;
+      if constexpr (sizeof(T) == 2) {
+        typedef __bf16 Out __attribute__((ext_vector_type(EPL)));
+        Out v;
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) v[e] = (__bf16)acc[e];
+        *reinterpret_cast<Out*>(to) = v;
+      } else {
+        *reinterpret_cast<float4*>(to) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) s_out[g * D + c * EPL + e] = acc[e];
+    __syncthreads();
+    if (tid < D) {
+      float v = 0.f;
+#pragma unroll
+      for (int k = 0; k < GROUPS; ++k) v += s_out[k * D + tid];
+      Elem<T>::store1(static_cast<T*>(x.O) + (int64_t)rh * D + tid, v);
+    }
   }
 }
 
@@ -813,9 +1042,9 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   Form f = {};
   // Sixteen rows of a stage lie in one page, and 16 token strides within a buffer's 32-bit offsets.
   const bool tiles = c.dtype == SL_BF16 && c.ps % 16 == 0 && c.tok < ((int64_t)1 << 26) && rh < ((int64_t)1 << 26);
-  f.window_tiles = tiles;
   const int64_t spans = div_up(b.L, a.S), buckets = (int64_t)b.B * c.Hkv * spans, items = rh * a.topk;
   f.routed_tiles = tiles && a.topk > 0 && items >= 4 * buckets && items < ((int64_t)1 << 30);
+  f.window_tiles = tiles && (f.routed_tiles || a.topk < 2);
   const int64_t columns = (int64_t)b.rows * a.G;  // of a kv head
   f.cols_log2 = columns <= 32 * (int64_t)b.B && !f.routed_tiles ? 5 : 7;
   const int cols = 1 << f.cols_log2;
@@ -832,7 +1061,7 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
     p.routed_tokens = (int)div_up(div_up(a.S, cut(a.S, units, f.routed_tiles ? 1024 : 4096, 64)), 16) * 16;
     p.routed = (int)div_up(a.S, p.routed_tokens);
   }
-  if (tiles) {
+  if (f.window_tiles) {
     f.plan.tiles = (int)(columns / cols) + b.B;
     const int64_t longest = window + cols / a.G + 17;  // a tile's rows may lie in two windows; it begins at a multiple of 16
     const int64_t n = cut(longest, (int64_t)f.plan.tiles * c.Hkv, cols == 32 ? 2048 : 1024, 256);
@@ -844,7 +1073,7 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
     p.window = (int)div_up(window, p.window_tokens);
   }
   p.count = a.topk * p.routed + p.window;
-  f.o_bytes = align_up((size_t)rh * p.count * c.D * sizeof(float), 256);
+  f.o_bytes = align_up((size_t)rh * p.count * c.D * (c.dtype == SL_BF16 ? sizeof(_Float16) : sizeof(float)), 256);
   f.lse_bytes = align_up((size_t)rh * p.count * sizeof(float), 256);
   if (f.routed_tiles) {
     f.plan.spans = (int)spans;
@@ -855,10 +1084,24 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   return f;
 }
 
+// The stages of a tile of 128 columns fill 64 KB of dynamic LDS beside the static arrays: more than a kernel has without asking.
 template <int D, int NW, int CB, int STEP>
-void launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
+bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
+  constexpr int kBytes = 2 * 2 * STEP * D * (int)sizeof(bf16_t);
+  static std::mutex mu;
+  static bool asked[64];
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return false;
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    if (!asked[dev])
+      asked[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(tile_kernel<D, NW, CB, STEP>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                       kBytes) == hipSuccess;
+    if (!asked[dev]) return false;
+  }
   const int64_t units = plan.window_units + (f.routed_tiles ? f.most_tiles * f.p.routed : 0);
-  tile_kernel<D, NW, CB, STEP><<<grid_of(units), 64 * NW, 0, st>>>(x, plan);
+  tile_kernel<D, NW, CB, STEP><<<grid_of(units), 64 * NW, kBytes, st>>>(x, plan);
+  return true;
 }
 
 template <typename T, int D>
@@ -868,7 +1111,7 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
     if (f.window_tiles) {
       TilePlan plan = f.plan;
       if (f.routed_tiles) {
-        plan.counts = reinterpret_cast<int32_t*>(ws + f.o_bytes + f.lse_bytes);
+        plan.counts = reinterpret_cast<int32_t*>(ws + f.o_bytes + 2 * f.lse_bytes);
         plan.first_tile = plan.counts + plan.buckets;
         plan.tile_count = plan.first_tile + plan.buckets;
         plan.tile_bucket = plan.tile_count + 64;
@@ -876,16 +1119,19 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
         plan.items = plan.ranks + rh * x.a.topk;
         const int64_t blocks = div_up(plan.buckets, 1024);
         zero_kernel<<<(unsigned)(blocks < 1024 ? blocks : 1024), 256, 0, st>>>(plan.counts, plan.buckets);
-        count_kernel<<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x, plan);
+        const int64_t runs = (int64_t)x.b.rows * x.a.G / kCountCols + x.b.B;
+        count_kernel<<<dim3((unsigned)runs, x.c.Hkv), 256, plan.spans <= kCountSpans ? plan.spans * sizeof(int32_t) : 0, st>>>(x, plan);
         tiles_kernel<<<1, 1024, 0, st>>>(plan, f.cols_log2);
         items_kernel<<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x, plan, f.cols_log2);
       }
-      if (f.cols_log2 == 5) launch_tiles<D, 1, 1, 32>(x, f, plan, st);
-      else launch_tiles<D, 4, 1, 64>(x, f, plan, st);
+      if (!(f.cols_log2 == 5 ? launch_tiles<D, 1, 1, 32>(x, f, plan, st) : launch_tiles<D, 4, 1, 64>(x, f, plan, st))) return SL_ERR_LAUNCH;
     }
   }
-  if (x.row_pieces > 0) rows_kernel<T, D><<<grid_of(div_up(rh * x.row_pieces, 4)), 256, 0, st>>>(x);
-  merge_kernel<T, D><<<grid_of(rh), 256, x.p.count * sizeof(float), st>>>(x);
+  if (x.row_pieces > 0) rows_kernel<T, D><<<grid_of(rh * x.row_pieces), 256, 0, st>>>(x);
+  if (x.p.count == 1 && x.row_pieces == 0) mend_kernel<T, D><<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x);
+  // a wavefront a row and head where there are enough of them
+  else if (rh >= 4096 && x.p.count <= 1024) merge_kernel<T, D, 1><<<grid_of(div_up(rh, 4)), 256, 4 * x.p.count * sizeof(float), st>>>(x);
+  else merge_kernel<T, D, 4><<<grid_of(rh), 256, x.p.count * sizeof(float), st>>>(x);
   return hipGetLastError() == hipSuccess ? SL_OK : SL_ERR_LAUNCH;
 }
 
@@ -893,14 +1139,15 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
 
 size_t paged_attention_ws_bytes(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   const Form f = form_of(c, b, a);
-  return f.o_bytes + f.lse_bytes + f.plan_bytes;
+  return f.o_bytes + 2 * f.lse_bytes + f.plan_bytes;
 }
 
 sl_status paged_attention(const PageCache& c, const PagedBatch& b, const PagedAttention& a, const void* Q, const int32_t* idx,
                           const float* scores, void* O, float* LSE, void* ws, hipStream_t st) {
   const Form f = form_of(c, b, a);
   char* const at = static_cast<char*>(ws);
-  PagedArgs x = {c, b, a, f.p, Q, idx, scores, O, LSE, static_cast<float*>(ws), reinterpret_cast<float*>(at + f.o_bytes), a.scale * kLog2e,
+  PagedArgs x = {c, b, a, f.p, Q, idx, scores, O, LSE, ws, reinterpret_cast<float*>(at + f.o_bytes),
+                 reinterpret_cast<float*>(at + f.o_bytes + f.lse_bytes), a.scale * kLog2e,
                  f.routed_tiles ? 0 : f.window_tiles ? a.topk * f.p.routed : f.p.count};
   if (c.dtype == SL_BF16) return c.D == 128 ? launch<bf16_t, 128>(x, f, at, st) : launch<bf16_t, 64>(x, f, at, st);
   return c.D == 128 ? launch<float, 128>(x, f, at, st) : launch<float, 64>(x, f, at, st);
