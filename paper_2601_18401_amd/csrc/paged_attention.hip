@@ -74,12 +74,37 @@ __device__ __forceinline__ float scale_above(float largest) {
   return largest > 0.f ? ldexpf(1.f, e < -100 ? -100 : e > 127 ? 127 : e) : 1.f;
 }
 
-struct RowPlace {
-  int s, pos;  // sequence and position; pos < 0: a row without a token
+// An entry of the batch as a wavefront sees it (all lanes alike).
+struct Entry {
+  int e, s, len;  // entry, sequence and its length (-1: no such sequence)
+  int r0, r1;     // cu[e], cu[e + 1]
 };
-__device__ __forceinline__ RowPlace place_of_row(const PagedArgs& x, int e, int row) {
-  const int s = x.b.seqs[e], len = length_of(x.c, s), pos = len - (x.b.cu[e + 1] - row);
-  return {s, pos >= len || pos >= x.b.L ? -1 : pos};
+// The last entry e with before(cu[e], e), which holds for entry 0 and up to some entry: 64 of them are looked at at once, with all that
+// is asked of the one that is found.  (A binary search is a chain of loads: a piece of 64 tokens took as long to find as to attend.)
+template <typename F>
+__device__ __forceinline__ Entry find_entry(const PagedArgs& x, F&& before) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = x.b.B;
+  while (n > 64) {
+    const int step = (n + 63) / 64, at = lo + lane * step;
+    const bool in = at < lo + n && before(x.b.cu[min(at, x.b.B - 1)], at);
+    const int k = max(__popcll(__builtin_amdgcn_ballot_w64(in)) - 1, 0);
+    n = min(step, n - k * step);
+    lo += k * step;
+  }
+  const int at = min(lo + lane, x.b.B - 1);
+  const int r0 = x.b.cu[at], r1 = x.b.cu[at + 1], s = x.b.seqs[at], len = length_of(x.c, s);
+  const int k = max(__popcll(__builtin_amdgcn_ballot_w64(lane < n && before(r0, at))) - 1, 0);
+  return {lo + k, __builtin_amdgcn_readlane(s, k), __builtin_amdgcn_readlane(len, k), __builtin_amdgcn_readlane(r0, k),
+          __builtin_amdgcn_readlane(r1, k)};
+}
+__device__ __forceinline__ Entry entry_with_row(const PagedArgs& x, int row) {
+  return find_entry(x, [=](int r0, int) { return r0 <= row; });
+}
+// position of a row; < 0: a row without a token
+__device__ __forceinline__ int position_of(const PagedArgs& x, const Entry& e, int row) {
+  const int pos = e.len - (e.r1 - row);
+  return pos >= e.len || pos >= x.b.L ? -1 : pos;
 }
 
 // ------------------------------------------------------------------ row by row
@@ -276,9 +301,10 @@ __global__ __launch_bounds__(256) void rows_kernel(const PagedArgs x) {
   if (u >= (int64_t)x.a.Hq * x.b.rows * x.row_pieces) return;
   const int rh = (int)(u / x.row_pieces), part = (int)(u - (int64_t)rh * x.row_pieces);
   const int h = rh / x.b.rows, row = rh - h * x.b.rows;
-  if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
-  const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, row), row);
-  const PieceRange r = at.pos < 0 ? PieceRange{0, 0} : range_of_piece(x, at.pos, part, x.idx + h * x.a.ish + row * x.a.ist);
+  const Entry at = entry_with_row(x, row);
+  if (row < at.r0 || row >= at.r1) return;
+  const int pos = position_of(x, at, row);
+  const PieceRange r = pos < 0 ? PieceRange{0, 0} : range_of_piece(x, pos, part, x.idx + h * x.a.ish + row * x.a.ist);
   take_piece<T, D, 4, false>(x, at.s, rh, r, (int64_t)rh * x.p.count + part, s_o, s_ml);
 }
 
@@ -307,6 +333,13 @@ __device__ __forceinline__ float across_halves_max(float v) {
 __device__ __forceinline__ float across_halves_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
   return __int_as_float(r[0]) + __int_as_float(r[1]);
+}
+
+// The lane's number, derived where it is used: two blocks of columns leave no register for what can be had again.
+__device__ __forceinline__ int lane_now() {
+  int x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(x));
+  return x;
 }
 
 #define SL_LDS(p) ((__attribute__((address_space(3))) void*)(p))
@@ -351,7 +384,6 @@ struct Tile {
   bf16x8 q[CB][KK];
   f32x16 o[CB][DT];
   float m[CB], l[CB];
-  int lo[CB], last[CB];  // tokens that the lane's column attends
   int kbase, vbase;
 
   __device__ __forceinline__ void clear(int lane) {
@@ -370,8 +402,10 @@ struct Tile {
         for (int r = 0; r < 16; ++r) o[cb][dt][r] = 0.f;
     }
   }
-  // 32 * KB tokens from t0 on, K rows at kt, V rows at vt (LDS); live: a bit for each sixteen of them whose page there is
-  __device__ __forceinline__ void attend(const bf16_t* kt, const bf16_t* vt, int t0, bool masked, uint32_t live, float sc, int lane) {
+  // 32 * KB tokens from t0 on, K rows at kt, V rows at vt (LDS); live: a bit for each sixteen of them whose page there is;
+  // lo, last (LDS): what each of the wavefront's columns attends
+  __device__ __forceinline__ void attend(const bf16_t* kt, const bf16_t* vt, int t0, bool masked, uint32_t live, float sc, const int* lo,
+                                         const int* last) {
     f32x16 s[CB][KB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
@@ -398,16 +432,19 @@ struct Tile {
     __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     __builtin_amdgcn_s_setprio(3);  // (few of the vector instructions fit beside another wavefront's products)
     if (masked) {
-      const int at = t0 + 8 * (lane >> 5);
+      const int ln = lane_now();
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb)
+      for (int cb = 0; cb < CB; ++cb) {
+        const int from = lo[32 * cb + (ln & 31)], width = last[32 * cb + (ln & 31)] - from;  // (nothing: INT_MAX, and below 0)
+        const int at = t0 + 8 * (ln >> 5) - from;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int t = at + 32 * kb + 16 * (r >> 3) + (r & 7);
-            s[cb][kb][r] = t >= lo[cb] && t <= last[cb] && (live >> (2 * kb + (r >> 3)) & 1) ? s[cb][kb][r] : -INFINITY;
+            s[cb][kb][r] = t >= 0 && t <= width && (live >> (2 * kb + (r >> 3)) & 1) ? s[cb][kb][r] : -INFINITY;
           }
+      }
     }
     bool grow[CB], any = false;
     float top[CB];
@@ -474,201 +511,254 @@ struct Tile {
 // The columns of a tile: rows and heads of one kv head's group, rows first.  Entry e's tiles start at floor(cu[e] * G / cols) + e, which
 // leaves room for ceil(new rows * G / cols) of them, since ceil(y - x) <= floor(y) - floor(x) + 1.
 struct ColumnRun {
-  int e, r0, r1;  // entry and its rows
-  int u0, n;      // columns u0 .. u0 + n - 1 of the entry: row r0 + u / G, head u % G of the group
+  Entry at;
+  int u0, n;  // columns u0 .. u0 + n - 1 of the entry: row r0 + u / G, head u % G of the group
 };
 __device__ __forceinline__ ColumnRun columns_of(const PagedArgs& x, int tile, int cols) {
-  int lo = 0, hi = x.b.B - 1;
-  auto first = [&](int e) { return (int)((int64_t)max(x.b.cu[e], 0) * x.a.G / cols) + e; };
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (first(mid) <= tile) lo = mid;
-    else hi = mid - 1;
-  }
+  auto first = [&](int r0, int e) { return (int)((int64_t)max(r0, 0) * x.a.G / cols) + e; };
   ColumnRun r;
-  r.e = lo;
-  r.r0 = x.b.cu[lo];
-  r.r1 = min(x.b.cu[lo + 1], x.b.rows);
-  const int64_t u0 = (int64_t)(tile - first(lo)) * cols, n = (int64_t)(r.r1 - r.r0) * x.a.G - u0;
+  r.at = find_entry(x, [&](int r0, int e) { return first(r0, e) <= tile; });
+  const int64_t u0 = (int64_t)(tile - first(r.at.r0, r.at.e)) * cols;
+  const int64_t n = (int64_t)(min(r.at.r1, x.b.rows) - r.at.r0) * x.a.G - u0;
   r.u0 = (int)u0;
-  r.n = r.r0 < 0 || u0 < 0 || n <= 0 ? 0 : (int)min(n, (int64_t)cols);
+  r.n = r.at.r0 < 0 || u0 < 0 || n <= 0 ? 0 : (int)min(n, (int64_t)cols);
   return r;
 }
 
-// What a workgroup works on.
-struct TileWork {
-  int s, head;       // sequence and kv head
-  int begin, end;    // tokens [begin, end), begin a multiple of 16
-};
-
-template <int NW>
-__device__ __forceinline__ void stage_barrier() {  // (LDS operations and the staged loads only: a fence would wait for stores)
+// Waits until at most `loads` of the wavefront's loads are on their way, and for its LDS operations.  (A fence would wait for
+// stores too.)
+template <int LOADS>
+__device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
-  if (NW > 1) __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_s_waitcnt(0x0070 | (LOADS & 15) | (LOADS >> 4) << 14);
   asm volatile("" ::: "memory");
 }
 
-template <int D, int NW, int CB, int STEP>
+// NW wavefronts of 32 * CB columns, STAGES stages of STEP tokens.
+//   4 wavefronts, two stages: the matrix cores are what bounds these
+//   1 wavefront, two stages: few columns, so that memory does; five workgroups (D = 128) of a compute unit have 16 KB each on
+//                the way (three and four stages leave room for fewer: 24 caches of up to 120000 tokens 119 -> 122, 153 us)
+// Workgroups of the window come first, then, of the spans' pieces,
+//   4 wavefronts: the buckets' tiles
+//   1 wavefront: one for every (row, head, slot).  Other heads and rows of its 32 columns may list the same span: the first one
+//                that does takes it for all, so that a span is read once for the group.
+template <int D, int NW, int CB, int STEP, int STAGES>
 __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
   constexpr int COLS = NW * 32 * CB;
   extern __shared__ __align__(1024) char s_dynamic[];  // (static, the compiler would wait for staging loads at every read)
   bf16_t(*const s_kv)[2][STEP * D] = reinterpret_cast<bf16_t(*)[2][STEP * D]>(s_dynamic);
   __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS];
-  __shared__ int s_range[2 * NW];
   const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t unit = workgroup();
-  TileWork w;
-  int part;
+  const bool window = unit < plan.window_units;
+  int seq, head, part;         // sequence, kv head, piece
+  int begin, end;              // tokens [begin, end) of the tile
+  int any_lo, any_last;        // ... that any of the wavefront's columns attends
+  int all_lo, all_last;        // ... that all of them attend
+  int early_page = -1;
   // columns
-  if (unit < plan.window_units) {
+  if (window) {
     // (tile, piece) of the kv heads in turn; the last tiles first, whose ranges are the longest
-    w.head = (int)(unit % x.c.Hkv);
-    const int at = (int)(unit / x.c.Hkv), tile = plan.tiles - 1 - at / x.p.window, piece = at % x.p.window;
+    head = (int)(unit % x.c.Hkv);
+    const int at = (int)(unit / x.c.Hkv);
+    if (at >= plan.tiles * x.p.window) return;
+    const int tile = plan.tiles - 1 - at / x.p.window, piece = at % x.p.window;
     part = x.a.topk * x.p.routed + piece;
     const ColumnRun run = columns_of(x, tile, COLS);
     if (run.n <= 0) return;
-    const int r0 = run.r0, u0 = run.u0;
-    w.s = x.b.seqs[run.e];
-    const int len = length_of(x.c, w.s), pos0 = len - (x.b.cu[run.e + 1] - r0);
+    const int r0 = run.at.r0, u0 = run.u0, len = run.at.len, pos0 = len - (run.at.r1 - r0);
+    seq = run.at.s;
     const int first = max(pos0 + u0 / x.a.G, 0);  // position of the tile's first row that has a token
+    const int most = min(len, x.b.L) - 1;         // of the last row that has one
     const int64_t origin = (int64_t)(first / x.a.S) * x.a.S / 16 * 16 + (int64_t)piece * x.p.window_tokens;
+    const int from = (int)min(origin, (int64_t)INT_MAX), upto = (int)min(origin + x.p.window_tokens - 1, (int64_t)INT_MAX);
+    auto lo_of = [&](int pos) { return max(pos / x.a.S * x.a.S, from); };
+    auto last_of = [&](int pos) { return min(pos, upto); };
     for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
       const int u = u0 + c, row = r0 + u / x.a.G, pos = pos0 + u / x.a.G;
       int rh = -1, clo = INT_MAX, clast = -1;
       if (c < run.n) {
-        rh = (w.head * x.a.G + u % x.a.G) * x.b.rows + row;
-        if (pos >= 0 && pos < len && pos < x.b.L) {
-          clo = (int)max((int64_t)(pos / x.a.S) * x.a.S, min(origin, (int64_t)INT_MAX));
-          clast = (int)min((int64_t)pos, origin + x.p.window_tokens - 1);
-          if (clo > clast) {
-            clo = INT_MAX;
-            clast = -1;
-          }
+        rh = (head * x.a.G + u % x.a.G) * x.b.rows + row;
+        if (pos >= 0 && pos <= most && lo_of(pos) <= last_of(pos)) {
+          clo = lo_of(pos);
+          clast = last_of(pos);
         }
       }
       s_rh[c] = rh;
       s_lo[c] = clo;
       s_last[c] = clast;
     }
-  } else {
+    // Later rows begin and end no earlier.
+    const int last = min(pos0 + (u0 + run.n - 1) / x.a.G, most);
+    begin = lo_of(first);
+    end = last_of(last) + 1;
+    if (first > last) end = begin;
+    const int c0 = wave * 32 * CB, c1 = min(c0 + 32 * CB, run.n) - 1;
+    const int p0 = pos0 + (u0 + c0) / x.a.G, p1 = pos0 + (u0 + c1) / x.a.G, q0 = max(p0, 0), q1 = min(p1, most);
+    const bool some = c0 <= c1 && q0 <= q1;
+    any_lo = some ? lo_of(q0) : INT_MAX;
+    any_last = some ? last_of(q1) : -1;
+    all_lo = p0 < 0 || p1 > most ? INT_MAX : lo_of(q1);  // (a row without a token attends nothing)
+    all_last = last_of(q0);
+  } else if (NW > 1) {
+    // Tiles of one bucket read the same rows: an eighth of the list is given to the workgroups of each XCD, which share an L2.
     const int64_t u = unit - plan.window_units;
-    const int tile = (int)(u / x.p.routed), piece = (int)(u - (int64_t)tile * x.p.routed);
-    if (tile >= *plan.tile_count) return;
+    const int count_all = *plan.tile_count, share = (count_all + 7) / 8;
+    const int64_t at = u / 8;
+    const int tile = (int)(u % 8) * share + (int)(at / x.p.routed);
+    part = (int)(at % x.p.routed);
+    if (at / x.p.routed >= share || tile >= count_all) return;
     const int bucket = plan.tile_bucket[tile], count = plan.counts[bucket] - (tile - plan.first_tile[bucket]) * COLS;
     const int j = bucket % plan.spans, eh = bucket / plan.spans;
-    w.head = eh % x.c.Hkv;
-    w.s = x.b.seqs[eh / x.c.Hkv];
-    const int t0 = j * x.a.S + piece * x.p.routed_tokens, last = min(t0 + x.p.routed_tokens, (j + 1) * x.a.S) - 1;
+    head = eh % x.c.Hkv;
+    seq = x.b.seqs[eh / x.c.Hkv];
+    begin = j * x.a.S + part * x.p.routed_tokens;
+    end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
     for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
       s_rh[c] = c < count ? plan.items[(int64_t)tile * COLS + c] : -1;  // (row and head) * 32 + slot
-      s_lo[c] = c < count ? t0 : INT_MAX;
-      s_last[c] = c < count ? last : -1;
+      s_lo[c] = c < count ? begin : INT_MAX;
+      s_last[c] = c < count ? end - 1 : -1;
     }
-    part = piece;
+    const bool some = wave * 32 * CB < count;
+    all_lo = begin;
+    all_last = end - 1;
+    any_lo = some ? all_lo : INT_MAX;
+    any_last = some ? all_last : -1;
+  } else {
+    const int64_t u = unit - plan.window_units;
+    part = (int)(u % x.p.routed);
+    const int64_t item = u / x.p.routed;
+    const int slot = (int)(item % x.a.topk), rh = (int)(item / x.a.topk);
+    if (rh >= x.a.Hq * x.b.rows) return;
+    const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+    const int j = x.idx[h * x.a.ish + row * x.a.ist + slot];
+    const Entry at = entry_with_row(x, row);
+    if (row < at.r0 || row >= at.r1) return;
+    head = h / x.a.G;
+    seq = at.s;
+    const int own = (row - at.r0) * x.a.G + h - head * x.a.G, u0 = own & ~31;  // columns u0 .. u0 + 31 of the entry
+    const int pos = position_of(x, at, row);
+    if (pos < 0 || j < 0 || j >= pos / x.a.S) {
+      if (lane == 0) x.part_lse[(int64_t)rh * x.p.count + slot * x.p.routed + part] = -INFINITY;
+      return;
+    }
+    const int cols = min((min(at.r1, x.b.rows) - at.r0) * x.a.G - u0, 32);
+    begin = any_lo = all_lo = j * x.a.S + part * x.p.routed_tokens;
+    end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
+    any_last = all_last = end - 1;
+    // (asked for before the other columns' lists: a unit is short, and a chain of loads)
+    const int t = begin / 16 * 16 + lane * 16;
+    if (t < end) early_page = x.c.tables[(int64_t)at.s * x.c.max_pages + (uint32_t)t / x.c.by_ps];
+    if (lane < 32) {
+      s_rh[lane] = -1;
+      s_lo[lane] = INT_MAX;
+      s_last[lane] = -1;
+    }
+    bool earlier = false;
+    for (int i = lane; i < cols * x.a.topk; i += 64) {
+      const int c = i / x.a.topk, k = i - c * x.a.topk;
+      const int row2 = at.r0 + (u0 + c) / x.a.G, h2 = head * x.a.G + (u0 + c) % x.a.G;
+      const int pos2 = position_of(x, at, row2);
+      if (pos2 >= 0 && j < pos2 / x.a.S && x.idx[h2 * x.a.ish + row2 * x.a.ist + k] == j) {
+        earlier = earlier || u0 + c < own || (u0 + c == own && k < slot);
+        s_rh[c] = (h2 * x.b.rows + row2) * 32 + k;
+        s_lo[c] = begin;
+        s_last[c] = end - 1;
+      }
+    }
+    if (__builtin_amdgcn_ballot_w64(earlier) != 0) return;
   }
-  const bool window = unit < plan.window_units;
   __syncthreads();
   constexpr int KB = CB == 2 || STEP == 32 ? 1 : 2;
   Tile<D, CB, KB> tile;
   tile.clear(lane);
-  int any_lo = INT_MAX, any_last = -1, all_lo = 0, all_last = INT_MAX;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
-    const int c = wave * 32 * CB + cb * 32 + (lane & 31);
-    const int lo = s_lo[c], last = s_last[c], item = s_rh[c];
-    tile.lo[cb] = lo;
-    tile.last[cb] = last;
-    any_lo = min(any_lo, lo);
-    any_last = max(any_last, last);
-    if (item >= 0) {
-      all_lo = max(all_lo, lo);
-      all_last = min(all_last, last);
-    }
+    const int item = s_rh[wave * 32 * CB + cb * 32 + (lane & 31)];
     const int rh = max(window ? item : item >> 5, 0);  // (a column of nobody reads some row: nothing is made of it)
     const int h = rh / x.b.rows, row = rh - h * x.b.rows;
     const bf16_t* const q = static_cast<const bf16_t*>(x.Q) + h * x.a.qsh + row * x.a.qst + (lane >> 5) * 8;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) tile.q[cb][kk] = *reinterpret_cast<const bf16x8*>(q + kk * 16);
   }
-#pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) {
-    any_lo = min(any_lo, __shfl_xor(any_lo, off, 64));
-    any_last = max(any_last, __shfl_xor(any_last, off, 64));
-    all_lo = max(all_lo, __shfl_xor(all_lo, off, 64));
-    all_last = min(all_last, __shfl_xor(all_last, off, 64));
-  }
+  const bool group = NW == 1 && !window;
   any_lo = __builtin_amdgcn_readfirstlane(any_lo);
   any_last = __builtin_amdgcn_readfirstlane(any_last);
   all_lo = __builtin_amdgcn_readfirstlane(all_lo);
   all_last = __builtin_amdgcn_readfirstlane(all_last);
-  w.begin = any_lo;
-  w.end = any_last + 1;
-  if (NW > 1) {
-    if (lane == 0) {
-      s_range[2 * wave] = any_lo;
-      s_range[2 * wave + 1] = any_last;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < NW; ++k) {
-      w.begin = min(w.begin, s_range[2 * k]);
-      w.end = max(w.end, s_range[2 * k + 1] + 1);
-    }
-    w.begin = __builtin_amdgcn_readfirstlane(w.begin);
-    w.end = __builtin_amdgcn_readfirstlane(w.end);
-  }
-  w.begin = w.begin / 16 * 16;
-
-  w.s = __builtin_amdgcn_readfirstlane(w.s);
-  w.head = __builtin_amdgcn_readfirstlane(w.head);
-  const int32_t* const table = x.c.tables + (int64_t)w.s * x.c.max_pages;
-  const int64_t base = x.b.layer * x.c.layer + w.head * x.c.head;
+  begin = __builtin_amdgcn_readfirstlane(begin) / 16 * 16;
+  end = __builtin_amdgcn_readfirstlane(end);
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  head = __builtin_amdgcn_readfirstlane(head);
+  const int32_t* const table = x.c.tables + (int64_t)seq * x.c.max_pages;
+  const int64_t base = x.b.layer * x.c.layer + head * x.c.head;
   const int row_bytes = (int)x.c.tok * 2;
-  // The pages of a step's rows are looked up a step before its rows are asked for; lane g has that of its rows 16 g, ...
+  // Lane g has the page of the g-th sixteen tokens from `batch` on; the next 64 pages are looked up while those are in use.
   constexpr int GROUPS = STEP / 16;
-  int page = -1;
-  uint32_t live[2];
+  constexpr int kLoads = 2 * GROUPS / NW * (16 / (64 / (D / 8)));  // of a wavefront and stage
   auto look_up = [&](int t0) {
-    const int t = t0 + lane % GROUPS * 16;
-    page = t < w.end ? table[(uint32_t)t / x.c.by_ps] : -1;
+    const int t = t0 + lane_now() * 16;
+    return t < end ? table[(uint32_t)t / x.c.by_ps] : -1;
   };
+  int batch = begin, page = -1, next_page = -1;
+  uint64_t alive = 0;  // which of them there are
+  uint32_t live = 0;   // those of the stages, GROUPS bits each
   auto stage = [&](int t0, int b) {
-    live[b] = (uint32_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages) & ((1u << GROUPS) - 1);
+    if (t0 - batch >= 1024) {
+      batch += 1024;
+      page = next_page;
+      alive = __builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages);
+      next_page = look_up(batch + 1024);
+    }
+    const int ln = lane_now(), at = (t0 - batch) / 16;
+    const uint32_t bits = (uint32_t)(alive >> at) & ((1u << GROUPS) - 1);
+    live = (live & ~(((1u << GROUPS) - 1) << b * GROUPS)) | bits << b * GROUPS;
 #pragma unroll
     for (int i = 0; i < GROUPS / NW; ++i) {
       const int g = NW == 1 ? i : wave, r0 = g * 16, t = __builtin_amdgcn_readfirstlane(t0 + r0);
-      const bool on = live[b] >> g & 1;
-      const int rows = on ? min(w.end - t, 16) : 0;
+      const bool on = bits >> g & 1;
+      const int rows = on ? min(end - t, 16) : 0;
       const int in_page = __builtin_amdgcn_readfirstlane((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps);
-      const int64_t at = on ? uniform64(base + __builtin_amdgcn_readlane(page, g) * x.c.page + in_page * x.c.tok) : 0;
-      stage_rows<D, 0>(&s_kv[b][0][r0 * D], r0, static_cast<const bf16_t*>(x.c.K) + at, rows, row_bytes, lane);
-      stage_rows<D, 1>(&s_kv[b][1][r0 * D], r0, static_cast<const bf16_t*>(x.c.V) + at, rows, row_bytes, lane);
+      const int64_t from = on ? uniform64(base + __builtin_amdgcn_readlane(page, at + g) * x.c.page + in_page * x.c.tok) : 0;
+      stage_rows<D, 0>(&s_kv[b][0][r0 * D], r0, static_cast<const bf16_t*>(x.c.K) + from, rows, row_bytes, ln);
+      stage_rows<D, 1>(&s_kv[b][1][r0 * D], r0, static_cast<const bf16_t*>(x.c.V) + from, rows, row_bytes, ln);
     }
-    look_up(t0 + STEP);
   };
-  if (w.begin < w.end) {
-    look_up(w.begin);
-    stage(w.begin, 0);
+  if (begin < end) {
+    page = group ? early_page : look_up(batch);
+    if (end - batch > 1024) next_page = look_up(batch + 1024);
+    alive = __builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages);
+#pragma unroll
+    for (int k = 0; k < STAGES - 1; ++k)
+      if (begin + k * STEP < end) stage(begin + k * STEP, k);
   }
   int b = 0;
-  for (int t0 = w.begin; t0 < w.end; t0 += STEP, b ^= 1) {
-    stage_barrier<NW>();
-    if (t0 + STEP < w.end) stage(t0 + STEP, b ^ 1);
+  for (int t0 = begin; t0 < end; t0 += STEP) {
+    // this stage's loads have arrived when only those of the stages behind it are on their way
+    if (STAGES > 3 && t0 + 2 * STEP < end) wait_loads<(STAGES > 3 ? 2 : 0) * kLoads>();
+    else if (STAGES > 2 && t0 + STEP < end) wait_loads<(STAGES > 2 ? 1 : 0) * kLoads>();
+    else wait_loads<0>();
+    if (NW > 1) {
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    }
+    if (t0 + (STAGES - 1) * STEP < end) stage(t0 + (STAGES - 1) * STEP, b == 0 ? STAGES - 1 : b - 1);
 #pragma unroll 1
     for (int at = 0; at < STEP; at += 32 * KB) {
       const int t = t0 + at, end = t + 32 * KB - 1;
       if (end < any_lo || t > any_last) continue;
       constexpr uint32_t kAll = (1u << 2 * KB) - 1;
-      const uint32_t there = live[b] >> (at / 16) & kAll;
-      tile.attend(&s_kv[b][0][at * D], &s_kv[b][1][at * D], t, t < all_lo || end > all_last || there != kAll, there, x.scale_log2e, lane);
+      const uint32_t there = live >> (b * GROUPS + at / 16) & kAll;
+      tile.attend(&s_kv[b][0][at * D], &s_kv[b][1][at * D], t, t < all_lo || end > all_last || there != kAll, there, x.scale_log2e,
+                  s_lo + wave * 32 * CB, s_last + wave * 32 * CB);
     }
+    b = b == STAGES - 1 ? 0 : b + 1;
   }
   // Partials.  A column with a value that is not finite is marked by an lse that is not a number: it may have come from a
   // token that the column does not attend, and the merge takes such a piece again, row by row.
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
-    const int item = s_rh[wave * 32 * CB + cb * 32 + (lane & 31)];
+    const int ln = lane_now(), item = s_rh[wave * 32 * CB + cb * 32 + (ln & 31)];
     const float sum = across_halves_sum(tile.l[cb]);
     const float inv = 1.f / sum;
     float check = 0.f, top = 0.f;
@@ -688,10 +778,10 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     typedef float f32x4 __attribute__((ext_vector_type(4)));
     const int64_t rec = (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
-    if (lane < 32) x.part_lse[rec] = lse;
+    if (ln < 32) x.part_lse[rec] = lse;
     if (x.p.count == 1) {  // the row's result
-      if (lane < 32 && x.LSE) x.LSE[rec] = lse * kLn2;
-      bf16_t* const to = static_cast<bf16_t*>(x.O) + rec * D + 4 * (lane >> 5);
+      if (ln < 32 && x.LSE) x.LSE[rec] = lse * kLn2;
+      bf16_t* const to = static_cast<bf16_t*>(x.O) + rec * D + 4 * (ln >> 5);
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -705,8 +795,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
     }
     if (none) continue;
     const float scale = scale_above(top * inv), by = inv / scale;
-    if (lane < 32) x.part_scale[rec] = scale;
-    _Float16* const to = static_cast<_Float16*>(x.part_o) + rec * D + 4 * (lane >> 5);
+    if (ln < 32) x.part_scale[rec] = scale;
+    _Float16* const to = static_cast<_Float16*>(x.part_o) + rec * D + 4 * (ln >> 5);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -738,12 +828,11 @@ __global__ __launch_bounds__(256) void count_kernel(const PagedArgs x, const Til
   if (local)
     for (int j = threadIdx.x; j < plan.spans; j += 256) s_count[j] = 0;
   __syncthreads();
-  int32_t* const counts = plan.counts + ((int64_t)run.e * x.c.Hkv + head) * plan.spans;
-  const int s = x.b.seqs[run.e], len = length_of(x.c, s), end = x.b.cu[run.e + 1];
+  int32_t* const counts = plan.counts + ((int64_t)run.at.e * x.c.Hkv + head) * plan.spans;
   for (int pass = local ? 0 : 1; pass < 2; ++pass) {
     for (int u = threadIdx.x; u < run.n; u += 256) {
-      const int row = run.r0 + (run.u0 + u) / x.a.G, h = head * x.a.G + (run.u0 + u) % x.a.G;
-      const int pos = len - (end - row), c = pos >= 0 && pos < len && pos < x.b.L ? pos / x.a.S : 0;
+      const int row = run.at.r0 + (run.u0 + u) / x.a.G, h = head * x.a.G + (run.u0 + u) % x.a.G;
+      const int pos = position_of(x, run.at, row), c = pos < 0 ? 0 : pos / x.a.S;
       const int64_t rh = (int64_t)h * x.b.rows + row;
       const int32_t* const slots = x.idx + h * x.a.ish + row * x.a.ist;
       for (int k = 0; k < x.a.topk; ++k) {
@@ -813,52 +902,57 @@ __global__ __launch_bounds__(256) void items_kernel(const PagedArgs x, const Til
 }
 
 // ------------------------------------------------------------------ merge
-// Pieces that a tile marked, once more, row by row: of the window, whose tiles cut it where they like, all into its first record.
-// By one wavefront.
-template <typename T, int D>
-__device__ __forceinline__ void take_marked(const PagedArgs& x, int rh, int h, int row) {
-  const float* const lse = x.part_lse + (int64_t)rh * x.p.count;
-  const int routed = x.a.topk * x.p.routed, lane = threadIdx.x & 63;
-  const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, row), row);
+// Pieces of a row and head that a tile marked, once more, row by row, by one wavefront: of the window, whose tiles cut it where they
+// like, all into its first record.  DIRECT: one piece a row, whose result the tile has written.
+template <typename T, int D, bool DIRECT>
+__device__ __forceinline__ void mend_row(const PagedArgs& x, int rh) {
+  const int h = rh / x.b.rows, row = rh - h * x.b.rows, P = x.p.count, routed = x.a.topk * x.p.routed;
+  const Entry at = entry_with_row(x, row);
+  const int pos = position_of(x, at, row);
+  const PieceRange window = {pos / x.a.S * x.a.S, pos + 1};
+  if (DIRECT) {
+    take_piece<T, D, 1, true>(x, at.s, rh, window, 0, nullptr, nullptr);
+    return;
+  }
+  const int64_t rec = (int64_t)rh * P;
+  const int32_t* const slots = x.idx + h * x.a.ish + row * x.a.ist;
   bool near = false;
-  for (int k = x.row_pieces; k < x.p.count; ++k) {
-    if (lse[k] == lse[k]) continue;
-    if (k < routed)
-      take_piece<T, D, 1, false>(x, at.s, rh, range_of_piece(x, at.pos, k, x.idx + h * x.a.ish + row * x.a.ist), (int64_t)rh * x.p.count + k,
-                                 nullptr, nullptr);
+  for (int k = 0; k < P; ++k) {
+    const float lse = x.part_lse[rec + k];
+    if (lse == lse) continue;
+    if (k < routed) take_piece<T, D, 1, false>(x, at.s, rh, range_of_piece(x, pos, k, slots), rec + k, nullptr, nullptr);
     else near = true;
   }
   if (near) {
-    take_piece<T, D, 1, false>(x, at.s, rh, {at.pos / x.a.S * x.a.S, at.pos + 1}, (int64_t)rh * x.p.count + routed, nullptr, nullptr);
-    for (int k = routed + 1 + lane; k < x.p.count; k += 64) x.part_lse[(int64_t)rh * x.p.count + k] = -INFINITY;
+    take_piece<T, D, 1, false>(x, at.s, rh, window, rec + routed, nullptr, nullptr);
+    for (int k = routed + 1 + (threadIdx.x & 63); k < P; k += 64) x.part_lse[rec + k] = -INFINITY;
   }
-  __threadfence_block();
 }
 
-// One piece a row: the tiles wrote the results themselves.
-template <typename T, int D>
+// A wavefront looks at the records of 64 rows and heads.
+template <typename T, int D, bool DIRECT>
 __global__ __launch_bounds__(256) void mend_kernel(const PagedArgs x) {
   const int64_t n = (int64_t)x.a.Hq * x.b.rows;
-  const int lane = threadIdx.x & 63;
-  const int64_t first = (workgroup() * 4 + (threadIdx.x >> 6)) * 64, mine = first + lane;
-  const int at_row = (int)(mine % x.b.rows);
-  const bool on = mine < n && at_row >= x.b.cu[0] && at_row < x.b.cu[x.b.B];
-  const float lse = on ? x.part_lse[mine] : 0.f;
-  uint64_t marked = __builtin_amdgcn_ballot_w64(lse != lse);
-  while (marked) {
-    const int rh = (int)first + __builtin_ctzll(marked);
-    marked &= marked - 1;
-    const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, rh % x.b.rows), rh % x.b.rows);
-    take_piece<T, D, 1, true>(x, at.s, rh, {at.pos / x.a.S * x.a.S, at.pos + 1}, 0, nullptr, nullptr);
-  }
+  const int P = x.p.count;
+  const int64_t first = (workgroup() * 4 + (threadIdx.x >> 6)) * 64, mine = first + (threadIdx.x & 63);
+  const int row = (int)(mine % x.b.rows);
+  bool bad = false;
+  if (mine < n && row >= x.b.cu[0] && row < x.b.cu[x.b.B])
+    for (int k = 0; k < P; ++k) {
+      const float lse = x.part_lse[mine * P + k];
+      bad = bad || lse != lse;
+    }
+  for (uint64_t marked = __builtin_amdgcn_ballot_w64(bad); marked; marked &= marked - 1)
+    mend_row<T, D, DIRECT>(x, (int)first + __builtin_ctzll(marked));
 }
 
 // WAVES wavefronts (of a workgroup's four) join the pieces of one row and head: weights to LDS, then D / 8 (fp32: D / 4) lanes
-// a piece.
+// a piece.  Nothing a wavefront asks for depends on what it has read: the first outputs are on their way before there are weights.
+// (Marked pieces are mended here where a workgroup takes a row; beside a wavefront a row, they would cost it half its occupancy.)
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   typedef typename Record<T>::Value Value;
-  constexpr int EPL = 16 / sizeof(Value), LANES = D / EPL, GROUPS = 64 * WAVES / LANES;
+  constexpr int EPL = 16 / sizeof(Value), LANES = D / EPL, N = 64 * WAVES, GROUPS = N / LANES, U = 4;
   typedef Value Values __attribute__((ext_vector_type(EPL)));
   extern __shared__ float s_dyn[];  // [4 / WAVES][count] weights
   __shared__ float s_red[4];
@@ -869,10 +963,23 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   if (unit >= (int64_t)x.a.Hq * x.b.rows) return;
   const int rh = (int)unit, sub = WAVES == 1 ? wave : 0;
   const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+  const int g = tid / LANES, c = tid % LANES;
+  const Values* const po = reinterpret_cast<const Values*>(static_cast<const Value*>(x.part_o) + (int64_t)rh * P * D) + c;
+  const float* const lse = x.part_lse + (int64_t)rh * P;
+  const float* const scales = x.part_scale + (int64_t)rh * P;
+  Values v[U];
+  float lse0, scale0 = 1.f;  // of piece tid; the others are read again where there are so many
+  auto ask = [&] {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (g + u * GROUPS < P) v[u] = __builtin_nontemporal_load(po + (int64_t)(g + u * GROUPS) * LANES);
+    lse0 = tid < P ? lse[tid] : -INFINITY;
+    if (sizeof(Value) == 2 && tid < P) scale0 = scales[tid];
+  };
+  ask();
   if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
   float* const s_w = s_dyn + sub * P;
   float *const s_gate = s_gates[sub], *const s_lse = s_lses[sub];
-  const float* const lse = x.part_lse + (int64_t)rh * P;
   auto barrier = [] {
     if (WAVES > 1) {
       __syncthreads();
@@ -881,16 +988,6 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
       __builtin_amdgcn_wave_barrier();
     }
   };
-  constexpr int N = 64 * WAVES;
-  if (x.row_pieces < P) {
-    bool marked = false;
-    for (int k = x.row_pieces + tid; k < P; k += N) marked = marked || lse[k] != lse[k];
-    const bool any = WAVES > 1 ? __syncthreads_or(marked) : __builtin_amdgcn_ballot_w64(marked) != 0;
-    if (any) {
-      if (WAVES == 1 || wave == 0) take_marked<T, D>(x, rh, h, row);
-      barrier();
-    }
-  }
   auto all_max = [&](float v) {
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) v = max_of(v, __shfl_xor(v, off, 64));
@@ -909,27 +1006,37 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
     __syncthreads();
     return (s_red[0] + s_red[1]) + (s_red[2] + s_red[3]);
   };
-  // log2-sum-exp2 of pieces [from, to)
-  auto lse_of = [&](int from, int to) {
-    float v = -INFINITY;
-    for (int k = from + tid; k < to; k += N) v = max_of(v, lse[k]);
+  // log2-sum-exp2 of the pieces from `from` on
+  auto lse_of = [&](int from) {
+    float v = tid >= from ? lse0 : -INFINITY;
+    for (int k = tid + N; k < P; k += N)
+      if (k >= from) v = max_of(v, lse[k]);
     const float m = all_max(v);
     if (m == -INFINITY) return m;
-    float l = 0.f;
-    for (int k = from + tid; k < to; k += N) l += weight_of(lse[k], m);
+    float l = tid >= from ? weight_of(lse0, m) : 0.f;
+    for (int k = tid + N; k < P; k += N)
+      if (k >= from) l += weight_of(lse[k], m);
     return m + __log2f(all_sum(l));
   };
   const int routed = x.a.topk * x.p.routed;
   bool any = false;  // a slot holds a span
+  float total = lse_of(0);
+  if (WAVES > 1 && total != total && x.row_pieces < P) {
+    if (wave == 0) mend_row<T, D, false>(x, rh);
+    __threadfence_block();
+    __syncthreads();
+    ask();
+    total = lse_of(0);
+  }
   if (x.a.combined) {
-    const RowPlace at = place_of_row(x, entry_of_row(x.b.cu, x.b.B, row), row);
-    const float near = lse_of(routed, P);
+    const int pos = position_of(x, entry_with_row(x, row), row);
+    const float near = lse_of(routed);
     float score = -INFINITY;
     bool mine = false;
     if (tid < x.a.topk) {
       const int64_t i = h * x.a.ish + row * x.a.ist + tid;
       const int j = x.idx[i];
-      mine = at.pos >= 0 && j >= 0 && j < at.pos / x.a.S;
+      mine = pos >= 0 && j >= 0 && j < pos / x.a.S;
       if (mine) score = x.scores[i];
       float m = near;
       for (int k = 0; k < x.p.routed; ++k) m = max_of(m, lse[tid * x.p.routed + k]);
@@ -944,51 +1051,43 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
       const float sum = all_sum(e);
       if (tid < x.a.topk) s_gate[tid] = e / sum;
       barrier();
-      for (int k = tid; k < P; k += N) {
-        float w = 0.f;
-        if (k < routed) {
-          const int t = k / x.p.routed;
-          if (s_gate[t] != 0.f) w = s_gate[t] * weight_of(lse[k], s_lse[t]);
-        } else {
-          for (int t = 0; t < x.a.topk; ++t)
-            if (s_gate[t] != 0.f) w += s_gate[t] * weight_of(lse[k], s_lse[t]);
-        }
-        s_w[k] = w;
-      }
+    } else {
+      total = near;
     }
+  } else if (tid == 0 && x.LSE) {
+    x.LSE[rh] = total * kLn2;
   }
-  if (!any) {
-    const float total = lse_of(x.a.combined ? routed : 0, P);
-    for (int k = tid; k < P; k += N) s_w[k] = x.a.combined && k < routed ? 0.f : weight_of(lse[k], total);
-    if (tid == 0 && x.LSE) x.LSE[rh] = total * kLn2;
+  for (int k = tid; k < P; k += N) {
+    const float mine = k == tid ? lse0 : lse[k];
+    float w = 0.f;
+    if (!any) {
+      if (!x.a.combined || k >= routed) w = weight_of(mine, total);
+    } else if (k < routed) {
+      const int t = k / x.p.routed;
+      if (s_gate[t] != 0.f) w = s_gate[t] * weight_of(mine, s_lse[t]);
+    } else {
+      for (int t = 0; t < x.a.topk; ++t)
+        if (s_gate[t] != 0.f) w += s_gate[t] * weight_of(mine, s_lse[t]);
+    }
+    // (a piece without tokens has written neither output nor scale)
+    if (sizeof(Value) == 2 && w != 0.f) w *= k == tid ? scale0 : scales[k];
+    s_w[k] = w;
   }
   barrier();
-  if (sizeof(Value) == 2) {  // (a piece without tokens has written neither output nor scale)
-    for (int k = tid; k < P; k += N)
-      if (s_w[k] != 0.f) s_w[k] *= x.part_scale[(int64_t)rh * P + k];
-    barrier();
-  }
-  const int g = tid / LANES, c = tid % LANES;
   float acc[EPL];
 #pragma unroll
   for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
-  const Values* const po = reinterpret_cast<const Values*>(static_cast<const Value*>(x.part_o) + (int64_t)rh * P * D) + c;
-  constexpr int U = 4;  // pieces asked for at once
   for (int k0 = g; k0 < P; k0 += U * GROUPS) {
-    Values v[U];
-    float w[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int k = k0 + u * GROUPS;
-      w[u] = k < P ? s_w[k] : 0.f;
-      if (w[u] != 0.f) v[u] = __builtin_nontemporal_load(po + (int64_t)k * LANES);
-    }
+      const float w = k < P ? s_w[k] : 0.f;
+      if (w != 0.f) {
+        if (k0 != g) v[u] = __builtin_nontemporal_load(po + (int64_t)k * LANES);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (w[u] != 0.f) {
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) acc[e] = fmaf(w[u], (float)v[u][e], acc[e]);
+        for (int e = 0; e < EPL; ++e) acc[e] = fmaf(w, (float)v[u][e], acc[e]);
       }
+    }
   }
   if (WAVES == 1) {
 #pragma unroll
@@ -999,10 +1098,10 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
       T* const to = static_cast<T*>(x.O) + (int64_t)rh * D + c * EPL;
       if constexpr (sizeof(T) == 2) {
         typedef __bf16 Out __attribute__((ext_vector_type(EPL)));
-        Out v;
+        Out o;
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) v[e] = (__bf16)acc[e];
-        *reinterpret_cast<Out*>(to) = v;
+        for (int e = 0; e < EPL; ++e) o[e] = (__bf16)acc[e];
+        *reinterpret_cast<Out*>(to) = o;
       } else {
         *reinterpret_cast<float4*>(to) = make_float4(acc[0], acc[1], acc[2], acc[3]);
       }
@@ -1012,10 +1111,10 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
     for (int e = 0; e < EPL; ++e) s_out[g * D + c * EPL + e] = acc[e];
     __syncthreads();
     if (tid < D) {
-      float v = 0.f;
+      float o = 0.f;
 #pragma unroll
-      for (int k = 0; k < GROUPS; ++k) v += s_out[k * D + tid];
-      Elem<T>::store1(static_cast<T*>(x.O) + (int64_t)rh * D + tid, v);
+      for (int k = 0; k < GROUPS; ++k) o += s_out[k * D + tid];
+      Elem<T>::store1(static_cast<T*>(x.O) + (int64_t)rh * D + tid, o);
     }
   }
 }
@@ -1030,10 +1129,11 @@ dim3 grid_of(int64_t workgroups) {
 // How a call is taken.
 struct Form {
   Pieces p;
-  bool window_tiles, routed_tiles;
-  int cols_log2;  // columns of a tile
-  TilePlan plan;  // (pointers unset)
-  int64_t most_tiles;
+  bool tiles;      // the matrix-core form
+  bool buckets;    // ... with the spans' rows in buckets
+  int cols_log2;   // columns of a tile
+  TilePlan plan;   // (pointers unset)
+  int64_t units, most_tiles;  // workgroups of the tile kernel; tiles of the buckets
   size_t o_bytes, lse_bytes, plan_bytes;
 };
 
@@ -1041,12 +1141,11 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   const int64_t rh = (int64_t)a.Hq * b.rows, window = a.S < b.L ? a.S : b.L;
   Form f = {};
   // Sixteen rows of a stage lie in one page, and 16 token strides within a buffer's 32-bit offsets.
-  const bool tiles = c.dtype == SL_BF16 && c.ps % 16 == 0 && c.tok < ((int64_t)1 << 26) && rh < ((int64_t)1 << 26);
+  f.tiles = c.dtype == SL_BF16 && c.ps % 16 == 0 && c.tok < ((int64_t)1 << 26) && rh < ((int64_t)1 << 26);
   const int64_t spans = div_up(b.L, a.S), buckets = (int64_t)b.B * c.Hkv * spans, items = rh * a.topk;
-  f.routed_tiles = tiles && a.topk > 0 && items >= 4 * buckets && items < ((int64_t)1 << 30);
-  f.window_tiles = tiles && (f.routed_tiles || a.topk < 2);
+  f.buckets = f.tiles && a.topk > 0 && items >= 4 * buckets && items < ((int64_t)1 << 30);
   const int64_t columns = (int64_t)b.rows * a.G;  // of a kv head
-  f.cols_log2 = columns <= 32 * (int64_t)b.B && !f.routed_tiles ? 5 : 7;
+  f.cols_log2 = (columns <= 32 * (int64_t)b.B || a.topk > 0) && !f.buckets ? 5 : columns * c.Hkv + items >= 256 * 1024 ? 8 : 7;
   const int cols = 1 << f.cols_log2;
   auto cut = [](int64_t tokens, int64_t units, int64_t wanted, int64_t most) {
     int64_t n = div_up(wanted, units);
@@ -1057,17 +1156,17 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   Pieces& p = f.p;
   p = {1, a.S, 1, (int)window, 0};
   if (a.topk > 0 && a.S <= b.L) {  // (no row has a longer span among its candidates)
-    const int64_t units = f.routed_tiles ? items / cols + 1 : items;
-    p.routed_tokens = (int)div_up(div_up(a.S, cut(a.S, units, f.routed_tiles ? 1024 : 4096, 64)), 16) * 16;
+    const int64_t units = f.buckets ? items / cols + 1 : items;
+    p.routed_tokens = (int)div_up(div_up(a.S, cut(a.S, units, 1024, 64)), 16) * 16;
     p.routed = (int)div_up(a.S, p.routed_tokens);
   }
-  if (f.window_tiles) {
+  if (f.tiles) {
     f.plan.tiles = (int)(columns / cols) + b.B;
     const int64_t longest = window + cols / a.G + 17;  // a tile's rows may lie in two windows; it begins at a multiple of 16
-    const int64_t n = cut(longest, (int64_t)f.plan.tiles * c.Hkv, cols == 32 ? 2048 : 1024, 256);
+    const int64_t n = cut(longest, (int64_t)f.plan.tiles * c.Hkv, cols == 32 ? 4096 : 1024, 256);
     p.window_tokens = (int)div_up(div_up(longest, n), 64) * 64;
     p.window = (int)div_up(longest, p.window_tokens);
-    f.plan.window_units = (int64_t)f.plan.tiles * p.window * c.Hkv;
+    f.plan.window_units = div_up((int64_t)f.plan.tiles * p.window * c.Hkv, 8) * 8;
   } else {
     p.window_tokens = (int)div_up(window, cut(window, rh, 4096, 256));
     p.window = (int)div_up(window, p.window_tokens);
@@ -1075,19 +1174,23 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   p.count = a.topk * p.routed + p.window;
   f.o_bytes = align_up((size_t)rh * p.count * c.D * (c.dtype == SL_BF16 ? sizeof(_Float16) : sizeof(float)), 256);
   f.lse_bytes = align_up((size_t)rh * p.count * sizeof(float), 256);
-  if (f.routed_tiles) {
+  f.units = f.plan.window_units;
+  if (f.buckets) {
     f.plan.spans = (int)spans;
     f.plan.buckets = (int)buckets;
     f.most_tiles = items / cols + (buckets < items ? buckets : items);
+    f.units += div_up(f.most_tiles, 8) * 8 * p.routed;
     f.plan_bytes = align_up(sizeof(int32_t) * (2 * (size_t)buckets + 64 + (size_t)f.most_tiles + (size_t)items + (size_t)f.most_tiles * cols), 256);
+  } else {
+    f.units += items * p.routed;
   }
   return f;
 }
 
-// The stages of a tile of 128 columns fill 64 KB of dynamic LDS beside the static arrays: more than a kernel has without asking.
-template <int D, int NW, int CB, int STEP>
+// The stages fill up to 64 KB of dynamic LDS beside the static arrays: more than a kernel has without asking.
+template <int D, int NW, int CB, int STEP, int STAGES>
 bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
-  constexpr int kBytes = 2 * 2 * STEP * D * (int)sizeof(bf16_t);
+  constexpr int kBytes = STAGES * 2 * STEP * D * (int)sizeof(bf16_t);
   static std::mutex mu;
   static bool asked[64];
   int dev = -1;
@@ -1095,12 +1198,11 @@ bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipSt
   {
     std::lock_guard<std::mutex> lock(mu);
     if (!asked[dev])
-      asked[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(tile_kernel<D, NW, CB, STEP>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                       kBytes) == hipSuccess;
+      asked[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(tile_kernel<D, NW, CB, STEP, STAGES>),
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) == hipSuccess;
     if (!asked[dev]) return false;
   }
-  const int64_t units = plan.window_units + (f.routed_tiles ? f.most_tiles * f.p.routed : 0);
-  tile_kernel<D, NW, CB, STEP><<<grid_of(units), 64 * NW, kBytes, st>>>(x, plan);
+  tile_kernel<D, NW, CB, STEP, STAGES><<<grid_of(f.units), 64 * NW, kBytes, st>>>(x, plan);
   return true;
 }
 
@@ -1108,9 +1210,9 @@ template <typename T, int D>
 sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
   const int64_t rh = (int64_t)x.a.Hq * x.b.rows;
   if constexpr (sizeof(T) == 2) {
-    if (f.window_tiles) {
+    if (f.tiles) {
       TilePlan plan = f.plan;
-      if (f.routed_tiles) {
+      if (f.buckets) {
         plan.counts = reinterpret_cast<int32_t*>(ws + f.o_bytes + 2 * f.lse_bytes);
         plan.first_tile = plan.counts + plan.buckets;
         plan.tile_count = plan.first_tile + plan.buckets;
@@ -1124,14 +1226,21 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
         tiles_kernel<<<1, 1024, 0, st>>>(plan, f.cols_log2);
         items_kernel<<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x, plan, f.cols_log2);
       }
-      if (!(f.cols_log2 == 5 ? launch_tiles<D, 1, 1, 32>(x, f, plan, st) : launch_tiles<D, 4, 1, 64>(x, f, plan, st))) return SL_ERR_LAUNCH;
+      const bool done = f.cols_log2 == 5   ? launch_tiles<D, 1, 1, 32, 2>(x, f, plan, st)
+                        : f.cols_log2 == 7 ? launch_tiles<D, 4, 1, 64, 2>(x, f, plan, st)
+                                           : launch_tiles<D, 4, 2, 64, 2>(x, f, plan, st);
+      if (!done) return SL_ERR_LAUNCH;
     }
   }
   if (x.row_pieces > 0) rows_kernel<T, D><<<grid_of(rh * x.row_pieces), 256, 0, st>>>(x);
-  if (x.p.count == 1 && x.row_pieces == 0) mend_kernel<T, D><<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x);
-  // a wavefront a row and head where there are enough of them
-  else if (rh >= 4096 && x.p.count <= 1024) merge_kernel<T, D, 1><<<grid_of(div_up(rh, 4)), 256, 4 * x.p.count * sizeof(float), st>>>(x);
-  else merge_kernel<T, D, 4><<<grid_of(rh), 256, x.p.count * sizeof(float), st>>>(x);
+  if (x.p.count == 1 && f.tiles) {
+    mend_kernel<T, D, true><<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x);
+  } else if (rh >= 4096 && x.p.count <= 1024) {  // enough rows to give each a wavefront
+    if (f.tiles) mend_kernel<T, D, false><<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x);
+    merge_kernel<T, D, 1><<<grid_of(div_up(rh, 4)), 256, 4 * x.p.count * sizeof(float), st>>>(x);
+  } else {
+    merge_kernel<T, D, 4><<<grid_of(rh), 256, x.p.count * sizeof(float), st>>>(x);
+  }
   return hipGetLastError() == hipSuccess ? SL_OK : SL_ERR_LAUNCH;
 }
 
@@ -1148,7 +1257,7 @@ sl_status paged_attention(const PageCache& c, const PagedBatch& b, const PagedAt
   char* const at = static_cast<char*>(ws);
   PagedArgs x = {c, b, a, f.p, Q, idx, scores, O, LSE, ws, reinterpret_cast<float*>(at + f.o_bytes),
                  reinterpret_cast<float*>(at + f.o_bytes + f.lse_bytes), a.scale * kLog2e,
-                 f.routed_tiles ? 0 : f.window_tiles ? a.topk * f.p.routed : f.p.count};
+                 f.tiles ? 0 : f.p.count};
   if (c.dtype == SL_BF16) return c.D == 128 ? launch<bf16_t, 128>(x, f, at, st) : launch<bf16_t, 64>(x, f, at, st);
   return c.D == 128 ? launch<float, 128>(x, f, at, st) : launch<float, 64>(x, f, at, st);
 }
