@@ -593,11 +593,15 @@ def sl_anchor_attention_decode_batched(batch: DecodeBatch, window, backward_fact
     return batch.O
 
 
+# Checks of the paged calls are plain integers too: a step of a serving loop makes several of them, a few microseconds each.
 def _int32(t, name, device, n=None):
-    """A contiguous int32 list on the cache's device."""
-    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.device != device or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{name} must be a contiguous int32 tensor{'' if n is None else f' of {n} values'} on {device}")
-    return t
+    """A contiguous int32 list on the cache's device (its index, -1 = host memory); returns its length."""
+    if t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != device or (n is not None and t.numel() != n):
+        raise ValueError(f"{name} must be a contiguous int32 tensor{'' if n is None else f' of {n} values'} on the cache's device")
+    return t.numel()
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 class PageCache:
@@ -614,8 +618,9 @@ class PageCache:
         layers, n_pages, Hkv, ps, D = K5.shape
         if tables.dtype != torch.int32 or tables.dim() != 2 or not tables.is_contiguous() or tables.device != K.device or V.device != K.device:
             raise ValueError("tables must be a contiguous int32 tensor [n_seqs, max_pages] on the device of K and V")
-        _int32(lens, "lens", K.device, tables.shape[0])
-        _int32(refs, "refs", K.device, n_pages)
+        self.index = K.get_device()
+        _int32(lens, "lens", self.index, tables.shape[0])
+        _int32(refs, "refs", self.index, n_pages)
         self.K, self.V, self.tables, self.lens, self.refs = K, V, tables, lens, refs
         self.dtype, self.device, self.layers, self.page_size, self.Hkv, self.D = K.dtype, K.device, layers, ps, Hkv, D
         st = K5.stride()
@@ -628,96 +633,102 @@ class PageCache:
         lens, refs = (torch.zeros(n, dtype=torch.int32, device=device) for n in (n_seqs, n_pages))
         return cls(K, V, torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device), lens, refs)
 
-    def check_device(self):
-        """Kernels are enqueued on the current device's current stream."""
-        if self.device.type != "cuda" or self.device.index != torch.cuda.current_device():
+    def stream(self):
+        """The current stream of the cache's device, which has to be the current one."""
+        if self.index < 0 or self.index != _current_device():
             raise ValueError(f"the cache lies on {self.device}, which is not the current device")
+        return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(self.index)
 
     def batch(self, seqs, cu_rows, rows=0, L=0, layer=0):
         """The sl_paged_batch of new tokens cu_rows[b] .. cu_rows[b + 1] - 1 of sequence seqs[b]."""
-        _int32(seqs, "seqs", self.device)
-        _int32(cu_rows, "cu_rows", self.device, seqs.shape[0] + 1)
-        self.check_device()
-        return SlPagedBatch(seqs.data_ptr(), cu_rows.data_ptr(), rows, int(L), seqs.shape[0], int(layer))
+        n = _int32(seqs, "seqs", self.index)
+        _int32(cu_rows, "cu_rows", self.index, n + 1)
+        return SlPagedBatch(seqs.data_ptr(), cu_rows.data_ptr(), rows, L, n, layer)
 
 
 def sl_pages_extend(cache: PageCache, seqs, cu_rows, ok=None):
     """Pages for the new tokens of each sequence, which lens counts from here on; ok[b]: 1 = served, 0 = left as it was."""
     b = cache.batch(seqs, cu_rows)
-    ok = torch.empty_like(seqs) if ok is None else _int32(ok, "ok", cache.device, seqs.shape[0])
-    _check(load().sl_pages_extend(ctypes.byref(cache.record), ctypes.byref(b), _ptr(ok), _stream()), "sl_pages_extend")
+    if ok is None:
+        ok = torch.empty_like(seqs)
+    else:
+        _int32(ok, "ok", cache.index, b.B)
+    _check(load().sl_pages_extend(cache.record, b, ok.data_ptr(), cache.stream()), "sl_pages_extend")
     return ok
 
 
 def sl_pages_fork(cache: PageCache, src, dst, ok=None):
     """Makes the empty sequence dst[i] a copy of src[i] that shares its full pages; ok[i]: 1 = made."""
-    _int32(src, "src", cache.device)
-    _int32(dst, "dst", cache.device, src.shape[0])
-    cache.check_device()
-    ok = torch.empty_like(src) if ok is None else _int32(ok, "ok", cache.device, src.shape[0])
-    _check(load().sl_pages_fork(ctypes.byref(cache.record), _ptr(src), _ptr(dst), src.shape[0], _ptr(ok), _stream()), "sl_pages_fork")
+    n = _int32(src, "src", cache.index)
+    _int32(dst, "dst", cache.index, n)
+    if ok is None:
+        ok = torch.empty_like(src)
+    else:
+        _int32(ok, "ok", cache.index, n)
+    _check(load().sl_pages_fork(cache.record, src.data_ptr(), dst.data_ptr(), n, ok.data_ptr(), cache.stream()), "sl_pages_fork")
     return ok
 
 
 def sl_pages_free(cache: PageCache, seqs):
     """Empties the listed sequences."""
-    _int32(seqs, "seqs", cache.device)
-    cache.check_device()
-    _check(load().sl_pages_free(ctypes.byref(cache.record), _ptr(seqs), seqs.shape[0], _stream()), "sl_pages_free")
+    n = _int32(seqs, "seqs", cache.index)
+    _check(load().sl_pages_free(cache.record, seqs.data_ptr(), n, cache.stream()), "sl_pages_free")
 
 
 def sl_pages_compact(cache: PageCache, map=None, ws=None):
     """Moves the pages in use to the front of the pool; returns the new number of each page, -1 for the free ones."""
-    lib = load()
-    cache.check_device()
-    map = torch.empty_like(cache.refs) if map is None else _int32(map, "map", cache.device, cache.refs.shape[0])
+    lib, stream = load(), cache.stream()
+    if map is None:
+        map = torch.empty_like(cache.refs)
+    else:
+        _int32(map, "map", cache.index, cache.refs.shape[0])
     ws = Workspace(cache.device) if ws is None else ws
-    wptr, wbytes = ws.get(_need(lib.sl_pages_compact_workspace_bytes(ctypes.byref(cache.record))))
-    _check(lib.sl_pages_compact(ctypes.byref(cache.record), _ptr(map), wptr, wbytes, _stream()), "sl_pages_compact")
+    wptr, wbytes = ws.get(_need(lib.sl_pages_compact_workspace_bytes(cache.record)))
+    _check(lib.sl_pages_compact(cache.record, map.data_ptr(), wptr, wbytes, stream), "sl_pages_compact")
     return map
 
 
 def sl_paged_append(cache: PageCache, seqs, cu_rows, K, V, layer=0):
     """Writes the new tokens' K and V [Hkv, rows, D] into their pages."""
-    if (K.dim() != 3 or K.shape[0] != cache.Hkv or K.shape[2] != cache.D or K.stride(2) != 1 or V.shape != K.shape
-            or V.stride() != K.stride() or K.dtype != cache.dtype or V.dtype != cache.dtype
-            or K.device != cache.device or V.device != cache.device):
+    shape, st = K.shape, K.stride()
+    if (len(shape) != 3 or shape[0] != cache.Hkv or shape[2] != cache.D or st[2] != 1 or V.shape != shape or V.stride() != st
+            or K.dtype is not cache.dtype or V.dtype is not cache.dtype or K.get_device() != cache.index or V.get_device() != cache.index):
         raise ValueError("expect K, V [Hkv, rows, D] of the cache's dtype and device, contiguous innermost, V with K's strides")
-    b = cache.batch(seqs, cu_rows, K.shape[1], 0, layer)
-    _check(load().sl_paged_append(ctypes.byref(cache.record), ctypes.byref(b), _ptr(K), _ptr(V), K.stride(0), K.stride(1), _stream()),
-           "sl_paged_append")
+    b = cache.batch(seqs, cu_rows, shape[1], 0, layer)
+    _check(load().sl_paged_append(cache.record, b, K.data_ptr(), V.data_ptr(), st[0], st[1], cache.stream()), "sl_paged_append")
 
 
 def sl_paged_span_keys(cache: PageCache, seqs, cu_rows, Ks, S, layer=0):
     """Keys of the spans that the new tokens complete, into Ks [n_seqs, Hkv, n_spans, D]; Ks[s] with L = n_spans * S is what
     span-search takes."""
-    if (Ks.dim() != 4 or Ks.shape[0] != cache.lens.shape[0] or Ks.shape[1] != cache.Hkv or Ks.shape[3] != cache.D
-            or not Ks.is_contiguous() or Ks.dtype != cache.dtype):
-        raise ValueError("expect contiguous Ks [n_seqs, Hkv, n_spans, D] of the cache's dtype")
+    shape = Ks.shape
+    if (len(shape) != 4 or shape[0] != cache.record.n_seqs or shape[1] != cache.Hkv or shape[3] != cache.D or not Ks.is_contiguous()
+            or Ks.dtype is not cache.dtype or Ks.get_device() != cache.index):
+        raise ValueError("expect contiguous Ks [n_seqs, Hkv, n_spans, D] of the cache's dtype and device")
     b = cache.batch(seqs, cu_rows, 0, 0, layer)
-    _check(load().sl_paged_span_keys(ctypes.byref(cache.record), ctypes.byref(b), int(S), Ks.shape[2], _ptr(Ks), _stream()),
-           "sl_paged_span_keys")
+    _check(load().sl_paged_span_keys(cache.record, b, S, shape[2], Ks.data_ptr(), cache.stream()), "sl_paged_span_keys")
     return Ks
 
 
 def _paged_attention(cache, seqs, cu_rows, Q, idx, scores, S, layer, L, scale, ws):
-    lib = load()
-    if Q.dim() != 3 or Q.shape[2] != cache.D or Q.stride(2) != 1 or Q.dtype != cache.dtype or Q.device != cache.device:
+    shape, st = Q.shape, Q.stride()
+    if len(shape) != 3 or shape[2] != cache.D or st[2] != 1 or Q.dtype is not cache.dtype or Q.get_device() != cache.index:
         raise ValueError("expect Q [Hq, rows, D] of the cache's dtype and device with contiguous innermost dimension")
-    Hq, T, _ = Q.shape
-    topk = 0 if idx is None else idx.shape[2]
-    a = SlPagedAttention(Hq, int(S), topk, float(scale), Q.stride(0), Q.stride(1), 0, 0)
-    if topk:
-        if idx.dtype != torch.int32 or idx.shape != (Hq, T, topk) or idx.stride(2) != 1:
-            raise ValueError("idx must be int32 [Hq, rows, topk] with contiguous innermost dimension")
-        a.idx_stride_h, a.idx_stride_t = idx.stride(0), idx.stride(1)
-    if scores is not None and (scores.dtype != torch.float32 or scores.shape != idx.shape or scores.stride() != idx.stride()):
-        raise ValueError("scores must be float32 with the shape and strides of idx")
+    Hq, T, _ = shape
+    topk, ih, it = 0, 0, 0
+    if idx is not None:
+        topk = idx.shape[-1]
+        if idx.dtype is not torch.int32 or idx.shape != (Hq, T, topk) or idx.get_device() != cache.index or (topk and idx.stride(2) != 1):
+            raise ValueError("idx must be int32 [Hq, rows, topk] on the cache's device with contiguous innermost dimension")
+        ih, it, _ = idx.stride()
+    if scores is not None and (idx is None or scores.dtype is not torch.float32 or scores.shape != idx.shape
+                               or scores.stride() != idx.stride() or scores.get_device() != cache.index):
+        raise ValueError("scores must be float32 with the shape, strides and device of idx")
+    a = SlPagedAttention(Hq, S, topk, scale, st[0], st[1], ih, it)
     b = cache.batch(seqs, cu_rows, T, L, layer)
-    need = _need(lib.sl_paged_attention_workspace_bytes(ctypes.byref(cache.record), ctypes.byref(b), ctypes.byref(a)))
     # Scratch is the call's own unless the caller gives a workspace: calls on different streams and graphs do not share it.
     ws = Workspace(cache.device) if ws is None else ws
-    return a, b, ws.get(need), ws
+    return a, b, ws.get(_need(load().sl_paged_attention_workspace_bytes(cache.record, b, a))), ws
 
 
 def sl_paged_span_attention(cache: PageCache, seqs, cu_rows, Q, idx, S, layer=0, L=0, scale=0.0, ws=None, out=None):
@@ -725,17 +736,18 @@ def sl_paged_span_attention(cache: PageCache, seqs, cu_rows, Q, idx, S, layer=0,
     sequence of the batch holds more tokens (0: as many as a table can).  Returns O [Hq, rows, D], LSE [Hq, rows]; rows that belong to no
     sequence are left as they were (with out) or undefined."""
     a, b, (wptr, wbytes), held = _paged_attention(cache, seqs, cu_rows, Q, idx, None, S, layer, L, scale, ws)
-    O, LSE = (torch.empty(Q.shape, dtype=Q.dtype, device=Q.device),
-              torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)) if out is None else out
-    _check(load().sl_paged_span_attention(ctypes.byref(cache.record), ctypes.byref(b), ctypes.byref(a), _ptr(Q), _ptr(idx), _ptr(O),
-                                          _ptr(LSE), wptr, wbytes, _stream()), "sl_paged_span_attention")
+    stream = cache.stream()
+    O, LSE = (Q.new_empty(Q.shape), Q.new_empty(Q.shape[:2], dtype=torch.float32)) if out is None else out
+    _check(load().sl_paged_span_attention(cache.record, b, a, Q.data_ptr(), _ptr(idx), O.data_ptr(), LSE.data_ptr(), wptr, wbytes, stream),
+           "sl_paged_span_attention")
     return O, LSE
 
 
 def sl_paged_span_attention_combined(cache: PageCache, seqs, cu_rows, Q, idx, scores, S, layer=0, L=0, scale=0.0, ws=None, out=None):
     """The gated form: scores as span-search wrote them beside idx.  Returns O [Hq, rows, D]."""
     a, b, (wptr, wbytes), held = _paged_attention(cache, seqs, cu_rows, Q, idx, scores, S, layer, L, scale, ws)
-    O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device) if out is None else out
-    _check(load().sl_paged_span_attention_combined(ctypes.byref(cache.record), ctypes.byref(b), ctypes.byref(a), _ptr(Q), _ptr(idx),
-                                                   _ptr(scores), _ptr(O), wptr, wbytes, _stream()), "sl_paged_span_attention_combined")
+    stream = cache.stream()
+    O = Q.new_empty(Q.shape) if out is None else out
+    _check(load().sl_paged_span_attention_combined(cache.record, b, a, Q.data_ptr(), _ptr(idx), _ptr(scores), O.data_ptr(), wptr, wbytes,
+                                                   stream), "sl_paged_span_attention_combined")
     return O

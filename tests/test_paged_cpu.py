@@ -144,8 +144,9 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     for seqs, cu in ((one.long(), two), (one, one), (one, two.float()), (two[::2][:1].expand(1), two[:1])):
         with pytest.raises(ValueError):
             cache.batch(seqs, cu)
+    assert cache.batch(one, two).B == 1
     with pytest.raises(ValueError):      # a cache in host memory
-        cache.batch(one, two)
+        cache.stream()
     with pytest.raises(ValueError):
         B.sl_pages_fork(cache, one, two)
     with pytest.raises(ValueError):
