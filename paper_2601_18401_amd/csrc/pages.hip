@@ -2,6 +2,8 @@
 //
 // All of it is data movement and small integers.  What decides who gets which page is one workgroup's
 // prefix sums, so that the result does not depend on an order of atomics; what moves data is spread over the chip.
+#include <climits>
+
 #include "paged.h"
 
 namespace sl {
@@ -9,25 +11,39 @@ namespace sl {
 namespace {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kPerThread = 16;  // reference counts a thread looks at per pass: four 16-byte loads
 
-// Sum of v over the threads before this one; total: over all.  (1024 threads)
-template <typename I>
-__device__ __forceinline__ I scan_before(I v, I* s_wave, I* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  I x = v;
+// Running sum over the lanes of a wavefront, own value included: rows of 16 lanes by shifts, then from row to row.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast:15 -> rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast:31 -> rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ int64_t wave_scan(int64_t v) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
-    const I y = __shfl_up(x, off, 64);
-    if (lane >= off) x += y;
+    const int64_t y = __shfl_up(v, off, 64);
+    if (lane >= off) v += y;
   }
-  __syncthreads();  // (the last call's readers of s_wave are done)
-  if (lane == 63) s_wave[wave] = x;
+  return v;
+}
+
+// Sum of v over the threads before this one; total: over all.  (1024 threads; turn alternates between calls, so that one
+// barrier a call is enough: a turn's sums are written again behind the barrier of the call between.)
+template <typename I>
+__device__ __forceinline__ I scan_before(I v, I (*s_wave)[kPlanThreads / 64], int turn, I* total) {
+  const int wave = threadIdx.x >> 6;
+  const I x = wave_scan(v);
+  if ((threadIdx.x & 63) == 63) s_wave[turn][wave] = x;
   __syncthreads();
   I before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kPlanThreads / 64; ++w) {
-    const I y = s_wave[w];
+    const I y = s_wave[turn][w];
     if (w < wave) before += y;
     all += y;
   }
@@ -35,11 +51,17 @@ __device__ __forceinline__ I scan_before(I v, I* s_wave, I* total) {
   return before + x - v;
 }
 
-// refs[at .. at + 15], 1 where there is no page: such are not free
-__device__ __forceinline__ void load_refs(const int32_t* __restrict__ refs, int at, int n, int (&r)[kPerThread]) {
-  if (at + kPerThread <= n) {
+// Reference counts a thread looks at in a pass: 4 to begin with, 16 in large pools, whose passes are many.  (The planning kernels run
+// once through their code, most of the time waiting for it: what is unrolled for nothing is paid for.  Eight forks in a
+// cache of 3000 pages: 11.7 us with 16 and the list's loops unrolled, 20 KB of code.)
+constexpr int kLargePool = 65536;
+
+// refs[at .. at + PER - 1], 1 where there is no page: such are not free
+template <int PER>
+__device__ __forceinline__ void load_refs(const int32_t* __restrict__ refs, int at, int n, int (&r)[PER]) {
+  if (at + PER <= n) {
 #pragma unroll
-    for (int i = 0; i < kPerThread / 4; ++i) {
+    for (int i = 0; i < PER / 4; ++i) {
       const int4 x = reinterpret_cast<const int4*>(refs + at)[i];
       r[4 * i] = x.x;
       r[4 * i + 1] = x.y;
@@ -48,131 +70,128 @@ __device__ __forceinline__ void load_refs(const int32_t* __restrict__ refs, int 
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i) r[i] = at + i < n ? refs[at + i] : 1;
+    for (int i = 0; i < PER; ++i) r[i] = at + i < n ? refs[at + i] : 1;
   }
 }
 
-// Entry i of a list (in LDS) is its sequence's first one.  Four entries a read, the same ones for the wavefront.
-__device__ __forceinline__ bool listed_first(const int32_t* list, int i) {
-  const int s = list[i], upto = __builtin_amdgcn_readfirstlane(i | 63);
-  bool first = true;
-#pragma unroll 4
-  for (int k = 0; k < upto; k += 4) {
-    const int4 x = *reinterpret_cast<const int4*>(list + k);
-    first = first && !(x.x == s && k < i) && !(x.y == s && k + 1 < i) && !(x.z == s && k + 2 < i) && !(x.w == s && k + 3 < i);
-  }
-  return first;
-}
-
-// Pages for new tokens (FORK: for copies of partly filled pages).  end[i]: pages that entries 0 .. i need together; an
-// entry is served if the free pages reach that far.  The counts are scanned from the front until the last page is found;
-// what one workgroup reads of them at once (64 KB) takes about a microsecond.
-template <bool FORK>
+// Pages for new tokens (FORK: for copies of partly filled pages).  s_end[i]: pages that entries 0 .. i need together (I: a
+// type that holds it); an entry is served if the free pages reach that far.  The counts are scanned from the front, a pass at a
+// time, until the last page is found; a pass lists its free pages in LDS, and a thread then takes each to its entry.
+// Chains of loads and barriers bound it, not bytes: the first counts are asked for before the entries, and an entry's lengths at once.
+template <bool FORK, typename I, int PER>
 __global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(const PageCache c, const int32_t* __restrict__ src,
                                                                   const int32_t* __restrict__ seqs, const int32_t* __restrict__ cu,
                                                                   int n, int32_t* __restrict__ ok) {
-  __shared__ int64_t s_end[SL_MAX_PAGE_OPS];
-  __shared__ __align__(16) int32_t s_seq[SL_MAX_PAGE_OPS];  // -1: not to be served
-  __shared__ int32_t s_have[SL_MAX_PAGE_OPS];  // FORK: tokens of the source; else: pages held
-  __shared__ int64_t s_wave64[kPlanThreads / 64];
-  __shared__ int32_t s_wave[kPlanThreads / 64];
+  constexpr int kPass = kPlanThreads * PER;
+  __shared__ I s_end[SL_MAX_PAGE_OPS];
+  __shared__ int32_t s_seq[SL_MAX_PAGE_OPS];
+  __shared__ int32_t s_have[SL_MAX_PAGE_OPS];  // tokens held (FORK: by the source); -1: not to be served
+  __shared__ I s_sums[2][kPlanThreads / 64];
+  __shared__ int32_t s_counts[2][kPlanThreads / 64];
+  // The first entry of every sequence (an open hash of twice as many places as entries), then a pass's free pages.
+  constexpr int kPlaces = 2 * SL_MAX_PAGE_OPS;
+  __shared__ __align__(16) int32_t s_shared[2 * kPlaces > kPass ? 2 * kPlaces : kPass];
+  int32_t *const s_key = s_shared, *const s_first = s_shared + kPlaces, *const s_free = s_shared;
   const int most = c.max_pages * c.ps;
-  for (int i = threadIdx.x; i < n; i += kPlanThreads) s_seq[i] = seqs[i];
+  int r[PER];
+  load_refs<PER>(c.refs, threadIdx.x * PER, c.n_pages, r);
+#pragma unroll 1
+  for (int k = threadIdx.x; k < 2 * kPlaces / 4; k += kPlanThreads) reinterpret_cast<int4*>(s_shared)[k] = make_int4(-1, -1, -1, -1);
   __syncthreads();
-  bool good[SL_MAX_PAGE_OPS / kPlanThreads];
-#pragma unroll
-  for (int q = 0; q < SL_MAX_PAGE_OPS / kPlanThreads; ++q) {
-    const int i = q * kPlanThreads + threadIdx.x;
-    good[q] = i < n && (uint32_t)s_seq[i] < (uint32_t)c.n_seqs && listed_first(s_seq, i);
+  auto place_of = [&](int s) {
+    uint32_t at = (uint32_t)s * 2654435761u / (0x100000000ull / kPlaces);
+    for (;; at = (at + 1) % kPlaces) {
+      const int there = atomicCAS(&s_key[at], -1, s);
+      if (there == -1 || there == s) return at;
+    }
+  };
+#pragma unroll 1
+  for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    const int s = seqs[i];
+    s_seq[i] = s;
+    if ((uint32_t)s < (uint32_t)c.n_seqs) atomicMin(reinterpret_cast<uint32_t*>(&s_first[place_of(s)]), (uint32_t)i);
   }
   __syncthreads();
-  int64_t before = 0;
-#pragma unroll
-  for (int q = 0; q < SL_MAX_PAGE_OPS / kPlanThreads; ++q) {
-    if (q * kPlanThreads >= n) break;
-    const int i = q * kPlanThreads + threadIdx.x;
-    int need = 0;
-    if (good[q]) {
-      const int len = c.lens[s_seq[i]];
-      if constexpr (FORK) {
-        const int from = src[i];
-        const int held = (uint32_t)from < (uint32_t)c.n_seqs && from != s_seq[i] ? c.lens[from] : -1;
-        good[q] = len == 0 && held >= 0 && held <= most;
-        if (good[q]) {
-          s_have[i] = held;
-          need = (uint32_t)held != (uint32_t)held / c.by_ps * c.ps;
-        }
-      } else {
-        const int64_t add = (int64_t)cu[i + 1] - cu[i];
-        good[q] = len >= 0 && add >= 0 && len + add <= most;
-        if (good[q]) {
-          s_have[i] = (uint32_t)(len + c.ps - 1) / c.by_ps;
-          need = (int)((uint32_t)(len + (int)add + c.ps - 1) / c.by_ps) - s_have[i];
-        }
-      }
-    }
-    int64_t all;
-    const int64_t at = before + scan_before<int64_t>(need, s_wave64, &all);
+  I total = 0;
+  int turn = 0;
+#pragma unroll 1
+  for (int at = 0; at < n; at += kPlanThreads, turn ^= 1) {
+    const int i = at + threadIdx.x;
+    int have = -1, need = 0;
     if (i < n) {
-      s_end[i] = at + need;
-      if (!good[q]) s_seq[i] = -1;
-    }
-    before += all;
-  }
-  __syncthreads();
-  const int64_t total = before;
-  // free pages, in order, to the entries
-  int64_t found = 0;
-  int r[kPerThread];
-  load_refs(c.refs, threadIdx.x * kPerThread, c.n_pages, r);
-  for (int64_t base = 0; base < c.n_pages && found < total; base += kPlanThreads * kPerThread) {
-    int next[kPerThread];
-    const int64_t ahead = base + kPlanThreads * kPerThread;
-    if (ahead < c.n_pages) load_refs(c.refs, (int)min(ahead + threadIdx.x * kPerThread, (int64_t)c.n_pages), c.n_pages, next);
-    int mine = 0;
-#pragma unroll
-    for (int k = 0; k < kPerThread; ++k) mine += r[k] <= 0;
-    int all;
-    int64_t rank = found + scan_before<int>(mine, s_wave, &all);
-    if (mine > 0 && rank < total) {
-      int e = 0;
-      {  // the entry that gets page `rank`: the first with end > rank
-        int lo = 0, hi = n - 1;
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (s_end[mid] > rank) hi = mid;
-          else lo = mid + 1;
+      const int s = s_seq[i];
+      if ((uint32_t)s < (uint32_t)c.n_seqs && s_first[place_of(s)] == i) {
+        const int len = c.lens[s];
+        if (FORK) {
+          const int from = src[i];
+          const int held = (uint32_t)from < (uint32_t)c.n_seqs && from != s ? c.lens[from] : -1;
+          if (len == 0 && held <= most) have = held;
+          need = (uint32_t)held != (uint32_t)held / c.by_ps * c.ps;
+        } else {
+          const int64_t add = (int64_t)cu[i + 1] - cu[i];
+          if (len >= 0 && add >= 0 && len + add <= most) have = len;
+          need = (int)((uint32_t)(len + (int)add + c.ps - 1) / c.by_ps - (uint32_t)(len + c.ps - 1) / c.by_ps);
         }
-        e = lo;
       }
+    }
+    if (have < 0) need = 0;
+    I all;
+    const I end = total + scan_before<I>(need, s_sums, turn, &all) + need;
+    if (i < n) {
+      s_end[i] = end;
+      s_have[i] = have;
+    }
+    total += all;
+  }
+  // free pages, in order, to the entries
+  I found = 0;
+#pragma unroll 1
+  for (int64_t base = 0; base < c.n_pages && found < total; base += kPass, turn ^= 1) {
+    int next[PER];
+    const int64_t ahead = base + kPass;
+    if (ahead < c.n_pages) load_refs<PER>(c.refs, (int)min(ahead + threadIdx.x * PER, (int64_t)c.n_pages), c.n_pages, next);
+    int mine = 0, all;
 #pragma unroll
-      for (int k = 0; k < kPerThread; ++k) {
-        if (r[k] > 0 || rank >= total) continue;
-        while (s_end[e] <= rank) ++e;
-        const int page = (int)base + threadIdx.x * kPerThread + k;
-        const int64_t first = e ? s_end[e - 1] : 0;
-        const int at = FORK ? (int)((uint32_t)s_have[e] / c.by_ps) : s_have[e] + (int)(rank - first);
-        c.tables[(int64_t)s_seq[e] * c.max_pages + at] = page;
-        c.refs[page] = 1;
-        ++rank;
+    for (int k = 0; k < PER; ++k) mine += r[k] <= 0;
+    int rank = scan_before<int>(mine, s_counts, turn, &all);
+    const I left = total - found;
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (r[k] <= 0) s_free[rank++] = (int)base + threadIdx.x * PER + k;
+    __syncthreads();
+    const int upto = left < all ? (int)left : all;
+#pragma unroll 1
+    for (int k = threadIdx.x; k < upto; k += kPlanThreads) {
+      const I place = found + k;
+      int lo = 0, hi = n - 1;
+      while (lo < hi) {  // the entry that gets it: the first with end > place
+        const int mid = (lo + hi) >> 1;
+        if (s_end[mid] > place) hi = mid;
+        else lo = mid + 1;
       }
+      const I first = lo ? s_end[lo - 1] : 0;
+      const int page = s_free[k], at = FORK ? (int)((uint32_t)s_have[lo] / c.by_ps) : (int)((uint32_t)(s_have[lo] + c.ps - 1) / c.by_ps) + (int)(place - first);
+      c.tables[(int64_t)s_seq[lo] * c.max_pages + at] = page;
+      c.refs[page] = 1;
     }
     found += all;
     if (ahead < c.n_pages) {
 #pragma unroll
-      for (int k = 0; k < kPerThread; ++k) r[k] = next[k];
+      for (int k = 0; k < PER; ++k) r[k] = next[k];
+      __syncthreads();  // (s_free is filled again)
     }
   }
   __syncthreads();
+#pragma unroll 1
   for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-    const int64_t first = i ? s_end[i - 1] : 0, end = s_end[i];
-    const bool served = s_seq[i] >= 0 && (end == first || end <= found);
+    const I first = i ? s_end[i - 1] : 0, end = s_end[i];
+    const int have = s_have[i];
+    const bool served = have >= 0 && (end == first || end <= found);
     if (served) {
-      if (FORK) c.lens[s_seq[i]] = s_have[i];
-      else c.lens[s_seq[i]] += cu[i + 1] - cu[i];
-    } else if (!FORK && s_seq[i] >= 0) {  // the entry at which the pages ran out gives back what it got
-      for (int64_t k = first; k < found && k < end; ++k) {
-        int32_t* const t = c.tables + (int64_t)s_seq[i] * c.max_pages + s_have[i] + (k - first);
+      c.lens[s_seq[i]] = FORK ? have : have + cu[i + 1] - cu[i];
+    } else if (!FORK && have >= 0) {  // the entry at which the pages ran out gives back what it got
+      for (I k = first; k < found && k < end; ++k) {
+        int32_t* const t = c.tables + (int64_t)s_seq[i] * c.max_pages + (uint32_t)(have + c.ps - 1) / c.by_ps + (int)(k - first);
         c.refs[*t] = 0;
         *t = -1;
       }
@@ -219,7 +238,8 @@ __device__ __forceinline__ void copy_part(const PageCache& c, int from, int to, 
 
 constexpr int kForkEntries = 1024;  // table entries of a workgroup
 
-// What plan_pages_kernel<true> decided: dst's table from src's, references, the copied last page.
+// What plan_pages_kernel<true> decided: dst's table from src's, references, the copied last page.  The first fork of a source adds the
+// references of all (200 forks of 16 sequences: 240000 atomics otherwise, of which as many wait for each other as forks share a source).
 __global__ __launch_bounds__(256) void fork_kernel(const PageCache c, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
                                                    const int32_t* __restrict__ ok, int n, int chunks) {
   const int f = blockIdx.x, y = blockIdx.y;
@@ -229,10 +249,29 @@ __global__ __launch_bounds__(256) void fork_kernel(const PageCache c, const int3
   const int32_t* const from = c.tables + (int64_t)s * c.max_pages;
   int32_t* const to = c.tables + (int64_t)d * c.max_pages;
   if (y < chunks) {
+    if (y * kForkEntries >= full) return;
+    __shared__ int s_forks, s_first;
+    if (threadIdx.x == 0) {
+      s_forks = 0;
+      s_first = n;
+    }
+    __syncthreads();
+    int forks = 0, first = n;
+    for (int k = threadIdx.x; k < n; k += 256)
+      if (src[k] == s && ok[k]) {
+        ++forks;
+        first = min(first, k);
+      }
+    if (forks) {
+      atomicAdd(&s_forks, forks);
+      atomicMin(&s_first, first);
+    }
+    __syncthreads();
+    forks = s_first == f ? s_forks : 0;
     for (int k = y * kForkEntries + threadIdx.x; k < full && k < (y + 1) * kForkEntries; k += 256) {
       const int page = from[k];
       to[k] = page;
-      if ((uint32_t)page < (uint32_t)c.n_pages) atomicAdd(&c.refs[page], 1);
+      if (forks && (uint32_t)page < (uint32_t)c.n_pages) atomicAdd(&c.refs[page], forks);
     }
   } else if (part) {
     const int page = from[full];
@@ -240,66 +279,90 @@ __global__ __launch_bounds__(256) void fork_kernel(const PageCache c, const int3
   }
 }
 
+// A sequence listed twice is emptied by its first entry.
 __global__ __launch_bounds__(256) void free_kernel(const PageCache c, const int32_t* __restrict__ seqs) {
   const int s = seqs[blockIdx.x];
   if ((uint32_t)s >= (uint32_t)c.n_seqs) return;
+  bool earlier = false;
+  for (int k = threadIdx.x; k < (int)blockIdx.x; k += 256) earlier = earlier || seqs[k] == s;
+  if (__syncthreads_or(earlier)) return;
   if (blockIdx.y == 0 && threadIdx.x == 0) c.lens[s] = 0;
   int32_t* const t = c.tables + (int64_t)s * c.max_pages;
   for (int k = blockIdx.y * kForkEntries + threadIdx.x; k < c.max_pages && k < ((int)blockIdx.y + 1) * kForkEntries; k += 256) {
-    if (t[k] == -1) continue;
-    const int page = atomicExch(&t[k], -1);  // (a sequence listed twice: one of the two gets the page)
+    const int page = t[k];
+    if (page == -1) continue;
+    t[k] = -1;
     if ((uint32_t)page < (uint32_t)c.n_pages) atomicSub(&c.refs[page], 1);
   }
 }
 
-// The pages that move: pair k is moves[k] -> moves[half + k], k < *count.
+// The pages that move: pair k is moves[k] -> moves[half + k], k < *count.  The first pass's counts stay in registers between the two
+// looks at them, and up to 4096 pairs in LDS: a round trip to memory is a tenth of a small cache's plan.
+constexpr int kKeptMoves = 4096;
+template <int PER>
 __global__ __launch_bounds__(kPlanThreads) void plan_compact_kernel(const PageCache c, int32_t* __restrict__ map, int32_t* __restrict__ count,
                                                                     int32_t* __restrict__ moves, int half) {
-  __shared__ int32_t s_wave[kPlanThreads / 64];
-  int used = 0;
-  int r[kPerThread];
-  for (int64_t base = 0; base < c.n_pages; base += kPlanThreads * kPerThread) {
-    load_refs(c.refs, (int)min(base + threadIdx.x * kPerThread, (int64_t)c.n_pages), c.n_pages, r);
-    const int at = (int)min(base + threadIdx.x * kPerThread, (int64_t)c.n_pages);
+  __shared__ int32_t s_sums[2][kPlanThreads / 64];
+  __shared__ int32_t s_from[kKeptMoves], s_to[kKeptMoves], s_refs[kKeptMoves];
+  constexpr int64_t kPass = kPlanThreads * PER;
+  int first[PER], r[PER];
+  auto place = [&](int64_t base) { return (int)min(base + threadIdx.x * PER, (int64_t)c.n_pages); };
+  load_refs<PER>(c.refs, place(0), c.n_pages, first);
+  int used = 0, n, turn = 0;
+#pragma unroll 1
+  for (int64_t base = 0; base < c.n_pages; base += kPass) {
+    const int at = place(base);
+    if (base > 0) load_refs<PER>(c.refs, at, c.n_pages, r);
 #pragma unroll
-    for (int k = 0; k < kPerThread; ++k) used += at + k < c.n_pages && r[k] > 0;
+    for (int k = 0; k < PER; ++k) used += at + k < c.n_pages && (base > 0 ? r[k] : first[k]) > 0;
   }
-  int n;
-  scan_before<int>(used, s_wave, &n);
+  scan_before<int>(used, s_sums, turn, &n);
   int holes = 0, movers = 0;  // so far
-  for (int64_t base = 0; base < c.n_pages; base += kPlanThreads * kPerThread) {
-    const int at = (int)min(base + threadIdx.x * kPerThread, (int64_t)c.n_pages);
-    load_refs(c.refs, at, c.n_pages, r);
-    int h = 0, m = 0, hs, ms;
 #pragma unroll
-    for (int k = 0; k < kPerThread; ++k) {
-      h += at + k < n && r[k] <= 0;
-      m += at + k >= n && at + k < c.n_pages && r[k] > 0;
+  for (int k = 0; k < PER; ++k) r[k] = first[k];
+#pragma unroll 1
+  for (int64_t base = 0; base < c.n_pages; base += kPass) {
+    const int at = place(base);
+    if (base > 0) load_refs<PER>(c.refs, at, c.n_pages, r);
+    int both = 0, all;  // holes, and movers in the upper half: 16384 of a pass at most
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      both += at + k < n && r[k] <= 0;
+      both += (at + k >= n && at + k < c.n_pages && r[k] > 0) << 16;
     }
-    int hk = holes + scan_before<int>(h, s_wave, &hs), mk = movers + scan_before<int>(m, s_wave, &ms);
+    const uint32_t before = (uint32_t)scan_before<int>(both, s_sums, turn ^= 1, &all);
+    int hk = holes + (int)(before & 0xffff), mk = movers + (int)(before >> 16);
 #pragma unroll
-    for (int k = 0; k < kPerThread; ++k) {
+    for (int k = 0; k < PER; ++k) {
       const int p = at + k;
       if (p >= c.n_pages) continue;
-      if (p < n) {
-        if (r[k] <= 0) moves[half + hk++] = p;
-        else map[p] = p;
-      } else if (r[k] > 0) {
+      const bool on = r[k] > 0;
+      if (!on || p < n) map[p] = on ? p : -1;
+      if (p < n && !on) {
+        if (hk < kKeptMoves) s_to[hk] = p;
+        moves[half + hk++] = p;
+      }
+      if (p >= n && on) {
+        if (mk < kKeptMoves) {
+          s_from[mk] = p;
+          s_refs[mk] = r[k];
+        }
         moves[mk++] = p;
       }
-      if (r[k] <= 0) map[p] = -1;
     }
-    holes += hs;
-    movers += ms;
-  }
-  __syncthreads();  // (also orders the workgroup's own writes to moves before the reads)
-  for (int k = threadIdx.x; k < movers; k += kPlanThreads) {
-    const int from = moves[k], to = moves[half + k];
-    map[from] = to;
-    c.refs[to] = c.refs[from];
-    c.refs[from] = 0;
+    holes += (uint32_t)all & 0xffff;
+    movers += (uint32_t)all >> 16;
   }
   if (threadIdx.x == 0) *count = movers;
+  __syncthreads();  // (also orders the workgroup's own writes to moves before the reads)
+#pragma unroll 1
+  for (int k = threadIdx.x; k < movers; k += kPlanThreads) {
+    const bool near = k < kKeptMoves;
+    const int from = near ? s_from[k] : moves[k], to = near ? s_to[k] : moves[half + k], refs = near ? s_refs[k] : c.refs[from];
+    map[from] = to;
+    c.refs[to] = refs;
+    c.refs[from] = 0;
+  }
 }
 
 // The first `tables` workgroups rewrite the tables, the others move pages.
@@ -367,15 +430,23 @@ sl_status launched() { return hipGetLastError() == hipSuccess ? SL_OK : SL_ERR_L
 
 }  // namespace
 
+template <bool FORK, typename I>
+static void plan_pages(const PageCache& c, const int32_t* src, const int32_t* seqs, const int32_t* cu, int n, int32_t* ok, hipStream_t st) {
+  if (c.n_pages > kLargePool) plan_pages_kernel<FORK, I, 16><<<1, kPlanThreads, 0, st>>>(c, src, seqs, cu, n, ok);
+  else plan_pages_kernel<FORK, I, 4><<<1, kPlanThreads, 0, st>>>(c, src, seqs, cu, n, ok);
+}
+
 sl_status pages_extend(const PageCache& c, const PagedBatch& b, int32_t* ok, hipStream_t st) {
   if (b.B == 0) return SL_OK;
-  plan_pages_kernel<false><<<1, kPlanThreads, 0, st>>>(c, nullptr, b.seqs, b.cu, b.B, ok);
+  // (an entry's need is at most a table's width)
+  if ((int64_t)b.B * c.max_pages < INT_MAX) plan_pages<false, int>(c, nullptr, b.seqs, b.cu, b.B, ok, st);
+  else plan_pages<false, int64_t>(c, nullptr, b.seqs, b.cu, b.B, ok, st);
   return launched();
 }
 
 sl_status pages_fork(const PageCache& c, const int32_t* src, const int32_t* dst, int n, int32_t* ok, hipStream_t st) {
   if (n == 0) return SL_OK;
-  plan_pages_kernel<true><<<1, kPlanThreads, 0, st>>>(c, src, dst, nullptr, n, ok);
+  plan_pages<true, int>(c, src, dst, nullptr, n, ok, st);
   const int chunks = (c.max_pages + kForkEntries - 1) / kForkEntries;
   fork_kernel<<<dim3(n, chunks + c.layers * 2 * c.Hkv), 256, 0, st>>>(c, src, dst, ok, n, chunks);
   return launched();
@@ -393,7 +464,8 @@ sl_status pages_compact(const PageCache& c, int32_t* map, void* ws, hipStream_t 
   int32_t* const count = static_cast<int32_t*>(ws);
   int32_t* const moves = count + 64;
   const int half = c.n_pages / 2 + 1;  // pages that move are above the used ones' number, holes below: at most half of the pool
-  plan_compact_kernel<<<1, kPlanThreads, 0, st>>>(c, map, count, moves, half);
+  if (c.n_pages > kLargePool) plan_compact_kernel<16><<<1, kPlanThreads, 0, st>>>(c, map, count, moves, half);
+  else plan_compact_kernel<4><<<1, kPlanThreads, 0, st>>>(c, map, count, moves, half);
   const int64_t entries = (int64_t)c.n_seqs * c.max_pages, units = (int64_t)(half - 1) * c.layers * 2 * c.Hkv;
   const int tables = (int)min((entries + 1023) / 1024, (int64_t)512), copies = (int)min(units, (int64_t)2048);
   compact_kernel<<<tables + copies, 256, 0, st>>>(c, map, count, moves, half, tables);
