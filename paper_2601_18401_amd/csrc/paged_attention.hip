@@ -41,7 +41,7 @@ struct TilePlan {
   int64_t window_units;  // tiles * pieces of a window * Hkv
   int spans, buckets;    // spans of the longest sequence; B * Hkv * spans
   int32_t *counts, *first_tile;  // [buckets]
-  int32_t *tile_count, *tile_bucket;
+  int4* records;   // [most_tiles] in the order of the workgroups: {first token of the span, entry, kv head, place of the tile << 9 | items}
   int32_t *ranks;  // [Hq * rows * topk] an item's place in its bucket, -1 for empty slots
   int32_t *items;  // [tiles][cols] (row and head) * 32 + slot
 };
@@ -514,12 +514,13 @@ struct ColumnRun {
   Entry at;
   int u0, n;  // columns u0 .. u0 + n - 1 of the entry: row r0 + u / G, head u % G of the group
 };
-__device__ __forceinline__ ColumnRun columns_of(const PagedArgs& x, int tile, int cols) {
-  auto first = [&](int r0, int e) { return (int)((int64_t)max(r0, 0) * x.a.G / cols) + e; };
+// (G: columns of a row)
+__device__ __forceinline__ ColumnRun columns_of(const PagedArgs& x, int tile, int cols, int G) {
+  auto first = [&](int r0, int e) { return (int)((int64_t)max(r0, 0) * G / cols) + e; };
   ColumnRun r;
   r.at = find_entry(x, [&](int r0, int e) { return first(r0, e) <= tile; });
   const int64_t u0 = (int64_t)(tile - first(r.at.r0, r.at.e)) * cols;
-  const int64_t n = (int64_t)(min(r.at.r1, x.b.rows) - r.at.r0) * x.a.G - u0;
+  const int64_t n = (int64_t)(min(r.at.r1, x.b.rows) - r.at.r0) * G - u0;
   r.u0 = (int)u0;
   r.n = r.at.r0 < 0 || u0 < 0 || n <= 0 ? 0 : (int)min(n, (int64_t)cols);
   return r;
@@ -564,7 +565,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
     if (at >= plan.tiles * x.p.window) return;
     const int tile = plan.tiles - 1 - at / x.p.window, piece = at % x.p.window;
     part = x.a.topk * x.p.routed + piece;
-    const ColumnRun run = columns_of(x, tile, COLS);
+    const ColumnRun run = columns_of(x, tile, COLS, x.a.G);
     if (run.n <= 0) return;
     const int r0 = run.at.r0, u0 = run.u0, len = run.at.len, pos0 = len - (run.at.r1 - r0);
     seq = run.at.s;
@@ -601,21 +602,19 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
     all_lo = p0 < 0 || p1 > most ? INT_MAX : lo_of(q1);  // (a row without a token attends nothing)
     all_last = last_of(q0);
   } else if (NW > 1) {
-    // Tiles of one bucket read the same rows: an eighth of the list is given to the workgroups of each XCD, which share an L2.
-    const int64_t u = unit - plan.window_units;
-    const int count_all = *plan.tile_count, share = (count_all + 7) / 8;
-    const int64_t at = u / 8;
-    const int tile = (int)(u % 8) * share + (int)(at / x.p.routed);
-    part = (int)(at % x.p.routed);
-    if (at / x.p.routed >= share || tile >= count_all) return;
-    const int bucket = plan.tile_bucket[tile], count = plan.counts[bucket] - (tile - plan.first_tile[bucket]) * COLS;
-    const int j = bucket % plan.spans, eh = bucket / plan.spans;
-    head = eh % x.c.Hkv;
-    seq = x.b.seqs[eh / x.c.Hkv];
+    // eight tiles, one for each XCD, and their pieces in turn
+    const int64_t u = unit - plan.window_units, group8 = u / (8 * x.p.routed);
+    const int in_group = (int)(u - group8 * 8 * x.p.routed);
+    part = in_group >> 3;
+    const int4 rec = plan.records[group8 * 8 + (in_group & 7)];
+    const int count = rec.w, j = rec.x;
+    if (count == 0) return;
+    head = rec.y % x.c.Hkv;
+    seq = x.b.seqs[rec.y / x.c.Hkv];
     begin = j * x.a.S + part * x.p.routed_tokens;
     end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
     for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
-      s_rh[c] = c < count ? plan.items[(int64_t)tile * COLS + c] : -1;  // (row and head) * 32 + slot
+      s_rh[c] = c < count ? plan.items[(int64_t)rec.z * COLS + c] : -1;  // (row and head) * 32 + slot
       s_lo[c] = c < count ? begin : INT_MAX;
       s_last[c] = c < count ? end - 1 : -1;
     }
@@ -814,55 +813,57 @@ __global__ __launch_bounds__(256) void zero_kernel(int32_t* __restrict__ to, int
   for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) to[i] = 0;
 }
 
-// An item's place in its bucket.  A workgroup takes kCountCols columns (rows and heads of an entry's kv head, as a window tile does): it
-// counts them in LDS, adds its counts to the buckets', and hands out the places that it got; their order among workgroups
-// may differ from run to run, which no result depends on.  Atomics on the buckets alone took 188 us for 512000 items of 512 buckets.
+// An item's place in its bucket.  A workgroup takes kCountRows rows of an entry with the heads of a kv head's group: it counts their items
+// in LDS, adds its counts to the buckets', and hands out the places that it got; their order among workgroups may differ from run to run,
+// which no result depends on.  Atomics on the buckets alone took 188 us for 512000 items of 512 buckets.
 // Pieces of empty slots are marked here: no tile writes them.
-constexpr int kCountCols = 1024, kCountSpans = 12288;
-__global__ __launch_bounds__(256) void count_kernel(const PagedArgs x, const TilePlan plan) {
+constexpr int kCountRows = 64, kCountSpans = 12288;
+__global__ __launch_bounds__(1024) void count_kernel(const PagedArgs x, const TilePlan plan) {
   extern __shared__ int32_t s_count[];  // [spans], if they fit
   const int head = blockIdx.y;
-  const ColumnRun run = columns_of(x, blockIdx.x, kCountCols);
+  const ColumnRun run = columns_of(x, blockIdx.x, kCountRows, 1);
   if (run.n <= 0) return;
   const bool local = plan.spans <= kCountSpans;
   if (local)
-    for (int j = threadIdx.x; j < plan.spans; j += 256) s_count[j] = 0;
+    for (int j = threadIdx.x; j < plan.spans; j += 1024) s_count[j] = 0;
   __syncthreads();
   int32_t* const counts = plan.counts + ((int64_t)run.at.e * x.c.Hkv + head) * plan.spans;
+  const int of_head = run.n * x.a.topk, items = of_head * x.a.G;
   for (int pass = local ? 0 : 1; pass < 2; ++pass) {
-    for (int u = threadIdx.x; u < run.n; u += 256) {
-      const int row = run.at.r0 + (run.u0 + u) / x.a.G, h = head * x.a.G + (run.u0 + u) % x.a.G;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < items; i += 1024) {
+      const int g = i / of_head, at = i - g * of_head, r = at / x.a.topk, k = at - r * x.a.topk;
+      const int h = head * x.a.G + g, row = run.at.r0 + run.u0 + r;
       const int pos = position_of(x, run.at, row), c = pos < 0 ? 0 : pos / x.a.S;
       const int64_t rh = (int64_t)h * x.b.rows + row;
-      const int32_t* const slots = x.idx + h * x.a.ish + row * x.a.ist;
-      for (int k = 0; k < x.a.topk; ++k) {
-        const int j = slots[k];
-        if (j >= 0 && j < c) {
-          if (pass == 0) atomicAdd(&s_count[j], 1);
-          else plan.ranks[rh * x.a.topk + k] = local ? atomicAdd(&s_count[j], 1) : atomicAdd(&counts[j], 1);
-        } else if (pass == 1) {
-          plan.ranks[rh * x.a.topk + k] = -1;
-          for (int q = 0; q < x.p.routed; ++q) x.part_lse[rh * x.p.count + k * x.p.routed + q] = -INFINITY;
-        }
+      const int j = x.idx[h * x.a.ish + row * x.a.ist + k];
+      if (j >= 0 && j < c) {
+        if (pass == 0) atomicAdd(&s_count[j], 1);
+        else plan.ranks[rh * x.a.topk + k] = local ? atomicAdd(&s_count[j], 1) : atomicAdd(&counts[j], 1);
+      } else if (pass == 1) {
+        plan.ranks[rh * x.a.topk + k] = -1;
+        for (int q = 0; q < x.p.routed; ++q) x.part_lse[rh * x.p.count + k * x.p.routed + q] = -INFINITY;
       }
     }
     if (pass == 0) {
       __syncthreads();
-      for (int j = threadIdx.x; j < plan.spans; j += 256)
+      for (int j = threadIdx.x; j < plan.spans; j += 1024)
         if (s_count[j]) s_count[j] = atomicAdd(&counts[j], s_count[j]);
       __syncthreads();
     }
   }
 }
 
-// Tiles of each bucket in the buckets' order; one workgroup.
-__global__ __launch_bounds__(1024) void tiles_kernel(const TilePlan plan, int cols_log2) {
+// Tiles of each bucket in the buckets' order; one workgroup.  Tiles of one bucket read the same rows: workgroups u = x (mod 8) run on
+// XCD x, which has an L2 of its own, and are given the x-th eighth of the list, in its order.
+__global__ __launch_bounds__(1024) void tiles_kernel(const TilePlan plan, int cols_log2, int most_tiles) {
   __shared__ int s_wave[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int before = 0;
+  auto tiles_of = [&](int i) { return i < plan.buckets ? (plan.counts[i] + (1 << cols_log2) - 1) >> cols_log2 : 0; };
+  int total = 0;
+#pragma unroll 1
   for (int base = 0; base < plan.buckets; base += 1024) {
-    const int i = base + threadIdx.x;
-    const int n = i < plan.buckets ? (plan.counts[i] + (1 << cols_log2) - 1) >> cols_log2 : 0;
+    const int i = base + threadIdx.x, n = tiles_of(i);
     int v = n;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -872,33 +873,39 @@ __global__ __launch_bounds__(1024) void tiles_kernel(const TilePlan plan, int co
     __syncthreads();
     if (lane == 63) s_wave[wave] = v;
     __syncthreads();
-    int at = before + v - n, all = 0;
+    int at = total + v - n;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       if (k < wave) at += s_wave[k];
-      all += s_wave[k];
+      total += s_wave[k];
     }
-    if (i < plan.buckets) {
-      plan.first_tile[i] = at;
-      for (int k = 0; k < n; ++k) plan.tile_bucket[at + k] = i;
-    }
-    before += all;
+    if (i < plan.buckets) plan.first_tile[i] = at;
   }
-  if (threadIdx.x == 0) *plan.tile_count = before;
+  const int share = (total + 7) / 8;
+#pragma unroll 1
+  for (int base = 0; base < plan.buckets; base += 1024) {
+    const int i = base + threadIdx.x, n = tiles_of(i);
+    if (n == 0) continue;
+    const int first = plan.first_tile[i], count = plan.counts[i];
+    for (int k = 0; k < n; ++k) {
+      const int tile = first + k, x = tile / share;
+      plan.records[(tile - x * share) * 8 + x] = make_int4(i % plan.spans, i / plan.spans, tile, min(count - (k << cols_log2), 1 << cols_log2));
+    }
+  }
+  for (int k = threadIdx.x; k < most_tiles; k += 1024)
+    if ((k & 7) * share + (k >> 3) >= total || (k >> 3) >= share) plan.records[k].w = 0;
 }
 
 __global__ __launch_bounds__(256) void items_kernel(const PagedArgs x, const TilePlan plan, int cols_log2) {
-  const int64_t rh = workgroup() * 256 + threadIdx.x;
-  if (rh >= (int64_t)x.a.Hq * x.b.rows) return;
-  const int h = (int)(rh / x.b.rows), row = (int)(rh - (int64_t)h * x.b.rows);
+  const int64_t i = workgroup() * 256 + threadIdx.x;
+  const int rh = (int)(i / x.a.topk), k = (int)(i - (int64_t)rh * x.a.topk);
+  if (rh >= x.a.Hq * x.b.rows) return;
+  const int h = rh / x.b.rows, row = rh - h * x.b.rows;
   if (row < x.b.cu[0] || row >= x.b.cu[x.b.B]) return;
-  const int e = entry_of_row(x.b.cu, x.b.B, row);
-  const int32_t* const slots = x.idx + h * x.a.ish + row * x.a.ist;
-  const int first = (e * x.c.Hkv + h / x.a.G) * plan.spans;
-  for (int k = 0; k < x.a.topk; ++k) {
-    const int rank = plan.ranks[rh * x.a.topk + k];
-    if (rank >= 0) plan.items[((int64_t)plan.first_tile[first + slots[k]] << cols_log2) + rank] = (int)rh * 32 + k;
-  }
+  const int rank = plan.ranks[i];
+  if (rank < 0) return;
+  const int e = entry_of_row(x.b.cu, x.b.B, row), j = x.idx[h * x.a.ish + row * x.a.ist + k];
+  plan.items[((int64_t)plan.first_tile[(e * x.c.Hkv + h / x.a.G) * plan.spans + j] << cols_log2) + rank] = rh * 32 + k;
 }
 
 // ------------------------------------------------------------------ merge
@@ -1178,9 +1185,10 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   if (f.buckets) {
     f.plan.spans = (int)spans;
     f.plan.buckets = (int)buckets;
-    f.most_tiles = items / cols + (buckets < items ? buckets : items);
-    f.units += div_up(f.most_tiles, 8) * 8 * p.routed;
-    f.plan_bytes = align_up(sizeof(int32_t) * (2 * (size_t)buckets + 64 + (size_t)f.most_tiles + (size_t)items + (size_t)f.most_tiles * cols), 256);
+    // (a share of eight may be a tile short of its length)
+    f.most_tiles = div_up(items / cols + (buckets < items ? buckets : items), 8) * 8;
+    f.units += f.most_tiles * p.routed;
+    f.plan_bytes = align_up(sizeof(int32_t) * (align_up(2 * (size_t)buckets, 64) + 4 * (size_t)f.most_tiles + (size_t)items + (size_t)f.most_tiles * cols), 256);
   } else {
     f.units += items * p.routed;
   }
@@ -1215,16 +1223,15 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
       if (f.buckets) {
         plan.counts = reinterpret_cast<int32_t*>(ws + f.o_bytes + 2 * f.lse_bytes);
         plan.first_tile = plan.counts + plan.buckets;
-        plan.tile_count = plan.first_tile + plan.buckets;
-        plan.tile_bucket = plan.tile_count + 64;
-        plan.ranks = plan.tile_bucket + f.most_tiles;
+        plan.records = reinterpret_cast<int4*>(plan.counts + align_up(2 * (size_t)plan.buckets, 64));
+        plan.ranks = reinterpret_cast<int32_t*>(plan.records + f.most_tiles);
         plan.items = plan.ranks + rh * x.a.topk;
         const int64_t blocks = div_up(plan.buckets, 1024);
         zero_kernel<<<(unsigned)(blocks < 1024 ? blocks : 1024), 256, 0, st>>>(plan.counts, plan.buckets);
-        const int64_t runs = (int64_t)x.b.rows * x.a.G / kCountCols + x.b.B;
-        count_kernel<<<dim3((unsigned)runs, x.c.Hkv), 256, plan.spans <= kCountSpans ? plan.spans * sizeof(int32_t) : 0, st>>>(x, plan);
-        tiles_kernel<<<1, 1024, 0, st>>>(plan, f.cols_log2);
-        items_kernel<<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x, plan, f.cols_log2);
+        const int64_t runs = (int64_t)x.b.rows / kCountRows + x.b.B;
+        count_kernel<<<dim3((unsigned)runs, x.c.Hkv), 1024, plan.spans <= kCountSpans ? plan.spans * sizeof(int32_t) : 0, st>>>(x, plan);
+        tiles_kernel<<<1, 1024, 0, st>>>(plan, f.cols_log2, (int)f.most_tiles);
+        items_kernel<<<grid_of(div_up(rh * x.a.topk, 256)), 256, 0, st>>>(x, plan, f.cols_log2);
       }
       const bool done = f.cols_log2 == 5   ? launch_tiles<D, 1, 1, 32, 2>(x, f, plan, st)
                         : f.cols_log2 == 7 ? launch_tiles<D, 4, 1, 64, 2>(x, f, plan, st)
