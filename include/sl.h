@@ -346,7 +346,7 @@ typedef struct sl_page_cache {
   int32_t* lens;    /* [n_seqs] tokens held                                       */
   int32_t* refs;    /* [n_pages]                                                  */
   int64_t layer_stride, page_stride;  /* element strides of K and V; 0 = packed; not below D */
-  int64_t kv_stride_h, kv_stride_t;   /* (0 = packed)                                        */
+  int64_t kv_stride_h, kv_stride_t;   /* (0 = packed; kv_stride_t at most 2^20)              */
   int32_t layers, n_pages, n_seqs, max_pages;  /* >= 1; max_pages * page_size <= 2^30 */
   int32_t page_size, Hkv, D, dtype;            /* D: 64 or 128 */
 } sl_page_cache;
@@ -358,7 +358,7 @@ typedef struct sl_page_cache {
 typedef struct sl_paged_batch {
   const int32_t* seqs;     /* [B] device */
   const int32_t* cu_rows;  /* [B + 1] device */
-  int64_t rows;            /* rows per head of the row tensors, 0 .. 2^25 */
+  int64_t rows;            /* rows per head of the row tensors, 0 .. 2^25 (attention: rows * Hq < 2^26) */
   int64_t L;               /* no sequence of the batch holds more tokens; 0 = max_pages * page_size.  Rows at
                               positions from L on are treated as rows without a token. */
   int32_t B;               /* 0 .. 65535 */

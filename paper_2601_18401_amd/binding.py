@@ -650,7 +650,7 @@ def sl_pages_extend(cache: PageCache, seqs, cu_rows, ok=None):
     """Pages for the new tokens of each sequence, which lens counts from here on; ok[b]: 1 = served, 0 = left as it was."""
     b = cache.batch(seqs, cu_rows)
     if ok is None:
-        ok = torch.empty_like(seqs)
+        ok = torch.empty(b.B, dtype=torch.int32, device=cache.device)
     else:
         _int32(ok, "ok", cache.index, b.B)
     _check(load().sl_pages_extend(cache.record, b, ok.data_ptr(), cache.stream()), "sl_pages_extend")
@@ -662,7 +662,7 @@ def sl_pages_fork(cache: PageCache, src, dst, ok=None):
     n = _int32(src, "src", cache.index)
     _int32(dst, "dst", cache.index, n)
     if ok is None:
-        ok = torch.empty_like(src)
+        ok = torch.empty(n, dtype=torch.int32, device=cache.device)
     else:
         _int32(ok, "ok", cache.index, n)
     _check(load().sl_pages_fork(cache.record, src.data_ptr(), dst.data_ptr(), n, ok.data_ptr(), cache.stream()), "sl_pages_fork")
@@ -679,7 +679,7 @@ def sl_pages_compact(cache: PageCache, map=None, ws=None):
     """Moves the pages in use to the front of the pool; returns the new number of each page, -1 for the free ones."""
     lib, stream = load(), cache.stream()
     if map is None:
-        map = torch.empty_like(cache.refs)
+        map = torch.empty(cache.record.n_pages, dtype=torch.int32, device=cache.device)
     else:
         _int32(map, "map", cache.index, cache.refs.shape[0])
     ws = Workspace(cache.device) if ws is None else ws
@@ -737,7 +737,11 @@ def sl_paged_span_attention(cache: PageCache, seqs, cu_rows, Q, idx, S, layer=0,
     sequence are left as they were (with out) or undefined."""
     a, b, (wptr, wbytes), held = _paged_attention(cache, seqs, cu_rows, Q, idx, None, S, layer, L, scale, ws)
     stream = cache.stream()
-    O, LSE = (Q.new_empty(Q.shape), Q.new_empty(Q.shape[:2], dtype=torch.float32)) if out is None else out
+    if out is None:
+        O = torch.empty(Q.shape, dtype=cache.dtype, device=cache.device)
+        LSE = torch.empty(Q.shape[:2], dtype=torch.float32, device=cache.device)
+    else:
+        O, LSE = out
     _check(load().sl_paged_span_attention(cache.record, b, a, Q.data_ptr(), _ptr(idx), O.data_ptr(), LSE.data_ptr(), wptr, wbytes, stream),
            "sl_paged_span_attention")
     return O, LSE
@@ -747,7 +751,7 @@ def sl_paged_span_attention_combined(cache: PageCache, seqs, cu_rows, Q, idx, sc
     """The gated form: scores as span-search wrote them beside idx.  Returns O [Hq, rows, D]."""
     a, b, (wptr, wbytes), held = _paged_attention(cache, seqs, cu_rows, Q, idx, scores, S, layer, L, scale, ws)
     stream = cache.stream()
-    O = Q.new_empty(Q.shape) if out is None else out
+    O = torch.empty(Q.shape, dtype=cache.dtype, device=cache.device) if out is None else out
     _check(load().sl_paged_span_attention_combined(cache.record, b, a, Q.data_ptr(), _ptr(idx), _ptr(scores), O.data_ptr(), wptr, wbytes,
                                                    stream), "sl_paged_span_attention_combined")
     return O

@@ -10,8 +10,10 @@ namespace {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-constexpr int64_t kMaxStride = (int64_t)1 << 40;  // elements: products with 32-bit counts stay inside 64 bits
-constexpr int64_t kMaxRows = (int64_t)1 << 25;    // 16-byte pieces of a row tensor's head count in 32 bits
+constexpr int64_t kMaxStride = (int64_t)1 << 40;     // elements: products with 32-bit counts stay inside 64 bits
+constexpr int64_t kMaxTokenStride = (int64_t)1 << 20;
+constexpr int64_t kMaxRows = (int64_t)1 << 25;       // 16-byte pieces of a row tensor's head count in 32 bits
+constexpr int64_t kMaxRowHeads = (int64_t)1 << 26;   // a row, its head and a slot of 32 count in 31 bits
 
 sl_status make_cache(const sl_page_cache* p, PageCache* c) {
   if (!p || !p->K || !p->V || !p->tables || !p->lens || !p->refs) return SL_ERR_INVALID_ARG;
@@ -25,7 +27,7 @@ sl_status make_cache(const sl_page_cache* p, PageCache* c) {
   if (p->Hkv > 1024 || p->layers > 4096 || (int64_t)p->layers * 2 * p->Hkv + p->max_pages / 1024 > 65000 || p->max_pages > (1 << 25))
     return SL_ERR_UNSUPPORTED;
   if (p->kv_stride_t < 0 || p->kv_stride_h < 0 || p->page_stride < 0 || p->layer_stride < 0) return SL_ERR_INVALID_ARG;
-  if (p->kv_stride_t > kMaxStride >> 12 || p->kv_stride_h > kMaxStride || p->page_stride > kMaxStride || p->layer_stride > kMaxStride << 8)
+  if (p->kv_stride_t > kMaxTokenStride || p->kv_stride_h > kMaxStride || p->page_stride > kMaxStride || p->layer_stride > kMaxStride << 8)
     return SL_ERR_UNSUPPORTED;
   c->tok = p->kv_stride_t ? p->kv_stride_t : p->D;
   c->head = p->kv_stride_h ? p->kv_stride_h : p->page_size * c->tok;
@@ -71,7 +73,7 @@ sl_status make_attention(const sl_paged_attention* p, const PageCache& c, const 
   if (!p || p->Hq < 1 || p->Hq % c.Hkv != 0 || p->S < 1 || p->topk < 0) return SL_ERR_INVALID_ARG;
   if (!(p->scale >= 0.f) || std::isinf(p->scale)) return SL_ERR_INVALID_ARG;
   if (p->topk > SL_MAX_TOPK || p->Hq / c.Hkv > 64 || p->Hq > 65535) return SL_ERR_UNSUPPORTED;
-  if ((int64_t)b.rows * p->Hq > ((int64_t)1 << 31) - 1) return SL_ERR_UNSUPPORTED;
+  if ((int64_t)b.rows * p->Hq >= kMaxRowHeads) return SL_ERR_UNSUPPORTED;
   if (p->q_stride_h < 0 || p->q_stride_t < 0 || p->idx_stride_h < 0 || p->idx_stride_t < 0) return SL_ERR_INVALID_ARG;
   if (p->q_stride_h > kMaxStride || p->q_stride_t > kMaxStride >> 8 || p->idx_stride_h > kMaxStride || p->idx_stride_t > kMaxStride >> 8)
     return SL_ERR_UNSUPPORTED;

@@ -5,6 +5,7 @@
 // joint form, and for the gated one alpha_t * exp2(lse_p - lse_t) summed over the slots t that the piece belongs to.
 #include <climits>
 #include <mutex>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -32,7 +33,7 @@ struct PagedArgs {
   float* part_lse;    // [Hq * rows][count] log2-sum-exp2; -inf: no token, and no output
   float* part_scale;  // [Hq * rows][count] of bf16 calls
   float scale_log2e;
-  int row_pieces;  // of a row, its first ones: taken row by row
+  bool marks;  // tiles write the records, and may have marked some
 };
 
 // Tiles of the matrix-core form.
@@ -93,8 +94,8 @@ __device__ __forceinline__ Entry find_entry(const PagedArgs& x, F&& before) {
     lo += k * step;
   }
   const int at = min(lo + lane, x.b.B - 1);
-  const int r0 = x.b.cu[at], r1 = x.b.cu[at + 1], s = x.b.seqs[at], len = length_of(x.c, s);
-  const int k = max(__popcll(__builtin_amdgcn_ballot_w64(lane < n && before(r0, at))) - 1, 0);
+  const int cu = x.b.cu[at], r0 = max(cu, 0), r1 = x.b.cu[at + 1], s = x.b.seqs[at], len = length_of(x.c, s);
+  const int k = max(__popcll(__builtin_amdgcn_ballot_w64(lane < n && before(cu, at))) - 1, 0);
   return {lo + k, __builtin_amdgcn_readlane(s, k), __builtin_amdgcn_readlane(len, k), __builtin_amdgcn_readlane(r0, k),
           __builtin_amdgcn_readlane(r1, k)};
 }
@@ -293,13 +294,13 @@ __device__ __forceinline__ void take_piece(const PagedArgs& x, int s, int rh, co
   if (lane < RS::LPR) *reinterpret_cast<Values*>(static_cast<Value*>(x.part_o) + rec * D + lane * RS::EPL) = v;
 }
 
-// Workgroup u takes piece u % row_pieces of row-and-head u / row_pieces.
+// Workgroup u takes piece u % count of row-and-head u / count.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void rows_kernel(const PagedArgs x) {
   __shared__ float s_o[4 * D], s_ml[8];
   const int64_t u = workgroup();
-  if (u >= (int64_t)x.a.Hq * x.b.rows * x.row_pieces) return;
-  const int rh = (int)(u / x.row_pieces), part = (int)(u - (int64_t)rh * x.row_pieces);
+  if (u >= (int64_t)x.a.Hq * x.b.rows * x.p.count) return;
+  const int rh = (int)(u / x.p.count), part = (int)(u - (int64_t)rh * x.p.count);
   const int h = rh / x.b.rows, row = rh - h * x.b.rows;
   const Entry at = entry_with_row(x, row);
   if (row < at.r0 || row >= at.r1) return;
@@ -308,23 +309,134 @@ __global__ __launch_bounds__(256) void rows_kernel(const PagedArgs x) {
   take_piece<T, D, 4, false>(x, at.s, rh, r, (int64_t)rh * x.p.count + part, s_o, s_ml);
 }
 
-// ------------------------------------------------------------------ tiles on the matrix cores (bf16)
+// All pieces of a row and head by one workgroup, whose four wavefronts share out the spans and cut the window in four: no
+// records, no merge.  Where there are rows enough to fill the chip (1000 rows and heads of 290 tokens: 33 -> 25 us).
+template <typename T, int D>
+__global__ __launch_bounds__(256) void whole_rows_kernel(const PagedArgs x) {
+  using RS = RowState<T, D>;
+  constexpr int RUN = 4 * RS::RPW;
+  __shared__ float s_o[4][D], s_ml[4][2];
+  if (workgroup() >= (int64_t)x.a.Hq * x.b.rows) return;
+  const int rh = (int)workgroup(), lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane % RS::LPR;
+  const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+  // asked for at once: the query, the slots and their scores, the row's entry
+  float q[RS::EPL];
+  Elem<T>::unpack(load16(static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst + lr * RS::EPL), q);
+  const int64_t at_slots = h * x.a.ish + row * x.a.ist;
+  int slot = lane < x.a.topk ? x.idx[at_slots + lane] : -1;
+  float score = x.a.combined && lane < x.a.topk ? x.scores[at_slots + lane] : -INFINITY;
+  const Entry at = entry_with_row(x, row);
+  if (row < at.r0 || row >= at.r1) return;
+  const int pos = position_of(x, at, row), c = pos < 0 ? 0 : pos / x.a.S;
+  if (slot >= c) slot = -1;
+#pragma unroll
+  for (int e = 0; e < RS::EPL; ++e) q[e] *= x.scale_log2e;
+  const int64_t base = x.b.layer * x.c.layer + h / x.a.G * x.c.head;
+  const T *const K = static_cast<const T*>(x.c.K) + base, *const V = static_cast<const T*>(x.c.V) + base;
+  const int32_t* const table = x.c.tables + (int64_t)max(at.s, 0) * x.c.max_pages;
+  RS st;
+  st.clear();
+  auto spans = [&](int k) {  // slot k's span, by this wavefront
+    const int j = __builtin_amdgcn_readlane(slot, k);
+    if (j >= 0) st.template attend<4>(x.c, K, V, table, q, j * x.a.S, (j + 1) * x.a.S, lane);
+  };
+  if (!x.a.combined)
+    for (int k = wave; k < x.a.topk; k += 4) spans(k);
+  if (pos >= 0) {
+    const int t0 = c * x.a.S, run = ((pos + 1 - t0 + 3) / 4 + RUN - 1) / RUN * RUN, from = t0 + wave * run;
+    st.template attend<4>(x.c, K, V, table, q, from, min(from + run, pos + 1), lane);
+  }
+  st.join_groups();
+  // the wavefronts' states into one, in every wavefront
+  if (lane == 0) {
+    s_ml[wave][0] = st.m;
+    s_ml[wave][1] = st.l;
+  }
+  if (lane < RS::LPR)
+#pragma unroll
+    for (int e = 0; e < RS::EPL; ++e) s_o[wave][lr * RS::EPL + e] = st.o[e];
+  __syncthreads();
+  float m = s_ml[0][0], l = 0.f, o[RS::EPL];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) m = max_of(m, s_ml[w][0]);
+#pragma unroll
+  for (int e = 0; e < RS::EPL; ++e) o[e] = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (s_ml[w][0] == -INFINITY) continue;
+    const float f = weight_of(s_ml[w][0], m);
+    l = fmaf(f, s_ml[w][1], l);
+#pragma unroll
+    for (int e = 0; e < RS::EPL; ++e) o[e] = fmaf(f, s_o[w][lr * RS::EPL + e], o[e]);
+  }
+  const bool gated = x.a.combined && __builtin_amdgcn_ballot_w64(slot >= 0) != 0;
+  if (!gated) {
+    if (wave != 0) return;
+    const bool none = m == -INFINITY;
+    const float inv = none ? 0.f : 1.f / l;
+    if (lane == 0 && x.LSE) x.LSE[rh] = none ? -INFINITY : (m + __log2f(l)) * kLn2;
+    if (lane < RS::LPR)
+#pragma unroll
+      for (int e = 0; e < RS::EPL; ++e)
+        Elem<T>::store1(static_cast<T*>(x.O) + (int64_t)rh * D + lr * RS::EPL + e, none ? 0.f : o[e] * inv);
+    return;
+  }
+  // m, l, o: the window.  Each slot's softmax goes over its span and the window.
+  if (slot < 0) score = -INFINITY;
+  float top = score;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) top = max_of(top, __shfl_xor(top, off, 64));
+  const float gate = slot >= 0 ? fast_exp2((score - top) * kLog2e) : 0.f;
+  float sum = gate, acc[RS::EPL];
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+#pragma unroll
+  for (int e = 0; e < RS::EPL; ++e) acc[e] = 0.f;
+  for (int k = wave; k < x.a.topk; k += 4) {
+    const float alpha = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(gate / sum), k));
+    if (alpha == 0.f) continue;
+    st.clear();
+    spans(k);
+    st.join_groups();
+    const float to = max_of(st.m, m);
+    if (to == -INFINITY) continue;
+    const float mine = weight_of(st.m, to), near = weight_of(m, to), by = alpha / (mine * st.l + near * l);
+#pragma unroll
+    for (int e = 0; e < RS::EPL; ++e) acc[e] = fmaf(by, mine * st.o[e] + near * o[e], acc[e]);
+  }
+  __syncthreads();
+  if (lane < RS::LPR)
+#pragma unroll
+    for (int e = 0; e < RS::EPL; ++e) s_o[wave][lr * RS::EPL + e] = acc[e];
+  __syncthreads();
+  if (threadIdx.x < D)
+    Elem<T>::store1(static_cast<T*>(x.O) + (int64_t)rh * D + threadIdx.x,
+                    (s_o[0][threadIdx.x] + s_o[1][threadIdx.x]) + (s_o[2][threadIdx.x] + s_o[3][threadIdx.x]));
+}
+
+// ------------------------------------------------------------------ tiles on the matrix cores
 // A tile is up to NW * 32 * CB query columns that attend one run of the sequence's tokens, each in a range of its own: rows and heads
 // of a kv head's group on their windows, or the rows that list a span.  Both products are taken transposed, so that a lane
 // owns a column:
 //   S^T[token][column] = K . Q^T      A = K rows from LDS, B = queries in registers
 //   O^T[d][column] += V^T . P^T       A = V through transposing LDS reads, B = P^T straight from the S^T accumulators
-// (v_mfma_f32_32x32x16_bf16: lane l of the result holds column l % 32 and rows 8 (r / 4) + 4 (l / 32) + r % 4; K rows are fed with
-// bits 2 and 3 of their number swapped, which makes a lane's eight consecutive accumulators eight consecutive tokens.)
+// (Lane l of a 32x32 result holds column l % 32 and rows 8 (r / 4) + 4 (l / 32) + r % 4.  bf16, 32x32x16: K rows are fed with bits 2 and 3
+// of their number swapped, which makes a lane's eight consecutive accumulators eight consecutive tokens.  fp32, 32x32x2: accumulator r of
+// the two halves is the pair of tokens that one product of V^T takes.)
 // K and V rows come by direct global -> LDS loads, 64 tokens a step in two stages, 16-byte pieces swizzled against bank conflicts.
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 
-template <int D>
-__device__ __forceinline__ int k_swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
-template <int D>
-__device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
+// Swizzle of a staged row's 16-byte pieces, so that those that lanes read together lie in different banks.
+template <typename T, int D>
+__device__ __forceinline__ int k_swizzle(int row) {
+  return sizeof(T) == 4 ? row & (D / 4 - 1) : D == 128 ? row & 15 : (row >> 1) & 7;
+}
+template <typename T, int D>
+__device__ __forceinline__ int v_swizzle(int row) {
+  return sizeof(T) == 4 ? 0 : D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
+}
 
 __device__ __forceinline__ float across_halves_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
@@ -342,27 +454,55 @@ __device__ __forceinline__ int lane_now() {
   return x;
 }
 
+__device__ uint4 g_zeros[32];  // what a row without a page is read from
+
 #define SL_LDS(p) ((__attribute__((address_space(3))) void*)(p))
 
-// Sixteen rows of a K or V stage: global -> LDS, 1 KB an instruction.  base: row 0 of the sixteen; rows from `rows` on become zeros
-// (what lies there may be anything, and zero times that need not be zero).
-template <int D, int TENSOR>
-__device__ __forceinline__ void stage_rows(bf16_t* to, int first_row, const bf16_t* base, int rows, int row_bytes, int lane) {
-  constexpr int LPR = D / 8, RPI = 64 / LPR;
+// Sixteen rows of a K (TENSOR 0) or V (1) stage: global -> LDS, 1 KB an instruction.
+template <typename T, int D>
+struct RowLanes {
+  static constexpr int LPR = D * (int)sizeof(T) / 16, RPI = 64 / LPR;  // lanes of a row, rows of an instruction
+};
+template <typename T, int D, int TENSOR>
+__device__ __forceinline__ int piece_of(int row, int lane) {
+  return lane % RowLanes<T, D>::LPR ^ (TENSOR == 0 ? k_swizzle<T, D>(row) : v_swizzle<T, D>(row));
+}
+// base: row 0 of the sixteen, which lie in one page; rows from `rows` on become zeros (what lies there may be anything, and zero times
+// that need not be zero).
+template <typename T, int D, int TENSOR>
+__device__ __forceinline__ void stage_rows(T* to, int first_row, const T* base, int rows, int row_bytes, int lane) {
+#if defined(__HIP_DEVICE_COMPILE__)  // (the host pass does not know the resource's type)
+  constexpr int LPR = RowLanes<T, D>::LPR, RPI = RowLanes<T, D>::RPI;
   const __amdgpu_buffer_rsrc_t from =
-      __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(base), 0, rows <= 0 ? 0 : (rows - 1) * row_bytes + D * 2, 0x00020000);
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, rows <= 0 ? 0 : (rows - 1) * row_bytes + D * (int)sizeof(T), 0x00020000);
 #pragma unroll
   for (int i = 0; i < 16 / RPI; ++i) {
     const int row = i * RPI + lane / LPR;
-    const int piece = lane % LPR ^ (TENSOR == 0 ? k_swizzle<D>(first_row + row) : v_swizzle<D>(first_row + row));
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, SL_LDS(to + i * 512), 16, row * row_bytes + piece * 16, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, SL_LDS(reinterpret_cast<char*>(to) + i * 1024), 16,
+                                             row * row_bytes + piece_of<T, D, TENSOR>(first_row + row, lane) * 16, 0, 0, 0);
+  }
+#endif
+}
+// Pages of any size: `at` of lane l is the element offset of row l of the stage, < 0: zeros.
+template <typename T, int D, int TENSOR>
+__device__ __forceinline__ void stage_rows_any(T* to, int first_row, const T* base, int64_t at, int lane) {
+  constexpr int LPR = RowLanes<T, D>::LPR, RPI = RowLanes<T, D>::RPI;
+#pragma unroll
+  for (int i = 0; i < 16 / RPI; ++i) {
+    const int row = first_row + i * RPI + lane / LPR;
+    const int lo = __shfl((int)(uint32_t)at, row, 64), hi = __shfl((int)(at >> 32), row, 64);
+    const char* const from =
+        hi < 0 ? reinterpret_cast<const char*>(g_zeros) : reinterpret_cast<const char*>(base + (((int64_t)hi << 32) | (uint32_t)lo));
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + piece_of<T, D, TENSOR>(row, lane) * 16),
+                                     SL_LDS(reinterpret_cast<char*>(to) + i * 1024), 16, 0, 0);
   }
 }
 
 // An LDS address that the compiler knows nothing of: where it sees that staged rows are read, it waits for every staging load
 // in flight, the next step's among them.
-__device__ __forceinline__ uint32_t lds_address(const bf16_t* p, int offset) {
-  uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) bf16_t*)p + offset;
+template <typename T>
+__device__ __forceinline__ uint32_t lds_address(const T* p, int offset) {
+  uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) T*)p + offset;
   asm volatile("" : "+v"(at));
   return at;
 }
@@ -378,20 +518,14 @@ __device__ __forceinline__ bf16x8 transposed8(const bf16_t* __restrict__ p) {
 }
 
 // A wavefront's CB blocks of 32 columns; it takes 32 * KB tokens at a time.
+// LIVE: which of the tokens have a page: a bit for each sixteen of them (uint32_t), or, where pages end anywhere, for each (uint64_t).
 template <int D, int CB, int KB>
-struct Tile {
-  static constexpr int KK = D / 16, DT = D / 32;
-  bf16x8 q[CB][KK];
-  f32x16 o[CB][DT];
+struct Softmax {
+  static constexpr int DT = D / 32;
+  f32x16 o[CB][DT], s[CB][KB];
   float m[CB], l[CB];
-  int kbase, vbase;
 
-  __device__ __forceinline__ void clear(int lane) {
-    const int col = lane & 31, hf = lane >> 5;
-    const int krow = (col & 0x13) | ((col & 4) << 1) | ((col & 8) >> 1);
-    kbase = 2 * (krow * D + ((hf ^ k_swizzle<D>(krow)) << 3));
-    const int vrow = (lane & 15) >> 2;
-    vbase = 2 * ((8 * hf + vrow) * D + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<D>(vrow)) << 3) + 4 * (lane & 1));
+  __device__ __forceinline__ void clear_sums() {
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       m[cb] = -INFINITY;
@@ -402,17 +536,96 @@ struct Tile {
         for (int r = 0; r < 16; ++r) o[cb][dt][r] = 0.f;
     }
   }
-  // 32 * KB tokens from t0 on, K rows at kt, V rows at vt (LDS); live: a bit for each sixteen of them whose page there is;
-  // lo, last (LDS): what each of the wavefront's columns attends
-  __device__ __forceinline__ void attend(const bf16_t* kt, const bf16_t* vt, int t0, bool masked, uint32_t live, float sc, const int* lo,
-                                         const int* last) {
-    f32x16 s[CB][KB];
+  __device__ __forceinline__ void clear_scores() {
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[cb][kb][r] = 0.f;
+  }
+  // token_of(r, half): token of accumulator r of a block of 32; lo, last (LDS): what each column attends
+  template <typename LIVE, typename F>
+  __device__ __forceinline__ void mask(int t0, LIVE live, const int* lo, const int* last, F&& token_of) {
+    const int ln = lane_now(), hf = ln >> 5;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const int from = lo[32 * cb + (ln & 31)], width = last[32 * cb + (ln & 31)] - from;  // (nothing: INT_MAX, and below 0)
+      const int at = t0 + token_of(0, hf) - from;
+      const LIVE bits = sizeof(LIVE) == 8 ? live >> token_of(0, hf) : live;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int ahead = 32 * kb + token_of(r, 0) - token_of(0, 0), t = at + ahead;
+          // (sixteen tokens at a time: token_of(r, 1) lies in the sixteen of token_of(r, 0))
+          const bool there = bits >> (sizeof(LIVE) == 8 ? ahead : (32 * kb + token_of(r, 0)) / 16) & 1;
+          s[cb][kb][r] = t >= 0 && t <= width && there ? s[cb][kb][r] : -INFINITY;
+        }
+    }
+  }
+  // Weights are taken against a bound, which moves, to the maximum + 8, only when a score passes it.
+  __device__ __forceinline__ void move_bounds(float sc) {
+    bool grow[CB], any = false;
+    float top[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      top[cb] = s[cb][0][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top[cb] = max_of(top[cb], s[cb][kb][r]);
+      top[cb] = across_halves_max(top[cb]) * sc;
+      grow[cb] = !(top[cb] <= m[cb]);
+      any = any || grow[cb];
+    }
+    if (__builtin_amdgcn_ballot_w64(any) == 0) return;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const float to = grow[cb] ? top[cb] + 8.f : m[cb];
+      const float f = grow[cb] ? weight_of(m[cb], to) : 1.f;
+      m[cb] = to;
+      l[cb] *= f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[cb][dt][r] *= f;
+    }
+  }
+  __device__ __forceinline__ float minus_bound(int cb) const { return m[cb] == -INFINITY ? 0.f : -m[cb]; }
+};
+
+template <typename T, int D, int CB, int KB>
+struct Tile;
+
+template <int D, int CB, int KB>
+struct Tile<bf16_t, D, CB, KB> : Softmax<D, CB, KB> {
+  typedef Softmax<D, CB, KB> Base;
+  using Base::DT;
+  using Base::l;
+  using Base::o;
+  using Base::s;
+  static constexpr int KK = D / 16;
+  bf16x8 q[CB][KK];
+  int kbase, vbase;
+
+  __device__ __forceinline__ void clear(int lane) {
+    const int col = lane & 31, hf = lane >> 5;
+    const int krow = (col & 0x13) | ((col & 4) << 1) | ((col & 8) >> 1);
+    kbase = 2 * (krow * D + ((hf ^ k_swizzle<bf16_t, D>(krow)) << 3));
+    const int vrow = (lane & 15) >> 2;
+    vbase = 2 * ((8 * hf + vrow) * D + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swizzle<bf16_t, D>(vrow)) << 3) + 4 * (lane & 1));
+    Base::clear_sums();
+  }
+  __device__ __forceinline__ void load_q(int cb, const bf16_t* row, int lane) {
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) q[cb][kk] = *reinterpret_cast<const bf16x8*>(row + (lane >> 5) * 8 + kk * 16);
+  }
+  // 32 * KB tokens from t0 on, K rows at kt, V rows at vt (LDS)
+  template <typename LIVE>
+  __device__ __forceinline__ void attend(const bf16_t* kt, const bf16_t* vt, int t0, bool masked, LIVE live, float sc, const int* lo,
+                                         const int* last) {
+    Base::clear_scores();
     const uint32_t ka = lds_address(kt, kbase);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
@@ -431,52 +644,12 @@ struct Tile {
     }
     __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     __builtin_amdgcn_s_setprio(3);  // (few of the vector instructions fit beside another wavefront's products)
-    if (masked) {
-      const int ln = lane_now();
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        const int from = lo[32 * cb + (ln & 31)], width = last[32 * cb + (ln & 31)] - from;  // (nothing: INT_MAX, and below 0)
-        const int at = t0 + 8 * (ln >> 5) - from;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int t = at + 32 * kb + 16 * (r >> 3) + (r & 7);
-            s[cb][kb][r] = t >= 0 && t <= width && (live >> (2 * kb + (r >> 3)) & 1) ? s[cb][kb][r] : -INFINITY;
-          }
-      }
-    }
-    bool grow[CB], any = false;
-    float top[CB];
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-      top[cb] = s[cb][0][0];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top[cb] = max_of(top[cb], s[cb][kb][r]);
-      top[cb] = across_halves_max(top[cb]) * sc;
-      grow[cb] = !(top[cb] <= m[cb]);
-      any = any || grow[cb];
-    }
-    // Weights are taken against a bound, which moves, to the maximum + 8, only when a score passes it.
-    if (__builtin_amdgcn_ballot_w64(any) != 0) {
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        const float to = grow[cb] ? top[cb] + 8.f : m[cb];
-        const float f = grow[cb] ? weight_of(m[cb], to) : 1.f;
-        m[cb] = to;
-        l[cb] *= f;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[cb][dt][r] *= f;
-      }
-    }
+    if (masked) Base::mask(t0, live, lo, last, [](int r, int hf) { return 8 * hf + 16 * (r >> 3) + (r & 7); });
+    Base::move_bounds(sc);
     bf16x8 p[CB][2 * KB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
-      const float minus = m[cb] == -INFINITY ? 0.f : -m[cb];
+      const float minus = Base::minus_bound(cb);
 #pragma unroll
       for (int ks = 0; ks < 2 * KB; ++ks) {
         f32x8 w;
@@ -484,6 +657,7 @@ struct Tile {
         for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(s[cb][ks >> 1][8 * (ks & 1) + e], sc, minus));
         // the unrounded weights' sum: lse is exact to fp32
         l[cb] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        // Rounded to bf16 for the product with V: an error of up to 2^-9 of each weight, about that of the rounded result.
         p[cb][ks] = __builtin_convertvector(w, bf16x8);
       }
     }
@@ -508,6 +682,59 @@ struct Tile {
   }
 };
 
+// fp32: a lane reads 16 bytes of a K row, elements 8 c + 4 (l / 32) + 0 .. 3, which feed four products of two elements each.
+template <int D>
+struct Tile<float, D, 1, 1> : Softmax<D, 1, 1> {
+  typedef Softmax<D, 1, 1> Base;
+  using Base::DT;
+  using Base::l;
+  using Base::o;
+  using Base::s;
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  f32x4 q[D / 8];
+  int kbase, vbase;
+
+  __device__ __forceinline__ void clear(int lane) {
+    const int row = lane & 31, hf = lane >> 5;
+    kbase = row * D * 4 + ((hf ^ k_swizzle<float, D>(row)) << 4);
+    vbase = 4 * hf * D * 4 + row * 4;
+    Base::clear_sums();
+  }
+  __device__ __forceinline__ void load_q(int, const float* row, int lane) {
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) q[c] = *reinterpret_cast<const f32x4*>(row + 8 * c + (lane >> 5) * 4);
+  }
+  template <typename LIVE>
+  __device__ __forceinline__ void attend(const float* kt, const float* vt, int t0, bool masked, LIVE live, float sc, const int* lo,
+                                         const int* last) {
+    Base::clear_scores();
+    const uint32_t ka = lds_address(kt, kbase);
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+      const f32x4 a = *reinterpret_cast<const __attribute__((address_space(3))) f32x4*>((uintptr_t)(ka ^ (c << 5)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[c][e], s[0][0], 0, 0, 0);
+    }
+    if (masked) Base::mask(t0, live, lo, last, [](int r, int hf) { return 8 * (r >> 2) + 4 * hf + (r & 3); });
+    Base::move_bounds(sc);
+    const float minus = Base::minus_bound(0);
+    f32x16 w;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w[r] = fast_exp2(fmaf(s[0][0][r], sc, minus));
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) l[0] += (w[r] + w[r + 1]) + (w[r + 2] + w[r + 3]);
+    const uint32_t va = lds_address(vt, vbase);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const float a = *reinterpret_cast<const __attribute__((address_space(3))) float*>(
+            (uintptr_t)(va + (8 * (r >> 2) + (r & 3)) * D * 4 + dt * 128));
+        o[0][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], o[0][dt], 0, 0, 0);
+      }
+  }
+};
+
 // The columns of a tile: rows and heads of one kv head's group, rows first.  Entry e's tiles start at floor(cu[e] * G / cols) + e, which
 // leaves room for ceil(new rows * G / cols) of them, since ceil(y - x) <= floor(y) - floor(x) + 1.
 struct ColumnRun {
@@ -522,32 +749,31 @@ __device__ __forceinline__ ColumnRun columns_of(const PagedArgs& x, int tile, in
   const int64_t u0 = (int64_t)(tile - first(r.at.r0, r.at.e)) * cols;
   const int64_t n = (int64_t)(min(r.at.r1, x.b.rows) - r.at.r0) * G - u0;
   r.u0 = (int)u0;
-  r.n = r.at.r0 < 0 || u0 < 0 || n <= 0 ? 0 : (int)min(n, (int64_t)cols);
+  r.n = u0 < 0 || n <= 0 ? 0 : (int)min(n, (int64_t)cols);
   return r;
 }
 
-// Waits until at most `loads` of the wavefront's loads are on their way, and for its LDS operations.  (A fence would wait for
-// stores too.)
-template <int LOADS>
+// Waits for the wavefront's loads and LDS operations.  (A fence would wait for stores too.)
 __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070 | (LOADS & 15) | (LOADS >> 4) << 14);
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
   asm volatile("" ::: "memory");
 }
 
-// NW wavefronts of 32 * CB columns, STAGES stages of STEP tokens.
-//   4 wavefronts, two stages: the matrix cores are what bounds these
-//   1 wavefront, two stages: few columns, so that memory does; five workgroups (D = 128) of a compute unit have 16 KB each on
-//                the way (three and four stages leave room for fewer: 24 caches of up to 120000 tokens 119 -> 122, 153 us)
+// NW wavefronts of 32 * CB columns, two stages of STEP tokens.
+//   4 wavefronts: the matrix cores are what bounds these
+//   1 wavefront: few columns, so that memory does; five workgroups (D = 128) of a compute unit have 16 KB each on the way
+//                (three and four stages leave room for fewer: 24 caches of up to 120000 tokens 119 -> 122, 153 us)
 // Workgroups of the window come first, then, of the spans' pieces,
 //   4 wavefronts: the buckets' tiles
 //   1 wavefront: one for every (row, head, slot).  Other heads and rows of its 32 columns may list the same span: the first one
 //                that does takes it for all, so that a span is read once for the group.
-template <int D, int NW, int CB, int STEP, int STAGES>
-__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
+//   ANY: pages of a size that is no multiple of 16: every row has a page of its own, at twice the instructions for its address
+template <typename T, int D, int NW, int CB, int STEP, bool ANY>
+__global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
   constexpr int COLS = NW * 32 * CB;
   extern __shared__ __align__(1024) char s_dynamic[];  // (static, the compiler would wait for staging loads at every read)
-  bf16_t(*const s_kv)[2][STEP * D] = reinterpret_cast<bf16_t(*)[2][STEP * D]>(s_dynamic);
+  T(*const s_kv)[2][STEP * D] = reinterpret_cast<T(*)[2][STEP * D]>(s_dynamic);
   __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS];
   const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t unit = workgroup();
@@ -646,7 +872,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
     end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
     any_last = all_last = end - 1;
     // (asked for before the other columns' lists: a unit is short, and a chain of loads)
-    const int t = begin / 16 * 16 + lane * 16;
+    const int t = begin / 16 * 16 + (ANY ? lane % STEP : lane * 16);
     if (t < end) early_page = x.c.tables[(int64_t)at.s * x.c.max_pages + (uint32_t)t / x.c.by_ps];
     if (lane < 32) {
       s_rh[lane] = -1;
@@ -668,17 +894,15 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
     if (__builtin_amdgcn_ballot_w64(earlier) != 0) return;
   }
   __syncthreads();
-  constexpr int KB = CB == 2 || STEP == 32 ? 1 : 2;
-  Tile<D, CB, KB> tile;
+  constexpr int KB = CB == 2 || STEP == 32 || sizeof(T) == 4 ? 1 : 2;
+  Tile<T, D, CB, KB> tile;
   tile.clear(lane);
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
     const int item = s_rh[wave * 32 * CB + cb * 32 + (lane & 31)];
     const int rh = max(window ? item : item >> 5, 0);  // (a column of nobody reads some row: nothing is made of it)
     const int h = rh / x.b.rows, row = rh - h * x.b.rows;
-    const bf16_t* const q = static_cast<const bf16_t*>(x.Q) + h * x.a.qsh + row * x.a.qst + (lane >> 5) * 8;
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) tile.q[cb][kk] = *reinterpret_cast<const bf16x8*>(q + kk * 16);
+    tile.load_q(cb, static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst, lane);
   }
   const bool group = NW == 1 && !window;
   any_lo = __builtin_amdgcn_readfirstlane(any_lo);
@@ -691,67 +915,78 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
   head = __builtin_amdgcn_readfirstlane(head);
   const int32_t* const table = x.c.tables + (int64_t)seq * x.c.max_pages;
   const int64_t base = x.b.layer * x.c.layer + head * x.c.head;
-  const int row_bytes = (int)x.c.tok * 2;
-  // Lane g has the page of the g-th sixteen tokens from `batch` on; the next 64 pages are looked up while those are in use.
+  const T *const K = static_cast<const T*>(x.c.K), *const V = static_cast<const T*>(x.c.V);
   constexpr int GROUPS = STEP / 16;
-  constexpr int kLoads = 2 * GROUPS / NW * (16 / (64 / (D / 8)));  // of a wavefront and stage
+  // !ANY: lane g has the page of the g-th sixteen tokens from `batch` on; the next 64 pages are looked up while those are in use.
+  // ANY: lane l has the page of row l of the next stage.
   auto look_up = [&](int t0) {
-    const int t = t0 + lane_now() * 16;
+    const int ln = lane_now(), t = t0 + (ANY ? ln % STEP : ln * 16);
     return t < end ? table[(uint32_t)t / x.c.by_ps] : -1;
   };
+  auto there = [&](int page) { return (uint64_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages); };
   int batch = begin, page = -1, next_page = -1;
-  uint64_t alive = 0;  // which of them there are
-  uint32_t live = 0;   // those of the stages, GROUPS bits each
+  uint64_t alive = 0;       // which of the looked up pages there are
+  uint64_t live[2] = {};    // of the stages: a bit for each sixteen rows (ANY: for each)
   auto stage = [&](int t0, int b) {
-    if (t0 - batch >= 1024) {
-      batch += 1024;
-      page = next_page;
-      alive = __builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages);
-      next_page = look_up(batch + 1024);
-    }
-    const int ln = lane_now(), at = (t0 - batch) / 16;
-    const uint32_t bits = (uint32_t)(alive >> at) & ((1u << GROUPS) - 1);
-    live = (live & ~(((1u << GROUPS) - 1) << b * GROUPS)) | bits << b * GROUPS;
+    const int ln = lane_now();
+    if constexpr (ANY) {
+      const int t = t0 + ln % STEP;
+      live[b] = there(page);
+      const int64_t at = (uint32_t)page < (uint32_t)x.c.n_pages
+                             ? base + page * x.c.page + (int64_t)((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps) * x.c.tok
+                             : -1;
 #pragma unroll
-    for (int i = 0; i < GROUPS / NW; ++i) {
-      const int g = NW == 1 ? i : wave, r0 = g * 16, t = __builtin_amdgcn_readfirstlane(t0 + r0);
-      const bool on = bits >> g & 1;
-      const int rows = on ? min(end - t, 16) : 0;
-      const int in_page = __builtin_amdgcn_readfirstlane((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps);
-      const int64_t from = on ? uniform64(base + __builtin_amdgcn_readlane(page, at + g) * x.c.page + in_page * x.c.tok) : 0;
-      stage_rows<D, 0>(&s_kv[b][0][r0 * D], r0, static_cast<const bf16_t*>(x.c.K) + from, rows, row_bytes, ln);
-      stage_rows<D, 1>(&s_kv[b][1][r0 * D], r0, static_cast<const bf16_t*>(x.c.V) + from, rows, row_bytes, ln);
+      for (int i = 0; i < GROUPS / NW; ++i) {
+        const int r0 = (NW == 1 ? i : wave) * 16;
+        stage_rows_any<T, D, 0>(&s_kv[b][0][r0 * D], r0, K, at, ln);
+        stage_rows_any<T, D, 1>(&s_kv[b][1][r0 * D], r0, V, at, ln);
+      }
+      page = look_up(t0 + STEP);
+    } else {
+      if (t0 - batch >= 1024) {
+        batch += 1024;
+        page = next_page;
+        alive = there(page);
+        next_page = look_up(batch + 1024);
+      }
+      const int first = (t0 - batch) / 16, row_bytes = (int)x.c.tok * (int)sizeof(T);
+      live[b] = alive >> first;
+#pragma unroll
+      for (int i = 0; i < GROUPS / NW; ++i) {
+        const int g = NW == 1 ? i : wave, r0 = g * 16, t = __builtin_amdgcn_readfirstlane(t0 + r0);
+        const bool on = live[b] >> g & 1;
+        const int rows = on ? min(end - t, 16) : 0;
+        const int in_page = __builtin_amdgcn_readfirstlane((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps);
+        const int64_t from = on ? uniform64(base + __builtin_amdgcn_readlane(page, first + g) * x.c.page + in_page * x.c.tok) : 0;
+        stage_rows<T, D, 0>(&s_kv[b][0][r0 * D], r0, K + from, rows, row_bytes, ln);
+        stage_rows<T, D, 1>(&s_kv[b][1][r0 * D], r0, V + from, rows, row_bytes, ln);
+      }
     }
   };
   if (begin < end) {
     page = group ? early_page : look_up(batch);
-    if (end - batch > 1024) next_page = look_up(batch + 1024);
-    alive = __builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages);
-#pragma unroll
-    for (int k = 0; k < STAGES - 1; ++k)
-      if (begin + k * STEP < end) stage(begin + k * STEP, k);
+    if (!ANY && end - batch > 1024) next_page = look_up(batch + 1024);
+    alive = there(page);
+    stage(begin, 0);
   }
   int b = 0;
-  for (int t0 = begin; t0 < end; t0 += STEP) {
-    // this stage's loads have arrived when only those of the stages behind it are on their way
-    if (STAGES > 3 && t0 + 2 * STEP < end) wait_loads<(STAGES > 3 ? 2 : 0) * kLoads>();
-    else if (STAGES > 2 && t0 + STEP < end) wait_loads<(STAGES > 2 ? 1 : 0) * kLoads>();
-    else wait_loads<0>();
+  for (int t0 = begin; t0 < end; t0 += STEP, b ^= 1) {
+    wait_loads();
     if (NW > 1) {
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
     }
-    if (t0 + (STAGES - 1) * STEP < end) stage(t0 + (STAGES - 1) * STEP, b == 0 ? STAGES - 1 : b - 1);
+    if (t0 + STEP < end) stage(t0 + STEP, b ^ 1);
 #pragma unroll 1
     for (int at = 0; at < STEP; at += 32 * KB) {
-      const int t = t0 + at, end = t + 32 * KB - 1;
-      if (end < any_lo || t > any_last) continue;
-      constexpr uint32_t kAll = (1u << 2 * KB) - 1;
-      const uint32_t there = live >> (b * GROUPS + at / 16) & kAll;
-      tile.attend(&s_kv[b][0][at * D], &s_kv[b][1][at * D], t, t < all_lo || end > all_last || there != kAll, there, x.scale_log2e,
+      const int t = t0 + at, upto = t + 32 * KB - 1;
+      if (upto < any_lo || t > any_last) continue;
+      typedef std::conditional_t<ANY, uint64_t, uint32_t> Live;
+      constexpr Live kAll = ANY ? (KB == 2 ? ~(Live)0 : (Live)0xffffffffu) : (Live)((1 << 2 * KB) - 1);
+      const Live now = (Live)(live[b] >> (ANY ? at : at / 16)) & kAll;
+      tile.attend(&s_kv[b][0][at * D], &s_kv[b][1][at * D], t, t < all_lo || upto > all_last || now != kAll, now, x.scale_log2e,
                   s_lo + wave * 32 * CB, s_last + wave * 32 * CB);
     }
-    b = b == STAGES - 1 ? 0 : b + 1;
   }
   // Partials.  A column with a value that is not finite is marked by an lse that is not a number: it may have come from a
   // token that the column does not attend, and the merge takes such a piece again, row by row.
@@ -773,38 +1008,36 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void tile_kernel(const Pa
     if (item < 0) continue;
     const bool none = tile.m[cb] == -INFINITY;
     const float lse = none ? -INFINITY : check == 0.f ? tile.m[cb] + __log2f(sum) : NAN;
-    typedef _Float16 Half4 __attribute__((ext_vector_type(4)));
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    typedef float f32x4 __attribute__((ext_vector_type(4)));
     const int64_t rec = (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
     if (ln < 32) x.part_lse[rec] = lse;
-    if (x.p.count == 1) {  // the row's result
-      if (ln < 32 && x.LSE) x.LSE[rec] = lse * kLn2;
-      bf16_t* const to = static_cast<bf16_t*>(x.O) + rec * D + 4 * (ln >> 5);
+    // four values of the lane's column at a time, from d = 32 dt + 8 g + 4 (ln / 32) on
+    auto write = [&](auto* to, float by) {
+      typedef std::remove_reference_t<decltype(*to)> Value;
+      typedef Value Four __attribute__((ext_vector_type(4)));
+      to += rec * D + 4 * (ln >> 5);
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          f32x4 v;
+          Four v;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = none ? 0.f : tile.o[cb][dt][4 * g + e] * inv;
-          *reinterpret_cast<bf16x4*>(to + dt * 32 + g * 8) = __builtin_convertvector(v, bf16x4);
+          for (int e = 0; e < 4; ++e) v[e] = (Value)(none ? 0.f : tile.o[cb][dt][4 * g + e] * by);
+          *reinterpret_cast<Four*>(to + dt * 32 + g * 8) = v;
         }
-      continue;
-    }
-    if (none) continue;
-    const float scale = scale_above(top * inv), by = inv / scale;
-    if (ln < 32) x.part_scale[rec] = scale;
-    _Float16* const to = static_cast<_Float16*>(x.part_o) + rec * D + 4 * (ln >> 5);
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        Half4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (_Float16)(tile.o[cb][dt][4 * g + e] * by);
-        *reinterpret_cast<Half4*>(to + dt * 32 + g * 8) = v;
+    };
+    if (x.p.count == 1) {  // the row's result
+      if (ln < 32 && x.LSE) x.LSE[rec] = lse * kLn2;
+      if constexpr (sizeof(T) == 2) write(static_cast<__bf16*>(x.O), inv);
+      else write(static_cast<float*>(x.O), inv);
+    } else if (!none) {
+      if constexpr (sizeof(T) == 2) {
+        const float scale = scale_above(top * inv);
+        if (ln < 32) x.part_scale[rec] = scale;
+        write(static_cast<_Float16*>(x.part_o), inv / scale);
+      } else {
+        write(static_cast<float*>(x.part_o), inv);
       }
+    }
   }
 }
 
@@ -1028,7 +1261,7 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   const int routed = x.a.topk * x.p.routed;
   bool any = false;  // a slot holds a span
   float total = lse_of(0);
-  if (WAVES > 1 && total != total && x.row_pieces < P) {
+  if (WAVES > 1 && total != total && x.marks) {
     if (wave == 0) mend_row<T, D, false>(x, rh);
     __threadfence_block();
     __syncthreads();
@@ -1138,6 +1371,7 @@ struct Form {
   Pieces p;
   bool tiles;      // the matrix-core form
   bool buckets;    // ... with the spans' rows in buckets
+  bool whole;      // row by row, a row a workgroup
   int cols_log2;   // columns of a tile
   TilePlan plan;   // (pointers unset)
   int64_t units, most_tiles;  // workgroups of the tile kernel; tiles of the buckets
@@ -1147,13 +1381,24 @@ struct Form {
 Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   const int64_t rh = (int64_t)a.Hq * b.rows, window = a.S < b.L ? a.S : b.L;
   Form f = {};
-  // Sixteen rows of a stage lie in one page, and 16 token strides within a buffer's 32-bit offsets.
-  f.tiles = c.dtype == SL_BF16 && c.ps % 16 == 0 && c.tok < ((int64_t)1 << 26) && rh < ((int64_t)1 << 26);
   const int64_t spans = div_up(b.L, a.S), buckets = (int64_t)b.B * c.Hkv * spans, items = rh * a.topk;
-  f.buckets = f.tiles && a.topk > 0 && items >= 4 * buckets && items < ((int64_t)1 << 30);
   const int64_t columns = (int64_t)b.rows * a.G;  // of a kv head
-  f.cols_log2 = (columns <= 32 * (int64_t)b.B || a.topk > 0) && !f.buckets ? 5 : columns * c.Hkv + items >= 256 * 1024 ? 8 : 7;
+  // Buckets read a span once for its rows, behind four launches that sort them.  us, 32:4 heads, top-8 of spans of 128, buckets and
+  // without: bf16, 2.2 items a bucket 56 and 51, 4.4 65 and 91, 17 77 and 321; fp32, where a tile costs as much as 128 items however
+  // few it has, 4.4 222 and 159, 8.7 228 and 312, 17 234 and 633.
+  // (fp32 calls below 2^19 keys: 250 rows of 4 heads, top-4 of spans of 64, 33 and 25)
+  f.buckets = a.topk > 0 && (c.dtype == SL_BF16 ? items >= 3 * buckets : items >= 6 * buckets && items * a.S >= 1 << 19);
+  // fp32: row by row where tiles of 128 columns would be all but empty.
+  f.tiles = c.dtype == SL_BF16 || f.buckets || (a.topk == 0 && columns > 32 * (int64_t)b.B);
+  f.cols_log2 = (columns <= 32 * (int64_t)b.B || a.topk > 0) && !f.buckets          ? 5
+                : c.dtype == SL_BF16 && columns * c.Hkv + items >= 256 * 1024 ? 8
+                                                                             : 7;
   const int cols = 1 << f.cols_log2;
+  f.whole = !f.tiles && rh >= 1024;
+  if (f.whole) {
+    f.p.count = 1;
+    return f;
+  }
   auto cut = [](int64_t tokens, int64_t units, int64_t wanted, int64_t most) {
     int64_t n = div_up(wanted, units);
     if (n > most) n = most;
@@ -1195,10 +1440,10 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   return f;
 }
 
-// The stages fill up to 64 KB of dynamic LDS beside the static arrays: more than a kernel has without asking.
-template <int D, int NW, int CB, int STEP, int STAGES>
-bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
-  constexpr int kBytes = STAGES * 2 * STEP * D * (int)sizeof(bf16_t);
+// The stages fill up to 128 KB of dynamic LDS beside the static arrays: more than a kernel has without asking.
+template <typename T, int D, int NW, int CB, int STEP, bool ANY>
+bool launch_tiles_as(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
+  constexpr int kBytes = 2 * 2 * STEP * D * (int)sizeof(T);
   static std::mutex mu;
   static bool asked[64];
   int dev = -1;
@@ -1206,40 +1451,52 @@ bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipSt
   {
     std::lock_guard<std::mutex> lock(mu);
     if (!asked[dev])
-      asked[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(tile_kernel<D, NW, CB, STEP, STAGES>),
+      asked[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(tile_kernel<T, D, NW, CB, STEP, ANY>),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) == hipSuccess;
     if (!asked[dev]) return false;
   }
-  tile_kernel<D, NW, CB, STEP, STAGES><<<grid_of(f.units), 64 * NW, kBytes, st>>>(x, plan);
+  tile_kernel<T, D, NW, CB, STEP, ANY><<<grid_of(f.units), 64 * NW, kBytes, st>>>(x, plan);
   return true;
+}
+template <typename T, int D, int NW, int CB, int STEP>
+bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
+  return x.c.ps % 16 == 0 ? launch_tiles_as<T, D, NW, CB, STEP, false>(x, f, plan, st) : launch_tiles_as<T, D, NW, CB, STEP, true>(x, f, plan, st);
 }
 
 template <typename T, int D>
 sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
   const int64_t rh = (int64_t)x.a.Hq * x.b.rows;
-  if constexpr (sizeof(T) == 2) {
-    if (f.tiles) {
-      TilePlan plan = f.plan;
-      if (f.buckets) {
-        plan.counts = reinterpret_cast<int32_t*>(ws + f.o_bytes + 2 * f.lse_bytes);
-        plan.first_tile = plan.counts + plan.buckets;
-        plan.records = reinterpret_cast<int4*>(plan.counts + align_up(2 * (size_t)plan.buckets, 64));
-        plan.ranks = reinterpret_cast<int32_t*>(plan.records + f.most_tiles);
-        plan.items = plan.ranks + rh * x.a.topk;
-        const int64_t blocks = div_up(plan.buckets, 1024);
-        zero_kernel<<<(unsigned)(blocks < 1024 ? blocks : 1024), 256, 0, st>>>(plan.counts, plan.buckets);
-        const int64_t runs = (int64_t)x.b.rows / kCountRows + x.b.B;
-        count_kernel<<<dim3((unsigned)runs, x.c.Hkv), 1024, plan.spans <= kCountSpans ? plan.spans * sizeof(int32_t) : 0, st>>>(x, plan);
-        tiles_kernel<<<1, 1024, 0, st>>>(plan, f.cols_log2, (int)f.most_tiles);
-        items_kernel<<<grid_of(div_up(rh * x.a.topk, 256)), 256, 0, st>>>(x, plan, f.cols_log2);
-      }
-      const bool done = f.cols_log2 == 5   ? launch_tiles<D, 1, 1, 32, 2>(x, f, plan, st)
-                        : f.cols_log2 == 7 ? launch_tiles<D, 4, 1, 64, 2>(x, f, plan, st)
-                                           : launch_tiles<D, 4, 2, 64, 2>(x, f, plan, st);
-      if (!done) return SL_ERR_LAUNCH;
+  if (f.tiles) {
+    TilePlan plan = f.plan;
+    if (f.buckets) {
+      plan.counts = reinterpret_cast<int32_t*>(ws + f.o_bytes + 2 * f.lse_bytes);
+      plan.first_tile = plan.counts + plan.buckets;
+      plan.records = reinterpret_cast<int4*>(plan.counts + align_up(2 * (size_t)plan.buckets, 64));
+      plan.ranks = reinterpret_cast<int32_t*>(plan.records + f.most_tiles);
+      plan.items = plan.ranks + rh * x.a.topk;
+      const int64_t blocks = div_up(plan.buckets, 1024);
+      zero_kernel<<<(unsigned)(blocks < 1024 ? blocks : 1024), 256, 0, st>>>(plan.counts, plan.buckets);
+      const int64_t runs = (int64_t)x.b.rows / kCountRows + x.b.B;
+      count_kernel<<<dim3((unsigned)runs, x.c.Hkv), 1024, plan.spans <= kCountSpans ? plan.spans * sizeof(int32_t) : 0, st>>>(x, plan);
+      tiles_kernel<<<1, 1024, 0, st>>>(plan, f.cols_log2, (int)f.most_tiles);
+      items_kernel<<<grid_of(div_up(rh * x.a.topk, 256)), 256, 0, st>>>(x, plan, f.cols_log2);
     }
+    bool done;
+    if constexpr (sizeof(T) == 2)
+      done = f.cols_log2 == 5   ? launch_tiles<T, D, 1, 1, 32>(x, f, plan, st)
+             : f.cols_log2 == 7 ? launch_tiles<T, D, 4, 1, 64>(x, f, plan, st)
+                                : launch_tiles<T, D, 4, 2, 64>(x, f, plan, st);
+    else
+      done = launch_tiles<T, D, 4, 1, 64>(x, f, plan, st);
+    if (!done) return SL_ERR_LAUNCH;
   }
-  if (x.row_pieces > 0) rows_kernel<T, D><<<grid_of(rh * x.row_pieces), 256, 0, st>>>(x);
+  if constexpr (sizeof(T) == 4) {
+    if (f.whole) {
+      whole_rows_kernel<T, D><<<grid_of(rh), 256, 0, st>>>(x);
+      return hipGetLastError() == hipSuccess ? SL_OK : SL_ERR_LAUNCH;
+    }
+    if (!f.tiles) rows_kernel<T, D><<<grid_of(rh * x.p.count), 256, 0, st>>>(x);
+  }
   if (x.p.count == 1 && f.tiles) {
     mend_kernel<T, D, true><<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x);
   } else if (rh >= 4096 && x.p.count <= 1024) {  // enough rows to give each a wavefront
@@ -1264,7 +1521,7 @@ sl_status paged_attention(const PageCache& c, const PagedBatch& b, const PagedAt
   char* const at = static_cast<char*>(ws);
   PagedArgs x = {c, b, a, f.p, Q, idx, scores, O, LSE, ws, reinterpret_cast<float*>(at + f.o_bytes),
                  reinterpret_cast<float*>(at + f.o_bytes + f.lse_bytes), a.scale * kLog2e,
-                 f.tiles ? 0 : f.p.count};
+                 f.tiles};
   if (c.dtype == SL_BF16) return c.D == 128 ? launch<bf16_t, 128>(x, f, at, st) : launch<bf16_t, 64>(x, f, at, st);
   return c.D == 128 ? launch<float, 128>(x, f, at, st) : launch<float, 64>(x, f, at, st);
 }

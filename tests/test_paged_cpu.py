@@ -37,7 +37,7 @@ def test_record_sizes():
 BAD_CACHE = [(dict(K=None), 1), (dict(V=P + 8), 1), (dict(tables=None), 1), (dict(tables=P + 2), 1), (dict(lens=None), 1), (dict(refs=None), 1),
              (dict(refs=P + 4), 1), (dict(layers=0), 1), (dict(n_pages=0), 1), (dict(n_seqs=0), 1), (dict(max_pages=0), 1),
              (dict(page_size=0), 1), (dict(Hkv=0), 1), (dict(dtype=2), 1), (dict(D=96), 2), (dict(max_pages=1 << 25, page_size=64), 2),
-             (dict(kv_stride_t=-8), 1), (dict(kv_stride_t=120), 1), (dict(kv_stride_t=132), 1), (dict(kv_stride_h=4), 1),
+             (dict(kv_stride_t=-8), 1), (dict(kv_stride_t=1 << 21, kv_stride_h=8, page_stride=1 << 22), 2), (dict(kv_stride_t=120), 1), (dict(kv_stride_t=132), 1), (dict(kv_stride_h=4), 1),
              (dict(page_stride=12), 1), (dict(layer_stride=-8), 1), (dict(page_stride=8), 1), (dict(page_stride=1 << 50), 2), (dict(Hkv=2048), 2)]
 BAD_BATCH = [(dict(B=-1), 1), (dict(B=65536), 2), (dict(rows=-1), 1), (dict(rows=(1 << 25) + 1), 2), (dict(L=-1), 1), (dict(layer=2), 1),
              (dict(layer=-1), 1), (dict(seqs=None), 1), (dict(cu_rows=None), 1), (dict(cu_rows=P + 2), 1)]
@@ -121,10 +121,14 @@ def test_nothing_to_do_enqueues_nothing():
 
 
 def test_the_largest_problems_ask_for_sizes_that_fit():
-    """Sizes are computed in 64 bits: 2^31 rows and heads, 32 spans of the longest length."""
-    size = need(rows=1 << 25, Hq=60, Hkv=60, topk=32, S=(1 << 31) - 1, max_pages=1 << 24, page_size=64)
-    assert size != B.WORKSPACE_INVALID and size >= (1 << 25) * 60 * 33 * 128 * 2
-    assert need(rows=1 << 25, Hq=64, Hkv=64) == B.WORKSPACE_INVALID     # row ids are 32-bit
+    """Sizes are computed in 64 bits: 2^26 rows and heads, 32 spans of the longest length."""
+    for kw in (dict(), dict(dtype=B.SL_F32)):
+        size = need(rows=(1 << 25) - 1, Hq=2, Hkv=2, topk=32, S=1 << 24, max_pages=1 << 24, page_size=64, **kw)
+        assert size != B.WORKSPACE_INVALID
+        size = need(rows=1 << 20, Hq=32, Hkv=4, topk=32, S=512, max_pages=1 << 15, page_size=32, B=4, **kw)
+        assert size != B.WORKSPACE_INVALID and (1 << 25) * 33 * 128 * 2 <= size < 1 << 46
+    assert need(rows=1 << 25, Hq=2, Hkv=2) == B.WORKSPACE_INVALID     # a row, its head and a slot count in 31 bits
+    assert need(rows=1 << 21, Hq=32) == B.WORKSPACE_INVALID
 
 
 def test_the_binding_refuses_tensors_that_do_not_fit():

@@ -87,6 +87,13 @@ CASES = [
     (F32, 4, 4, 64, 7, 50, 8, [64], [333], False),
     (F32, 2, 1, 64, 1, 5, 32, [20], [64], False),             # pages of one token, all spans asked for
     (BF16, 2, 2, 128, 1, 3, 1, [17], [17], False),
+    (BF16, 8, 2, 128, 50, 96, 4, [160, 77], [420, 300], False),   # buckets, pages of no multiple of 16
+    (BF16, 6, 2, 64, 21, 64, 3, [300], [300], True),
+    (BF16, 8, 1, 128, 100, 1000, 2, [7], [2500], False),      # spans that cross many pages, a few rows
+    (F32, 6, 2, 128, 64, 48, 3, [200, 90], [300, 260], False),    # buckets in fp32
+    (F32, 4, 4, 64, 13, 40, 2, [250], [250], True),
+    (F32, 4, 2, 64, 32, 20, 2, [1] * 150 + [0, 3] + [1] * 120, list(range(3, 275)), False),   # many sequences of one token each
+    (BF16, 4, 2, 64, 32, 20, 2, [1] * 150 + [0, 3] + [1] * 120, list(range(3, 275)), False),
 ]
 
 
@@ -113,7 +120,9 @@ def test_attention(case, form):
 @pytest.mark.parametrize("dtype,Hq,Hkv,D,ps,ns,Ls", [
     (BF16, 8, 2, 128, 64, [1, 1], [1500, 3]), (BF16, 8, 1, 64, 20, [4, 1, 7], [900, 513, 7]), (BF16, 4, 4, 128, 32, [200], [200]),
     (BF16, 12, 4, 128, 64, [150, 1, 64], [900, 64, 65]), (F32, 4, 2, 64, 16, [100, 3], [100, 600]), (BF16, 2, 1, 64, 64, [300, 129], [300, 640]),
-    (BF16, 5, 5, 128, 16, [257], [300]), (F32, 3, 1, 128, 64, [1], [3000])])
+    (BF16, 5, 5, 128, 16, [257], [300]), (F32, 3, 1, 128, 64, [1], [3000]), (F32, 8, 2, 128, 32, [150, 70], [200, 70]),
+    (F32, 2, 1, 64, 10, [130], [400]), (BF16, 4, 1, 128, 37, [300], [333]), (BF16, 8, 2, 64, 70, [2, 1], [600, 71]),
+    (BF16, 8, 1, 64, 16, [40], [2300])])
 def test_dense(dtype, Hq, Hkv, D, ps, ns, Ls):
     """No spans and S beyond every length: causal attention over all of the sequence."""
     g = torch.Generator().manual_seed(sum(Ls))
