@@ -782,7 +782,20 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
   int begin, end;              // tokens [begin, end) of the tile
   int any_lo, any_last;        // ... that any of the wavefront's columns attends
   int all_lo, all_last;        // ... that all of them attend
-  int early_page = -1;
+  // The pages of the first rows are asked for as soon as a tile knows its sequence and tokens.
+  // !ANY: lane g has the page of the g-th sixteen tokens from `batch` on; the next 64 pages are looked up while those are in use.
+  // ANY: lane l has the page of row l of the next stage.
+  int page = -1;
+  auto look_up = [&](int t0) {
+    const int ln = lane_now(), t = t0 + (ANY ? ln % STEP : ln * 16);
+    return t < end ? x.c.tables[(int64_t)seq * x.c.max_pages + (uint32_t)t / x.c.by_ps] : -1;
+  };
+  auto ask_pages = [&] {
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    begin = __builtin_amdgcn_readfirstlane(begin);
+    end = __builtin_amdgcn_readfirstlane(end);
+    if (begin < end) page = look_up(begin / 16 * 16);
+  };
   // columns
   if (window) {
     // (tile, piece) of the kv heads in turn; the last tiles first, whose ranges are the longest
@@ -801,6 +814,11 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
     const int from = (int)min(origin, (int64_t)INT_MAX), upto = (int)min(origin + x.p.window_tokens - 1, (int64_t)INT_MAX);
     auto lo_of = [&](int pos) { return max(pos / x.a.S * x.a.S, from); };
     auto last_of = [&](int pos) { return min(pos, upto); };
+    // Later rows begin and end no earlier.
+    const int last = min(pos0 + (u0 + run.n - 1) / x.a.G, most);
+    begin = lo_of(first);
+    end = first > last ? begin : last_of(last) + 1;
+    ask_pages();
     for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
       const int u = u0 + c, row = r0 + u / x.a.G, pos = pos0 + u / x.a.G;
       int rh = -1, clo = INT_MAX, clast = -1;
@@ -815,11 +833,6 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
       s_lo[c] = clo;
       s_last[c] = clast;
     }
-    // Later rows begin and end no earlier.
-    const int last = min(pos0 + (u0 + run.n - 1) / x.a.G, most);
-    begin = lo_of(first);
-    end = last_of(last) + 1;
-    if (first > last) end = begin;
     const int c0 = wave * 32 * CB, c1 = min(c0 + 32 * CB, run.n) - 1;
     const int p0 = pos0 + (u0 + c0) / x.a.G, p1 = pos0 + (u0 + c1) / x.a.G, q0 = max(p0, 0), q1 = min(p1, most);
     const bool some = c0 <= c1 && q0 <= q1;
@@ -839,6 +852,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
     seq = x.b.seqs[rec.y / x.c.Hkv];
     begin = j * x.a.S + part * x.p.routed_tokens;
     end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
+    ask_pages();
     for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
       s_rh[c] = c < count ? plan.items[(int64_t)rec.z * COLS + c] : -1;  // (row and head) * 32 + slot
       s_lo[c] = c < count ? begin : INT_MAX;
@@ -871,9 +885,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
     begin = any_lo = all_lo = j * x.a.S + part * x.p.routed_tokens;
     end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
     any_last = all_last = end - 1;
-    // (asked for before the other columns' lists: a unit is short, and a chain of loads)
-    const int t = begin / 16 * 16 + (ANY ? lane % STEP : lane * 16);
-    if (t < end) early_page = x.c.tables[(int64_t)at.s * x.c.max_pages + (uint32_t)t / x.c.by_ps];
+    ask_pages();  // (before the other columns' lists: a unit is short, and a chain of loads)
     if (lane < 32) {
       s_rh[lane] = -1;
       s_lo[lane] = INT_MAX;
@@ -897,34 +909,17 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
   constexpr int KB = CB == 2 || STEP == 32 || sizeof(T) == 4 ? 1 : 2;
   Tile<T, D, CB, KB> tile;
   tile.clear(lane);
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb) {
-    const int item = s_rh[wave * 32 * CB + cb * 32 + (lane & 31)];
-    const int rh = max(window ? item : item >> 5, 0);  // (a column of nobody reads some row: nothing is made of it)
-    const int h = rh / x.b.rows, row = rh - h * x.b.rows;
-    tile.load_q(cb, static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst, lane);
-  }
-  const bool group = NW == 1 && !window;
   any_lo = __builtin_amdgcn_readfirstlane(any_lo);
   any_last = __builtin_amdgcn_readfirstlane(any_last);
   all_lo = __builtin_amdgcn_readfirstlane(all_lo);
   all_last = __builtin_amdgcn_readfirstlane(all_last);
-  begin = __builtin_amdgcn_readfirstlane(begin) / 16 * 16;
-  end = __builtin_amdgcn_readfirstlane(end);
-  seq = __builtin_amdgcn_readfirstlane(seq);
+  begin = begin / 16 * 16;
   head = __builtin_amdgcn_readfirstlane(head);
-  const int32_t* const table = x.c.tables + (int64_t)seq * x.c.max_pages;
   const int64_t base = x.b.layer * x.c.layer + head * x.c.head;
   const T *const K = static_cast<const T*>(x.c.K), *const V = static_cast<const T*>(x.c.V);
   constexpr int GROUPS = STEP / 16;
-  // !ANY: lane g has the page of the g-th sixteen tokens from `batch` on; the next 64 pages are looked up while those are in use.
-  // ANY: lane l has the page of row l of the next stage.
-  auto look_up = [&](int t0) {
-    const int ln = lane_now(), t = t0 + (ANY ? ln % STEP : ln * 16);
-    return t < end ? table[(uint32_t)t / x.c.by_ps] : -1;
-  };
   auto there = [&](int page) { return (uint64_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages); };
-  int batch = begin, page = -1, next_page = -1;
+  int batch = begin, next_page = -1;
   uint64_t alive = 0;       // which of the looked up pages there are
   uint64_t live[2] = {};    // of the stages: a bit for each sixteen rows (ANY: for each)
   auto stage = [&](int t0, int b) {
@@ -964,10 +959,16 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
     }
   };
   if (begin < end) {
-    page = group ? early_page : look_up(batch);
-    if (!ANY && end - batch > 1024) next_page = look_up(batch + 1024);
     alive = there(page);
+    if (!ANY && end - batch > 1024) next_page = look_up(batch + 1024);
     stage(begin, 0);
+  }
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    const int item = s_rh[wave * 32 * CB + cb * 32 + (lane & 31)];
+    const int rh = max(window ? item : item >> 5, 0);  // (a column of nobody reads some row: nothing is made of it)
+    const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+    tile.load_q(cb, static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst, lane);
   }
   int b = 0;
   for (int t0 = begin; t0 < end; t0 += STEP, b ^= 1) {
@@ -988,11 +989,18 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
                   s_lo + wave * 32 * CB, s_last + wave * 32 * CB);
     }
   }
-  // Partials.  A column with a value that is not finite is marked by an lse that is not a number: it may have come from a
+  // Results.  A column with a value that is not finite is marked by an lse that is not a number: it may have come from a
   // token that the column does not attend, and the merge takes such a piece again, row by row.
+  // Values go out by way of the stages, whose rows are free by now: a lane has four of them of one column, 8 or 16 bytes of a row's 256.
+  if (NW > 1) __syncthreads();
+  const bool direct = x.p.count == 1;
+  typedef typename Record<T>::Value Value;
+  typedef std::conditional_t<sizeof(T) == 2, __bf16, float> Out;
+  constexpr int LPR = D * (int)sizeof(Value) / 16, RPI = 64 / LPR;  // lanes of a row, rows of an instruction
+  char* const s_out = s_dynamic + wave * (32 * D * (int)sizeof(Value));
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
-    const int ln = lane_now(), item = s_rh[wave * 32 * CB + cb * 32 + (ln & 31)];
+    const int ln = lane_now(), own = wave * 32 * CB + cb * 32 + (ln & 31), item = s_rh[own];
     const float sum = across_halves_sum(tile.l[cb]);
     const float inv = 1.f / sum;
     float check = 0.f, top = 0.f;
@@ -1005,39 +1013,49 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
       }
     check = across_halves_sum(check);
     top = across_halves_max(top);
-    if (item < 0) continue;
     const bool none = tile.m[cb] == -INFINITY;
     const float lse = none ? -INFINITY : check == 0.f ? tile.m[cb] + __log2f(sum) : NAN;
-    const int64_t rec = (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
-    if (ln < 32) x.part_lse[rec] = lse;
-    // four values of the lane's column at a time, from d = 32 dt + 8 g + 4 (ln / 32) on
-    auto write = [&](auto* to, float by) {
-      typedef std::remove_reference_t<decltype(*to)> Value;
-      typedef Value Four __attribute__((ext_vector_type(4)));
-      to += rec * D + 4 * (ln >> 5);
+    auto record = [&](int item) {
+      return (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
+    };
+    const float scale = direct || sizeof(T) == 4 ? 1.f : scale_above(top * inv);
+    if (item >= 0 && ln < 32) {
+      const int64_t rec = record(item);
+      x.part_lse[rec] = lse;
+      if (direct && x.LSE) x.LSE[rec] = lse * kLn2;
+      if (!direct && sizeof(T) == 2) x.part_scale[rec] = scale;
+    }
+    // d = 32 dt + 8 g + 4 (ln / 32) on: a 16-byte unit, or half of one, swizzled by the row
+    auto put = [&](auto zero, float by) {
+      typedef decltype(zero) V;
+      typedef V Four __attribute__((ext_vector_type(4)));
+      const int row = ln & 31, hf = ln >> 5;
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           Four v;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = (Value)(none ? 0.f : tile.o[cb][dt][4 * g + e] * by);
-          *reinterpret_cast<Four*>(to + dt * 32 + g * 8) = v;
+          for (int e = 0; e < 4; ++e) v[e] = (V)(none ? 0.f : tile.o[cb][dt][4 * g + e] * by);
+          const int unit = sizeof(V) == 2 ? 4 * dt + g : 8 * dt + 2 * g + hf;
+          *reinterpret_cast<Four*>(s_out + (row * LPR + (unit ^ row % LPR)) * 16 + (sizeof(V) == 2 ? 8 * hf : 0)) = v;
         }
     };
-    if (x.p.count == 1) {  // the row's result
-      if (ln < 32 && x.LSE) x.LSE[rec] = lse * kLn2;
-      if constexpr (sizeof(T) == 2) write(static_cast<__bf16*>(x.O), inv);
-      else write(static_cast<float*>(x.O), inv);
-    } else if (!none) {
-      if constexpr (sizeof(T) == 2) {
-        const float scale = scale_above(top * inv);
-        if (ln < 32) x.part_scale[rec] = scale;
-        write(static_cast<_Float16*>(x.part_o), inv / scale);
-      } else {
-        write(static_cast<float*>(x.part_o), inv);
-      }
+    if (direct) put(Out(), inv);
+    else put(Value(), inv / scale);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    char* const to = static_cast<char*>(direct ? x.O : x.part_o);
+    const uint64_t write = __builtin_amdgcn_ballot_w64(item >= 0 && (direct || !none));
+#pragma unroll
+    for (int i = 0; i < 32 / RPI; ++i) {
+      const int row = i * RPI + ln / LPR, piece = ln % LPR;
+      if (!(write >> row & 1)) continue;
+      const uint4 v = *reinterpret_cast<const uint4*>(s_out + (row * LPR + (piece ^ row % LPR)) * 16);
+      store16_stream(to + record(s_rh[wave * 32 * CB + cb * 32 + row]) * (D * (int)sizeof(Value)) + piece * 16, v);
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -1188,8 +1206,8 @@ __global__ __launch_bounds__(256) void mend_kernel(const PagedArgs x) {
 
 // WAVES wavefronts (of a workgroup's four) join the pieces of one row and head: weights to LDS, then D / 8 (fp32: D / 4) lanes
 // a piece.  Nothing a wavefront asks for depends on what it has read: the first outputs are on their way before there are weights.
-// (Marked pieces are mended here where a workgroup takes a row; beside a wavefront a row, they would cost it half its occupancy.)
-template <typename T, int D, int WAVES>
+// MEND: marked pieces are mended here.  (Where there are rows enough to fill the chip, that would cost half its occupancy.)
+template <typename T, int D, int WAVES, bool MEND>
 __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   typedef typename Record<T>::Value Value;
   constexpr int EPL = 16 / sizeof(Value), LANES = D / EPL, N = 64 * WAVES, GROUPS = N / LANES, U = 4;
@@ -1261,10 +1279,10 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   const int routed = x.a.topk * x.p.routed;
   bool any = false;  // a slot holds a span
   float total = lse_of(0);
-  if (WAVES > 1 && total != total && x.marks) {
-    if (wave == 0) mend_row<T, D, false>(x, rh);
+  if (MEND && total != total && x.marks) {
+    if (WAVES == 1 || wave == 0) mend_row<T, D, false>(x, rh);
     __threadfence_block();
-    __syncthreads();
+    barrier();
     ask();
     total = lse_of(0);
   }
@@ -1415,7 +1433,9 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   if (f.tiles) {
     f.plan.tiles = (int)(columns / cols) + b.B;
     const int64_t longest = window + cols / a.G + 17;  // a tile's rows may lie in two windows; it begins at a multiple of 16
-    const int64_t n = cut(longest, (int64_t)f.plan.tiles * c.Hkv, cols == 32 ? 4096 : 1024, 256);
+    // Enough workgroups of the narrow form for what fits the chip at once, four or (D = 64) nine to a compute unit: 32 caches of 1000
+    // tokens, 32:8 heads, 39 us with four times as many, 33 so; of the wide one, twice.
+    const int64_t n = cut(longest, (int64_t)f.plan.tiles * c.Hkv, cols == 32 && c.D == 64 ? 2048 : 1024, 256);
     p.window_tokens = (int)div_up(div_up(longest, n), 64) * 64;
     p.window = (int)div_up(longest, p.window_tokens);
     f.plan.window_units = div_up((int64_t)f.plan.tiles * p.window * c.Hkv, 8) * 8;
@@ -1499,11 +1519,18 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
   }
   if (x.p.count == 1 && f.tiles) {
     mend_kernel<T, D, true><<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x);
-  } else if (rh >= 4096 && x.p.count <= 1024) {  // enough rows to give each a wavefront
-    if (f.tiles) mend_kernel<T, D, false><<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x);
-    merge_kernel<T, D, 1><<<grid_of(div_up(rh, 4)), 256, 4 * x.p.count * sizeof(float), st>>>(x);
   } else {
-    merge_kernel<T, D, 4><<<grid_of(rh), 256, x.p.count * sizeof(float), st>>>(x);
+    // A wavefront a row where there are rows enough, or pieces few enough to be asked for at once (16 dense sequences, 1100 rows and
+    // heads of 30 pieces: 7.2 -> MERGE us).
+    constexpr int kAtOnce = 4 * 64 / (D * (int)sizeof(typename Record<T>::Value) / 16);
+    if (rh >= 4096 && x.p.count <= 1024) {
+      if (f.tiles) mend_kernel<T, D, false><<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x);
+      merge_kernel<T, D, 1, false><<<grid_of(div_up(rh, 4)), 256, 4 * x.p.count * sizeof(float), st>>>(x);
+    } else if (x.p.count <= kAtOnce) {
+      merge_kernel<T, D, 1, true><<<grid_of(div_up(rh, 4)), 256, 4 * x.p.count * sizeof(float), st>>>(x);
+    } else {
+      merge_kernel<T, D, 4, true><<<grid_of(rh), 256, x.p.count * sizeof(float), st>>>(x);
+    }
   }
   return hipGetLastError() == hipSuccess ? SL_OK : SL_ERR_LAUNCH;
 }

@@ -386,23 +386,49 @@ __global__ __launch_bounds__(256) void compact_kernel(const PageCache c, const i
   }
 }
 
-// A lane takes 16 bytes of a row of K and of V; rows of one head follow each other.
+// A workgroup takes 32 rows of a head: a lane for each row finds its place, then all lanes copy, 16 bytes at a time.  Bound by memory:
+// 170000 rows of 8 heads at 4.9 TB/s, where a large copy reaches 4.9 to 5.2; with every 16 bytes finding their own place 4.6.
+constexpr int kAppendRows = 32;
 __global__ __launch_bounds__(256) void append_kernel(const PageCache c, const PagedBatch b, const char* __restrict__ K,
                                                      const char* __restrict__ V, int64_t sh, int64_t st, int pieces_log2) {
-  const int at = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
-  const int row = at >> pieces_log2, piece = at & ((1 << pieces_log2) - 1);
-  if (row < b.cu[0] || row >= min(b.cu[b.B], b.rows)) return;
-  const int e = entry_of_row(b.cu, b.B, row), s = b.seqs[e], len = length_of(c, s);
-  const int t = len - (b.cu[e + 1] - row);
-  if (t < 0 || t >= b.L || t >= len) return;
-  const int k = (uint32_t)t / c.by_ps, page = c.tables[(int64_t)s * c.max_pages + k];
-  if ((uint32_t)page >= (uint32_t)c.n_pages) return;
-  const int es = element_bytes(c);
-  const int64_t from = (head * sh + row * st) * es + piece * 16;
-  const int64_t to = (b.layer * c.layer + page * c.page + head * c.head + (t - k * c.ps) * c.tok) * es + piece * 16;
-  const uint4 x = load16(K + from), y = load16(V + from);
-  *reinterpret_cast<uint4*>(reinterpret_cast<char*>(c.K) + to) = x;
-  *reinterpret_cast<uint4*>(reinterpret_cast<char*>(c.V) + to) = y;
+  __shared__ int64_t s_to[kAppendRows];
+  const int first = blockIdx.x * kAppendRows, head = blockIdx.y, es = element_bytes(c);
+  if (threadIdx.x < kAppendRows) {
+    const int row = first + threadIdx.x;
+    int64_t to = -1;
+    if (row < b.rows && row >= b.cu[0] && row < b.cu[b.B]) {
+      const int e = entry_of_row(b.cu, b.B, row), s = b.seqs[e], len = length_of(c, s), t = len - (b.cu[e + 1] - row);
+      if (t >= 0 && t < b.L && t < len) {
+        const int k = (uint32_t)t / c.by_ps, page = c.tables[(int64_t)s * c.max_pages + k];
+        if ((uint32_t)page < (uint32_t)c.n_pages) to = (b.layer * c.layer + page * c.page + head * c.head + (t - k * c.ps) * c.tok) * es;
+      }
+    }
+    s_to[threadIdx.x] = to;
+  }
+  __syncthreads();
+  const char *const k0 = K + (head * sh + first * st) * es, *const v0 = V + (head * sh + first * st) * es;
+  const int n = kAppendRows << pieces_log2, mask = (1 << pieces_log2) - 1;
+  constexpr int U = 2;  // of K and as many of V: rows have 8, 16 or 32 pieces, so that n is a multiple of 256, if not of 512
+  for (int p = threadIdx.x; p < n; p += U * 256) {
+    uint4 x[U], y[U];
+    int64_t to[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int q = p + u * 256, row = q >> pieces_log2;
+      to[u] = q < n ? s_to[row] : -1;
+      if (to[u] < 0) continue;
+      const int64_t from = row * st * es + (q & mask) * 16;
+      x[u] = load16_stream(k0 + from);
+      y[u] = load16_stream(v0 + from);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (to[u] < 0) continue;
+      const int64_t at = to[u] + ((p + u * 256) & mask) * 16;
+      *reinterpret_cast<uint4*>(reinterpret_cast<char*>(c.K) + at) = x[u];
+      *reinterpret_cast<uint4*>(reinterpret_cast<char*>(c.V) + at) = y[u];
+    }
+  }
 }
 
 constexpr int kKeySpans = 64;  // spans of a workgroup
@@ -475,8 +501,7 @@ sl_status pages_compact(const PageCache& c, int32_t* map, void* ws, hipStream_t 
 sl_status paged_append(const PageCache& c, const PagedBatch& b, const void* K, const void* V, int64_t sh, int64_t st_, hipStream_t st) {
   if (b.B == 0 || b.rows == 0) return SL_OK;
   const int pl = pieces_log2_of(c);
-  const int64_t blocks = (((int64_t)b.rows << pl) + 255) / 256;
-  append_kernel<<<dim3((unsigned)blocks, c.Hkv), 256, 0, st>>>(c, b, static_cast<const char*>(K), static_cast<const char*>(V), sh, st_, pl);
+  append_kernel<<<dim3((unsigned)((b.rows + kAppendRows - 1) / kAppendRows), c.Hkv), 256, 0, st>>>(c, b, static_cast<const char*>(K), static_cast<const char*>(V), sh, st_, pl);
   return launched();
 }
 
