@@ -467,9 +467,11 @@ template <typename T, int D, int TENSOR>
 __device__ __forceinline__ int piece_of(int row, int lane) {
   return lane % RowLanes<T, D>::LPR ^ (TENSOR == 0 ? k_swizzle<T, D>(row) : v_swizzle<T, D>(row));
 }
+// STREAM: with the non-temporal hint, where a row is read once (one token behind a million 62 -> 56 us, 24 caches of up to 120000 tokens
+// 116 -> 103; prompts, whose rows are read by many tiles, 760 -> 802).
 // base: row 0 of the sixteen, which lie in one page; rows from `rows` on become zeros (what lies there may be anything, and zero times
 // that need not be zero).
-template <typename T, int D, int TENSOR>
+template <typename T, int D, int TENSOR, bool STREAM>
 __device__ __forceinline__ void stage_rows(T* to, int first_row, const T* base, int rows, int row_bytes, int lane) {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host pass does not know the resource's type)
   constexpr int LPR = RowLanes<T, D>::LPR, RPI = RowLanes<T, D>::RPI;
@@ -479,12 +481,12 @@ __device__ __forceinline__ void stage_rows(T* to, int first_row, const T* base, 
   for (int i = 0; i < 16 / RPI; ++i) {
     const int row = i * RPI + lane / LPR;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, SL_LDS(reinterpret_cast<char*>(to) + i * 1024), 16,
-                                             row * row_bytes + piece_of<T, D, TENSOR>(first_row + row, lane) * 16, 0, 0, 0);
+                                             row * row_bytes + piece_of<T, D, TENSOR>(first_row + row, lane) * 16, 0, 0, STREAM ? 2 : 0);
   }
 #endif
 }
 // Pages of any size: `at` of lane l is the element offset of row l of the stage, < 0: zeros.
-template <typename T, int D, int TENSOR>
+template <typename T, int D, int TENSOR, bool STREAM>
 __device__ __forceinline__ void stage_rows_any(T* to, int first_row, const T* base, int64_t at, int lane) {
   constexpr int LPR = RowLanes<T, D>::LPR, RPI = RowLanes<T, D>::RPI;
 #pragma unroll
@@ -494,7 +496,7 @@ __device__ __forceinline__ void stage_rows_any(T* to, int first_row, const T* ba
     const char* const from =
         hi < 0 ? reinterpret_cast<const char*>(g_zeros) : reinterpret_cast<const char*>(base + (((int64_t)hi << 32) | (uint32_t)lo));
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + piece_of<T, D, TENSOR>(row, lane) * 16),
-                                     SL_LDS(reinterpret_cast<char*>(to) + i * 1024), 16, 0, 0);
+                                     SL_LDS(reinterpret_cast<char*>(to) + i * 1024), 16, 0, STREAM ? 2 : 0);
   }
 }
 
@@ -933,8 +935,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
 #pragma unroll
       for (int i = 0; i < GROUPS / NW; ++i) {
         const int r0 = (NW == 1 ? i : wave) * 16;
-        stage_rows_any<T, D, 0>(&s_kv[b][0][r0 * D], r0, K, at, ln);
-        stage_rows_any<T, D, 1>(&s_kv[b][1][r0 * D], r0, V, at, ln);
+        stage_rows_any<T, D, 0, NW == 1>(&s_kv[b][0][r0 * D], r0, K, at, ln);
+        stage_rows_any<T, D, 1, NW == 1>(&s_kv[b][1][r0 * D], r0, V, at, ln);
       }
       page = look_up(t0 + STEP);
     } else {
@@ -953,8 +955,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
         const int rows = on ? min(end - t, 16) : 0;
         const int in_page = __builtin_amdgcn_readfirstlane((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps);
         const int64_t from = on ? uniform64(base + __builtin_amdgcn_readlane(page, first + g) * x.c.page + in_page * x.c.tok) : 0;
-        stage_rows<T, D, 0>(&s_kv[b][0][r0 * D], r0, K + from, rows, row_bytes, ln);
-        stage_rows<T, D, 1>(&s_kv[b][1][r0 * D], r0, V + from, rows, row_bytes, ln);
+        stage_rows<T, D, 0, NW == 1>(&s_kv[b][0][r0 * D], r0, K + from, rows, row_bytes, ln);
+        stage_rows<T, D, 1, NW == 1>(&s_kv[b][1][r0 * D], r0, V + from, rows, row_bytes, ln);
       }
     }
   };
@@ -1052,7 +1054,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
       const int row = i * RPI + ln / LPR, piece = ln % LPR;
       if (!(write >> row & 1)) continue;
       const uint4 v = *reinterpret_cast<const uint4*>(s_out + (row * LPR + (piece ^ row % LPR)) * 16);
-      store16_stream(to + record(s_rh[wave * 32 * CB + cb * 32 + row]) * (D * (int)sizeof(Value)) + piece * 16, v);
+      *reinterpret_cast<uint4*>(to + record(s_rh[wave * 32 * CB + cb * 32 + row]) * (D * (int)sizeof(Value)) + piece * 16) = v;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
