@@ -211,12 +211,12 @@ __device__ __forceinline__ void copy_rows(const char* __restrict__ from, char* _
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int q = p + u * threads;
-      x[u] = load16(from + (q >> pieces_log2) * row_bytes + (q & mask) * 16);
+      x[u] = load16_stream(from + (q >> pieces_log2) * row_bytes + (q & mask) * 16);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int q = p + u * threads;
-      *reinterpret_cast<uint4*>(to + (q >> pieces_log2) * row_bytes + (q & mask) * 16) = x[u];
+      store16_stream(to + (q >> pieces_log2) * row_bytes + (q & mask) * 16, x[u]);
     }
   }
   for (; p < n; p += threads)
@@ -387,7 +387,8 @@ __global__ __launch_bounds__(256) void compact_kernel(const PageCache c, const i
 }
 
 // A workgroup takes 32 rows of a head: a lane for each row finds its place, then all lanes copy, 16 bytes at a time.  Bound by memory:
-// 170000 rows of 8 heads at 4.9 TB/s, where a large copy reaches 4.9 to 5.2; with every 16 bytes finding their own place 4.6.
+// 120000 rows of 8 heads at 5.1 TB/s, where a large copy reaches 4.9 to 5.2; without the non-temporal hint 4.9, with every 16 bytes finding
+// their own place 4.6.
 constexpr int kAppendRows = 32;
 __global__ __launch_bounds__(256) void append_kernel(const PageCache c, const PagedBatch b, const char* __restrict__ K,
                                                      const char* __restrict__ V, int64_t sh, int64_t st, int pieces_log2) {
@@ -425,8 +426,8 @@ __global__ __launch_bounds__(256) void append_kernel(const PageCache c, const Pa
     for (int u = 0; u < U; ++u) {
       if (to[u] < 0) continue;
       const int64_t at = to[u] + ((p + u * 256) & mask) * 16;
-      *reinterpret_cast<uint4*>(reinterpret_cast<char*>(c.K) + at) = x[u];
-      *reinterpret_cast<uint4*>(reinterpret_cast<char*>(c.V) + at) = y[u];
+      store16_stream(reinterpret_cast<char*>(c.K) + at, x[u]);
+      store16_stream(reinterpret_cast<char*>(c.V) + at, y[u]);
     }
   }
 }
@@ -493,7 +494,7 @@ sl_status pages_compact(const PageCache& c, int32_t* map, void* ws, hipStream_t 
   if (c.n_pages > kLargePool) plan_compact_kernel<16><<<1, kPlanThreads, 0, st>>>(c, map, count, moves, half);
   else plan_compact_kernel<4><<<1, kPlanThreads, 0, st>>>(c, map, count, moves, half);
   const int64_t entries = (int64_t)c.n_seqs * c.max_pages, units = (int64_t)(half - 1) * c.layers * 2 * c.Hkv;
-  const int tables = (int)min((entries + 1023) / 1024, (int64_t)512), copies = (int)min(units, (int64_t)2048);
+  const int tables = (int)min((entries + 1023) / 1024, (int64_t)512), copies = (int)min(units, (int64_t)8192);
   compact_kernel<<<tables + copies, 256, 0, st>>>(c, map, count, moves, half, tables);
   return launched();
 }
