@@ -335,6 +335,8 @@ sl_status sl_anchor_attention_decode_batched(const sl_params* p, const sl_anchor
  *     the last, partly filled page), so that appending never writes into another sequence's tokens.
  *   - Entries of tables[s] from ceil(lens[s] / page_size) on are -1.
  * An empty cache: tables all -1, lens and refs all 0.
+ * Calls on one cache must be ordered, on one stream or with events.  None of them allocates,
+ * synchronises or records profile events.
  * What the device arrays hold cannot be checked by the host.  Sequence numbers outside
  * 0 .. n_seqs - 1, table entries that name no page, lengths beyond the table and rows without
  * a token are passed over as described at each call; no content leads to an access outside the
@@ -360,7 +362,8 @@ typedef struct sl_paged_batch {
   const int32_t* cu_rows;  /* [B + 1] device */
   int64_t rows;            /* rows per head of the row tensors, 0 .. 2^25 (attention: rows * Hq < 2^26) */
   int64_t L;               /* no sequence of the batch holds more tokens; 0 = max_pages * page_size.  Rows at
-                              positions from L on are treated as rows without a token. */
+                              positions from L on are treated as rows without a token.  The work is cut up
+                              for sequences of L tokens: a bound near the longest one is fastest. */
   int32_t B;               /* 0 .. 65535 */
   int32_t layer;           /* layer of the cache that is read or written */
 } sl_paged_batch;
@@ -384,7 +387,7 @@ sl_status sl_pages_fork(const sl_page_cache* c, const int32_t* src, const int32_
 
 /* Empties the n listed sequences: their table entries become -1, refs falls by one for each, lens
  * becomes 0.  Listing a sequence twice, or an empty one, does no harm; numbers out of range are
- * passed over. */
+ * passed over.  n <= 65535. */
 sl_status sl_pages_free(const sl_page_cache* c, const int32_t* seqs, int32_t n, void* hip_stream);
 
 /* Moves the pages in use to the front of the pool: with u of them, the i-th lowest free page below
@@ -394,7 +397,8 @@ sl_status sl_pages_free(const sl_page_cache* c, const int32_t* seqs, int32_t n, 
 size_t sl_pages_compact_workspace_bytes(const sl_page_cache* c);
 sl_status sl_pages_compact(const sl_page_cache* c, int32_t* map, void* ws, size_t ws_bytes, void* hip_stream);
 
-/* Writes the batch's new tokens into their pages.  K, V: [Hkv][rows][D] with element strides
+/* Writes the batch's new tokens into their pages (a sequence's tokens by one entry: of entries that
+ * list it twice, which one's rows stay is unspecified).  K, V: [Hkv][rows][D] with element strides
  * (stride_h, stride_t, 1), 0 = packed. */
 sl_status sl_paged_append(const sl_page_cache* c, const sl_paged_batch* b, const void* K, const void* V,
                           int64_t stride_h, int64_t stride_t, void* hip_stream);

@@ -601,6 +601,17 @@ def _int32(t, name, device, n=None):
     return t.numel()
 
 
+def _strides(t, name):
+    """Strides as the library takes them, where 0 means packed: of dimensions of one element any will do, but a tensor that repeats
+    its elements (expand) has none that can be said."""
+    out = t.stride()
+    if 0 in out or 1 in t.shape:
+        if any(st == 0 and n > 1 for n, st in zip(t.shape, out)):
+            raise ValueError(f"{name} repeats its elements along a dimension: make it contiguous")
+        out = tuple(0 if n == 1 else st for n, st in zip(t.shape[:-1], out)) + (1 if t.shape[-1] == 1 else out[-1],)
+    return out
+
+
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
@@ -613,7 +624,7 @@ class PageCache:
 
     def __init__(self, K, V, tables, lens, refs):
         K5, V5 = (x.unsqueeze(0) if x.dim() == 4 else x for x in (K, V))
-        if K5.dim() != 5 or K5.stride(4) != 1 or V5.shape != K5.shape or V5.stride() != K5.stride() or V.dtype != K.dtype:
+        if K5.dim() != 5 or K5.stride(4) != 1 or 0 in K5.shape or V5.shape != K5.shape or V5.stride() != K5.stride() or V.dtype != K.dtype:
             raise ValueError("expect K, V [layers, n_pages, Hkv, page_size, D] of one dtype, contiguous innermost, V with K's strides")
         layers, n_pages, Hkv, ps, D = K5.shape
         if tables.dtype != torch.int32 or tables.dim() != 2 or not tables.is_contiguous() or tables.device != K.device or V.device != K.device:
@@ -623,7 +634,7 @@ class PageCache:
         _int32(refs, "refs", self.index, n_pages)
         self.K, self.V, self.tables, self.lens, self.refs = K, V, tables, lens, refs
         self.dtype, self.device, self.layers, self.page_size, self.Hkv, self.D = K.dtype, K.device, layers, ps, Hkv, D
-        st = K5.stride()
+        st = _strides(K5, "K")
         self.record = SlPageCache(K.data_ptr(), V.data_ptr(), tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), st[0], st[1], st[2],
                                   st[3], layers, n_pages, tables.shape[0], tables.shape[1], ps, Hkv, D, _dtype_code(K))
 
@@ -690,8 +701,8 @@ def sl_pages_compact(cache: PageCache, map=None, ws=None):
 
 def sl_paged_append(cache: PageCache, seqs, cu_rows, K, V, layer=0):
     """Writes the new tokens' K and V [Hkv, rows, D] into their pages."""
-    shape, st = K.shape, K.stride()
-    if (len(shape) != 3 or shape[0] != cache.Hkv or shape[2] != cache.D or st[2] != 1 or V.shape != shape or V.stride() != st
+    shape, st = K.shape, _strides(K, "K")
+    if (len(shape) != 3 or shape[0] != cache.Hkv or shape[2] != cache.D or st[2] != 1 or V.shape != shape or _strides(V, "V") != st
             or K.dtype is not cache.dtype or V.dtype is not cache.dtype or K.get_device() != cache.index or V.get_device() != cache.index):
         raise ValueError("expect K, V [Hkv, rows, D] of the cache's dtype and device, contiguous innermost, V with K's strides")
     b = cache.batch(seqs, cu_rows, shape[1], 0, layer)
@@ -710,19 +721,26 @@ def sl_paged_span_keys(cache: PageCache, seqs, cu_rows, Ks, S, layer=0):
     return Ks
 
 
+def _result(t, shape, dtype, device):
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"expect out contiguous, {tuple(shape)} of {dtype}, on the cache's device")
+
+
 def _paged_attention(cache, seqs, cu_rows, Q, idx, scores, S, layer, L, scale, ws):
-    shape, st = Q.shape, Q.stride()
+    shape, st = Q.shape, _strides(Q, "Q")
     if len(shape) != 3 or shape[2] != cache.D or st[2] != 1 or Q.dtype is not cache.dtype or Q.get_device() != cache.index:
         raise ValueError("expect Q [Hq, rows, D] of the cache's dtype and device with contiguous innermost dimension")
     Hq, T, _ = shape
     topk, ih, it = 0, 0, 0
     if idx is not None:
         topk = idx.shape[-1]
-        if idx.dtype is not torch.int32 or idx.shape != (Hq, T, topk) or idx.get_device() != cache.index or (topk and idx.stride(2) != 1):
-            raise ValueError("idx must be int32 [Hq, rows, topk] on the cache's device with contiguous innermost dimension")
-        ih, it, _ = idx.stride()
+        if idx.dtype is not torch.int32 or idx.shape != (Hq, T, topk) or idx.get_device() != cache.index:
+            raise ValueError("idx must be int32 [Hq, rows, topk] on the cache's device")
+        ih, it, one = _strides(idx, "idx")
+        if topk and one != 1:
+            raise ValueError("idx must be contiguous in its innermost dimension")
     if scores is not None and (idx is None or scores.dtype is not torch.float32 or scores.shape != idx.shape
-                               or scores.stride() != idx.stride() or scores.get_device() != cache.index):
+                               or _strides(scores, "scores") != (ih, it, one) or scores.get_device() != cache.index):
         raise ValueError("scores must be float32 with the shape, strides and device of idx")
     a = SlPagedAttention(Hq, S, topk, scale, st[0], st[1], ih, it)
     b = cache.batch(seqs, cu_rows, T, L, layer)
@@ -742,6 +760,8 @@ def sl_paged_span_attention(cache: PageCache, seqs, cu_rows, Q, idx, S, layer=0,
         LSE = torch.empty(Q.shape[:2], dtype=torch.float32, device=cache.device)
     else:
         O, LSE = out
+        _result(O, Q.shape, cache.dtype, cache.index)
+        _result(LSE, Q.shape[:2], torch.float32, cache.index)
     _check(load().sl_paged_span_attention(cache.record, b, a, Q.data_ptr(), _ptr(idx), O.data_ptr(), LSE.data_ptr(), wptr, wbytes, stream),
            "sl_paged_span_attention")
     return O, LSE
@@ -752,6 +772,7 @@ def sl_paged_span_attention_combined(cache: PageCache, seqs, cu_rows, Q, idx, sc
     a, b, (wptr, wbytes), held = _paged_attention(cache, seqs, cu_rows, Q, idx, scores, S, layer, L, scale, ws)
     stream = cache.stream()
     O = torch.empty(Q.shape, dtype=cache.dtype, device=cache.device) if out is None else out
+    _result(O, Q.shape, cache.dtype, cache.index)
     _check(load().sl_paged_span_attention_combined(cache.record, b, a, Q.data_ptr(), _ptr(idx), _ptr(scores), O.data_ptr(), wptr, wbytes,
                                                    stream), "sl_paged_span_attention_combined")
     return O

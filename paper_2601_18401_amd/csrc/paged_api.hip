@@ -142,6 +142,7 @@ sl_status sl_pages_free(const sl_page_cache* pc, const int32_t* seqs, int32_t n,
   sl_status s = sl::make_cache(pc, &c);
   if (s != SL_OK) return s;
   if (n < 0 || (n > 0 && (!seqs || !sl::aligned4(seqs)))) return SL_ERR_INVALID_ARG;
+  if (n > 65535) return SL_ERR_UNSUPPORTED;
   return sl::pages_free(c, seqs, n, static_cast<hipStream_t>(hip_stream));
 }
 

@@ -99,7 +99,7 @@ def test_missing_pointers_workspaces_and_long_lists():
     assert lib.sl_pages_extend(c, b, None, None) == 1
     assert lib.sl_pages_fork(c, None, P, 1, P, None) == 1 and lib.sl_pages_fork(c, P, P, -1, P, None) == 1
     assert lib.sl_pages_fork(c, P, P, 4097, P, None) == 2
-    assert lib.sl_pages_free(c, None, 1, None) == 1 and lib.sl_pages_free(c, P, -1, None) == 1
+    assert lib.sl_pages_free(c, None, 1, None) == 1 and lib.sl_pages_free(c, P, -1, None) == 1 and lib.sl_pages_free(c, P, 65536, None) == 2
     assert lib.sl_pages_compact(c, None, P, 1 << 20, None) == 1 and lib.sl_pages_compact(c, P, P, 16, None) == 3
     assert lib.sl_paged_append(c, b, None, P, 0, 0, None) == 1 and lib.sl_paged_append(c, b, P, P, 0, 100, None) == 1
     assert lib.sl_paged_append(c, b, P, P, -8, 0, None) == 1 and lib.sl_paged_append(c, b, P, P, 1 << 50, 0, None) == 2
@@ -161,6 +161,18 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         B.sl_paged_span_keys(cache, one, two, K[0], 16)
     Q = torch.zeros((4, 1, 64), dtype=torch.bfloat16)
     idx = torch.zeros((4, 1, 2), dtype=torch.int32)
+    wide = torch.zeros((4, 3, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError):      # rows that are one row repeated: no stride says that
+        B._paged_attention(cache, one, two, wide[:, :1].expand(4, 3, 64), None, None, 16, 0, 0, 0.0, None)
+    with pytest.raises(ValueError):
+        B._paged_attention(cache, one, two, wide, idx.expand(4, 3, 2), None, 16, 0, 0, 0.0, None)
+    with pytest.raises(ValueError):
+        B.PageCache(K[:, :1].expand(1, 6, 2, 16, 64), K[:, :1].expand(1, 6, 2, 16, 64), tables, lens, refs)
+    with pytest.raises(ValueError):
+        B.sl_paged_append(cache, one, two, wide[:2, :1].expand(2, 3, 64), wide[:2, :1].expand(2, 3, 64))
+    for out in (Q.float(), Q[:2], wide[:, :1]):
+        with pytest.raises(ValueError):
+            B._result(out, Q.shape, Q.dtype, -1)
     for q, i, s in ((Q.float(), idx, None), (Q[0], idx, None), (Q, idx.long(), None), (Q, idx[:2], None), (Q, idx, idx),
                     (Q, idx, torch.zeros((4, 1, 1)))):
         with pytest.raises(ValueError):

@@ -172,43 +172,109 @@ def test_rows_without_tokens_and_rows_of_nobody(dtype, topk, S, n):
     cache.V.copy_(V)
 
 
-@pytest.mark.parametrize("n", [3, 130])
+@pytest.mark.parametrize("dtype,n,ps", [(BF16, 3, 32), (BF16, 130, 32), (BF16, 130, 27), (F32, 130, 32), (F32, 3, 32), (F32, 270, 27)])
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
-def test_not_finite_where_some_rows_attend(what, n):
+def test_not_finite_where_some_rows_attend(what, dtype, n, ps):
     """A token that is not finite makes those rows not finite that attend it, as the formula has it, and no other: rows
     before it, rows whose spans leave it out."""
     g = torch.Generator().manual_seed(n)
     L, S = 400, 50
-    cache = make_cache(g, [L], 32, 2, 128, BF16)
+    cache = make_cache(g, [L], ps, 2, 128, dtype)
     bad = [L - 2, 120]  # one of the new tokens, and one in span 2
-    for t in bad:
-        page = int(cache.tables[0, t // 32])
-        cache.V[0, page, :, t % 32, 5] = what
-    Q = torch.randn((4, n, 128), generator=g).to(BF16).to(DEV)
-    idx = torch.tensor([[[0, 2], [0, 1]][(h + r) % 2] for h in range(4) for r in range(n)], dtype=torch.int32, device=DEV).view(4, n, 2)
-    O, LSE = B.sl_paged_span_attention(cache, i32([0]), i32([0, n]), Q, idx, S)
-    G = B.sl_paged_span_attention_combined(cache, i32([0]), i32([0, n]), Q, idx, torch.zeros(idx.shape, device=DEV), S)
-    torch.cuda.synchronize()
     clean_V = cache.V.clone()
     for t in bad:
-        clean_V[0, int(cache.tables[0, t // 32]), :, t % 32, 5] = 0
+        cache.V[0, int(cache.tables[0, t // ps]), :, t % ps, 5] = what
+        clean_V[0, int(cache.tables[0, t // ps]), :, t % ps, 5] = 0
     clean = B.PageCache(cache.K, clean_V, cache.tables, cache.lens, cache.refs)
-    wO, wL = B.sl_paged_span_attention(clean, i32([0]), i32([0, n]), Q, idx, S)
-    wG = B.sl_paged_span_attention_combined(clean, i32([0]), i32([0, n]), Q, idx, torch.zeros(idx.shape, device=DEV), S)
-    torch.cuda.synchronize()
-    for h in range(4):
-        for r in range(n):
-            pos = L - n + r
-            hit = any((t // S == pos // S and t <= pos) or (t // S < pos // S and t // S in idx[h, r].tolist()) for t in bad)
-            for x, w in ((O, wO), (G, wG)):
-                row = x[h, r].double()
+    Q = torch.randn((4, n, 128), generator=g).to(dtype).to(DEV)
+    idx = torch.tensor([[[0, 2], [0, 1]][(h + r) % 2] for h in range(4) for r in range(n)], dtype=torch.int32, device=DEV).view(4, n, 2)
+    zeros = torch.zeros(idx.shape, device=DEV)
+    seqs, cu = i32([0]), i32([0, n])
+    calls = [(lambda c: B.sl_paged_span_attention(c, seqs, cu, Q, idx, S)[0], S), (lambda c: B.sl_paged_span_attention_combined(c, seqs, cu, Q, idx, zeros, S), S),
+             (lambda c: B.sl_paged_span_attention(c, seqs, cu, Q, None, 10 * L)[0], 10 * L)]
+    for call, S in calls:
+        x, w = call(cache).double().cpu(), call(clean).double().cpu()
+        for h in range(4):
+            for r in range(n):
+                pos = L - n + r
+                hit = any((t // S == pos // S and t <= pos) or (t // S < pos // S and t // S in idx[h, r].tolist()) for t in bad)
                 if hit:
-                    assert torch.isnan(row[5]) if math.isnan(what) else row[5].item() == what
-                    row, w_row = torch.cat([row[:5], row[6:]]), torch.cat([w[h, r][:5], w[h, r][6:]]).double()
-                else:
-                    w_row = w[h, r].double()
-                assert float((row - w_row).abs().max()) <= 2.0 ** -7 * 5  # (the two may take different kernels: two roundings each)
-    assert float((LSE - wL).abs().max()) <= 1e-4
+                    assert torch.isnan(x[h, r, 5]) if math.isnan(what) else x[h, r, 5].item() == what
+                    x[h, r, 5] = w[h, r, 5]
+        # (the two may take different kernels: two roundings each of outputs below 5)
+        assert float((x - w).abs().max()) <= (2.0 ** -7 * 5 if dtype == BF16 else 1e-4)
+    LSE, want = (B.sl_paged_span_attention(c, seqs, cu, Q, idx, 50)[1] for c in (cache, clean))
+    assert float((LSE - want).abs().max()) <= 1e-4
+
+
+def test_scores_that_are_not_finite_are_masked_like_others():
+    """Keys that are not finite, behind every row's position or in spans that nobody lists, change nothing."""
+    g = torch.Generator().manual_seed(21)
+    for dtype, n in ((BF16, 2), (BF16, 140), (F32, 140), (F32, 2)):
+        cache = make_cache(g, [500], 16, 2, 64, dtype)
+        Q = torch.randn((4, n, 64), generator=g).to(dtype).to(DEV)
+        idx = torch.tensor([0, 3], dtype=torch.int32, device=DEV).expand(4, n, 2).contiguous()
+        cache.lens[0] = 470       # the last 30 tokens are behind the sequence's end
+        args = (cache, i32([0]), i32([0, n]), Q, idx, 60)
+        want = B.sl_paged_span_attention(*args)
+        for k, t in enumerate([470, 480, 499, 61, 100, 179, 250]):
+            cache.K[0, int(cache.tables[0, t // 16]), :, t % 16] = [math.nan, math.inf, -math.inf][k % 3]
+        got = B.sl_paged_span_attention(*args)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_lists_in_the_layout_of_the_batched_search():
+    """idx and scores [B][Hq][topk] of one new token per sequence, as views [Hq, B, topk]."""
+    g = torch.Generator().manual_seed(22)
+    for dtype in (BF16, F32):
+        cache = make_cache(g, [300, 500, 90], 32, 2, 128, dtype)
+        Q = torch.randn((8, 3, 128), generator=g).to(dtype).to(DEV)
+        idx = choose(g, 8, 3, 4, 8).transpose(0, 1).contiguous().transpose(0, 1)
+        scores = torch.randn((3, 8, 4), generator=g).to(DEV).transpose(0, 1)
+        assert idx.stride() == (4, 32, 1) and scores.stride() == (4, 32, 1)
+        O, LSE = B.sl_paged_span_attention(cache, i32([0, 1, 2]), i32([0, 1, 2, 3]), Q, idx, 40)
+        check(cache, [0, 1, 2], [0, 1, 2, 3], Q, idx, None, 40, O, LSE)
+        O = B.sl_paged_span_attention_combined(cache, i32([0, 1, 2]), i32([0, 1, 2, 3]), Q, idx, scores, 40)
+        check(cache, [0, 1, 2], [0, 1, 2, 3], Q, idx, scores, 40, O)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_results_do_not_change_from_run_to_run(dtype):
+    """Places in a bucket are handed out by atomics: no result may depend on them."""
+    g = torch.Generator().manual_seed(23)
+    cache = make_cache(g, [3000], 64, 2, 128, dtype)
+    Q = torch.randn((8, 900, 128), generator=g).to(dtype).to(DEV)
+    idx = choose(g, 8, 900, 4, 40)
+    want = None
+    for _ in range(6):
+        got = B.sl_paged_span_attention(cache, i32([0]), i32([0, 900]), Q, idx, 64)
+        want = want or got
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_two_captured_graphs_and_eager_calls_between():
+    """Scratch of a captured call is the graph's own: replays in any order, with eager calls of other sizes between them."""
+    g = torch.Generator().manual_seed(24)
+    cache = make_cache(g, [2000, 700], 64, 2, 128, BF16)
+    jobs = []
+    for seq, n, topk in ((0, 200, 4), (1, 1, 3)):
+        Q = torch.randn((8, n, 128), generator=g).to(BF16).to(DEV)
+        idx, cu, seqs = choose(g, 8, n, topk, 20), i32([0, n]), i32([seq])
+        jobs.append((lambda q=Q, i=idx, c=cu, s=seqs: B.sl_paged_span_attention(cache, s, c, q, i, 64)))
+    want = [tuple(x.clone() for x in job()) for job in jobs]
+    graphs, outs = [], []
+    for job in jobs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(job())
+        graphs.append(graph)
+    for k in (0, 1, 1, 0, 1, 0, 0):
+        for x in outs[k]:
+            x.zero_()
+        graphs[k].replay()
+        jobs[1 - k]()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs[k], want[k]))
 
 
 def test_append_and_span_keys():
