@@ -42,9 +42,10 @@ struct TilePlan {
   int64_t window_units;  // tiles * pieces of a window * Hkv
   int spans, buckets;    // spans of the longest sequence; B * Hkv * spans
   int32_t *counts, *first_tile;  // [buckets]
-  int4* records;   // [most_tiles] in the order of the workgroups: {first token of the span, entry, kv head, place of the tile << 9 | items}
+  int most_tiles;  // of the buckets; a multiple of 8
+  int4* records;   // [most_tiles] in the order of the workgroups: {span, entry * Hkv + kv head, place of the tile, items; 0: no tile}
   int32_t *ranks;  // [Hq * rows * topk] an item's place in its bucket, -1 for empty slots
-  int32_t *items;  // [tiles][cols] (row and head) * 32 + slot
+  int32_t *items;  // [most_tiles][cols] (row and head) * 32 + slot
 };
 
 __device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }  // NaN stays
@@ -856,7 +857,9 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
     end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
     ask_pages();
     for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
-      s_rh[c] = c < count ? plan.items[(int64_t)rec.z * COLS + c] : -1;  // (row and head) * 32 + slot
+      const int item = c < count ? plan.items[(int64_t)rec.z * COLS + c] : -1;  // (row and head) * 32 + slot
+      // (where cu_rows decreases, some that are counted have no row: their items hold anything)
+      s_rh[c] = item >= 0 && item >> 5 < x.a.Hq * x.b.rows && (item & 31) < x.a.topk ? item : -1;
       s_lo[c] = c < count ? begin : INT_MAX;
       s_last[c] = c < count ? end - 1 : -1;
     }
@@ -1109,7 +1112,8 @@ __global__ __launch_bounds__(1024) void count_kernel(const PagedArgs x, const Ti
 
 // Tiles of each bucket in the buckets' order; one workgroup.  Tiles of one bucket read the same rows: workgroups u = x (mod 8) run on
 // XCD x, which has an L2 of its own, and are given the x-th eighth of the list, in its order.
-__global__ __launch_bounds__(1024) void tiles_kernel(const TilePlan plan, int cols_log2, int most_tiles) {
+// (Where cu_rows decreases, rows may be counted more than once: what the list has no room for is left out.)
+__global__ __launch_bounds__(1024) void tiles_kernel(const TilePlan plan, int cols_log2) {
   __shared__ int s_wave[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   auto tiles_of = [&](int i) { return i < plan.buckets ? (plan.counts[i] + (1 << cols_log2) - 1) >> cols_log2 : 0; };
@@ -1134,18 +1138,19 @@ __global__ __launch_bounds__(1024) void tiles_kernel(const TilePlan plan, int co
     }
     if (i < plan.buckets) plan.first_tile[i] = at;
   }
+  total = min(total, plan.most_tiles);
   const int share = (total + 7) / 8;
 #pragma unroll 1
   for (int base = 0; base < plan.buckets; base += 1024) {
     const int i = base + threadIdx.x, n = tiles_of(i);
     if (n == 0) continue;
     const int first = plan.first_tile[i], count = plan.counts[i];
-    for (int k = 0; k < n; ++k) {
+    for (int k = 0; k < n && first + k < total; ++k) {
       const int tile = first + k, x = tile / share;
       plan.records[(tile - x * share) * 8 + x] = make_int4(i % plan.spans, i / plan.spans, tile, min(count - (k << cols_log2), 1 << cols_log2));
     }
   }
-  for (int k = threadIdx.x; k < most_tiles; k += 1024)
+  for (int k = threadIdx.x; k < plan.most_tiles; k += 1024)
     if ((k & 7) * share + (k >> 3) >= total || (k >> 3) >= share) plan.records[k].w = 0;
 }
 
@@ -1158,7 +1163,8 @@ __global__ __launch_bounds__(256) void items_kernel(const PagedArgs x, const Til
   const int rank = plan.ranks[i];
   if (rank < 0) return;
   const int e = entry_of_row(x.b.cu, x.b.B, row), j = x.idx[h * x.a.ish + row * x.a.ist + k];
-  plan.items[((int64_t)plan.first_tile[(e * x.c.Hkv + h / x.a.G) * plan.spans + j] << cols_log2) + rank] = rh * 32 + k;
+  const int64_t at = ((int64_t)plan.first_tile[(e * x.c.Hkv + h / x.a.G) * plan.spans + j] << cols_log2) + rank;
+  if (at < (int64_t)plan.most_tiles << cols_log2) plan.items[at] = rh * 32 + k;
 }
 
 // ------------------------------------------------------------------ merge
@@ -1169,7 +1175,8 @@ __device__ __forceinline__ void mend_row(const PagedArgs& x, int rh) {
   const int h = rh / x.b.rows, row = rh - h * x.b.rows, P = x.p.count, routed = x.a.topk * x.p.routed;
   const Entry at = entry_with_row(x, row);
   const int pos = position_of(x, at, row);
-  const PieceRange window = {pos / x.a.S * x.a.S, pos + 1};
+  // (a row without a token is marked only where cu_rows decreases and no tile took it)
+  const PieceRange window = pos < 0 ? PieceRange{0, 0} : PieceRange{pos / x.a.S * x.a.S, pos + 1};
   if (DIRECT) {
     take_piece<T, D, 1, true>(x, at.s, rh, window, 0, nullptr, nullptr);
     return;
@@ -1491,6 +1498,7 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
   if (f.tiles) {
     TilePlan plan = f.plan;
     if (f.buckets) {
+      plan.most_tiles = (int)f.most_tiles;
       plan.counts = reinterpret_cast<int32_t*>(ws + f.o_bytes + 2 * f.lse_bytes);
       plan.first_tile = plan.counts + plan.buckets;
       plan.records = reinterpret_cast<int4*>(plan.counts + align_up(2 * (size_t)plan.buckets, 64));
@@ -1500,7 +1508,7 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
       zero_kernel<<<(unsigned)(blocks < 1024 ? blocks : 1024), 256, 0, st>>>(plan.counts, plan.buckets);
       const int64_t runs = (int64_t)x.b.rows / kCountRows + x.b.B;
       count_kernel<<<dim3((unsigned)runs, x.c.Hkv), 1024, plan.spans <= kCountSpans ? plan.spans * sizeof(int32_t) : 0, st>>>(x, plan);
-      tiles_kernel<<<1, 1024, 0, st>>>(plan, f.cols_log2, (int)f.most_tiles);
+      tiles_kernel<<<1, 1024, 0, st>>>(plan, f.cols_log2);
       items_kernel<<<grid_of(div_up(rh * x.a.topk, 256)), 256, 0, st>>>(x, plan, f.cols_log2);
     }
     bool done;

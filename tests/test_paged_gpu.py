@@ -277,6 +277,58 @@ def test_two_captured_graphs_and_eager_calls_between():
         assert all(torch.equal(a, b) for a, b in zip(outs[k], want[k]))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("topk", [0, 8])
+@pytest.mark.parametrize("cu,rows", [([0, 512] * 50 + [512], 512), ([0, 4] * 6 + [4], 4), ([300, 20, 512, -40, 512, 1 << 30, 7], 512),
+                                     ([0, -5, 1 << 30, 3, 512], 512)])
+def test_rows_out_of_order_stay_inside_the_arrays(cu, rows, topk, dtype):
+    """cu_rows that decrease name rows twice, or rows that are none: results may be anything, what lies around them stays."""
+    g = torch.Generator().manual_seed(25)
+    cache = make_cache(g, [6400, 300], 64, 1, 64, dtype)
+    B_ = len(cu) - 1
+    seqs, cu = i32([0] * (B_ - 1) + [1]), i32(cu)
+    Q = torch.randn((16, rows, 64), generator=g).to(dtype).to(DEV)
+    idx = choose(g, 16, rows, topk, 18) if topk else None
+    S = 320 if topk else 10000
+    tables, lens, refs = cache.tables.clone(), cache.lens.clone(), cache.refs.clone()
+    a = B.SlPagedAttention(16, S, topk, 0.0, 0, 0, 0, 0)
+    b = cache.batch(seqs, cu, rows, 6400)
+    need = B.load().sl_paged_attention_workspace_bytes(cache.record, b, a)
+    ws = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device=DEV)   # (every float in it is NaN)
+    O = torch.full((Q.numel() + 2048,), 7.0, dtype=dtype, device=DEV)
+    LSE = torch.full((16 * rows + 2048,), 7.0, device=DEV)
+    for n in range(2):
+        st = B.load().sl_paged_span_attention(cache.record, b, a, Q.data_ptr(), None if idx is None else idx.data_ptr(), O.data_ptr() + 2048,
+                                              LSE.data_ptr() + 4096, ws.data_ptr(), need, cache.stream())
+        assert st == 0
+        torch.cuda.synchronize()
+        edge = 2048 // O.element_size()
+        assert bool((ws[need:] == 0xFF).all()) and bool((O[:edge] == 7).all()) and bool((O[edge + Q.numel():] == 7).all())
+        assert bool((LSE[:1024] == 7).all()) and bool((LSE[1024 + 16 * rows:] == 7).all())
+    before = cache.K.clone()
+    new = torch.randn((1, rows, 64), generator=g).to(dtype).to(DEV)
+    B.sl_paged_append(cache, seqs, cu, new, new)
+    cache.K.copy_(before)
+    B.sl_paged_span_keys(cache, seqs, cu, torch.empty((2, 1, 20, 64), dtype=dtype, device=DEV), 320)
+    torch.cuda.synchronize()
+    assert torch.equal(cache.tables, tables) and torch.equal(cache.lens, lens) and torch.equal(cache.refs, refs)
+
+
+@pytest.mark.parametrize("dtype,n", [(BF16, 2), (BF16, 150), (F32, 2), (F32, 60), (F32, 150)])
+def test_a_row_that_lists_a_span_twice_spoils_no_other(dtype, n):
+    g = torch.Generator().manual_seed(26)
+    cache = make_cache(g, [700], 32, 2, 64, dtype)
+    Q = torch.randn((8, n, 64), generator=g).to(dtype).to(DEV)
+    idx = choose(g, 8, n, 4, 14)
+    idx[:, 0] = 3
+    want, other = B.sl_paged_span_attention(cache, i32([0]), i32([0, n]), Q, idx, 40), idx.clone()
+    other[:, 0] = i32([3, -1, -1, -1])
+    got = B.sl_paged_span_attention(cache, i32([0]), i32([0, n]), Q, other, 40)
+    check(cache, [0], [0, n], Q, other, None, 40, *got)
+    tol = 1e-4 if dtype == F32 else 2.0 ** -7 * 5      # (places in a tile differ: two roundings each of outputs below 5)
+    assert float((want[0] - got[0])[:, 1:].float().abs().max()) <= tol and float((want[1] - got[1])[:, 1:].abs().max()) <= 1e-4
+
+
 def test_append_and_span_keys():
     for dtype, Hkv, D, ps, S, ns, have, token_major in [
             (BF16, 2, 128, 64, 32, [1, 1, 1], [31, 0, 100], False), (F32, 3, 64, 10, 7, [50, 0, 13], [3, 5, 69], True),
