@@ -349,7 +349,7 @@ typedef struct sl_page_cache {
   int32_t* refs;    /* [n_pages]                                                  */
   int64_t layer_stride, page_stride;  /* element strides of K and V; 0 = packed; not below D */
   int64_t kv_stride_h, kv_stride_t;   /* (0 = packed; kv_stride_t at most 2^20)              */
-  int32_t layers, n_pages, n_seqs, max_pages;  /* >= 1; max_pages * page_size <= 2^30 */
+  int32_t layers, n_pages, n_seqs, max_pages;  /* >= 1; max_pages * page_size, n_pages <= 2^30 */
   int32_t page_size, Hkv, D, dtype;            /* D: 64 or 128 */
 } sl_page_cache;
 

@@ -10,7 +10,9 @@ namespace {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-constexpr int64_t kMaxStride = (int64_t)1 << 40;     // elements: products with 32-bit counts stay inside 64 bits
+constexpr int64_t kMaxStride = (int64_t)1 << 40;     // elements
+constexpr int64_t kMaxExtent = (int64_t)1 << 56;     // ... of the cache: byte offsets stay inside 64 bits
+constexpr int32_t kMaxPages = 1 << 30;               // a page's number and a pass of a thousand threads count in 32 bits
 constexpr int64_t kMaxTokenStride = (int64_t)1 << 20;
 constexpr int64_t kMaxRows = (int64_t)1 << 25;       // 16-byte pieces of a row tensor's head count in 32 bits
 constexpr int64_t kMaxRowHeads = (int64_t)1 << 26;   // a row, its head and a slot of 32 count in 31 bits
@@ -22,7 +24,7 @@ sl_status make_cache(const sl_page_cache* p, PageCache* c) {
   if (p->layers < 1 || p->n_pages < 1 || p->n_seqs < 1 || p->max_pages < 1 || p->page_size < 1 || p->Hkv < 1) return SL_ERR_INVALID_ARG;
   if (p->dtype != SL_F32 && p->dtype != SL_BF16) return SL_ERR_INVALID_ARG;
   if (p->D != 64 && p->D != 128) return SL_ERR_UNSUPPORTED;
-  if ((int64_t)p->max_pages * p->page_size > (int64_t)1 << 30) return SL_ERR_UNSUPPORTED;
+  if ((int64_t)p->max_pages * p->page_size > (int64_t)1 << 30 || p->n_pages > kMaxPages) return SL_ERR_UNSUPPORTED;
   // (grid dimensions are 16 bits wide in y)
   if (p->Hkv > 1024 || p->layers > 4096 || (int64_t)p->layers * 2 * p->Hkv + p->max_pages / 1024 > 65000 || p->max_pages > (1 << 25))
     return SL_ERR_UNSUPPORTED;
@@ -33,6 +35,7 @@ sl_status make_cache(const sl_page_cache* p, PageCache* c) {
   c->head = p->kv_stride_h ? p->kv_stride_h : p->page_size * c->tok;
   c->page = p->page_stride ? p->page_stride : p->Hkv * c->head;
   c->layer = p->layer_stride ? p->layer_stride : p->n_pages * c->page;
+  if (c->head > kMaxExtent / p->Hkv || c->page > kMaxExtent / p->n_pages || c->layer > kMaxExtent / p->layers) return SL_ERR_UNSUPPORTED;
   const int64_t epl = p->dtype == SL_BF16 ? 8 : 4;
   if (c->tok % epl || c->head % epl || c->page % epl || c->layer % epl) return SL_ERR_INVALID_ARG;
   if (c->tok < p->D || (p->Hkv > 1 && c->head < p->D) || (p->n_pages > 1 && c->page < p->D) || (p->layers > 1 && c->layer < p->D))

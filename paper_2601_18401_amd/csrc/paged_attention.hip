@@ -61,7 +61,7 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 }
 
 // A piece's normalised output: fp32, or for bf16 calls fp16 beside a power of two above the row's largest value: half the
-// bytes, and 2^-12 of that value is a sixteenth of the step that rounds the result (bf16 there would be as large as that step).
+// bytes, off by up to 2^-11 of the largest value, where rounding the result to bf16 costs 2^-8 (and bf16 here would cost as much again).
 template <typename T>
 struct Record {
   typedef float Value;
@@ -660,7 +660,7 @@ struct Tile<bf16_t, D, CB, KB> : Softmax<D, CB, KB> {
         for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(s[cb][ks >> 1][8 * (ks & 1) + e], sc, minus));
         // the unrounded weights' sum: lse is exact to fp32
         l[cb] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-        // Rounded to bf16 for the product with V: an error of up to 2^-9 of each weight, about that of the rounded result.
+        // Rounded to bf16 for the product with V: an error of up to 2^-8 of each weight, as large as rounding the result makes.
         p[cb][ks] = __builtin_convertvector(w, bf16x8);
       }
     }
@@ -1453,7 +1453,9 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
     p.window = (int)div_up(window, p.window_tokens);
   }
   p.count = a.topk * p.routed + p.window;
-  f.o_bytes = align_up((size_t)rh * p.count * c.D * (c.dtype == SL_BF16 ? sizeof(_Float16) : sizeof(float)), 256);
+  // (one piece a row: the tiles write results, and what the merge would ask for is not there)
+  const bool direct = f.tiles && p.count == 1;
+  f.o_bytes = direct ? 0 : align_up((size_t)rh * p.count * c.D * (c.dtype == SL_BF16 ? sizeof(_Float16) : sizeof(float)), 256);
   f.lse_bytes = align_up((size_t)rh * p.count * sizeof(float), 256);
   f.units = f.plan.window_units;
   if (f.buckets) {

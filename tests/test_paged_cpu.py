@@ -38,7 +38,8 @@ BAD_CACHE = [(dict(K=None), 1), (dict(V=P + 8), 1), (dict(tables=None), 1), (dic
              (dict(refs=P + 4), 1), (dict(layers=0), 1), (dict(n_pages=0), 1), (dict(n_seqs=0), 1), (dict(max_pages=0), 1),
              (dict(page_size=0), 1), (dict(Hkv=0), 1), (dict(dtype=2), 1), (dict(D=96), 2), (dict(max_pages=1 << 25, page_size=64), 2),
              (dict(kv_stride_t=-8), 1), (dict(kv_stride_t=1 << 21, kv_stride_h=8, page_stride=1 << 22), 2), (dict(kv_stride_t=120), 1), (dict(kv_stride_t=132), 1), (dict(kv_stride_h=4), 1),
-             (dict(page_stride=12), 1), (dict(layer_stride=-8), 1), (dict(page_stride=8), 1), (dict(page_stride=1 << 50), 2), (dict(Hkv=2048), 2)]
+             (dict(page_stride=12), 1), (dict(layer_stride=-8), 1), (dict(page_stride=8), 1), (dict(page_stride=1 << 50), 2), (dict(Hkv=2048), 2),
+             (dict(n_pages=(1 << 30) + 1), 2), (dict(n_pages=1 << 20, page_stride=1 << 40), 2), (dict(layers=512, layer_stride=1 << 48), 2)]
 BAD_BATCH = [(dict(B=-1), 1), (dict(B=65536), 2), (dict(rows=-1), 1), (dict(rows=(1 << 25) + 1), 2), (dict(L=-1), 1), (dict(layer=2), 1),
              (dict(layer=-1), 1), (dict(seqs=None), 1), (dict(cu_rows=None), 1), (dict(cu_rows=P + 2), 1)]
 BAD_ATTENTION = [(dict(Hq=0), 1), (dict(Hq=30), 1), (dict(Hq=512), 2), (dict(S=0), 1), (dict(topk=-1), 1), (dict(topk=33), 2), (dict(scale=-1.0), 1),
