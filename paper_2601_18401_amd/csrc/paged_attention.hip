@@ -763,6 +763,10 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
+// NW wavefronts of 32 * CB columns, two stages of STEP tokens.  Measured (bf16, D = 128): four prompts of 2500 to 6000 tokens, 32:8 heads,
+// 770 us = 1.05 PFLOP/s, where a large library product reaches 1.2; 2000 rows behind 64K tokens, 32:4 heads, eight spans of 512, 215 us =
+// 0.66 PFLOP/s (tiles of 8 steps, whose beginnings and ends are a quarter of them); one token behind a million 49 us = 5.2 TB/s, 24 caches
+// of up to 120000 tokens 93 us = 5.6 TB/s, where a pure read reaches 6.4.
 // NW wavefronts of 32 * CB columns, two stages of STEP tokens.
 //   4 wavefronts: the matrix cores are what bounds these
 //   1 wavefront: few columns, so that memory does; five workgroups (D = 128) of a compute unit have 16 KB each on the way
@@ -1213,22 +1217,24 @@ __global__ __launch_bounds__(256) void mend_kernel(const PagedArgs x) {
     mend_row<T, D, DIRECT>(x, (int)first + __builtin_ctzll(marked));
 }
 
-// WAVES wavefronts (of a workgroup's four) join the pieces of one row and head: weights to LDS, then D / 8 (fp32: D / 4) lanes
-// a piece.  Nothing a wavefront asks for depends on what it has read: the first outputs are on their way before there are weights.
+// N lanes of a workgroup's 256 join the pieces of one row and head: weights to LDS, then D / 8 (fp32: D / 4) lanes a piece.  Nothing they
+// ask for depends on what they have read: the first outputs are on their way before there are weights.  Bound by memory where rows fill
+// the chip: 64000 rows and heads of 10 pieces of 256 bytes, 185 MB, in 42 us (4.4 TB/s; with a wavefront a row 47: its instructions).
 // MEND: marked pieces are mended here.  (Where there are rows enough to fill the chip, that would cost half its occupancy.)
-template <typename T, int D, int WAVES, bool MEND>
+template <typename T, int D, int N, bool MEND>
 __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   typedef typename Record<T>::Value Value;
-  constexpr int EPL = 16 / sizeof(Value), LANES = D / EPL, N = 64 * WAVES, GROUPS = N / LANES, U = 4;
+  constexpr int EPL = 16 / sizeof(Value), LANES = D / EPL, GROUPS = N / LANES, U = N == 32 ? 8 : 4, ROWS = 256 / N;
+  static_assert(N == 32 || N == 64 || N == 256, "half a wavefront, one, or four");
   typedef Value Values __attribute__((ext_vector_type(EPL)));
-  extern __shared__ float s_dyn[];  // [4 / WAVES][count] weights
+  extern __shared__ float s_dyn[];  // [ROWS][count] weights
   __shared__ float s_red[4];
-  __shared__ float s_gates[4 / WAVES][SL_MAX_TOPK], s_lses[4 / WAVES][SL_MAX_TOPK];
-  __shared__ float s_out[WAVES == 1 ? 1 : GROUPS * D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = WAVES == 1 ? lane : threadIdx.x, P = x.p.count;
-  const int64_t unit = WAVES == 1 ? workgroup() * 4 + wave : workgroup();
+  __shared__ float s_gates[ROWS][SL_MAX_TOPK], s_lses[ROWS][SL_MAX_TOPK];
+  __shared__ float s_out[N < 256 ? 1 : GROUPS * D];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tid = threadIdx.x % N, sub = threadIdx.x / N, P = x.p.count;
+  const int64_t unit = workgroup() * ROWS + sub;
   if (unit >= (int64_t)x.a.Hq * x.b.rows) return;
-  const int rh = (int)unit, sub = WAVES == 1 ? wave : 0;
+  const int rh = (int)unit;
   const int h = rh / x.b.rows, row = rh - h * x.b.rows;
   const int g = tid / LANES, c = tid % LANES;
   const Values* const po = reinterpret_cast<const Values*>(static_cast<const Value*>(x.part_o) + (int64_t)rh * P * D) + c;
@@ -1248,7 +1254,7 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   float* const s_w = s_dyn + sub * P;
   float *const s_gate = s_gates[sub], *const s_lse = s_lses[sub];
   auto barrier = [] {
-    if (WAVES > 1) {
+    if (N == 256) {
       __syncthreads();
     } else {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -1257,8 +1263,8 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   };
   auto all_max = [&](float v) {
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v = max_of(v, __shfl_xor(v, off, 64));
-    if (WAVES == 1) return v;
+    for (int off = N < 64 ? N / 2 : 32; off >= 1; off >>= 1) v = max_of(v, __shfl_xor(v, off, 64));
+    if (N < 256) return v;
     __syncthreads();
     if (lane == 0) s_red[wave] = v;
     __syncthreads();
@@ -1266,8 +1272,8 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   };
   auto all_sum = [&](float v) {
 #pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-    if (WAVES == 1) return v;
+    for (int off = N < 64 ? N / 2 : 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+    if (N < 256) return v;
     __syncthreads();
     if (lane == 0) s_red[wave] = v;
     __syncthreads();
@@ -1289,14 +1295,20 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
   bool any = false;  // a slot holds a span
   float total = lse_of(0);
   if (MEND && total != total && x.marks) {
-    if (WAVES == 1 || wave == 0) mend_row<T, D, false>(x, rh);
+    if (N == 64 || wave == 0) mend_row<T, D, false>(x, rh);
     __threadfence_block();
     barrier();
     ask();
     total = lse_of(0);
   }
   if (x.a.combined) {
-    const int pos = position_of(x, entry_with_row(x, row), row);
+    int pos;
+    if constexpr (N == 32) {  // (rows of a wavefront differ)
+      const int e = entry_of_row(x.b.cu, x.b.B, row);
+      pos = position_of(x, {e, 0, length_of(x.c, x.b.seqs[e]), 0, x.b.cu[e + 1]}, row);
+    } else {
+      pos = position_of(x, entry_with_row(x, row), row);
+    }
     const float near = lse_of(routed);
     float score = -INFINITY;
     bool mine = false;
@@ -1311,7 +1323,8 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
       for (int k = 0; k < x.p.routed; ++k) l += weight_of(lse[tid * x.p.routed + k], m);
       s_lse[tid] = m == -INFINITY ? m : m + __log2f(l);
     }
-    any = WAVES > 1 ? __syncthreads_or(mine) : __builtin_amdgcn_ballot_w64(mine) != 0;
+    if (N == 256) any = __syncthreads_or(mine);
+    else any = (N == 64 ? __builtin_amdgcn_ballot_w64(mine) : __builtin_amdgcn_ballot_w64(mine) >> (lane & 32) & 0xffffffffu) != 0;
     if (any) {
       const float top = all_max(score);
       const float e = mine ? fast_exp2((score - top) * kLog2e) : 0.f;
@@ -1356,9 +1369,9 @@ __global__ __launch_bounds__(256) void merge_kernel(const PagedArgs x) {
       }
     }
   }
-  if (WAVES == 1) {
+  if constexpr (N < 256) {
 #pragma unroll
-    for (int off = LANES; off < 64; off <<= 1)
+    for (int off = LANES; off < N; off <<= 1)
 #pragma unroll
       for (int e = 0; e < EPL; ++e) acc[e] += __shfl_xor(acc[e], off, 64);
     if (g == 0) {
@@ -1532,16 +1545,17 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
   if (x.p.count == 1 && f.tiles) {
     mend_kernel<T, D, true><<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x);
   } else {
-    // A wavefront a row where there are rows enough, or pieces few enough to be asked for at once (16 dense sequences, 1100 rows and
-    // heads of 30 pieces: 7.2 -> MERGE us).
+    // A wavefront a row, or half of one, where there are rows enough, or pieces few enough to be asked for at once (16 dense sequences,
+    // 1100 rows and heads of 30 pieces: 7.0 us by four wavefronts, 4.0 so).
     constexpr int kAtOnce = 4 * 64 / (D * (int)sizeof(typename Record<T>::Value) / 16);
     if (rh >= 4096 && x.p.count <= 1024) {
       if (f.tiles) mend_kernel<T, D, false><<<grid_of(div_up(rh, 256)), 256, 0, st>>>(x);
-      merge_kernel<T, D, 1, false><<<grid_of(div_up(rh, 4)), 256, 4 * x.p.count * sizeof(float), st>>>(x);
+      if (x.p.count <= 32) merge_kernel<T, D, 32, false><<<grid_of(div_up(rh, 8)), 256, 8 * x.p.count * sizeof(float), st>>>(x);
+      else merge_kernel<T, D, 64, false><<<grid_of(div_up(rh, 4)), 256, 4 * x.p.count * sizeof(float), st>>>(x);
     } else if (x.p.count <= kAtOnce) {
-      merge_kernel<T, D, 1, true><<<grid_of(div_up(rh, 4)), 256, 4 * x.p.count * sizeof(float), st>>>(x);
+      merge_kernel<T, D, 64, true><<<grid_of(div_up(rh, 4)), 256, 4 * x.p.count * sizeof(float), st>>>(x);
     } else {
-      merge_kernel<T, D, 4, true><<<grid_of(rh), 256, x.p.count * sizeof(float), st>>>(x);
+      merge_kernel<T, D, 256, true><<<grid_of(rh), 256, x.p.count * sizeof(float), st>>>(x);
     }
   }
   return hipGetLastError() == hipSuccess ? SL_OK : SL_ERR_LAUNCH;

@@ -94,6 +94,13 @@ CASES = [
     (F32, 4, 4, 64, 13, 40, 2, [250], [250], True),
     (F32, 4, 2, 64, 32, 20, 2, [1] * 150 + [0, 3] + [1] * 120, list(range(3, 275)), False),   # many sequences of one token each
     (BF16, 4, 2, 64, 32, 20, 2, [1] * 150 + [0, 3] + [1] * 120, list(range(3, 275)), False),
+    (BF16, 32, 4, 64, 16, 24, 3, [90, 50], [200, 60], False),     # more than 4096 rows and heads
+    (BF16, 32, 4, 128, 16, 24, 7, [90, 50], [200, 60], True),
+    (BF16, 32, 8, 64, 16, 4, 32, [140], [300], False),
+    (BF16, 32, 8, 128, 32, 4, 1, [150], [3000], False),
+    (F32, 32, 4, 64, 16, 48, 3, [90, 60], [300, 110], False),
+    (F32, 32, 4, 128, 16, 48, 9, [90, 60], [500, 70], False),
+    (F32, 32, 8, 128, 16, 16, 32, [140], [700], False),
 ]
 
 
@@ -172,9 +179,10 @@ def test_rows_without_tokens_and_rows_of_nobody(dtype, topk, S, n):
     cache.V.copy_(V)
 
 
-@pytest.mark.parametrize("dtype,n,ps", [(BF16, 3, 32), (BF16, 130, 32), (BF16, 130, 27), (F32, 130, 32), (F32, 3, 32), (F32, 270, 27)])
+@pytest.mark.parametrize("dtype,n,ps,Hq", [(BF16, 3, 32, 4), (BF16, 130, 32, 4), (BF16, 130, 27, 4), (F32, 130, 32, 4), (F32, 3, 32, 4),
+                                           (F32, 270, 27, 4), (BF16, 150, 32, 32), (F32, 200, 16, 32)])
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
-def test_not_finite_where_some_rows_attend(what, dtype, n, ps):
+def test_not_finite_where_some_rows_attend(what, dtype, n, ps, Hq):
     """A token that is not finite makes those rows not finite that attend it, as the formula has it, and no other: rows
     before it, rows whose spans leave it out."""
     g = torch.Generator().manual_seed(n)
@@ -186,15 +194,15 @@ def test_not_finite_where_some_rows_attend(what, dtype, n, ps):
         cache.V[0, int(cache.tables[0, t // ps]), :, t % ps, 5] = what
         clean_V[0, int(cache.tables[0, t // ps]), :, t % ps, 5] = 0
     clean = B.PageCache(cache.K, clean_V, cache.tables, cache.lens, cache.refs)
-    Q = torch.randn((4, n, 128), generator=g).to(dtype).to(DEV)
-    idx = torch.tensor([[[0, 2], [0, 1]][(h + r) % 2] for h in range(4) for r in range(n)], dtype=torch.int32, device=DEV).view(4, n, 2)
+    Q = torch.randn((Hq, n, 128), generator=g).to(dtype).to(DEV)
+    idx = torch.tensor([[[0, 2], [0, 1]][(h + r) % 2] for h in range(Hq) for r in range(n)], dtype=torch.int32, device=DEV).view(Hq, n, 2)
     zeros = torch.zeros(idx.shape, device=DEV)
     seqs, cu = i32([0]), i32([0, n])
     calls = [(lambda c: B.sl_paged_span_attention(c, seqs, cu, Q, idx, S)[0], S), (lambda c: B.sl_paged_span_attention_combined(c, seqs, cu, Q, idx, zeros, S), S),
              (lambda c: B.sl_paged_span_attention(c, seqs, cu, Q, None, 10 * L)[0], 10 * L)]
     for call, S in calls:
         x, w = call(cache).double().cpu(), call(clean).double().cpu()
-        for h in range(4):
+        for h in range(Hq):
             for r in range(n):
                 pos = L - n + r
                 hit = any((t // S == pos // S and t <= pos) or (t // S < pos // S and t // S in idx[h, r].tolist()) for t in bad)
