@@ -98,6 +98,7 @@ CASES = [
     (BF16, 32, 4, 128, 16, 24, 7, [90, 50], [200, 60], True),
     (BF16, 32, 8, 64, 16, 4, 32, [140], [300], False),
     (BF16, 32, 8, 128, 32, 4, 1, [150], [3000], False),
+    (BF16, 32, 1, 64, 16, 1, 8, [160], [13000], False),          # more spans than are counted in LDS
     (F32, 32, 4, 64, 16, 48, 3, [90, 60], [300, 110], False),
     (F32, 32, 4, 128, 16, 48, 9, [90, 60], [500, 70], False),
     (F32, 32, 8, 128, 16, 16, 32, [140], [700], False),
@@ -335,6 +336,23 @@ def test_a_row_that_lists_a_span_twice_spoils_no_other(dtype, n):
     check(cache, [0], [0, n], Q, other, None, 40, *got)
     tol = 1e-4 if dtype == F32 else 2.0 ** -7 * 5      # (places in a tile differ: two roundings each of outputs below 5)
     assert float((want[0] - got[0])[:, 1:].float().abs().max()) <= tol and float((want[1] - got[1])[:, 1:].abs().max()) <= 1e-4
+
+
+def test_more_workgroups_than_a_grid_dimension_takes():
+    """1200 rows of 64 heads with 16 spans of 4 tokens each, all but alone in their spans: 1.2 million pieces, against calls of 300 rows."""
+    g = torch.Generator(device=DEV).manual_seed(27)
+    L, ps, n, topk = 1 << 20, 64, 1200, 16
+    K, V = (torch.randn((1, L // ps, 2, ps, 64), generator=g, device=DEV).to(BF16) for _ in range(2))
+    tables = torch.randperm(L // ps, generator=g, device=DEV).to(torch.int32).view(1, -1)
+    cache = B.PageCache(K, V, tables, i32([L]), torch.ones(L // ps, dtype=torch.int32, device=DEV))
+    Q = torch.randn((64, n, 64), generator=g, device=DEV).to(BF16)
+    idx = torch.randint(0, L // 4 // topk, (64, n, topk), generator=g, device=DEV, dtype=torch.int32) * topk + torch.arange(topk, dtype=torch.int32, device=DEV)
+    O, LSE = B.sl_paged_span_attention(cache, i32([0]), i32([0, n]), Q, idx, 4)
+    for r in range(0, n, 300):
+        cache.lens.fill_(L - n + r + 300)
+        o, lse = B.sl_paged_span_attention(cache, i32([0]), i32([0, 300]), Q[:, r:r + 300].contiguous(), idx[:, r:r + 300].contiguous(), 4)
+        assert float((LSE[:, r:r + 300] - lse).abs().max()) <= 1e-4
+        assert float((O[:, r:r + 300].float() - o.float()).abs().max()) <= 2.0 ** -7 * 5     # (two roundings each of outputs below 5)
 
 
 def test_append_and_span_keys():
