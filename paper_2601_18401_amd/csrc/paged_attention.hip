@@ -776,7 +776,8 @@ __device__ __forceinline__ void wait_loads() {
 //   1 wavefront: one for every (row, head, slot).  Other heads and rows of its 32 columns may list the same span: the first one
 //                that does takes it for all, so that a span is read once for the group.
 //   ANY: pages of a size that is no multiple of 16: every row has a page of its own, at twice the instructions for its address
-template <typename T, int D, int NW, int CB, int STEP, bool ANY>
+//   PAST: records go past the caches
+template <typename T, int D, int NW, int CB, int STEP, bool ANY, bool PAST>
 __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
   constexpr int COLS = NW * 32 * CB;
   extern __shared__ __align__(1024) char s_dynamic[];  // (static, the compiler would wait for staging loads at every read)
@@ -1061,7 +1062,9 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
       const int row = i * RPI + ln / LPR, piece = ln % LPR;
       if (!(write >> row & 1)) continue;
       const uint4 v = *reinterpret_cast<const uint4*>(s_out + (row * LPR + (piece ^ row % LPR)) * 16);
-      *reinterpret_cast<uint4*>(to + record(s_rh[wave * 32 * CB + cb * 32 + row]) * (D * (int)sizeof(Value)) + piece * 16) = v;
+      char* const at = to + record(s_rh[wave * 32 * CB + cb * 32 + row]) * (D * (int)sizeof(Value)) + piece * 16;
+      if (PAST) store16_stream(at, v);
+      else *reinterpret_cast<uint4*>(at) = v;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -1406,6 +1409,10 @@ dim3 grid_of(int64_t workgroups) {
   return workgroups <= kMost ? dim3((unsigned)workgroups) : dim3((unsigned)kMost, (unsigned)div_up(workgroups, kMost));
 }
 
+// Records that the Infinity Cache (256 MB) would not keep until they are merged are written past the caches: 222 MB of them (3000 rows
+// behind 60000 tokens, 32:4 heads, eight spans of 128) 260 -> 237 us the call, 5 GB (64K tokens, spans of 256) 5.57 -> 5.24 ms; 169 MB 259 -> 262.
+constexpr size_t kStreamedRecords = (size_t)200 << 20;
+
 // How a call is taken.
 struct Form {
   Pieces p;
@@ -1485,7 +1492,7 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
 }
 
 // The stages fill up to 128 KB of dynamic LDS beside the static arrays: more than a kernel has without asking.
-template <typename T, int D, int NW, int CB, int STEP, bool ANY>
+template <typename T, int D, int NW, int CB, int STEP, bool ANY, bool PAST>
 bool launch_tiles_as(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
   constexpr int kBytes = 2 * 2 * STEP * D * (int)sizeof(T);
   static std::mutex mu;
@@ -1495,16 +1502,20 @@ bool launch_tiles_as(const PagedArgs& x, const Form& f, const TilePlan& plan, hi
   {
     std::lock_guard<std::mutex> lock(mu);
     if (!asked[dev])
-      asked[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(tile_kernel<T, D, NW, CB, STEP, ANY>),
+      asked[dev] = hipFuncSetAttribute(reinterpret_cast<const void*>(tile_kernel<T, D, NW, CB, STEP, ANY, PAST>),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) == hipSuccess;
     if (!asked[dev]) return false;
   }
-  tile_kernel<T, D, NW, CB, STEP, ANY><<<grid_of(f.units), 64 * NW, kBytes, st>>>(x, plan);
+  tile_kernel<T, D, NW, CB, STEP, ANY, PAST><<<grid_of(f.units), 64 * NW, kBytes, st>>>(x, plan);
   return true;
 }
 template <typename T, int D, int NW, int CB, int STEP>
 bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
-  return x.c.ps % 16 == 0 ? launch_tiles_as<T, D, NW, CB, STEP, false>(x, f, plan, st) : launch_tiles_as<T, D, NW, CB, STEP, true>(x, f, plan, st);
+  const bool any = x.c.ps % 16 != 0;
+  if constexpr (NW > 1)
+    if (f.o_bytes >= kStreamedRecords)
+      return any ? launch_tiles_as<T, D, NW, CB, STEP, true, true>(x, f, plan, st) : launch_tiles_as<T, D, NW, CB, STEP, false, true>(x, f, plan, st);
+  return any ? launch_tiles_as<T, D, NW, CB, STEP, true, false>(x, f, plan, st) : launch_tiles_as<T, D, NW, CB, STEP, false, false>(x, f, plan, st);
 }
 
 template <typename T, int D>
