@@ -350,7 +350,8 @@ typedef struct sl_page_cache {
   int64_t layer_stride, page_stride;  /* element strides of K and V; 0 = packed; not below D */
   int64_t kv_stride_h, kv_stride_t;   /* (0 = packed; kv_stride_t at most 2^20)              */
   int32_t layers, n_pages, n_seqs, max_pages;  /* >= 1; max_pages * page_size, n_pages <= 2^30 */
-  int32_t page_size, Hkv, D, dtype;            /* D: 64 or 128 */
+  int32_t page_size, Hkv, D, dtype;            /* D: 64 or 128; Hkv at most 1024, layers at most 4096,
+                                                  layers * 2 * Hkv + max_pages / 1024 at most 65000 */
 } sl_page_cache;
 
 /* New tokens of B sequences: rows cu_rows[b] .. cu_rows[b+1] - 1 of the row tensors are the LAST
@@ -415,7 +416,7 @@ sl_status sl_paged_span_keys(const sl_page_cache* c, const sl_paged_batch* b, in
  * i = lens - (new tokens of b) + (r - cu_rows[b]); c = i / S; its window is [c*S, i].  With
  * topk = 0 and S >= L this is dense causal attention. */
 typedef struct sl_paged_attention {
-  int32_t Hq;     /* query heads, a multiple of the cache's Hkv */
+  int32_t Hq;     /* query heads, a multiple of the cache's Hkv, at most 64 times it */
   int32_t S;      /* span length, >= 1 */
   int32_t topk;   /* 0 .. SL_MAX_TOPK */
   float scale;    /* 0 means 1/sqrt(D) */

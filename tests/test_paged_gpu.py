@@ -355,6 +355,33 @@ def test_more_workgroups_than_a_grid_dimension_takes():
         assert float((O[:, r:r + 300].float() - o.float()).abs().max()) <= 2.0 ** -7 * 5     # (two roundings each of outputs below 5)
 
 
+@pytest.mark.parametrize("dtype,n,D,ps", [(BF16, 3400, 128, 64), (BF16, 6700, 64, 40), (F32, 1800, 128, 16)])
+def test_records_beyond_the_caches(dtype, n, D, ps):
+    """Calls with more than 200 MB of records, joint and gated, against calls of 400 rows."""
+    g = torch.Generator(device=DEV).manual_seed(28)
+    L, S, topk, Hq = 20000, 128, 8, 32
+    pages = -(-L // ps)
+    K, V = (torch.randn((1, pages, 4, ps, D), generator=g, device=DEV).to(dtype) for _ in range(2))
+    tables = torch.randperm(pages, generator=g, device=DEV).to(torch.int32).view(1, -1)
+    cache = B.PageCache(K, V, tables, i32([L]), torch.ones(pages, dtype=torch.int32, device=DEV))
+    Q = torch.randn((Hq, n, D), generator=g, device=DEV).to(dtype)
+    idx = torch.randint(0, (L - n) // S // topk, (Hq, n, topk), generator=g, device=DEV, dtype=torch.int32) * topk
+    idx += torch.arange(topk, dtype=torch.int32, device=DEV)
+    scores = torch.randn(idx.shape, generator=g, device=DEV)
+    O, LSE = B.sl_paged_span_attention(cache, i32([0]), i32([0, n]), Q, idx, S)
+    C = B.sl_paged_span_attention_combined(cache, i32([0]), i32([0, n]), Q, idx, scores, S)
+    tol = 1e-4 if dtype == F32 else 2.0 ** -7 * 5     # (two roundings each of outputs below 5)
+    for r in range(0, n, 400):
+        rows = slice(r, min(r + 400, n))
+        m = rows.stop - r
+        cache.lens.fill_(L - n + rows.stop)
+        q, i, sc = (x[:, rows].contiguous() for x in (Q, idx, scores))
+        o, lse = B.sl_paged_span_attention(cache, i32([0]), i32([0, m]), q, i, S)
+        c = B.sl_paged_span_attention_combined(cache, i32([0]), i32([0, m]), q, i, sc, S)
+        assert float((LSE[:, rows] - lse).abs().max()) <= 1e-4
+        assert float((O[:, rows].float() - o.float()).abs().max()) <= tol and float((C[:, rows].float() - c.float()).abs().max()) <= tol
+
+
 def test_append_and_span_keys():
     for dtype, Hkv, D, ps, S, ns, have, token_major in [
             (BF16, 2, 128, 64, 32, [1, 1, 1], [31, 0, 100], False), (F32, 3, 64, 10, 7, [50, 0, 13], [3, 5, 69], True),
