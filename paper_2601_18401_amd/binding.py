@@ -742,7 +742,7 @@ def _paged_attention(cache, seqs, cu_rows, Q, idx, scores, S, layer, L, scale, w
     if scores is not None and (idx is None or scores.dtype is not torch.float32 or scores.shape != idx.shape
                                or _strides(scores, "scores") != (ih, it, one) or scores.get_device() != cache.index):
         raise ValueError("scores must be float32 with the shape, strides and device of idx")
-    a = SlPagedAttention(Hq, S, topk, scale, st[0], st[1], ih, it)
+    a = SlPagedAttention(Hq, min(S, 0x7fffffff), topk, scale, st[0], st[1], ih, it)  # (no sequence is longer)
     b = cache.batch(seqs, cu_rows, T, L, layer)
     # Scratch is the call's own unless the caller gives a workspace: calls on different streams and graphs do not share it.
     ws = Workspace(cache.device) if ws is None else ws

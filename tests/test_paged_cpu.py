@@ -178,3 +178,18 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
                     (Q, idx, torch.zeros((4, 1, 1)))):
         with pytest.raises(ValueError):
             B._paged_attention(cache, one, two, q, i, s, 16, 0, 0, 0.0, None)
+
+
+def test_a_span_longer_than_any_sequence_is_not_cut_off():
+    """S is 32 bits wide in the record; ctypes would drop the bits above without a word."""
+    K = torch.zeros((6, 2, 16, 64), dtype=torch.bfloat16)
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)
+    cache = B.PageCache(K, K.clone(), i32(3, 4), i32(3), i32(6))
+
+    class Room:
+        def get(self, n):
+            return 0, n
+
+    for S, want in ((1 << 40, 0x7fffffff), ((1 << 32) + 5, 0x7fffffff), (100, 100)):
+        a, *_ = B._paged_attention(cache, i32(1), i32(2), torch.zeros((4, 1, 64), dtype=torch.bfloat16), None, None, S, 0, 0, 0.0, Room())
+        assert a.S == want
