@@ -756,7 +756,7 @@ __device__ __forceinline__ ColumnRun columns_of(const PagedArgs& x, int tile, in
   return r;
 }
 
-// Waits for the wavefront's loads and LDS operations.  (A fence would wait for stores too.)
+// Waits for the wavefront's loads, staging ones too, and LDS operations.
 __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
@@ -767,9 +767,8 @@ __device__ __forceinline__ void wait_loads() {
 // 770 us = 1.05 PFLOP/s, where a large library product reaches 1.2; 2000 rows behind 64K tokens, 32:4 heads, eight spans of 512, 215 us =
 // 0.66 PFLOP/s (tiles of 8 steps, whose beginnings and ends are a quarter of them); one token behind a million 49 us = 5.2 TB/s, 24 caches
 // of up to 120000 tokens 93 us = 5.6 TB/s, where a pure read reaches 6.4.
-// NW wavefronts of 32 * CB columns, two stages of STEP tokens.
 //   4 wavefronts: the matrix cores are what bounds these
-//   1 wavefront: few columns, so that memory does; five workgroups (D = 128) of a compute unit have 16 KB each on the way
+//   1 wavefront: few columns, so that memory does; four workgroups (D = 128) of a compute unit have 16 KB each on the way
 //                (three and four stages leave room for fewer: 24 caches of up to 120000 tokens 119 -> 122, 153 us)
 // Workgroups of the window come first, then, of the spans' pieces,
 //   4 wavefronts: the buckets' tiles
