@@ -40,6 +40,7 @@ struct PagedArgs {
 struct TilePlan {
   int tiles;             // window tiles of a kv head
   int64_t window_units;  // tiles * pieces of a window * Hkv
+  int64_t units;         // ... and the spans' pieces: workgroups that have something to do
   int spans, buckets;    // spans of the longest sequence; B * Hkv * spans
   int32_t *counts, *first_tile;  // [buckets]
   int most_tiles;  // of the buckets; a multiple of 8
@@ -784,6 +785,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
   __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS];
   const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t unit = workgroup();
+  if (unit >= plan.units) return;  // (grid_of rounds up)
   const bool window = unit < plan.window_units;
   int seq, head, part;         // sequence, kv head, piece
   int begin, end;              // tokens [begin, end) of the tile
@@ -877,7 +879,6 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
     part = (int)(u % x.p.routed);
     const int64_t item = u / x.p.routed;
     const int slot = (int)(item % x.a.topk), rh = (int)(item / x.a.topk);
-    if (rh >= x.a.Hq * x.b.rows) return;
     const int h = rh / x.b.rows, row = rh - h * x.b.rows;
     const int j = x.idx[h * x.a.ish + row * x.a.ist + slot];
     const Entry at = entry_with_row(x, row);
@@ -1420,7 +1421,7 @@ struct Form {
   bool whole;      // row by row, a row a workgroup
   int cols_log2;   // columns of a tile
   TilePlan plan;   // (pointers unset)
-  int64_t units, most_tiles;  // workgroups of the tile kernel; tiles of the buckets
+  int64_t most_tiles;  // of the buckets
   size_t o_bytes, lse_bytes, plan_bytes;
 };
 
@@ -1476,23 +1477,23 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   const bool direct = f.tiles && p.count == 1;
   f.o_bytes = direct ? 0 : align_up((size_t)rh * p.count * c.D * (c.dtype == SL_BF16 ? sizeof(_Float16) : sizeof(float)), 256);
   f.lse_bytes = align_up((size_t)rh * p.count * sizeof(float), 256);
-  f.units = f.plan.window_units;
+  f.plan.units = f.plan.window_units;
   if (f.buckets) {
     f.plan.spans = (int)spans;
     f.plan.buckets = (int)buckets;
     // (a share of eight may be a tile short of its length)
     f.most_tiles = div_up(items / cols + (buckets < items ? buckets : items), 8) * 8;
-    f.units += f.most_tiles * p.routed;
+    f.plan.units += f.most_tiles * p.routed;
     f.plan_bytes = align_up(sizeof(int32_t) * (align_up(2 * (size_t)buckets, 64) + 4 * (size_t)f.most_tiles + (size_t)items + (size_t)f.most_tiles * cols), 256);
   } else {
-    f.units += items * p.routed;
+    f.plan.units += items * p.routed;
   }
   return f;
 }
 
 // The stages fill up to 128 KB of dynamic LDS beside the static arrays: more than a kernel has without asking.
 template <typename T, int D, int NW, int CB, int STEP, bool ANY, bool PAST>
-bool launch_tiles_as(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
+bool launch_tiles_as(const PagedArgs& x, const TilePlan& plan, hipStream_t st) {
   constexpr int kBytes = 2 * 2 * STEP * D * (int)sizeof(T);
   static std::mutex mu;
   static bool asked[64];
@@ -1505,7 +1506,7 @@ bool launch_tiles_as(const PagedArgs& x, const Form& f, const TilePlan& plan, hi
                                        hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) == hipSuccess;
     if (!asked[dev]) return false;
   }
-  tile_kernel<T, D, NW, CB, STEP, ANY, PAST><<<grid_of(f.units), 64 * NW, kBytes, st>>>(x, plan);
+  tile_kernel<T, D, NW, CB, STEP, ANY, PAST><<<grid_of(plan.units), 64 * NW, kBytes, st>>>(x, plan);
   return true;
 }
 template <typename T, int D, int NW, int CB, int STEP>
@@ -1513,8 +1514,8 @@ bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipSt
   const bool any = x.c.ps % 16 != 0;
   if constexpr (NW > 1)
     if (f.o_bytes >= kStreamedRecords)
-      return any ? launch_tiles_as<T, D, NW, CB, STEP, true, true>(x, f, plan, st) : launch_tiles_as<T, D, NW, CB, STEP, false, true>(x, f, plan, st);
-  return any ? launch_tiles_as<T, D, NW, CB, STEP, true, false>(x, f, plan, st) : launch_tiles_as<T, D, NW, CB, STEP, false, false>(x, f, plan, st);
+      return any ? launch_tiles_as<T, D, NW, CB, STEP, true, true>(x, plan, st) : launch_tiles_as<T, D, NW, CB, STEP, false, true>(x, plan, st);
+  return any ? launch_tiles_as<T, D, NW, CB, STEP, true, false>(x, plan, st) : launch_tiles_as<T, D, NW, CB, STEP, false, false>(x, plan, st);
 }
 
 template <typename T, int D>

@@ -355,6 +355,61 @@ def test_more_workgroups_than_a_grid_dimension_takes():
         assert float((O[:, r:r + 300].float() - o.float()).abs().max()) <= 2.0 ** -7 * 5     # (two roundings each of outputs below 5)
 
 
+def test_more_tiles_of_buckets_than_a_grid_dimension_takes():
+    """3200 rows of 64 heads, each with sixteen of 262144 spans of 4 tokens, in buckets: a launch goes on in y beyond 2^20 workgroups, and
+    what it is rounded up by has nothing to do.  Against calls of 400 rows, which take the spans one by one."""
+    g = torch.Generator(device=DEV).manual_seed(29)
+    L, S, ps, n, topk, Hq, Hkv = 1 << 20, 4, 64, 3200, 16, 64, 4
+    items, buckets = Hq * n * topk, Hkv * (L // S)
+    tiles = items // 256 + min(items, buckets)       # of the buckets
+    assert items >= 3 * buckets and tiles > 1 << 20 and tiles + (n * Hq // Hkv // 256 + 1) * Hkv < 2 << 20   # (or this tests something else)
+    K, V = (torch.randn((1, L // ps, Hkv, ps, 64), generator=g, device=DEV).to(BF16) for _ in range(2))
+    tables = torch.randperm(L // ps, generator=g, device=DEV).to(torch.int32).view(1, -1)
+    cache = B.PageCache(K, V, tables, i32([L]), torch.ones(L // ps, dtype=torch.int32, device=DEV))
+    Q = torch.randn((Hq, n, 64), generator=g, device=DEV).to(BF16)
+    idx = torch.randint(0, (L - n) // S // topk, (Hq, n, topk), generator=g, device=DEV, dtype=torch.int32) * topk
+    idx += torch.arange(topk, dtype=torch.int32, device=DEV)
+    O, LSE = B.sl_paged_span_attention(cache, i32([0]), i32([0, n]), Q, idx, S)
+    for r in range(0, n, 400):
+        assert Hq * 400 * topk < 3 * buckets
+        cache.lens.fill_(L - n + r + 400)
+        o, lse = B.sl_paged_span_attention(cache, i32([0]), i32([0, 400]), Q[:, r:r + 400].contiguous(), idx[:, r:r + 400].contiguous(), S)
+        assert float((LSE[:, r:r + 400] - lse).abs().max()) <= 1e-4
+        assert float((O[:, r:r + 400].float() - o.float()).abs().max()) <= 2.0 ** -7 * 5     # (two roundings each of outputs below 5)
+
+
+@pytest.mark.parametrize("dtype,B_,Hkv,n", [(BF16, 32768, 32, 1), (BF16, 29200, 32, 33), (F32, 26300, 32, 33)])
+def test_more_tiles_of_windows_than_a_grid_dimension_takes(dtype, B_, Hkv, n):
+    """Dense calls of many short sequences (they share a page: attention does not look at refs) without any spans, narrow and wide tiles,
+    against calls of an eighth of the sequences."""
+    g = torch.Generator(device=DEV).manual_seed(30)
+    narrow = n * B_ <= 32 * B_
+    cols = 32 if narrow else 128 if dtype == F32 else 256
+    assert 1 << 20 < (B_ * n // cols + B_) * Hkv < 2 << 20 and B_ * n * Hkv < 1 << 26
+    K, V = (torch.randn((1, 1, Hkv, 40, 64), generator=g, device=DEV).to(dtype) for _ in range(2))
+    lens = torch.randint(n, 41, (B_,), generator=g, device=DEV, dtype=torch.int32)
+    cache = B.PageCache(K, V, torch.zeros((B_, 1), dtype=torch.int32, device=DEV), lens, i32([B_]))
+    seqs, cu = torch.arange(B_, dtype=torch.int32, device=DEV), torch.arange(B_ + 1, dtype=torch.int32, device=DEV) * n
+    Q = torch.randn((Hkv, B_ * n, 64), generator=g, device=DEV, dtype=dtype)
+    O, LSE = B.sl_paged_span_attention(cache, seqs, cu, Q, None, 1000)
+    tol = 1e-4 if dtype == F32 else 2.0 ** -7 * 5     # (two roundings each of outputs below 5)
+    m = -(-B_ // 8)
+    for b in range(0, B_, m):
+        part = seqs[b:b + m]
+        rows = slice(b * n, (b + part.numel()) * n)
+        o, lse = B.sl_paged_span_attention(cache, part, cu[:part.numel() + 1], Q[:, rows], None, 1000)
+        assert float((LSE[:, rows] - lse).abs().max()) <= 1e-4
+        assert float((O[:, rows].float() - o.float()).abs().max()) <= tol
+    # a few rows by hand
+    for e in (0, B_ // 2, B_ - 1):
+        for r in (0, n - 1):
+            pos = int(lens[e]) - n + r
+            z = torch.einsum("hd,htd->ht", Q[:, e * n + r].double().cpu(), K[0, 0, :, :pos + 1].double().cpu()) / 8
+            want = torch.einsum("ht,htd->hd", torch.softmax(z, 1), V[0, 0, :, :pos + 1].double().cpu())
+            assert float((LSE[:, e * n + r].double().cpu() - torch.logsumexp(z, 1)).abs().max()) <= 1e-4
+            assert float((O[:, e * n + r].double().cpu() - want).abs().max()) <= tol
+
+
 @pytest.mark.parametrize("dtype,n,D,ps", [(BF16, 3400, 128, 64), (BF16, 6700, 64, 40), (F32, 1800, 128, 16)])
 def test_records_beyond_the_caches(dtype, n, D, ps):
     """Calls with more than 200 MB of records, joint and gated, against calls of 400 rows."""
