@@ -1170,8 +1170,10 @@ __global__ __launch_bounds__(256) void items_kernel(const PagedArgs x, const Til
   const int rank = plan.ranks[i];
   if (rank < 0) return;
   const int e = entry_of_row(x.b.cu, x.b.B, row), j = x.idx[h * x.a.ish + row * x.a.ist + k];
+  // (Where cu_rows decreases, count_kernel may have passed this row over, or given it to another entry: its rank is then anything, and so is j.)
+  if ((uint32_t)j >= (uint32_t)plan.spans) return;
   const int64_t at = ((int64_t)plan.first_tile[(e * x.c.Hkv + h / x.a.G) * plan.spans + j] << cols_log2) + rank;
-  if (at < (int64_t)plan.most_tiles << cols_log2) plan.items[at] = rh * 32 + k;
+  if (at >= 0 && at < (int64_t)plan.most_tiles << cols_log2) plan.items[at] = rh * 32 + k;
 }
 
 // ------------------------------------------------------------------ merge

@@ -323,6 +323,38 @@ def test_rows_out_of_order_stay_inside_the_arrays(cu, rows, topk, dtype):
     assert torch.equal(cache.tables, tables) and torch.equal(cache.lens, lens) and torch.equal(cache.refs, refs)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("fill", [0, 1, 0x7F, 0x80])
+@pytest.mark.parametrize("cu", [[0, 0, 300, 10, 400], [0, 400, 0, 400, 400], [20, 390, 7, 1 << 30, 400]])
+def test_rows_out_of_order_whatever_the_workspace_held(cu, fill, dtype):
+    """Rows that no entry counted have places in the item list that nobody wrote, and spans that nobody checked."""
+    g = torch.Generator().manual_seed(31)
+    rows, topk, S = 400, 8, 320
+    cache = make_cache(g, [6400, 300], 64, 1, 64, dtype)
+    n = len(cu) - 1
+    seqs, cu = i32([0] * (n - 1) + [1]), i32(cu)
+    Q = torch.randn((16, rows, 64), generator=g).to(dtype).to(DEV)
+    idx = choose(g, 16, rows, topk, 18).cpu()
+    wild = torch.tensor([1 << 30, (1 << 31) - 1, -(1 << 31), -77, 20, 21], dtype=torch.int32)
+    idx = torch.where(torch.rand(idx.shape, generator=g) < 0.3, wild[torch.randint(0, len(wild), idx.shape, generator=g)], idx).to(DEV)
+    assert 16 * rows * topk >= 6 * n * 20 and 16 * rows * topk * S >= 1 << 19      # (buckets)
+    a, b = B.SlPagedAttention(16, S, topk, 0.0, 0, 0, 0, 0), cache.batch(seqs, cu, rows, 6400)
+    need = B.load().sl_paged_attention_workspace_bytes(cache.record, b, a)
+    ws = torch.full((need + 8192,), fill, dtype=torch.uint8, device=DEV)
+    O = torch.full((Q.numel() + 2048,), 7.0, dtype=dtype, device=DEV)
+    LSE = torch.full((16 * rows + 2048,), 7.0, device=DEV)
+    edge = 2048 // O.element_size()
+    for _ in range(2):
+        ws.fill_(fill)
+        st = B.load().sl_paged_span_attention(cache.record, b, a, Q.data_ptr(), idx.data_ptr(), O.data_ptr() + 2048, LSE.data_ptr() + 4096,
+                                              ws.data_ptr() + 4096, need, cache.stream())
+        assert st == 0
+        torch.cuda.synchronize()
+        assert bool((ws[:4096] == fill).all()) and bool((ws[4096 + need:] == fill).all())
+        assert bool((O[:edge] == 7).all()) and bool((O[edge + Q.numel():] == 7).all())
+        assert bool((LSE[:1024] == 7).all()) and bool((LSE[1024 + 16 * rows:] == 7).all())
+
+
 @pytest.mark.parametrize("dtype,n", [(BF16, 2), (BF16, 150), (F32, 2), (F32, 60), (F32, 150)])
 def test_a_row_that_lists_a_span_twice_spoils_no_other(dtype, n):
     g = torch.Generator().manual_seed(26)
