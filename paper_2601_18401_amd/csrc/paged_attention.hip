@@ -1119,33 +1119,39 @@ __global__ __launch_bounds__(1024) void count_kernel(const PagedArgs x, const Ti
 
 // Tiles of each bucket in the buckets' order; one workgroup.  Tiles of one bucket read the same rows: workgroups u = x (mod 8) run on
 // XCD x, which has an L2 of its own, and are given the x-th eighth of the list, in its order.
-// (Where cu_rows decreases, rows may be counted more than once: what the list has no room for is left out.)
+// (Where cu_rows decreases, rows may be counted once for each of 65535 entries: sums stop at most_tiles, which is below 2^30, and what the
+// list has no room for is left out.)
 __global__ __launch_bounds__(1024) void tiles_kernel(const TilePlan plan, int cols_log2) {
   __shared__ int s_wave[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  auto tiles_of = [&](int i) { return i < plan.buckets ? (plan.counts[i] + (1 << cols_log2) - 1) >> cols_log2 : 0; };
+  auto tiles_of = [&](int i) {
+    const int n = i < plan.buckets ? (plan.counts[i] + (1 << cols_log2) - 1) >> cols_log2 : 0;
+    return min(max(n, 0), plan.most_tiles);
+  };
+  auto sum = [&](int a, int b) { return min(a + b, plan.most_tiles); };
   int total = 0;
 #pragma unroll 1
   for (int base = 0; base < plan.buckets; base += 1024) {
-    const int i = base + threadIdx.x, n = tiles_of(i);
-    int v = n;
+    const int i = base + threadIdx.x;
+    int v = tiles_of(i);
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
       const int y = __shfl_up(v, off, 64);
-      if (lane >= off) v += y;
+      if (lane >= off) v = sum(v, y);
     }
+    const int before = __shfl_up(v, 1, 64);
     __syncthreads();
     if (lane == 63) s_wave[wave] = v;
     __syncthreads();
-    int at = total + v - n;
+    int at = total;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      if (k < wave) at += s_wave[k];
-      total += s_wave[k];
+      if (k < wave) at = sum(at, s_wave[k]);
+      total = sum(total, s_wave[k]);
     }
+    if (lane > 0) at = sum(at, before);
     if (i < plan.buckets) plan.first_tile[i] = at;
   }
-  total = min(total, plan.most_tiles);
   const int share = (total + 7) / 8;
 #pragma unroll 1
   for (int base = 0; base < plan.buckets; base += 1024) {
