@@ -332,7 +332,8 @@ sl_status sl_anchor_attention_decode_batched(const sl_params* p, const sl_anchor
  *     attention, rows appended there are dropped.
  *   - refs[p] is the number of table entries that name page p; a page is free when refs[p] <= 0.
  *     A page named by several sequences holds page_size tokens of each of them (sl_pages_fork copies
- *     the last, partly filled page), so that appending never writes into another sequence's tokens.
+ *     the last, partly filled page).  Appending never writes into another sequence's tokens: rows whose
+ *     page has refs above 1 are dropped.
  *   - Entries of tables[s] from ceil(lens[s] / page_size) on are -1.
  * An empty cache: tables all -1, lens and refs all 0.
  * Calls on one cache must be ordered, on one stream or with events.  None of them allocates,

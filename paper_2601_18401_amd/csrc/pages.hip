@@ -401,7 +401,9 @@ __global__ __launch_bounds__(256) void append_kernel(const PageCache c, const Pa
       const int e = entry_of_row(b.cu, b.B, row), s = b.seqs[e], len = length_of(c, s), t = len - (b.cu[e + 1] - row);
       if (t >= 0 && t < b.L && t < len) {
         const int k = (uint32_t)t / c.by_ps, page = c.tables[(int64_t)s * c.max_pages + k];
-        if ((uint32_t)page < (uint32_t)c.n_pages) to = (b.layer * c.layer + page * c.page + head * c.head + (t - k * c.ps) * c.tok) * es;
+        // (a page of several sequences holds tokens of each, whatever the batch says of this one)
+        if ((uint32_t)page < (uint32_t)c.n_pages && c.refs[page] <= 1)
+          to = (b.layer * c.layer + page * c.page + head * c.head + (t - k * c.ps) * c.tok) * es;
       }
     }
     s_to[threadIdx.x] = to;

@@ -523,6 +523,32 @@ def test_appending_past_the_sequence_writes_nothing():
     assert int((cache.K == 1).all(-1).sum()) == 20
 
 
+@pytest.mark.parametrize("dtype,ps", [(BF16, 16), (F32, 7)])
+def test_rows_that_no_page_was_found_for_leave_other_sequences_tokens(dtype, ps):
+    """A fork of a sequence that ends on a page's end shares its last page.  Without a free page it is not extended, and rows appended to it
+    all the same would lie at its last tokens, which are the source's too."""
+    g = torch.Generator().manual_seed(32)
+    cache = B.PageCache.empty(3, ps, 2, 64, 4, 4, layers=2, dtype=dtype)
+    seqs, cu = i32([0]), i32([0, 3 * ps])
+    K, V = (torch.randn((2, 3 * ps, 64), generator=g).to(dtype).to(DEV) for _ in range(2))
+    assert B.sl_pages_extend(cache, seqs, cu).tolist() == [1]
+    for layer in range(2):
+        B.sl_paged_append(cache, seqs, cu, K, V, layer)
+    assert B.sl_pages_fork(cache, i32([0, 0]), i32([2, 3])).tolist() == [1, 1]
+    before = cache.K.clone(), cache.V.clone()
+    new = torch.ones((2, 2 * ps, 64), dtype=dtype, device=DEV)
+    assert B.sl_pages_extend(cache, i32([2, 3]), i32([0, ps, 2 * ps])).tolist() == [0, 0]
+    B.sl_paged_append(cache, i32([2, 3]), i32([0, ps, 2 * ps]), new, new, 1)
+    torch.cuda.synchronize()
+    assert torch.equal(cache.K, before[0]) and torch.equal(cache.V, before[1])
+    # a source that goes on writes into a page of its own, and into its last one again once the forks are gone
+    B.sl_pages_free(cache, i32([2, 3]))
+    B.sl_paged_append(cache, seqs, i32([0, ps]), new[:, :ps], new[:, :ps], 1)
+    torch.cuda.synchronize()
+    last = int(cache.tables[0, 2])
+    assert bool((cache.K[1, last] == 1).all()) and int((cache.K == 1).all(-1).sum()) == 2 * ps and torch.equal(cache.K[0], before[0][0])
+
+
 @pytest.mark.parametrize("seed,n_pages,ps,n_seqs,dtype,layers", [(1, 40, 4, 12, BF16, 1), (2, 300, 3, 30, F32, 2), (3, 70, 1, 9, BF16, 1),
                                                                  (4, 17000, 2, 40, BF16, 1), (5, 1, 8, 3, BF16, 1)])
 def test_page_turns(seed, n_pages, ps, n_seqs, dtype, layers):
