@@ -348,8 +348,8 @@ typedef struct sl_page_cache {
   int32_t* tables;  /* [n_seqs][max_pages]                                        */
   int32_t* lens;    /* [n_seqs] tokens held                                       */
   int32_t* refs;    /* [n_pages]                                                  */
-  int64_t layer_stride, page_stride;  /* element strides of K and V; 0 = packed; not below D */
-  int64_t kv_stride_h, kv_stride_t;   /* (0 = packed; kv_stride_t at most 2^20)              */
+  int64_t layer_stride, page_stride;  /* element strides of K and V; 0 = packed; not below D.  A packed page is the larger of */
+  int64_t kv_stride_h, kv_stride_t;   /* Hkv heads and page_size tokens; kv_stride_t is at most 2^20                          */
   int32_t layers, n_pages, n_seqs, max_pages;  /* >= 1; max_pages * page_size, n_pages <= 2^30 */
   int32_t page_size, Hkv, D, dtype;            /* D: 64 or 128; Hkv at most 1024, layers at most 4096,
                                                   layers * 2 * Hkv + max_pages / 1024 at most 65000 */

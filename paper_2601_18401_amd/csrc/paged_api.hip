@@ -1,4 +1,5 @@
 // C-ABI layer of the paged cache: argument validation on the host, then dispatch to the launchers.
+#include <algorithm>
 #include <cmath>
 
 #include "paged.h"
@@ -33,7 +34,8 @@ sl_status make_cache(const sl_page_cache* p, PageCache* c) {
     return SL_ERR_UNSUPPORTED;
   c->tok = p->kv_stride_t ? p->kv_stride_t : p->D;
   c->head = p->kv_stride_h ? p->kv_stride_h : p->page_size * c->tok;
-  c->page = p->page_stride ? p->page_stride : p->Hkv * c->head;
+  // (heads first or tokens first: whichever is the outer one of the two has the larger extent)
+  c->page = p->page_stride ? p->page_stride : std::max(p->Hkv * c->head, p->page_size * c->tok);
   c->layer = p->layer_stride ? p->layer_stride : p->n_pages * c->page;
   if (c->head > kMaxExtent / p->Hkv || c->page > kMaxExtent / p->n_pages || c->layer > kMaxExtent / p->layers) return SL_ERR_UNSUPPORTED;
   const int64_t epl = p->dtype == SL_BF16 ? 8 : 4;

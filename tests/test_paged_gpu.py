@@ -709,6 +709,24 @@ def test_a_captured_step_is_replayed():
             assert torch.equal(got, O2)
 
 
+def test_the_packed_strides_of_pages_whose_tokens_come_first():
+    """[n_pages][page_size][Hkv][D]: a page stride of 0 stands for page_size * kv_stride_t there."""
+    g = torch.Generator().manual_seed(33)
+    ps, Hkv, D = 16, 3, 64
+    K, V = (torch.zeros((2, 4, ps, Hkv, D), dtype=BF16, device=DEV) for _ in range(2))
+    whole = B.PageCache(K.transpose(2, 3), V.transpose(2, 3), i32([[2, 0, 3]]), i32([40]), i32([1, 0, 1, 1]))
+    assert (whole.record.page_stride, whole.record.layer_stride) == (ps * Hkv * D, 4 * ps * Hkv * D)
+    whole.record.page_stride = whole.record.layer_stride = 0
+    new = torch.randn((Hkv, 40, D), generator=g).to(BF16).to(DEV)
+    B.sl_paged_append(whole, i32([0]), i32([0, 40]), new, new, layer=1)
+    for t in range(40):
+        assert torch.equal(K[1, [2, 0, 3][t // ps], t % ps], new[:, t])
+    assert int((K != 0).any(-1).sum()) == 40 * Hkv and torch.equal(K, V)
+    Q = torch.randn((6, 40, D), generator=g).to(BF16).to(DEV)
+    O, LSE = B.sl_paged_span_attention(whole, i32([0]), i32([0, 40]), Q, None, 100, layer=1)
+    check(whole, [0], [0, 40], Q, None, None, 100, O, LSE, layer=1)
+
+
 def test_two_streams_at_once():
     """Calls without a workspace of the caller's do not share scratch."""
     g = torch.Generator().manual_seed(13)
