@@ -36,8 +36,9 @@ sl_status make_cache(const sl_page_cache* p, PageCache* c) {
   c->head = p->kv_stride_h ? p->kv_stride_h : p->page_size * c->tok;
   // (heads first or tokens first: whichever is the outer one of the two has the larger extent)
   c->page = p->page_stride ? p->page_stride : std::max(p->Hkv * c->head, p->page_size * c->tok);
+  if (c->head > kMaxExtent / p->Hkv || c->page > kMaxExtent / p->n_pages) return SL_ERR_UNSUPPORTED;
   c->layer = p->layer_stride ? p->layer_stride : p->n_pages * c->page;
-  if (c->head > kMaxExtent / p->Hkv || c->page > kMaxExtent / p->n_pages || c->layer > kMaxExtent / p->layers) return SL_ERR_UNSUPPORTED;
+  if (c->layer > kMaxExtent / p->layers) return SL_ERR_UNSUPPORTED;
   const int64_t epl = p->dtype == SL_BF16 ? 8 : 4;
   if (c->tok % epl || c->head % epl || c->page % epl || c->layer % epl) return SL_ERR_INVALID_ARG;
   if (c->tok < p->D || (p->Hkv > 1 && c->head < p->D) || (p->n_pages > 1 && c->page < p->D) || (p->layers > 1 && c->layer < p->D))

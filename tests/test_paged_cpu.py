@@ -193,3 +193,25 @@ def test_a_span_longer_than_any_sequence_is_not_cut_off():
     for S, want in ((1 << 40, 0x7fffffff), ((1 << 32) + 5, 0x7fffffff), (100, 100)):
         a, *_ = B._paged_attention(cache, i32(1), i32(2), torch.zeros((4, 1, 64), dtype=torch.bfloat16), None, None, S, 0, 0, 0.0, Room())
         assert a.S == want
+
+
+def test_sizes_at_the_limits_under_address_and_undefined_sanitizers(tmp_path):
+    """Validation and size arithmetic of records at and beyond every limit, in a build of the host side with ASan + UBSan."""
+    import glob
+    import os
+    import shutil
+    import subprocess
+    from paper_2601_18401_amd import build as _build
+    clang = "/opt/rocm/lib/llvm/bin/clang"
+    if not os.path.exists(clang) or not shutil.which("hipcc"):
+        pytest.skip("no ROCm clang")
+    lib = _build.build(sanitize=True)
+    exe = str(tmp_path / "size_paged_from_c")
+    subprocess.run([clang, "-std=c99", "-Wall", "-Wextra", "-Werror", "-g", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=undefined", "-shared-libsan", "-I", os.path.join(_build.ROOT, "include"),
+                    os.path.join(_build.ROOT, "tests", "cabi", "size_paged_from_c.c"), "-o", exe, "-ldl"], check=True)
+    rt = os.path.dirname(glob.glob("/opt/rocm*/lib/llvm/lib/clang/*/lib/*/libclang_rt.asan*.so")[0])
+    env = dict(os.environ, LD_LIBRARY_PATH=rt, ASAN_OPTIONS="detect_leaks=0")
+    run = subprocess.run([exe, lib], capture_output=True, text=True, env=env, timeout=300)
+    assert run.returncode == 0 and "wrong=0" in run.stdout, (run.stdout, run.stderr[-3000:])
+    assert "runtime error" not in run.stderr and "AddressSanitizer" not in run.stderr, run.stderr[-3000:]
