@@ -371,13 +371,19 @@ typedef struct sl_paged_batch {
 } sl_paged_batch;
 
 /* Gives the sequences of a batch pages for their new tokens and adds those to lens: call it before
- * the step's sl_paged_append.  Free pages are given out lowest number first, to the entries in their
+ * the step's sl_paged_append, and sl_pages_served between the two.  Free pages are given out lowest number first, to the entries in their
  * order; an entry that the free pages do not suffice for is left as it was, and so is every later one
  * that needs a page.  Not served either: sequences out of range, a sequence's second entry, a
  * length beyond the table.  ok [B]: 1 = served, 0 = left as it was.  (rows, L and layer are not
  * read; B <= SL_MAX_PAGE_OPS.) */
 #define SL_MAX_PAGE_OPS 4096
 sl_status sl_pages_extend(const sl_page_cache* c, const sl_paged_batch* b, int32_t* ok, void* hip_stream);
+
+/* The list that the rest of a step takes: served[i] = seqs[i] where ok[i] is not 0, else -1, i < n (served may be seqs).  An entry that
+ * was not served must not keep its number: its rows would be taken for its sequence's present last tokens, and sl_paged_append
+ * would write over those.  Entries of -1 are passed over: nothing is written into their pages or keys, their rows' attention is
+ * O = 0, LSE = -inf.  n <= 65535. */
+sl_status sl_pages_served(const int32_t* seqs, const int32_t* ok, int32_t n, int32_t* served, void* hip_stream);
 
 /* Makes dst[i] a copy of src[i], i < n: its table names the full pages of src, and a partly filled
  * last page is copied (all layers, the filled rows) into a free page, lowest number first in the list's
@@ -400,7 +406,7 @@ size_t sl_pages_compact_workspace_bytes(const sl_page_cache* c);
 sl_status sl_pages_compact(const sl_page_cache* c, int32_t* map, void* ws, size_t ws_bytes, void* hip_stream);
 
 /* Writes the batch's new tokens into their pages (a sequence's tokens by one entry: of entries that
- * list it twice, which one's rows stay is unspecified).  K, V: [Hkv][rows][D] with element strides
+ * list it twice, which one's rows stay is unspecified).  Entries that sl_pages_extend did not serve are to be -1 in seqs.  K, V: [Hkv][rows][D] with element strides
  * (stride_h, stride_t, 1), 0 = packed. */
 sl_status sl_paged_append(const sl_page_cache* c, const sl_paged_batch* b, const void* K, const void* V,
                           int64_t stride_h, int64_t stride_t, void* hip_stream);

@@ -30,7 +30,7 @@ EXPORTS = ("sl_workspace_bytes", "sl_span_keys", "sl_span_search_prefill", "sl_s
            "sl_span_attention_decode_batched", "sl_span_attention_combined_decode_batched",
            "sl_anchor_batched_workspace_bytes", "sl_anchor_search_decode_batched",
            "sl_anchor_attention_decode_batched", "sl_set_profile_events", "sl_status_string", "sl_version",
-           "sl_pages_extend", "sl_pages_fork", "sl_pages_free", "sl_pages_compact_workspace_bytes", "sl_pages_compact",
+           "sl_pages_extend", "sl_pages_served", "sl_pages_fork", "sl_pages_free", "sl_pages_compact_workspace_bytes", "sl_pages_compact",
            "sl_paged_append", "sl_paged_span_keys", "sl_paged_attention_workspace_bytes", "sl_paged_span_attention",
            "sl_paged_span_attention_combined")
 
@@ -149,7 +149,8 @@ def load():
     lib.sl_anchor_attention_decode_batched.argtypes = [pp, gp, vp, ctypes.c_int32, vp, ctypes.c_size_t, vp]
     cp, bp, ap, i32, i64 = (ctypes.POINTER(SlPageCache), ctypes.POINTER(SlPagedBatch), ctypes.POINTER(SlPagedAttention),
                             ctypes.c_int32, ctypes.c_int64)
-    for name, argtypes in (("sl_pages_extend", [cp, bp, i32p, vp]), ("sl_pages_fork", [cp, i32p, i32p, i32, i32p, vp]),
+    for name, argtypes in (("sl_pages_extend", [cp, bp, i32p, vp]), ("sl_pages_served", [i32p, i32p, i32, i32p, vp]),
+                           ("sl_pages_fork", [cp, i32p, i32p, i32, i32p, vp]),
                            ("sl_pages_free", [cp, i32p, i32, vp]), ("sl_pages_compact", [cp, i32p, vp, ctypes.c_size_t, vp]),
                            ("sl_paged_append", [cp, bp, vp, vp, i64, i64, vp]),
                            ("sl_paged_span_keys", [cp, bp, i32, i32, vp, vp]),
@@ -658,7 +659,8 @@ class PageCache:
 
 
 def sl_pages_extend(cache: PageCache, seqs, cu_rows, ok=None):
-    """Pages for the new tokens of each sequence, which lens counts from here on; ok[b]: 1 = served, 0 = left as it was."""
+    """Pages for the new tokens of each sequence, which lens counts from here on; ok[b]: 1 = served, 0 = left as it was.  The rest of the
+    step takes sl_pages_served(cache, seqs, ok) in place of seqs."""
     b = cache.batch(seqs, cu_rows)
     if ok is None:
         ok = torch.empty(b.B, dtype=torch.int32, device=cache.device)
@@ -666,6 +668,18 @@ def sl_pages_extend(cache: PageCache, seqs, cu_rows, ok=None):
         _int32(ok, "ok", cache.index, b.B)
     _check(load().sl_pages_extend(cache.record, b, ok.data_ptr(), cache.stream()), "sl_pages_extend")
     return ok
+
+
+def sl_pages_served(cache: PageCache, seqs, ok, out=None):
+    """seqs with -1 for the entries that were not served: what the step's appends, keys and attention pass over."""
+    n = _int32(seqs, "seqs", cache.index)
+    _int32(ok, "ok", cache.index, n)
+    if out is None:
+        out = torch.empty(n, dtype=torch.int32, device=cache.device)
+    else:
+        _int32(out, "out", cache.index, n)
+    _check(load().sl_pages_served(seqs.data_ptr(), ok.data_ptr(), n, out.data_ptr(), cache.stream()), "sl_pages_served")
+    return out
 
 
 def sl_pages_fork(cache: PageCache, src, dst, ok=None):

@@ -434,6 +434,6 @@ const char* sl_status_string(sl_status status) {
   return "unknown sl_status";
 }
 
-int sl_version(void) { return 500; }  // 0.5.0: paged cache (sl_pages_*, sl_paged_*)
+int sl_version(void) { return 501; }  // 0.5.0: paged cache (sl_pages_*, sl_paged_*); 0.5.1: sl_pages_served
 
 }  // extern "C"

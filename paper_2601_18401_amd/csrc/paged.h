@@ -39,6 +39,7 @@ struct PagedAttention {
 };
 
 sl_status pages_extend(const PageCache& c, const PagedBatch& b, int32_t* ok, hipStream_t st);
+sl_status pages_served(const int32_t* seqs, const int32_t* ok, int n, int32_t* served, hipStream_t st);
 sl_status pages_fork(const PageCache& c, const int32_t* src, const int32_t* dst, int n, int32_t* ok, hipStream_t st);
 sl_status pages_free(const PageCache& c, const int32_t* seqs, int n, hipStream_t st);
 size_t pages_compact_ws_bytes(const PageCache& c);

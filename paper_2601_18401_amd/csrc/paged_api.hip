@@ -134,6 +134,13 @@ sl_status sl_pages_extend(const sl_page_cache* pc, const sl_paged_batch* pb, int
   return sl::pages_extend(c, b, ok, static_cast<hipStream_t>(hip_stream));
 }
 
+sl_status sl_pages_served(const int32_t* seqs, const int32_t* ok, int32_t n, int32_t* served, void* hip_stream) {
+  if (n < 0 || (n > 0 && (!seqs || !ok || !served || !sl::aligned4(seqs) || !sl::aligned4(ok) || !sl::aligned4(served))))
+    return SL_ERR_INVALID_ARG;
+  if (n > 65535) return SL_ERR_UNSUPPORTED;
+  return sl::pages_served(seqs, ok, n, served, static_cast<hipStream_t>(hip_stream));
+}
+
 sl_status sl_pages_fork(const sl_page_cache* pc, const int32_t* src, const int32_t* dst, int32_t n, int32_t* ok, void* hip_stream) {
   sl::PageCache c;
   sl_status s = sl::make_cache(pc, &c);

@@ -200,6 +200,11 @@ __global__ __launch_bounds__(kPlanThreads) void plan_pages_kernel(const PageCach
   }
 }
 
+__global__ __launch_bounds__(256) void served_kernel(const int32_t* seqs, const int32_t* ok, int n, int32_t* served) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) served[i] = ok[i] ? seqs[i] : -1;
+}
+
 // Copies rows [0, rows) of one head's part of a page, 16 bytes a lane.
 __device__ __forceinline__ void copy_rows(const char* __restrict__ from, char* __restrict__ to, int64_t row_bytes, int pieces_log2,
                                           int rows, int thread, int threads) {
@@ -470,6 +475,12 @@ sl_status pages_extend(const PageCache& c, const PagedBatch& b, int32_t* ok, hip
   // (an entry's need is at most a table's width)
   if ((int64_t)b.B * c.max_pages < INT_MAX) plan_pages<false, int>(c, nullptr, b.seqs, b.cu, b.B, ok, st);
   else plan_pages<false, int64_t>(c, nullptr, b.seqs, b.cu, b.B, ok, st);
+  return launched();
+}
+
+sl_status pages_served(const int32_t* seqs, const int32_t* ok, int n, int32_t* served, hipStream_t st) {
+  if (n == 0) return SL_OK;
+  served_kernel<<<(n + 255) / 256, 256, 0, st>>>(seqs, ok, n, served);
   return launched();
 }
 

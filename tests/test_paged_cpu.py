@@ -195,6 +195,19 @@ def test_a_span_longer_than_any_sequence_is_not_cut_off():
         assert a.S == want
 
 
+def test_the_served_list_refuses():
+    lib = B.load()
+    assert lib.sl_pages_served(P, P, 0, P, None) == 0 and lib.sl_pages_served(None, None, 0, None, None) == 0
+    for args, status in (((P, P, -1, P), 1), ((None, P, 3, P), 1), ((P, None, 3, P), 1), ((P, P, 3, None), 1), ((P + 2, P, 3, P), 1),
+                         ((P, P + 1, 3, P), 1), ((P, P, 3, P + 3), 1), ((P, P, 65536, P), 2)):
+        assert lib.sl_pages_served(*args, None) == status
+    cache = B.PageCache.empty(6, 16, 2, 64, 3, 4, device="cpu")
+    three, two = torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    for args in ((three, two), (three, three.long()), (three.float(), three), (three, three, two)):
+        with pytest.raises(ValueError):
+            B.sl_pages_served(cache, *args)
+
+
 def test_sizes_at_the_limits_under_address_and_undefined_sanitizers(tmp_path):
     """Validation and size arithmetic of records at and beyond every limit, in a build of the host side with ASan + UBSan."""
     import glob

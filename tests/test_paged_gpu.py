@@ -727,6 +727,80 @@ def test_the_packed_strides_of_pages_whose_tokens_come_first():
     check(whole, [0], [0, 40], Q, None, None, 100, O, LSE, layer=1)
 
 
+def test_a_captured_step_goes_on_where_pages_run_out():
+    """extend, the served list, append, keys and attention in one graph, over a pool that runs out: sequences that no page is found for keep
+    their tokens and keys, and their rows are rows without a token; once others are freed they go on."""
+    g = torch.Generator().manual_seed(34)
+    Hq, Hkv, D, S, ps, n, layers = 4, 2, 64, 8, 4, 3, 2
+    cache = B.PageCache.empty(9, ps, Hkv, D, 4, 12, layers)
+    model = ref.Pages(cache)
+    Ks = torch.zeros((4, Hkv, 12 * ps // S, D), dtype=BF16, device=DEV)
+    want_Ks = Ks.clone()
+    seqs, cu = i32([2, 0, 3]), i32([0, n, 2 * n, 3 * n])
+    K, V, Q = (torch.randn((h, 3 * n, D), generator=g).to(BF16).to(DEV) for h in (Hkv, Hkv, Hq))
+    O, LSE = torch.empty_like(Q), torch.empty((Hq, 3 * n), device=DEV)
+    ok, served = torch.empty(3, dtype=torch.int32, device=DEV), torch.empty(3, dtype=torch.int32, device=DEV)
+    ws = B.Workspace()
+    ws.get(1 << 22)
+
+    def step():
+        B.sl_pages_extend(cache, seqs, cu, ok)
+        B.sl_pages_served(cache, seqs, ok, served)
+        for layer in range(layers):
+            B.sl_paged_append(cache, served, cu, K, V, layer)
+        B.sl_paged_span_keys(cache, served, cu, Ks, S, layer=1)
+        B.sl_paged_span_attention(cache, served, cu, Q, None, 1000, layer=1, ws=ws, out=(O, LSE))
+
+    def follow():
+        torch.cuda.synchronize()
+        got = model.extend([2, 0, 3], [0, n, 2 * n, 3 * n])
+        assert ok.tolist() == got and served.tolist() == [s if k else -1 for s, k in zip([2, 0, 3], got)]
+        for b, (s, k) in enumerate(zip([2, 0, 3], got)):
+            for r in range(n if k else 0):
+                t = model.lens[s] - n + r
+                page = model.tables[s][t // ps]
+                for mine, new in ((model.K, K), (model.V, V)):
+                    mine[:, page, :, t % ps] = new[:, b * n + r].double().cpu()
+                if (t + 1) % S == 0:
+                    want_Ks[s, :, t // S] = K[:, b * n + r]
+        model.agrees(cache)
+        assert torch.equal(Ks, want_Ks)
+        check(cache, served.tolist(), [0, n, 2 * n, 3 * n], Q, None, None, 1000, O, LSE, layer=1)
+        for b, k in enumerate(got):
+            rows = slice(b * n, b * n + n)
+            assert bool((LSE[:, rows] == -math.inf).all()) == (not k) and bool((O[:, rows] == 0).all()) == (not k)
+        return got
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.current_stream().wait_stream(stream)
+    follow()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    seen = []
+    for turn in range(14):
+        for x in (K, V, Q):
+            x.copy_(torch.randn(x.shape, generator=g))
+        graph.replay()
+        seen.append(follow())
+        if turn == 6:
+            B.sl_pages_free(cache, i32([2]))
+            model.free([2])
+        if turn == 9:      # a fork shares its source's pages, and goes on where there are some
+            B.sl_pages_free(cache, i32([3]))
+            model.free([3])
+            assert B.sl_pages_fork(cache, i32([0]), i32([3])).tolist() == model.fork([0], [3])
+        if turn == 11:
+            B.sl_pages_free(cache, i32([0]))
+            model.free([0])
+    assert any(0 in k for k in seen[:7]) and any(all(k) for k in seen[:3]) and any(0 in k and 1 in k for k in seen)
+    seqs_too = seqs.clone()
+    assert B.sl_pages_served(cache, seqs_too, i32([0, 5, -1]), seqs_too) is seqs_too and seqs_too.tolist() == [-1, 0, 3]
+
+
 def test_two_streams_at_once():
     """Calls without a workspace of the caller's do not share scratch."""
     g = torch.Generator().manual_seed(13)
