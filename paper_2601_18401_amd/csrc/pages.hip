@@ -233,12 +233,17 @@ __host__ __device__ inline int element_bytes(const PageCache& c) { return c.dtyp
 // 16-byte pieces of a row: 8, 16 or 32
 __host__ __device__ inline int pieces_log2_of(const PageCache& c) { return (c.D == 128 ? 4 : 3) + (c.dtype == SL_BF16 ? 0 : 1); }
 
-// One (layer, K or V, head) part of a page: unit in [0, layers * 2 * Hkv)
+// One (layer, K or V, head) part of a page: unit in [0, layers * 2 * Hkv).  Pieces of kCopyRows rows count in 32 bits (pages may have 2^30).
+constexpr int kCopyRows = 1 << 24;
 __device__ __forceinline__ void copy_part(const PageCache& c, int from, int to, int unit, int rows, int thread, int threads) {
   const int es = element_bytes(c);
   const int head = unit % c.Hkv, lt = unit / c.Hkv;
   char* const base = reinterpret_cast<char*>(lt & 1 ? c.V : c.K) + ((lt >> 1) * c.layer + head * c.head) * es;
-  copy_rows(base + from * c.page * es, base + to * c.page * es, c.tok * es, pieces_log2_of(c), rows, thread, threads);
+  const int64_t row_bytes = c.tok * es;
+#pragma unroll 1
+  for (int row = 0; row < rows; row += kCopyRows)
+    copy_rows(base + from * c.page * es + row * row_bytes, base + to * c.page * es + row * row_bytes, row_bytes, pieces_log2_of(c),
+              min(rows - row, kCopyRows), thread, threads);
 }
 
 constexpr int kForkEntries = 1024;  // table entries of a workgroup

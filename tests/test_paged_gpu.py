@@ -853,3 +853,26 @@ def test_a_cache_beyond_32_bit_offsets():
     assert sorted(cache.tables[0, :4].tolist()) == [0, 1, 2, 3] or int((cache.refs > 0).sum()) == 5
     last = int(cache.tables[0, 3])
     assert bool((K[0, last, :, 55:58] == 1).all())
+
+
+def test_pages_of_more_pieces_than_32_bits_count():
+    """A page of 2^26 tokens has 2^31 pieces of 16 bytes a head: compaction moves all of them, and a fork copies all that are filled.  (34 GB a
+    page; K and V are one tensor here.)"""
+    torch.cuda.empty_cache()
+    ps, D = 1 << 26, 128
+    K = torch.empty((1, 2, 1, ps, D), device=DEV)
+    for x in K[0, 0, 0], K[0, 1, 0]:
+        x.fill_(-1.0)
+    mark = torch.arange(ps, dtype=torch.float32, device=DEV)      # (a row's number, rounded, and its last bits)
+    K[0, 1, 0, :, 0], K[0, 1, 0, :, D - 1] = mark, mark.remainder(1021)
+    cache = B.PageCache(K, K, i32([[1], [-1]]), i32([ps, 0]), i32([0, 1]))
+    assert B.sl_pages_compact(cache).tolist() == [-1, 0] and cache.tables.tolist() == [[0], [-1]]
+    assert torch.equal(K[0, 0, 0, :, 0], mark) and torch.equal(K[0, 0, 0, :, D - 1], mark.remainder(1021))
+    K[0, 1].fill_(-1.0)
+    filled = ps - 3
+    cache.lens[0] = filled
+    assert B.sl_pages_fork(cache, i32([0]), i32([1])).tolist() == [1] and cache.tables.tolist() == [[0], [1]]
+    assert torch.equal(K[0, 1, 0, :filled, 0], mark[:filled]) and torch.equal(K[0, 1, 0, :filled, D - 1], mark[:filled].remainder(1021))
+    assert bool((K[0, 1, 0, filled:] == -1).all()) and bool((K[0, 1, 0, :filled:4099, 1:D - 1] == -1).all())
+    del cache, K
+    torch.cuda.empty_cache()
