@@ -613,6 +613,11 @@ def _strides(t, name):
     return out
 
 
+def _to32(v):
+    """The nearest value that a 32-bit field holds (ctypes drops the bits above): as refused as v, or as long as every sequence."""
+    return v if -0x80000000 <= v <= 0x7fffffff else 0x7fffffff if v > 0 else -0x80000000
+
+
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
@@ -655,7 +660,7 @@ class PageCache:
         """The sl_paged_batch of new tokens cu_rows[b] .. cu_rows[b + 1] - 1 of sequence seqs[b]."""
         n = _int32(seqs, "seqs", self.index)
         _int32(cu_rows, "cu_rows", self.index, n + 1)
-        return SlPagedBatch(seqs.data_ptr(), cu_rows.data_ptr(), rows, L, n, layer)
+        return SlPagedBatch(seqs.data_ptr(), cu_rows.data_ptr(), rows, L, n, _to32(layer))
 
 
 def sl_pages_extend(cache: PageCache, seqs, cu_rows, ok=None):
@@ -731,7 +736,7 @@ def sl_paged_span_keys(cache: PageCache, seqs, cu_rows, Ks, S, layer=0):
             or Ks.dtype is not cache.dtype or Ks.get_device() != cache.index):
         raise ValueError("expect contiguous Ks [n_seqs, Hkv, n_spans, D] of the cache's dtype and device")
     b = cache.batch(seqs, cu_rows, 0, 0, layer)
-    _check(load().sl_paged_span_keys(cache.record, b, S, shape[2], Ks.data_ptr(), cache.stream()), "sl_paged_span_keys")
+    _check(load().sl_paged_span_keys(cache.record, b, _to32(S), shape[2], Ks.data_ptr(), cache.stream()), "sl_paged_span_keys")
     return Ks
 
 
@@ -756,7 +761,7 @@ def _paged_attention(cache, seqs, cu_rows, Q, idx, scores, S, layer, L, scale, w
     if scores is not None and (idx is None or scores.dtype is not torch.float32 or scores.shape != idx.shape
                                or _strides(scores, "scores") != (ih, it, one) or scores.get_device() != cache.index):
         raise ValueError("scores must be float32 with the shape, strides and device of idx")
-    a = SlPagedAttention(Hq, min(S, 0x7fffffff), topk, scale, st[0], st[1], ih, it)  # (no sequence is longer)
+    a = SlPagedAttention(Hq, _to32(S), topk, scale, st[0], st[1], ih, it)
     b = cache.batch(seqs, cu_rows, T, L, layer)
     # Scratch is the call's own unless the caller gives a workspace: calls on different streams and graphs do not share it.
     ws = Workspace(cache.device) if ws is None else ws

@@ -195,6 +195,39 @@ def test_a_span_longer_than_any_sequence_is_not_cut_off():
         assert a.S == want
 
 
+def test_integers_beyond_32_bits_are_not_cut_off(monkeypatch):
+    """What the records hold in 32 bits: ctypes would drop the bits above, and a span of 2^32 + 4 would be one of 4."""
+    K = torch.zeros((6, 2, 16, 64), dtype=torch.bfloat16)
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)
+    cache = B.PageCache(K, K.clone(), i32(3, 4), i32(3), i32(6))
+    seen = []
+
+    class Lib:
+        def sl_paged_span_keys(self, c, b, S, n_spans, Ks, stream):
+            seen.append(ctypes.c_int32(S).value)        # what the library gets
+            return 0
+
+    monkeypatch.setattr(B, "load", lambda: Lib())
+    monkeypatch.setattr(B.PageCache, "stream", lambda self: None)
+    Ks = torch.zeros((3, 2, 5, 64), dtype=torch.bfloat16)
+    for S in (1 << 40, (1 << 32) + 4, 0x7fffffff, 100, 0, -4, -(1 << 32) + 4):
+        B.sl_paged_span_keys(cache, i32(1), i32(2), Ks, S)
+    assert seen[:4] == [0x7fffffff] * 3 + [100] and all(S <= 0 for S in seen[4:])
+    for layer, want in ((0, 0), (1 << 32, 0x7fffffff), ((1 << 33) + 1, 0x7fffffff), (7, 7)):
+        assert cache.batch(i32(1), i32(2), layer=layer).layer == want
+    for layer in (-1, -(1 << 32), -(1 << 32) + 1):
+        assert cache.batch(i32(1), i32(2), layer=layer).layer < 0
+
+    class Room:
+        def get(self, n):
+            return 0, n
+
+    monkeypatch.undo()
+    for S in (0, -1, -(1 << 32) + 5):
+        a, *_ = B._paged_attention(cache, i32(1), i32(2), torch.zeros((4, 1, 64), dtype=torch.bfloat16), None, None, S, 0, 0, 0.0, Room())
+        assert a.S <= 0
+
+
 def test_the_served_list_refuses():
     lib = B.load()
     assert lib.sl_pages_served(P, P, 0, P, None) == 0 and lib.sl_pages_served(None, None, 0, None, None) == 0
