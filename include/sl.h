@@ -327,7 +327,8 @@ sl_status sl_anchor_attention_decode_batched(const sl_params* p, const sl_anchor
 /* ---- A paged KV cache: sequences that grow, fork and end share one pool of pages.
  * Token t of sequence s lies in page tables[s][t / page_size], at row t % page_size of that page.
  * All arrays are device memory of the caller; the calls below read and update them on the stream,
- * so that a whole serving step can be captured into a graph.
+ * so that a step's calls can be captured into a graph (the span-search apart, whose positions are
+ * arguments of the host).
  *   - A table entry outside 0 .. n_pages - 1 names no page (write -1): tokens there take no part in
  *     attention, rows appended there are dropped.
  *   - refs[p] is the number of table entries that name page p; a page is free when refs[p] <= 0.
@@ -413,8 +414,10 @@ sl_status sl_paged_append(const sl_page_cache* c, const sl_paged_batch* b, const
 
 /* Span keys (sl_span_keys) of the spans of S tokens that the batch's new tokens complete:
  * Ks[seqs[b]][kv][j] = K of token (j+1)*S - 1.  Ks: [n_seqs][Hkv][n_spans][D], packed; spans from n_spans
- * on are left out (rows is not read).  Ks of one sequence is what the span-search entry points take with
- * L = n_spans * S.  (A batch whose chunks are whole sequences makes all keys anew.) */
+ * on are left out (rows is not read).  Ks of one sequence is what sl_span_search_prefill takes, with K NULL, L = n_spans * S (not below
+ * the sequence's length) and q_pos0 the position of its first new token; a single token is a chunk of one.  (The decode entry points
+ * put the query at L - 1 and read tables of ceil(L / S) spans, which these are only where the sequence has n_spans * S tokens.)
+ * (A batch whose chunks are whole sequences makes all keys anew.) */
 sl_status sl_paged_span_keys(const sl_page_cache* c, const sl_paged_batch* b, int32_t S, int32_t n_spans,
                              void* Ks, void* hip_stream);
 

@@ -301,7 +301,13 @@ def sl_span_keys(K, S, out=None):
 
 def _search(fn_name, op, Qs, K, Ks, S, topk, q_pos0, want_scores, ws, prof):
     lib = load()
-    p = make_params(Qs, K, S, topk, q_pos0)
+    if K is None:
+        if Ks is None or Ks.dim() != 3 or not Ks.is_contiguous() or Ks.dtype != Qs.dtype:
+            raise ValueError("without K, expect contiguous Ks [Hkv, n_spans, D] of Q's dtype")
+        p = make_params(Qs, Ks, S, topk, q_pos0)
+        p.L, p.kv_stride_h, p.kv_stride_t = Ks.shape[1] * S, 0, 0
+    else:
+        p = make_params(Qs, K, S, topk, q_pos0)
     Hq, Lq, _ = Qs.shape
     idx = torch.empty((Hq, Lq, topk), dtype=torch.int32, device=Qs.device)
     scores = torch.empty((Hq, Lq, topk), dtype=torch.float32, device=Qs.device) if want_scores else None
@@ -314,6 +320,7 @@ def _search(fn_name, op, Qs, K, Ks, S, topk, q_pos0, want_scores, ws, prof):
 
 
 def sl_span_search_prefill(Qs, K, Ks, S, topk, q_pos0=0, want_scores=False, ws=None, prof=None):
+    """K may be None where Ks is given: L is n_spans * S then."""
     return _search("sl_span_search_prefill", OP_SEARCH_PREFILL, Qs, K, Ks, S, topk, q_pos0,
                    want_scores, ws, prof)
 
@@ -729,8 +736,8 @@ def sl_paged_append(cache: PageCache, seqs, cu_rows, K, V, layer=0):
 
 
 def sl_paged_span_keys(cache: PageCache, seqs, cu_rows, Ks, S, layer=0):
-    """Keys of the spans that the new tokens complete, into Ks [n_seqs, Hkv, n_spans, D]; Ks[s] with L = n_spans * S is what
-    span-search takes."""
+    """Keys of the spans that the new tokens complete, into Ks [n_seqs, Hkv, n_spans, D].  sl_span_search_prefill(Q, None, Ks[s], S, topk,
+    q_pos0=position of the first row) searches those of one sequence; n_spans * S must not be below its length."""
     shape = Ks.shape
     if (len(shape) != 4 or shape[0] != cache.record.n_seqs or shape[1] != cache.Hkv or shape[3] != cache.D or not Ks.is_contiguous()
             or Ks.dtype is not cache.dtype or Ks.get_device() != cache.index):

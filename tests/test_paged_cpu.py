@@ -228,6 +228,13 @@ def test_integers_beyond_32_bits_are_not_cut_off(monkeypatch):
         assert a.S <= 0
 
 
+def test_search_without_a_key_tensor_refuses_tables_that_do_not_fit():
+    Q, Ks = torch.zeros((4, 1, 64)), torch.zeros((2, 6, 64))
+    for bad in (None, Ks[0], Ks[:, ::2], Ks.bfloat16(), Ks.transpose(0, 1)):
+        with pytest.raises(ValueError):
+            B.sl_span_search_prefill(Q, None, bad, 16, 2)
+
+
 def test_the_served_list_refuses():
     lib = B.load()
     assert lib.sl_pages_served(P, P, 0, P, None) == 0 and lib.sl_pages_served(None, None, 0, None, None) == 0

@@ -667,6 +667,30 @@ def test_a_serving_run_equals_the_contiguous_entry_points():
     step([0, 3, 4, 5, 1], [1, 1, 1, 1, 100])
 
 
+@pytest.mark.parametrize("dtype,D,S,n", [(BF16, 128, 64, 1), (BF16, 128, 64, 300), (BF16, 64, 40, 70), (F32, 128, 32, 130), (F32, 64, 17, 1)])
+def test_search_over_the_keys_of_a_paged_sequence(dtype, D, S, n):
+    """Ks[s] without any K, against the contiguous search over the sequence's own tokens."""
+    g = torch.Generator().manual_seed(35)
+    Hq, Hkv, ps, L, spans = 8, 2, 16, 1000, 70
+    cache = B.PageCache.empty(80, ps, Hkv, D, 5, 64, dtype=dtype)
+    Ks = torch.full((5, Hkv, spans, D), math.nan, dtype=dtype, device=DEV)
+    K = torch.randn((Hkv, 2 * L, D), generator=g).to(dtype).to(DEV)
+    seqs, cu = i32([3, 1]), i32([0, L, 2 * L - 250])
+    assert B.sl_pages_extend(cache, seqs, cu).tolist() == [1, 0]        # (80 pages)
+    seqs = B.sl_pages_served(cache, seqs, i32([1, 0]))
+    B.sl_paged_append(cache, seqs, cu, K, K)
+    B.sl_paged_span_keys(cache, seqs, cu, Ks, S)
+    Q = torch.randn((Hq, n, D), generator=g).to(dtype).to(DEV)
+    want = B.sl_span_search_prefill(Q, K[:, :L].contiguous(), None, S, 4, q_pos0=L - n, want_scores=True)
+
+    def same(got):      # (a sum of 128 products below 30, in another order)
+        assert torch.equal(got[0], want[0]) and float((got[1] - want[1]).abs().nan_to_num(0).max()) <= 1e-3
+
+    same(B.sl_span_search_prefill(Q, None, Ks[3], S, 4, q_pos0=L - n, want_scores=True))
+    with pytest.raises(B.SlError):      # rows at positions that the table has no spans for
+        B.sl_span_search_prefill(Q, None, Ks[3], S, 4, q_pos0=spans * S - n + 1)
+
+
 def test_a_captured_step_is_replayed():
     """extend, append, keys and attention in one graph: each replay is the next step, eager calls in between."""
     g = torch.Generator().manual_seed(12)
