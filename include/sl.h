@@ -417,7 +417,7 @@ sl_status sl_paged_append(const sl_page_cache* c, const sl_paged_batch* b, const
  * on are left out (rows is not read).  Ks of one sequence is what sl_span_search_prefill takes, with K NULL, L = n_spans * S (not below
  * the sequence's length) and q_pos0 the position of its first new token; a single token is a chunk of one.  (The decode entry points
  * put the query at L - 1 and read tables of ceil(L / S) spans, which these are only where the sequence has n_spans * S tokens.)
- * (A batch whose chunks are whole sequences makes all keys anew.) */
+ * A batch whose chunks are whole sequences makes all keys anew: sl_pages_fork copies pages, not keys, and its dst need that. */
 sl_status sl_paged_span_keys(const sl_page_cache* c, const sl_paged_batch* b, int32_t S, int32_t n_spans,
                              void* Ks, void* hip_stream);
 

@@ -669,7 +669,7 @@ def test_a_serving_run_equals_the_contiguous_entry_points():
 
 @pytest.mark.parametrize("dtype,D,S,n", [(BF16, 128, 64, 1), (BF16, 128, 64, 300), (BF16, 64, 40, 70), (F32, 128, 32, 130), (F32, 64, 17, 1)])
 def test_search_over_the_keys_of_a_paged_sequence(dtype, D, S, n):
-    """Ks[s] without any K, against the contiguous search over the sequence's own tokens."""
+    """Ks[s] without any K, against the contiguous search over the sequence's own tokens; after a fork, the keys made anew."""
     g = torch.Generator().manual_seed(35)
     Hq, Hkv, ps, L, spans = 8, 2, 16, 1000, 70
     cache = B.PageCache.empty(80, ps, Hkv, D, 5, 64, dtype=dtype)
@@ -687,6 +687,13 @@ def test_search_over_the_keys_of_a_paged_sequence(dtype, D, S, n):
         assert torch.equal(got[0], want[0]) and float((got[1] - want[1]).abs().nan_to_num(0).max()) <= 1e-3
 
     same(B.sl_span_search_prefill(Q, None, Ks[3], S, 4, q_pos0=L - n, want_scores=True))
+    src, dst = i32([3, 3, 3]), i32([0, 4, 3])        # (the last is not made)
+    assert B.sl_pages_fork(cache, src, dst).tolist() == [1, 1, 0]
+    B.sl_paged_span_keys(cache, dst, torch.nn.functional.pad(cache.lens[dst].cumsum(0), (1, 0)).int(), Ks, S)
+    for s in (0, 4, 3):
+        assert torch.equal(Ks[s].nan_to_num(5.0), Ks[3].nan_to_num(5.0))
+        same(B.sl_span_search_prefill(Q, None, Ks[s], S, 4, q_pos0=L - n, want_scores=True))
+    assert bool(Ks[[1, 2]].isnan().all())
     with pytest.raises(B.SlError):      # rows at positions that the table has no spans for
         B.sl_span_search_prefill(Q, None, Ks[3], S, 4, q_pos0=spans * S - n + 1)
 
