@@ -886,6 +886,34 @@ def test_a_cache_beyond_32_bit_offsets():
     assert bool((K[0, last, :, 55:58] == 1).all())
 
 
+def test_compaction_beyond_32_bit_offsets_moves_every_page():
+    """Two sequences, forked, in pages at the far end of a pool of 9 GB: tables, counts, the map and all that the pages held."""
+    ps, Hkv, D = 64, 4, 128
+    n_pages = (9 << 30) // 2 // (ps * Hkv * D)
+    K, V = (torch.zeros((1, n_pages, Hkv, ps, D), dtype=BF16, device=DEV) for _ in range(2))
+    g = torch.Generator().manual_seed(36)
+    first, second = [n_pages - 1, 3, n_pages // 2 + 1, n_pages - 2], [n_pages - 7, 1]
+    for p in first + second:
+        K[0, p], V[0, p] = (torch.randn((Hkv, ps, D), generator=g).to(BF16).to(DEV) for _ in range(2))
+    tables = torch.full((4, 6), -1, dtype=torch.int32, device=DEV)
+    tables[0, :4], tables[2, :2] = i32(first), i32(second)
+    refs = torch.zeros(n_pages, dtype=torch.int32, device=DEV)
+    refs[torch.tensor(first + second, device=DEV)] = 1
+    cache = B.PageCache(K, V, tables, i32([250, 0, 128, 0]), refs)
+    assert B.sl_pages_fork(cache, i32([0, 2]), i32([1, 3])).tolist() == [1, 1]      # (page 0 for the last, partly filled one)
+    held = {(s, k): (K[0, int(tables[s, k])].clone(), V[0, int(tables[s, k])].clone()) for s in range(4) for k in range(6) if tables[s, k] >= 0}
+    used = {0: 1, 1: 2, 3: 2, n_pages // 2 + 1: 2, n_pages - 7: 2, n_pages - 2: 1, n_pages - 1: 2}
+    assert {int(p): int(refs[p]) for p in (refs != 0).nonzero()} == used
+    where = B.sl_pages_compact(cache)
+    to = {0: 0, 1: 1, 3: 3, n_pages // 2 + 1: 2, n_pages - 7: 4, n_pages - 2: 5, n_pages - 1: 6}
+    assert {int(p): int(where[p]) for p in (where != -1).nonzero()} == to
+    assert tables.tolist() == [[to[p] for p in first] + [-1] * 2, [to[p] for p in first[:3]] + [0] + [-1] * 2,
+                               [to[p] for p in second] + [-1] * 4, [to[p] for p in second] + [-1] * 4]
+    assert refs[:7].tolist() == [n for _, n in sorted((to[p], n) for p, n in used.items())] and int((refs != 0).sum()) == 7
+    for (s, k), (kept_K, kept_V) in held.items():
+        assert torch.equal(K[0, int(tables[s, k])], kept_K) and torch.equal(V[0, int(tables[s, k])], kept_V)
+
+
 def test_pages_of_more_pieces_than_32_bits_count():
     """A page of 2^26 tokens has 2^31 pieces of 16 bytes a head: compaction moves all of them, and a fork copies all that are filled.  (34 GB a
     page; K and V are one tensor here.)"""
