@@ -1417,9 +1417,10 @@ dim3 grid_of(int64_t workgroups) {
   return workgroups <= kMost ? dim3((unsigned)workgroups) : dim3((unsigned)kMost, (unsigned)div_up(workgroups, kMost));
 }
 
-// Records that the Infinity Cache (256 MB) would not keep until they are merged are written past the caches: 222 MB of them (3000 rows
-// behind 60000 tokens, 32:4 heads, eight spans of 128) 260 -> 237 us the call, 5 GB (64K tokens, spans of 256) 5.57 -> 5.24 ms; 169 MB 259 -> 262.
-constexpr size_t kStreamedRecords = (size_t)200 << 20;
+// Records that the Infinity Cache (256 MB) would not keep until they are merged are written past the caches.  By the MiB reserved for them
+// (32:4 heads, eight spans; us of the call, and past the caches): 193 (1900 rows, spans of 512) 248 and 252, 203 262 and 265, 232 (2700 rows, spans of
+// 128) 239.9 and 238.7, 258 254.5 and 253.4, 344 335.5 and 332.7, 740 833 and 775, 4800 (64K rows, spans of 256) 5570 and 5260.
+constexpr size_t kStreamedRecords = (size_t)230 << 20;
 
 // How a call is taken.
 struct Form {
