@@ -587,6 +587,29 @@ def test_page_turns(seed, n_pages, ps, n_seqs, dtype, layers):
     assert int(cache.refs.abs().sum()) == 0 and int((cache.tables != -1).sum()) == 0
 
 
+@pytest.mark.parametrize("seed,n_pages,ps,n_seqs", [(6, 70000, 1, 12), (7, 140000, 2, 7)])
+def test_page_turns_in_large_pools(seed, n_pages, ps, n_seqs):
+    """Pools whose counts are looked at sixteen at a time, in several passes."""
+    test_page_turns(seed, n_pages, ps, n_seqs, BF16, 1)
+
+
+@pytest.mark.parametrize("n_pages", [3000, 70000])
+def test_tables_whose_pages_together_pass_32_bits(n_pages):
+    """4096 entries of tables of 2^20 pages each: needs are summed in 64 bits.  Chunks of less than nothing are not served."""
+    cache = B.PageCache.empty(n_pages, 1, 1, 64, 8, 1 << 20)
+    model = ref.Pages(cache)
+    rng = random.Random(n_pages)
+    for _ in range(3):
+        seqs = [rng.choice([-1, 8, 1 << 30, rng.randint(0, 7)]) for _ in range(4096)]
+        cu = [0]
+        for _ in seqs:
+            cu.append(max(0, cu[-1] + rng.choice([0, 1, 3, n_pages // 5, -2, -n_pages // 5])))
+        ok = B.sl_pages_extend(cache, i32(seqs), i32(cu))
+        assert ok.tolist() == model.extend(seqs, cu) and 1 in ok.tolist()
+        assert cache.lens.tolist() == model.lens and cache.refs.tolist() == model.refs
+        assert cache.tables[:, :n_pages].tolist() == [t[:n_pages] for t in model.tables] and bool((cache.tables[:, n_pages:] == -1).all())
+
+
 def test_lists_as_long_as_they_may_be():
     """4096 entries of one token each, with 4000 pages: the entry at which they run out, and that every later one is refused."""
     cache = B.PageCache.empty(4000, 16, 1, 64, 5000, 2)
