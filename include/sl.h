@@ -442,7 +442,8 @@ size_t sl_paged_attention_workspace_bytes(const sl_page_cache* c, const sl_paged
  *          empty slots, a span must not be listed twice in a row.
  *   O      out: [Hq][rows][D] packed; LSE out: [Hq][rows] packed.
  * A row that no token is left for (pages missing, a position outside the sequence) gets O = 0,
- * LSE = -inf. */
+ * LSE = -inf.  Accuracy of bf16 calls, beside the output's own rounding: weights may be rounded to bf16 for the product with V (2^-8 of
+ * sum p |v|) and partial results to 11 bits of their largest element; sums and LSE are fp32. */
 sl_status sl_paged_span_attention(const sl_page_cache* c, const sl_paged_batch* b, const sl_paged_attention* a, const void* Q,
                                   const int32_t* idx, void* O, float* LSE, void* ws, size_t ws_bytes, void* hip_stream);
 /* The gated form: scores as idx, finite in non-empty slots; no LSE. */
