@@ -64,7 +64,13 @@ typedef enum {
   SL_ERR_LAUNCH = 4       /* HIP reported an error when enqueueing                             */
 } sl_status;
 
-typedef enum { SL_F32 = 0, SL_BF16 = 1 } sl_dtype;
+typedef enum {
+  SL_F32 = 0,
+  SL_BF16 = 1,
+  /* Page caches alone: K and V are held in 4 bits (see sl_page_cache), the rows that are written, read and attended are ... */
+  SL_MXFP4_F32 = 16, /* ... fp32 */
+  SL_MXFP4_BF16 = 17 /* ... bf16 */
+} sl_dtype;
 
 typedef enum {
   SL_OP_SEARCH_PREFILL = 0,
@@ -339,10 +345,19 @@ sl_status sl_anchor_attention_decode_batched(const sl_params* p, const sl_anchor
  * An empty cache: tables all -1, lens and refs all 0.
  * Calls on one cache must be ordered, on one stream or with events.  None of them allocates,
  * synchronises or records profile events.
+ * A cache in 4 bits (dtype SL_MXFP4_*).  A row of D channels is D / 32 blocks of 32: codes of 4 bits (e2m1: bit 3 the sign, the others 0, 0.5,
+ * 1, 1.5, 2, 3, 4 or 6) and a scale of 8 bits; a channel is its code's value times 2^(scale - 127), and a scale of 255 makes all of its
+ * block NaN.  The part of a page that holds one head is SL_MXFP4_PAGE_BYTES(page_size, D) bytes: page_size rows of D / 2 bytes of codes
+ * (channel 2 i in the low half of byte i), then page_size rows of D / 32 scales; what is left of the last 16 bytes is not used.  K and V are
+ * [layers][n_pages][Hkv] of such parts; the strides count bytes, are multiples of 16 and not below a part; kv_stride_t is 0 or D / 2.
+ * sl_paged_append rounds: a block with the largest value x gets the smallest power of two that leaves x / 2^e below 7 (scale e + 127, kept
+ * within 2 .. 252), and each value the code nearest to value / 2^e, half way the even one, at most 6.  A value that is not finite
+ * makes its block NaN.  Pages are given out, forked, freed and compacted as others are.
  * What the device arrays hold cannot be checked by the host.  Sequence numbers outside
  * 0 .. n_seqs - 1, table entries that name no page, lengths beyond the table and rows without
  * a token are passed over as described at each call; no content leads to an access outside the
  * arrays that the records describe. */
+#define SL_MXFP4_PAGE_BYTES(page_size, D) (((int64_t)(page_size) * ((D) / 2 + (D) / 32) + 15) / 16 * 16)
 typedef struct sl_page_cache {
   void* K;          /* [layers][n_pages][Hkv][page_size][D], innermost contiguous */
   void* V;          /* the same layout and strides                                */
@@ -407,13 +422,19 @@ size_t sl_pages_compact_workspace_bytes(const sl_page_cache* c);
 sl_status sl_pages_compact(const sl_page_cache* c, int32_t* map, void* ws, size_t ws_bytes, void* hip_stream);
 
 /* Writes the batch's new tokens into their pages (a sequence's tokens by one entry: of entries that
- * list it twice, which one's rows stay is unspecified).  Entries that sl_pages_extend did not serve are to be -1 in seqs.  K, V: [Hkv][rows][D] with element strides
+ * list it twice, which one's rows stay is unspecified), rounded to 4 bits where the cache holds those.  Entries that sl_pages_extend did not serve are to be -1 in seqs.  K, V: [Hkv][rows][D] with element strides
  * (stride_h, stride_t, 1), 0 = packed. */
 sl_status sl_paged_append(const sl_page_cache* c, const sl_paged_batch* b, const void* K, const void* V,
                           int64_t stride_h, int64_t stride_t, void* hip_stream);
 
+/* The batch's tokens as rows again: K, V [Hkv][rows][D] of the rows' type, element strides (stride_h, stride_t, 1), 0 = packed; a chunk
+ * that is a whole sequence reads all of it.  Rows without a token, or whose token has no page, become zeros; rows of no entry are left as
+ * they were.  What a cache in 4 bits hands back is what its codes stand for, exactly.  Any dtype. */
+sl_status sl_paged_read(const sl_page_cache* c, const sl_paged_batch* b, void* K, void* V, int64_t stride_h, int64_t stride_t,
+                        void* hip_stream);
+
 /* Span keys (sl_span_keys) of the spans of S tokens that the batch's new tokens complete:
- * Ks[seqs[b]][kv][j] = K of token (j+1)*S - 1.  Ks: [n_seqs][Hkv][n_spans][D], packed; spans from n_spans
+ * Ks[seqs[b]][kv][j] = K of token (j+1)*S - 1, as the cache holds it.  Ks: [n_seqs][Hkv][n_spans][D], packed; spans from n_spans
  * on are left out (rows is not read).  Ks of one sequence is what sl_span_search_prefill takes, with K NULL, L = n_spans * S (not below
  * the sequence's length) and q_pos0 the position of its first new token; a single token is a chunk of one.  (The decode entry points
  * put the query at L - 1 and read tables of ceil(L / S) spans, which these are only where the sequence has n_spans * S tokens.)

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_PKG, "libsl.so")
 
 SL_OK = 0
 SL_F32, SL_BF16 = 0, 1
+SL_MXFP4 = 16  # added to the rows' type: a page cache that holds them in 4 bits
 OP_SEARCH_PREFILL, OP_SEARCH_DECODE, OP_ATTENTION_PREFILL, OP_ATTENTION_DECODE = 0, 1, 2, 3
 SL_MAX_TOPK = 32
 
@@ -31,7 +32,7 @@ EXPORTS = ("sl_workspace_bytes", "sl_span_keys", "sl_span_search_prefill", "sl_s
            "sl_anchor_batched_workspace_bytes", "sl_anchor_search_decode_batched",
            "sl_anchor_attention_decode_batched", "sl_set_profile_events", "sl_status_string", "sl_version",
            "sl_pages_extend", "sl_pages_served", "sl_pages_fork", "sl_pages_free", "sl_pages_compact_workspace_bytes", "sl_pages_compact",
-           "sl_paged_append", "sl_paged_span_keys", "sl_paged_attention_workspace_bytes", "sl_paged_span_attention",
+           "sl_paged_append", "sl_paged_read", "sl_paged_span_keys", "sl_paged_attention_workspace_bytes", "sl_paged_span_attention",
            "sl_paged_span_attention_combined")
 
 
@@ -152,7 +153,7 @@ def load():
     for name, argtypes in (("sl_pages_extend", [cp, bp, i32p, vp]), ("sl_pages_served", [i32p, i32p, i32, i32p, vp]),
                            ("sl_pages_fork", [cp, i32p, i32p, i32, i32p, vp]),
                            ("sl_pages_free", [cp, i32p, i32, vp]), ("sl_pages_compact", [cp, i32p, vp, ctypes.c_size_t, vp]),
-                           ("sl_paged_append", [cp, bp, vp, vp, i64, i64, vp]),
+                           ("sl_paged_append", [cp, bp, vp, vp, i64, i64, vp]), ("sl_paged_read", [cp, bp, vp, vp, i64, i64, vp]),
                            ("sl_paged_span_keys", [cp, bp, i32, i32, vp, vp]),
                            ("sl_paged_span_attention", [cp, bp, ap, vp, i32p, vp, f32p, vp, ctypes.c_size_t, vp]),
                            ("sl_paged_span_attention_combined", [cp, bp, ap, vp, i32p, f32p, vp, vp, ctypes.c_size_t, vp])):
@@ -177,12 +178,16 @@ def status_string(status: int) -> str:
     return load().sl_status_string(int(status)).decode()
 
 
-def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
+def _code_of(dtype) -> int:
+    if dtype == torch.float32:
         return SL_F32
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return SL_BF16
-    raise TypeError(f"unsupported dtype {t.dtype}: fp32 or bf16 only")
+    raise TypeError(f"unsupported dtype {dtype}: fp32 or bf16 only")
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    return _code_of(t.dtype)
 
 
 # A short decode step is bound by this module: its kernels take 17 us, its two calls took 28.
@@ -633,29 +638,54 @@ class PageCache:
 
     K, V: [layers, n_pages, Hkv, page_size, D] (or without the layers), innermost contiguous, V with K's strides;
     tables [n_seqs, max_pages], lens [n_seqs], refs [n_pages]: int32, contiguous, on the same device.  The tensors belong to the
-    caller and are read and updated in place; PageCache.empty makes those of an empty cache."""
+    caller and are read and updated in place; PageCache.empty makes those of an empty cache.
 
-    def __init__(self, K, V, tables, lens, refs):
-        K5, V5 = (x.unsqueeze(0) if x.dim() == 4 else x for x in (K, V))
-        if K5.dim() != 5 or K5.stride(4) != 1 or 0 in K5.shape or V5.shape != K5.shape or V5.stride() != K5.stride() or V.dtype != K.dtype:
-            raise ValueError("expect K, V [layers, n_pages, Hkv, page_size, D] of one dtype, contiguous innermost, V with K's strides")
-        layers, n_pages, Hkv, ps, D = K5.shape
+    A cache in 4 bits (the header says how a page holds them): K, V uint8 [layers, n_pages, Hkv, page_bytes(page_size, D)], with
+    page_size, D and the dtype of the rows that are written, read and attended, which is the cache's dtype."""
+
+    def __init__(self, K, V, tables, lens, refs, page_size=None, D=None, dtype=None):
+        self.fp4 = K.dtype is torch.uint8
+        dims = 4 if self.fp4 else 5
+        K5, V5 = (x.unsqueeze(0) if x.dim() == dims - 1 else x for x in (K, V))
+        if (K5.dim() != dims or K5.stride(-1) != 1 or 0 in K5.shape or V5.shape != K5.shape or V5.stride() != K5.stride() or V.dtype != K.dtype):
+            raise ValueError("expect K, V [layers, n_pages, Hkv, page_size, D] (4 bits: [layers, n_pages, Hkv, bytes]) of one dtype, contiguous "
+                             "innermost, V with K's strides")
+        if self.fp4:
+            layers, n_pages, Hkv, size = K5.shape
+            ps, D, dtype = int(page_size or 0), int(D or 0), torch.bfloat16 if dtype is None else dtype
+            if ps < 1 or D not in (64, 128) or size != self.page_bytes(ps, D):
+                raise ValueError("a cache in 4 bits takes page_size and D (64 or 128), and parts of page_bytes(page_size, D) bytes")
+            if K.data_ptr() % 16 or V.data_ptr() % 16:
+                raise ValueError("K and V must begin at a multiple of 16 bytes")
+        else:
+            layers, n_pages, Hkv, ps, last = K5.shape
+            if (page_size or ps) != ps or (D or last) != last or (dtype or K.dtype) != K.dtype:
+                raise ValueError("page_size, D and dtype are those of K")
+            D, dtype = last, K.dtype
         if tables.dtype != torch.int32 or tables.dim() != 2 or not tables.is_contiguous() or tables.device != K.device or V.device != K.device:
             raise ValueError("tables must be a contiguous int32 tensor [n_seqs, max_pages] on the device of K and V")
         self.index = K.get_device()
         _int32(lens, "lens", self.index, tables.shape[0])
         _int32(refs, "refs", self.index, n_pages)
         self.K, self.V, self.tables, self.lens, self.refs = K, V, tables, lens, refs
-        self.dtype, self.device, self.layers, self.page_size, self.Hkv, self.D = K.dtype, K.device, layers, ps, Hkv, D
+        self.dtype, self.device, self.layers, self.page_size, self.Hkv, self.D = dtype, K.device, layers, ps, Hkv, D
         st = _strides(K5, "K")
         self.record = SlPageCache(K.data_ptr(), V.data_ptr(), tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), st[0], st[1], st[2],
-                                  st[3], layers, n_pages, tables.shape[0], tables.shape[1], ps, Hkv, D, _dtype_code(K))
+                                  0 if self.fp4 else st[3], layers, n_pages, tables.shape[0], tables.shape[1], ps, Hkv, D,
+                                  _code_of(dtype) + (SL_MXFP4 if self.fp4 else 0))
 
     @classmethod
-    def empty(cls, n_pages, page_size, Hkv, D, n_seqs, max_pages, layers=1, dtype=torch.bfloat16, device="cuda"):
-        K, V = (torch.zeros((layers, n_pages, Hkv, page_size, D), dtype=dtype, device=device) for _ in range(2))
+    def empty(cls, n_pages, page_size, Hkv, D, n_seqs, max_pages, layers=1, dtype=torch.bfloat16, device="cuda", fp4=False):
+        """fp4: held in 4 bits, 3.76 (bf16 rows) times as many tokens in as many bytes."""
+        shape = (cls.page_bytes(page_size, D),) if fp4 else (page_size, D)
+        K, V = (torch.zeros((layers, n_pages, Hkv, *shape), dtype=torch.uint8 if fp4 else dtype, device=device) for _ in range(2))
         lens, refs = (torch.zeros(n, dtype=torch.int32, device=device) for n in (n_seqs, n_pages))
-        return cls(K, V, torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device), lens, refs)
+        return cls(K, V, torch.full((n_seqs, max_pages), -1, dtype=torch.int32, device=device), lens, refs, page_size, D, dtype)
+
+    @staticmethod
+    def page_bytes(page_size, D):
+        """Bytes that one head's K, or V, of a page takes in 4 bits: codes, scales, and what fills 16."""
+        return -(-page_size * (D // 2 + D // 32) // 16) * 16
 
     def stream(self):
         """The current stream of the cache's device, which has to be the current one."""
@@ -733,6 +763,22 @@ def sl_paged_append(cache: PageCache, seqs, cu_rows, K, V, layer=0):
         raise ValueError("expect K, V [Hkv, rows, D] of the cache's dtype and device, contiguous innermost, V with K's strides")
     b = cache.batch(seqs, cu_rows, shape[1], 0, layer)
     _check(load().sl_paged_append(cache.record, b, K.data_ptr(), V.data_ptr(), st[0], st[1], cache.stream()), "sl_paged_append")
+
+
+def sl_paged_read(cache: PageCache, seqs, cu_rows, rows, layer=0, out=None):
+    """The batch's tokens as rows again: K, V [Hkv, rows, D] of the cache's dtype, from a cache in 4 bits what its codes stand for.  rows:
+    how many rows the tensors have (cu_rows ends at it, or before).  Rows without a token or a page become zeros, rows of no entry
+    stay as they were (with out) or undefined."""
+    if out is None:
+        out = tuple(torch.empty((cache.Hkv, rows, cache.D), dtype=cache.dtype, device=cache.device) for _ in range(2))
+    K, V = out
+    shape, st = K.shape, _strides(K, "K")
+    if (shape != (cache.Hkv, rows, cache.D) or st[2] != 1 or V.shape != shape or _strides(V, "V") != st or K.dtype is not cache.dtype
+            or V.dtype is not cache.dtype or K.get_device() != cache.index or V.get_device() != cache.index):
+        raise ValueError("expect out = K, V [Hkv, rows, D] of the cache's dtype and device, contiguous innermost, V with K's strides")
+    b = cache.batch(seqs, cu_rows, rows, 0, layer)
+    _check(load().sl_paged_read(cache.record, b, K.data_ptr(), V.data_ptr(), st[0], st[1], cache.stream()), "sl_paged_read")
+    return out
 
 
 def sl_paged_span_keys(cache: PageCache, seqs, cu_rows, Ks, S, layer=0):

@@ -20,9 +20,10 @@ inline FastDiv fast_div(uint32_t d) {
 struct PageCache {
   void *K, *V;
   int32_t *tables, *lens, *refs;
-  int64_t layer, page, head, tok;  // element strides
-  int layers, n_pages, n_seqs, max_pages, ps, Hkv, D, dtype;
+  int64_t layer, page, head, tok;  // strides in elements; of a cache in 4 bits in bytes, tok of its codes
+  int layers, n_pages, n_seqs, max_pages, ps, Hkv, D, dtype;  // dtype: of the rows
   FastDiv by_ps;
+  bool fp4;  // a head's part of a page: ps rows of D / 2 bytes of codes, then ps of D / 32 scales (fp4.h)
 };
 
 struct PagedBatch {
@@ -45,10 +46,15 @@ sl_status pages_free(const PageCache& c, const int32_t* seqs, int n, hipStream_t
 size_t pages_compact_ws_bytes(const PageCache& c);
 sl_status pages_compact(const PageCache& c, int32_t* map, void* ws, hipStream_t st);
 sl_status paged_append(const PageCache& c, const PagedBatch& b, const void* K, const void* V, int64_t sh, int64_t st_, hipStream_t st);
+sl_status paged_append_fp4(const PageCache& c, const PagedBatch& b, const void* K, const void* V, int64_t sh, int64_t st_, hipStream_t st);
+sl_status paged_read(const PageCache& c, const PagedBatch& b, void* K, void* V, int64_t sh, int64_t st_, hipStream_t st);
 sl_status paged_span_keys(const PageCache& c, const PagedBatch& b, int S, int n_spans, void* Ks, hipStream_t st);
+sl_status paged_span_keys_fp4(const PageCache& c, const PagedBatch& b, int S, int n_spans, void* Ks, hipStream_t st);
 size_t paged_attention_ws_bytes(const PageCache& c, const PagedBatch& b, const PagedAttention& a);
 sl_status paged_attention(const PageCache& c, const PagedBatch& b, const PagedAttention& a, const void* Q, const int32_t* idx,
                           const float* scores, void* O, float* LSE, void* ws, hipStream_t st);
+sl_status paged_attention_fp4(const PageCache& c, const PagedBatch& b, const PagedAttention& a, const void* Q, const int32_t* idx,
+                              const float* scores, void* O, float* LSE, void* ws, hipStream_t st);
 
 #if defined(__HIPCC__)
 
@@ -76,6 +82,19 @@ __device__ __forceinline__ int length_of(const PageCache& c, int s) {
   if ((uint32_t)s >= (uint32_t)c.n_seqs) return -1;
   const int most = c.max_pages * c.ps, len = c.lens[s];
   return len < 0 ? 0 : len < most ? len : most;
+}
+
+// Where a batch's row lies: its page and its place there; page < 0: the row is no entry's, holds no token, or its token has no page.
+struct RowPlace {
+  int page, at;
+  bool listed;  // a row of some entry
+};
+__device__ __forceinline__ RowPlace place_of_row(const PageCache& c, const PagedBatch& b, int row) {
+  if (row >= b.rows || row < b.cu[0] || row >= b.cu[b.B]) return {-1, 0, false};
+  const int e = entry_of_row(b.cu, b.B, row), s = b.seqs[e], len = length_of(c, s), t = len - (b.cu[e + 1] - row);
+  if (t < 0 || t >= b.L || t >= len) return {-1, 0, true};
+  const int k = (uint32_t)t / c.by_ps, page = c.tables[(int64_t)s * c.max_pages + k];
+  return {(uint32_t)page < (uint32_t)c.n_pages ? page : -1, t - k * c.ps, true};
 }
 
 #endif

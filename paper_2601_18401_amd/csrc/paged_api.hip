@@ -23,7 +23,8 @@ sl_status make_cache(const sl_page_cache* p, PageCache* c) {
   if (!aligned16(p->K) || !aligned16(p->V) || !aligned16(p->refs) || !aligned4(p->tables) || !aligned4(p->lens))
     return SL_ERR_INVALID_ARG;
   if (p->layers < 1 || p->n_pages < 1 || p->n_seqs < 1 || p->max_pages < 1 || p->page_size < 1 || p->Hkv < 1) return SL_ERR_INVALID_ARG;
-  if (p->dtype != SL_F32 && p->dtype != SL_BF16) return SL_ERR_INVALID_ARG;
+  const bool fp4 = p->dtype == SL_MXFP4_F32 || p->dtype == SL_MXFP4_BF16;
+  if (p->dtype != SL_F32 && p->dtype != SL_BF16 && !fp4) return SL_ERR_INVALID_ARG;
   if (p->D != 64 && p->D != 128) return SL_ERR_UNSUPPORTED;
   if ((int64_t)p->max_pages * p->page_size > (int64_t)1 << 30 || p->n_pages > kMaxPages) return SL_ERR_UNSUPPORTED;
   // (grid dimensions are 16 bits wide in y)
@@ -32,16 +33,19 @@ sl_status make_cache(const sl_page_cache* p, PageCache* c) {
   if (p->kv_stride_t < 0 || p->kv_stride_h < 0 || p->page_stride < 0 || p->layer_stride < 0) return SL_ERR_INVALID_ARG;
   if (p->kv_stride_t > kMaxTokenStride || p->kv_stride_h > kMaxStride || p->page_stride > kMaxStride || p->layer_stride > kMaxStride << 8)
     return SL_ERR_UNSUPPORTED;
-  c->tok = p->kv_stride_t ? p->kv_stride_t : p->D;
-  c->head = p->kv_stride_h ? p->kv_stride_h : p->page_size * c->tok;
+  // A head's part of a page in 4 bits is one block of bytes, which no stride takes apart.
+  const int64_t width = fp4 ? p->D / 2 : p->D, block = fp4 ? SL_MXFP4_PAGE_BYTES(p->page_size, p->D) : 0;
+  if (fp4 && p->kv_stride_t != 0 && p->kv_stride_t != width) return SL_ERR_INVALID_ARG;
+  c->tok = p->kv_stride_t ? p->kv_stride_t : width;
+  c->head = p->kv_stride_h ? p->kv_stride_h : fp4 ? block : p->page_size * c->tok;
   // (heads first or tokens first: whichever is the outer one of the two has the larger extent)
   c->page = p->page_stride ? p->page_stride : std::max(p->Hkv * c->head, p->page_size * c->tok);
   if (c->head > kMaxExtent / p->Hkv || c->page > kMaxExtent / p->n_pages) return SL_ERR_UNSUPPORTED;
   c->layer = p->layer_stride ? p->layer_stride : p->n_pages * c->page;
   if (c->layer > kMaxExtent / p->layers) return SL_ERR_UNSUPPORTED;
-  const int64_t epl = p->dtype == SL_BF16 ? 8 : 4;
+  const int64_t epl = fp4 ? 16 : p->dtype == SL_BF16 ? 8 : 4, least = fp4 ? block : p->D;
   if (c->tok % epl || c->head % epl || c->page % epl || c->layer % epl) return SL_ERR_INVALID_ARG;
-  if (c->tok < p->D || (p->Hkv > 1 && c->head < p->D) || (p->n_pages > 1 && c->page < p->D) || (p->layers > 1 && c->layer < p->D))
+  if (c->tok < width || (p->Hkv > 1 && c->head < least) || (p->n_pages > 1 && c->page < least) || (p->layers > 1 && c->layer < least))
     return SL_ERR_INVALID_ARG;
   c->K = p->K;
   c->V = p->V;
@@ -55,7 +59,8 @@ sl_status make_cache(const sl_page_cache* p, PageCache* c) {
   c->ps = p->page_size;
   c->Hkv = p->Hkv;
   c->D = p->D;
-  c->dtype = p->dtype;
+  c->dtype = p->dtype == SL_MXFP4_F32 ? SL_F32 : p->dtype == SL_MXFP4_BF16 ? SL_BF16 : p->dtype;
+  c->fp4 = fp4;
   c->by_ps = fast_div((uint32_t)p->page_size);
   return SL_OK;
 }
@@ -96,6 +101,22 @@ sl_status make_attention(const sl_paged_attention* p, const PageCache& c, const 
   a->scale = p->scale > 0.f ? p->scale : 1.0f / std::sqrt((float)c.D);
   a->combined = false;
   return SL_OK;
+}
+
+// Row tensors [Hkv][rows][D] with the cache and the batch that they belong to; 0 strides become packed ones.
+sl_status rows_of(const sl_page_cache* pc, const sl_paged_batch* pb, const void* K, const void* V, int64_t* stride_h, int64_t* stride_t,
+                  PageCache* c, PagedBatch* b) {
+  sl_status s = make_cache(pc, c);
+  if (s == SL_OK) s = make_batch(pb, *c, b);
+  if (s != SL_OK) return s;
+  if (*stride_h < 0 || *stride_t < 0) return SL_ERR_INVALID_ARG;
+  if (*stride_h > kMaxStride || *stride_t > kMaxStride >> 8) return SL_ERR_UNSUPPORTED;
+  if (b->B == 0 || b->rows == 0) return SL_OK;
+  if (!K || !V || !aligned16(K) || !aligned16(V)) return SL_ERR_INVALID_ARG;
+  const int64_t epl = c->dtype == SL_BF16 ? 8 : 4;
+  if (!*stride_t) *stride_t = c->D;
+  if (!*stride_h) *stride_h = b->rows * *stride_t;
+  return *stride_t < c->D || *stride_t % epl || *stride_h % epl ? SL_ERR_INVALID_ARG : SL_OK;
 }
 
 sl_status attention_entry(const sl_page_cache* pc, const sl_paged_batch* pb, const sl_paged_attention* pa, const void* Q,
@@ -177,16 +198,20 @@ sl_status sl_paged_append(const sl_page_cache* pc, const sl_paged_batch* pb, con
                           int64_t stride_t, void* hip_stream) {
   sl::PageCache c;
   sl::PagedBatch b;
-  sl_status s = sl::make_cache(pc, &c);
-  if (s == SL_OK) s = sl::make_batch(pb, c, &b);
-  if (s != SL_OK) return s;
-  if (stride_h < 0 || stride_t < 0) return SL_ERR_INVALID_ARG;
-  if (stride_h > sl::kMaxStride || stride_t > sl::kMaxStride >> 8) return SL_ERR_UNSUPPORTED;
-  if (b.B == 0 || b.rows == 0) return SL_OK;
-  if (!K || !V || !sl::aligned16(K) || !sl::aligned16(V)) return SL_ERR_INVALID_ARG;
-  const int64_t epl = c.dtype == SL_BF16 ? 8 : 4, st = stride_t ? stride_t : c.D, sh = stride_h ? stride_h : b.rows * st;
-  if (st < c.D || st % epl || sh % epl) return SL_ERR_INVALID_ARG;
-  return sl::paged_append(c, b, K, V, sh, st, static_cast<hipStream_t>(hip_stream));
+  const sl_status s = sl::rows_of(pc, pb, K, V, &stride_h, &stride_t, &c, &b);
+  if (s != SL_OK || b.B == 0 || b.rows == 0) return s;
+  return sl::paged_append(c, b, K, V, stride_h, stride_t, static_cast<hipStream_t>(hip_stream));
+}
+
+sl_status sl_paged_read(const sl_page_cache* pc, const sl_paged_batch* pb, void* K, void* V, int64_t stride_h, int64_t stride_t,
+                        void* hip_stream) {
+  sl::PageCache c;
+  sl::PagedBatch b;
+  const sl_status s = sl::rows_of(pc, pb, K, V, &stride_h, &stride_t, &c, &b);
+  if (s != SL_OK || b.B == 0 || b.rows == 0) return s;
+  // (heads of one row may lie in any order; rows that share elements would be written twice)
+  if (c.Hkv > 1 && stride_h < c.D) return SL_ERR_INVALID_ARG;
+  return sl::paged_read(c, b, K, V, stride_h, stride_t, static_cast<hipStream_t>(hip_stream));
 }
 
 sl_status sl_paged_span_keys(const sl_page_cache* pc, const sl_paged_batch* pb, int32_t S, int32_t n_spans, void* Ks, void* hip_stream) {

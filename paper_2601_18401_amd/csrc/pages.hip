@@ -229,9 +229,11 @@ __device__ __forceinline__ void copy_rows(const char* __restrict__ from, char* _
         load16(from + (p >> pieces_log2) * row_bytes + (p & mask) * 16);
 }
 
-__host__ __device__ inline int element_bytes(const PageCache& c) { return c.dtype == SL_BF16 ? 2 : 4; }
-// 16-byte pieces of a row: 8, 16 or 32
-__host__ __device__ inline int pieces_log2_of(const PageCache& c) { return (c.D == 128 ? 4 : 3) + (c.dtype == SL_BF16 ? 0 : 1); }
+__host__ __device__ inline int element_bytes(const PageCache& c) { return c.fp4 ? 1 : c.dtype == SL_BF16 ? 2 : 4; }
+// 16-byte pieces of a row: 8, 16 or 32; of a row's codes 2 or 4
+__host__ __device__ inline int pieces_log2_of(const PageCache& c) {
+  return (c.D == 128 ? 4 : 3) + (c.fp4 ? -2 : c.dtype == SL_BF16 ? 0 : 1);
+}
 
 // One (layer, K or V, head) part of a page: unit in [0, layers * 2 * Hkv).  Pieces of kCopyRows rows count in 32 bits (pages may have 2^30).
 constexpr int kCopyRows = 1 << 24;
@@ -244,6 +246,17 @@ __device__ __forceinline__ void copy_part(const PageCache& c, int from, int to, 
   for (int row = 0; row < rows; row += kCopyRows)
     copy_rows(base + from * c.page * es + row * row_bytes, base + to * c.page * es + row * row_bytes, row_bytes, pieces_log2_of(c),
               min(rows - row, kCopyRows), thread, threads);
+  if (!c.fp4) return;
+  // the rows' scales, which begin at a multiple of 32 bytes: pieces of 16, and what is left, two at a time
+  const int64_t at = (int64_t)c.ps * c.tok;
+  const char* const s = base + from * c.page + at;
+  char* const d = base + to * c.page + at;
+  const int n = rows * (c.D / 32);
+#pragma unroll 1
+  for (int p = thread; p < n >> 4; p += threads) *reinterpret_cast<uint4*>(d + (int64_t)p * 16) = load16(s + (int64_t)p * 16);
+#pragma unroll 1
+  for (int p = (n >> 4 << 3) + thread; p < n >> 1; p += threads)
+    *reinterpret_cast<uint16_t*>(d + (int64_t)p * 2) = *reinterpret_cast<const uint16_t*>(s + (int64_t)p * 2);
 }
 
 constexpr int kForkEntries = 1024;  // table entries of a workgroup
@@ -519,6 +532,7 @@ sl_status pages_compact(const PageCache& c, int32_t* map, void* ws, hipStream_t 
 
 sl_status paged_append(const PageCache& c, const PagedBatch& b, const void* K, const void* V, int64_t sh, int64_t st_, hipStream_t st) {
   if (b.B == 0 || b.rows == 0) return SL_OK;
+  if (c.fp4) return paged_append_fp4(c, b, K, V, sh, st_, st);
   const int pl = pieces_log2_of(c);
   append_kernel<<<dim3((unsigned)((b.rows + kAppendRows - 1) / kAppendRows), c.Hkv), 256, 0, st>>>(c, b, static_cast<const char*>(K), static_cast<const char*>(V), sh, st_, pl);
   return launched();
@@ -526,6 +540,7 @@ sl_status paged_append(const PageCache& c, const PagedBatch& b, const void* K, c
 
 sl_status paged_span_keys(const PageCache& c, const PagedBatch& b, int S, int n_spans, void* Ks, hipStream_t st) {
   if (b.B == 0) return SL_OK;
+  if (c.fp4) return paged_span_keys_fp4(c, b, S, n_spans, Ks, st);
   const int chunks = (n_spans + kKeySpans - 1) / kKeySpans;
   span_keys_kernel<<<dim3(b.B, chunks, c.Hkv), 256, 0, st>>>(c, b, S, n_spans, static_cast<char*>(Ks), pieces_log2_of(c));
   return launched();
