@@ -844,6 +844,257 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
+// What few columns attend of a cache in 4 bits, by one wavefront: CB blocks of 16 columns, 32 tokens at a time, in products of 16x16x32.
+//   S^T[token][column] = K . Q^T      A: lane l has token row l % 16 and the channels of quarter l / 16 of a row, which come from its codes
+//                                     in registers: neither K's codes nor its values pass LDS
+//   O^T[d][column] += V^T . P^T       A: V's values through transposing LDS reads, B = P^T straight from the accumulators
+// (Lane l of a 16x16 result holds column l % 16 and rows 4 (l / 16) + r.  Row m of the token block tb of two is token 8 (m / 4) + 4 tb +
+// m % 4, so that a lane's eight accumulators are eight consecutive tokens, 8 (l / 16) on.)  A lane's codes of K and V are of the same tokens
+// and channels, D / 4 of them: one address for both.  Codes are asked for 64 tokens ahead.
+template <int D, int CB>
+struct NarrowCodes {
+  static constexpr int KK = D / 32, DB = D / 16, WORDS = D / 32;  // products of a token block; blocks of 16 channels; words of a lane's codes
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  f32x4 o[CB][DB], s[CB][2];
+  bf16x8 q[CB][KK];
+  float m[CB], l[CB];
+
+  // the codes of K and V of 32 tokens
+  struct Raw {
+    uint32_t k[2][WORDS], v[2][WORDS];
+    int ks[2], vs[2];
+  };
+  __device__ __forceinline__ static int token_of(int tb, int lane) { return 8 * ((lane & 15) >> 2) + 4 * tb + (lane & 3); }
+  __device__ __forceinline__ static void read_words(const uint8_t* from, uint32_t (&w)[WORDS]) {
+    typedef uint32_t Words __attribute__((ext_vector_type(WORDS)));
+    const Words x = __builtin_nontemporal_load(reinterpret_cast<const Words*>(from));
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = x[i];
+  }
+  // page: of lane l, of token t0 + l; the block begins at t0 + first
+  __device__ __forceinline__ static void ask(Raw& raw, const PageCache& c, const uint8_t* K, const uint8_t* V, int page, int t0, int first,
+                                             int lane) {
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+      const int ahead = first + token_of(tb, lane), p = __shfl(page, ahead, 64), part = lane >> 4;
+      const uint32_t t = (uint32_t)(t0 + ahead);
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) raw.k[tb][i] = raw.v[tb][i] = 0;
+      raw.ks[tb] = raw.vs[tb] = 0;
+      if ((uint32_t)p < (uint32_t)c.n_pages) {
+        const uint32_t row = t - t / c.by_ps * c.ps;
+        const int64_t at = p * c.page, codes = at + (int64_t)row * (D / 2) + part * (D / 8);
+        const int64_t scales = at + (int64_t)c.ps * (D / 2) + (int64_t)row * (D / 32) + part * (D / 4) / 32;
+        read_words(K + codes, raw.k[tb]);
+        read_words(V + codes, raw.v[tb]);
+        raw.ks[tb] = K[scales];
+        raw.vs[tb] = V[scales];
+      }
+    }
+  }
+  // Swizzle of a staged V row's 16-byte pieces: eight lanes that write together lie in eight rows, 0 .. 3 and 8 .. 11 of them, and sixteen
+  // that read in four, two pieces each.
+  __device__ __forceinline__ static int swizzle(int row) { return (row & 3) << 1 | (row >> 3 & 1); }
+  __device__ __forceinline__ static void stage_v(const Raw& raw, char* vt, int lane) {
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+      const int row = token_of(tb, lane);
+      const float by = fp4_power(raw.vs[tb]);
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i)
+        *reinterpret_cast<uint4*>(vt + row * (2 * D) + (((lane >> 4) * WORDS + i) ^ swizzle(row)) * 16) = fp4_to_bf16(raw.v[tb][i], by);
+    }
+  }
+  __device__ __forceinline__ void scores(const Raw& raw) {
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+      const float by = fp4_power(raw.ks[tb]);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const bf16x8 a = __builtin_bit_cast(bf16x8, fp4_to_bf16(raw.k[tb][kk], by));
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+          s[cb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[cb][kk], kk ? s[cb][tb] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      }
+    }
+  }
+  // live: a bit for each token that has a page
+  __device__ __forceinline__ void mask(int t0, uint32_t live, const int* lo, const int* last, int lane) {
+    const int own = 8 * (lane >> 4);
+    const uint32_t bits = live >> own;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const int from = lo[16 * cb + (lane & 15)], width = last[16 * cb + (lane & 15)] - from;  // (nothing: INT_MAX, and below 0)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int t = t0 + own + e - from;
+        s[cb][e >> 2][e & 3] = t >= 0 && t <= width && (bits >> e & 1) ? s[cb][e >> 2][e & 3] : -INFINITY;
+      }
+    }
+  }
+  __device__ __forceinline__ static float across_max(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return across_halves_max(max_of(__int_as_float(r[0]), __int_as_float(r[1])));
+  }
+  __device__ __forceinline__ static float across_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return across_halves_sum(__int_as_float(r[0]) + __int_as_float(r[1]));
+  }
+  // (as Softmax::move_bounds)
+  __device__ __forceinline__ void move_bounds(float sc) {
+    bool grow[CB], any = false;
+    float top[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      top[cb] = s[cb][0][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top[cb] = max_of(top[cb], s[cb][e >> 2][e & 3]);
+      top[cb] = across_max(top[cb]) * sc;
+      grow[cb] = !(top[cb] <= m[cb]);
+      any = any || grow[cb];
+    }
+    if (__builtin_amdgcn_ballot_w64(any) == 0) return;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const float to = grow[cb] ? top[cb] + 8.f : m[cb];
+      const float f = grow[cb] ? weight_of(m[cb], to) : 1.f;
+      m[cb] = to;
+      l[cb] *= f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[cb][db] *= f;
+    }
+  }
+  __device__ __forceinline__ void values(char* vt, float sc, int lane) {
+    bf16x8 p[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const float minus = m[cb] == -INFINITY ? 0.f : -m[cb];
+      f32x8 w;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(s[cb][e >> 2][e & 3], sc, minus));
+      // the unrounded weights' sum; rounded to bf16 for the product with V (as in Tile)
+      l[cb] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+      p[cb] = __builtin_convertvector(w, bf16x8);
+    }
+    const int i = lane & 15, row = 8 * (lane >> 4) + (i >> 2);
+    const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)vt + row * (2 * D) +
+                        ((((i & 3) >> 1) ^ swizzle(row)) << 4) + 8 * (i & 1);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const bf16x8 a = transposed8<D>((const bf16_t*)(const __attribute__((address_space(3))) bf16_t*)(uintptr_t)(at ^ (db << 5)));
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[cb], o[cb][db], 0, 0, 0);
+    }
+  }
+
+  // A unit of tile_kernel, whose columns lie in s_rh, s_lo, s_last; page: as look_up(begin) gives it; s_room: 32 rows of D values.
+  __device__ static __forceinline__ void run(const PagedArgs& x, bool window, int part, int seq, int begin, int end, int all_lo, int all_last,
+                                             int64_t base, int page, const int* s_rh, const int* s_lo, const int* s_last, char* s_room) {
+    const int lane = threadIdx.x & 63;
+    const uint8_t *const K = static_cast<const uint8_t*>(x.c.K) + base, *const V = static_cast<const uint8_t*>(x.c.V) + base;
+    const int32_t* const table = x.c.tables + (int64_t)seq * x.c.max_pages;
+    auto look_up = [&](int t0) { return t0 + lane < end ? table[(uint32_t)(t0 + lane) / x.c.by_ps] : -1; };
+    auto there = [&](int page) { return (uint64_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages); };
+    NarrowCodes n;
+    Raw raw[2];
+    uint64_t live = 0;
+    if (begin < end) {
+      live = there(page);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) ask(raw[k], x.c, K, V, page, begin, 32 * k, lane);
+      page = look_up(begin + 64);
+    }
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const int item = s_rh[cb * 16 + (lane & 15)];
+      const int rh = max(window ? item : item >> 5, 0);  // (a column of nobody reads some row: nothing is made of it)
+      const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+      const bf16_t* const from = static_cast<const bf16_t*>(x.Q) + h * x.a.qsh + row * x.a.qst + (lane >> 4) * (D / 4);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) n.q[cb][kk] = *reinterpret_cast<const bf16x8*>(from + 8 * kk);
+      n.m[cb] = -INFINITY;
+      n.l[cb] = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) n.o[cb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll 1
+    for (int t0 = begin; t0 < end; t0 += 64) {
+      const uint64_t next = there(page);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int t = t0 + 32 * k;
+        const uint32_t now = (uint32_t)(live >> (32 * k));
+        stage_v(raw[k], s_room, lane);
+        n.scores(raw[k]);
+        if (t0 + 64 < end) ask(raw[k], x.c, K, V, page, t0 + 64, 32 * k, lane);
+        if (t < all_lo || t + 31 > all_last || now != 0xffffffffu) n.mask(t, now, s_lo, s_last, lane);
+        n.move_bounds(x.scale_log2e);
+        n.values(s_room, x.scale_log2e, lane);
+      }
+      live = next;
+      page = look_up(t0 + 128);
+    }
+    // Results, as tile_kernel's: a column with a value that is not finite is marked.
+    const bool direct = x.p.count == 1;
+    constexpr int LPR = D / 8, RPI = 64 / LPR;  // lanes of a row, rows of an instruction
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const int item = s_rh[cb * 16 + (lane & 15)];
+      const float sum = across_sum(n.l[cb]), inv = 1.f / sum;
+      float check = 0.f, top = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          check = fmaf(n.o[cb][db][r], 0.f, check);
+          top = max_of(top, fabsf(n.o[cb][db][r]));
+        }
+      check = across_sum(check);
+      top = across_max(top);
+      const bool none = n.m[cb] == -INFINITY;
+      const float lse = none ? -INFINITY : check == 0.f ? n.m[cb] + __log2f(sum) : NAN;
+      auto record = [&](int item) {
+        return (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
+      };
+      const float scale = direct ? 1.f : scale_above(top * inv);
+      if (item >= 0 && lane < 16) {
+        const int64_t rec = record(item);
+        x.part_lse[rec] = lse;
+        if (direct && x.LSE) x.LSE[rec] = lse * kLn2;
+        if (!direct) x.part_scale[rec] = scale;
+      }
+      // d = 16 db + 4 (lane / 16) on: half of a 16-byte unit, swizzled by the row
+      auto put = [&](auto zero, float by) {
+        typedef decltype(zero) Out;
+        typedef Out Four __attribute__((ext_vector_type(4)));
+        const int row = lane & 15, part = lane >> 4;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          Four v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (Out)(none ? 0.f : n.o[cb][db][e] * by);
+          *reinterpret_cast<Four*>(s_room + (row * LPR + ((2 * db + (part >> 1)) ^ row % LPR)) * 16 + 8 * (part & 1)) = v;
+        }
+      };
+      if (direct) put(__bf16(), inv);
+      else put((_Float16)0, inv / scale);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      char* const to = static_cast<char*>(direct ? x.O : x.part_o);
+      const uint64_t write = __builtin_amdgcn_ballot_w64(item >= 0 && (direct || !none));
+#pragma unroll
+      for (int i = 0; i < 16 / RPI; ++i) {
+        const int row = i * RPI + lane / LPR, piece = lane % LPR;
+        if (!(write >> row & 1)) continue;
+        const uint4 v = *reinterpret_cast<const uint4*>(s_room + (row * LPR + (piece ^ row % LPR)) * 16);
+        *reinterpret_cast<uint4*>(to + record(s_rh[cb * 16 + row]) * (2 * D) + piece * 16) = v;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+};
+
 // NW wavefronts of 32 * CB columns, two stages of STEP tokens.  Measured (bf16, D = 128): four prompts of 2500 to 6000 tokens, 32:8 heads,
 // 770 us = 1.05 PFLOP/s, where a large library product reaches 1.2; 2000 rows behind 64K tokens, 32:4 heads, eight spans of 512, 215 us =
 // 0.66 PFLOP/s (tiles of 8 steps, whose beginnings and ends are a quarter of them); one token behind a million 49 us = 5.2 TB/s, 24 caches
@@ -858,8 +1109,9 @@ __device__ __forceinline__ void wait_loads() {
 //   ANY: pages of a size that is no multiple of 16: every row has a page of its own, at twice the instructions for its address
 //   PAST: records go past the caches
 template <typename T, int D, bool FP4, int NW, int CB, int STEP, bool ANY, bool PAST>
-__global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
-  constexpr int COLS = NW * 32 * CB;
+__global__ __launch_bounds__(64 * NW, FP4 && NW == 1 ? 3 - CB + 1 : NW == 1 || sizeof(T) == 4 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
+  constexpr bool CODES = FP4 && NW == 1;  // NarrowCodes
+  constexpr int COLS = CODES ? 16 * CB : NW * 32 * CB;
   extern __shared__ __align__(1024) char s_dynamic[];  // (static, the compiler would wait for staging loads at every read)
   T(*const s_kv)[2][STEP * D] = reinterpret_cast<T(*)[2][STEP * D]>(s_dynamic);
   __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS];
@@ -965,18 +1217,18 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
     if (row < at.r0 || row >= at.r1) return;
     head = h / x.a.G;
     seq = at.s;
-    const int own = (row - at.r0) * x.a.G + h - head * x.a.G, u0 = own & ~31;  // columns u0 .. u0 + 31 of the entry
+    const int own = (row - at.r0) * x.a.G + h - head * x.a.G, u0 = own & ~(COLS - 1);  // columns u0 .. of the entry
     const int pos = position_of(x, at, row);
     if (pos < 0 || j < 0 || j >= pos / x.a.S) {
       if (lane == 0) x.part_lse[(int64_t)rh * x.p.count + slot * x.p.routed + part] = -INFINITY;
       return;
     }
-    const int cols = min((min(at.r1, x.b.rows) - at.r0) * x.a.G - u0, 32);
+    const int cols = min((min(at.r1, x.b.rows) - at.r0) * x.a.G - u0, COLS);
     begin = any_lo = all_lo = j * x.a.S + part * x.p.routed_tokens;
     end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
     any_last = all_last = end - 1;
     ask_pages();  // (before the other columns' lists: a unit is short, and a chain of loads)
-    if (lane < 32) {
+    if (lane < COLS) {
       s_rh[lane] = -1;
       s_lo[lane] = INT_MAX;
       s_last[lane] = -1;
@@ -1006,6 +1258,10 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
   begin = begin / 16 * 16;
   head = __builtin_amdgcn_readfirstlane(head);
   const int64_t base = x.b.layer * x.c.layer + head * x.c.head;
+  if constexpr (CODES) {
+    NarrowCodes<D, CB>::run(x, window, part, seq, begin, end, all_lo, all_last, base, page, s_rh, s_lo, s_last, s_dynamic);
+    return;
+  }
   const T *const K = static_cast<const T*>(x.c.K), *const V = static_cast<const T*>(x.c.V);
   CodeStage<T, D, NW, STEP> codes;
   constexpr int GROUPS = STEP / 16;
@@ -1535,6 +1791,10 @@ struct Form {
   size_t o_bytes, lse_bytes, plan_bytes;
 };
 
+#ifndef CODE_UNITS
+#define CODE_UNITS 4096
+#endif
+constexpr int kCodeUnits = CODE_UNITS;
 Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   const int64_t rh = (int64_t)a.Hq * b.rows, window = a.S < b.L ? a.S : b.L;
   Form f = {};
@@ -1547,7 +1807,9 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   f.buckets = a.topk > 0 && (c.dtype == SL_BF16 ? items >= 3 * buckets : items >= 6 * buckets && items * a.S >= 1 << 19);
   // fp32: row by row where tiles of 128 columns would be all but empty.
   f.tiles = c.dtype == SL_BF16 || f.buckets || (a.topk == 0 && columns > 32 * (int64_t)b.B);
-  f.cols_log2 = (columns <= 32 * (int64_t)b.B || a.topk > 0) && !f.buckets          ? 5
+  const bool narrow = (columns <= 32 * (int64_t)b.B || a.topk > 0) && !f.buckets;
+  const bool codes = narrow && c.fp4 && c.dtype == SL_BF16;
+  f.cols_log2 = narrow                                                              ? (codes && columns <= 16 * (int64_t)b.B ? 4 : 5)
                 : c.dtype == SL_BF16 && columns * c.Hkv + items >= 256 * 1024 ? 8
                                                                              : 7;
   const int cols = 1 << f.cols_log2;
@@ -1566,7 +1828,7 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   p = {1, a.S, 1, (int)window, 0};
   if (a.topk > 0 && a.S <= b.L) {  // (no row has a longer span among its candidates)
     const int64_t units = f.buckets ? items / cols + 1 : items;
-    p.routed_tokens = (int)div_up(div_up(a.S, cut(a.S, units, 1024, 64)), 16) * 16;
+    p.routed_tokens = (int)div_up(div_up(a.S, cut(a.S, units, codes ? kCodeUnits : 1024, 64)), 16) * 16;
     p.routed = (int)div_up(a.S, p.routed_tokens);
   }
   if (f.tiles) {
@@ -1574,7 +1836,7 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
     const int64_t longest = window + cols / a.G + 17;  // a tile's rows may lie in two windows; it begins at a multiple of 16
     // Enough workgroups of the narrow form for what fits the chip at once, four or (D = 64) nine to a compute unit: 32 caches of 1000
     // tokens, 32:8 heads, 39 us with four times as many, 33 so; of the wide one, twice.
-    const int64_t n = cut(longest, (int64_t)f.plan.tiles * c.Hkv, cols == 32 && c.D == 64 ? 2048 : 1024, 256);
+    const int64_t n = cut(longest, (int64_t)f.plan.tiles * c.Hkv, codes ? kCodeUnits : cols == 32 && c.D == 64 ? 2048 : 1024, 256);
     p.window_tokens = (int)div_up(div_up(longest, n), 64) * 64;
     p.window = (int)div_up(longest, p.window_tokens);
     f.plan.window_units = div_up((int64_t)f.plan.tiles * p.window * c.Hkv, 8) * 8;
@@ -1604,7 +1866,7 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
 // The stages fill up to 128 KB of dynamic LDS beside the static arrays: more than a kernel has without asking.
 template <typename T, int D, bool FP4, int NW, int CB, int STEP, bool ANY, bool PAST>
 bool launch_tiles_as(const PagedArgs& x, const TilePlan& plan, hipStream_t st) {
-  constexpr int kBytes = 2 * 2 * STEP * D * (int)sizeof(T);
+  constexpr int kBytes = FP4 && NW == 1 ? 32 * D * (int)sizeof(T) : 2 * 2 * STEP * D * (int)sizeof(T);
   static std::mutex mu;
   static bool asked[64];
   int dev = -1;
@@ -1655,7 +1917,8 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
     }
     bool done;
     if constexpr (sizeof(T) == 2)
-      done = f.cols_log2 == 5   ? launch_tiles<T, D, FP4, 1, 1, 32>(x, f, plan, st)
+      done = f.cols_log2 == 4   ? launch_tiles<T, D, FP4, 1, 1, FP4 ? 64 : 32>(x, f, plan, st)
+             : f.cols_log2 == 5 ? launch_tiles<T, D, FP4, 1, FP4 ? 2 : 1, FP4 ? 64 : 32>(x, f, plan, st)
              : f.cols_log2 == 7 ? launch_tiles<T, D, FP4, 4, 1, 64>(x, f, plan, st)
                                 : launch_tiles<T, D, FP4, 4, 2, 64>(x, f, plan, st);
     else
