@@ -666,6 +666,7 @@ struct Softmax {
     if (__builtin_amdgcn_ballot_w64(any) == 0) return;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
+      grow[cb] = grow[cb] && top[cb] != -INFINITY;  // (nothing attended here: a bound that is NaN stays)
       const float to = grow[cb] ? top[cb] + 8.f : m[cb];
       const float f = grow[cb] ? weight_of(m[cb], to) : 1.f;
       m[cb] = to;
@@ -871,26 +872,44 @@ struct NarrowCodes {
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) w[i] = x[i];
   }
-  // page: of lane l, of token t0 + l; the block begins at t0 + first
+  // page: of lane l, of token t0 + l; the block begins at t0 + first.  A token without a page gets what lies in page 0: its score is masked,
+  // and `values_only` takes its V.  Where no 32 tokens lie in two pages their address is the wavefront's: no vector instruction is spent on
+  // it (a block has 130 without, and 200 with each lane's own; 40 caches of up to 200000 tokens MEASURE).
   __device__ __forceinline__ static void ask(Raw& raw, const PageCache& c, const uint8_t* K, const uint8_t* V, int page, int t0, int first,
                                              int lane) {
+    const int part = lane >> 4;
+    if (c.ps % 32 == 0) {
+      const uint32_t p = __builtin_amdgcn_readlane(page, first), t = __builtin_amdgcn_readfirstlane(t0 + first);
+      const uint32_t row = __builtin_amdgcn_readfirstlane(t - t / c.by_ps * c.ps);
+      const int64_t at = uniform64((int64_t)(p < (uint32_t)c.n_pages ? p : 0) * c.page);
+      const int64_t codes = at + (int64_t)row * (D / 2), scales = at + (int64_t)c.ps * (D / 2) + (int64_t)row * (D / 32);
+      const uint32_t mine = token_of(0, lane) * (D / 2) + part * (D / 8), my_scale = token_of(0, lane) * (D / 32) + part * (D / 4) / 32;
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb) {
+        read_words(K + codes + (mine + 4 * tb * (D / 2)), raw.k[tb]);
+        read_words(V + codes + (mine + 4 * tb * (D / 2)), raw.v[tb]);
+        raw.ks[tb] = (K + scales)[my_scale + 4 * tb * (D / 32)];
+        raw.vs[tb] = (V + scales)[my_scale + 4 * tb * (D / 32)];
+      }
+      return;
+    }
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
-      const int ahead = first + token_of(tb, lane), p = __shfl(page, ahead, 64), part = lane >> 4;
-      const uint32_t t = (uint32_t)(t0 + ahead);
-#pragma unroll
-      for (int i = 0; i < WORDS; ++i) raw.k[tb][i] = raw.v[tb][i] = 0;
-      raw.ks[tb] = raw.vs[tb] = 0;
-      if ((uint32_t)p < (uint32_t)c.n_pages) {
-        const uint32_t row = t - t / c.by_ps * c.ps;
-        const int64_t at = p * c.page, codes = at + (int64_t)row * (D / 2) + part * (D / 8);
-        const int64_t scales = at + (int64_t)c.ps * (D / 2) + (int64_t)row * (D / 32) + part * (D / 4) / 32;
-        read_words(K + codes, raw.k[tb]);
-        read_words(V + codes, raw.v[tb]);
-        raw.ks[tb] = K[scales];
-        raw.vs[tb] = V[scales];
-      }
+      const int ahead = first + token_of(tb, lane);
+      const uint32_t p = __shfl(page, ahead, 64), t = (uint32_t)(t0 + ahead), row = t - t / c.by_ps * c.ps;
+      const int64_t at = (int64_t)(p < (uint32_t)c.n_pages ? p : 0) * c.page, codes = at + (int64_t)row * (D / 2) + part * (D / 8);
+      const int64_t scales = at + (int64_t)c.ps * (D / 2) + (int64_t)row * (D / 32) + part * (D / 4) / 32;
+      read_words(K + codes, raw.k[tb]);
+      read_words(V + codes, raw.v[tb]);
+      raw.ks[tb] = K[scales];
+      raw.vs[tb] = V[scales];
     }
+  }
+  // Values of tokens that there are, of 32: what else lies there may be NaN, and zero times that need not be zero.
+  __device__ __forceinline__ static void values_only(Raw& raw, uint32_t live, int lane) {
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb)
+      if (!(live >> token_of(tb, lane) & 1)) raw.vs[tb] = 0;
   }
   // Swizzle of a staged V row's 16-byte pieces: eight lanes that write together lie in eight rows, 0 .. 3 and 8 .. 11 of them, and sixteen
   // that read in four, two pieces each.
@@ -956,6 +975,7 @@ struct NarrowCodes {
     if (__builtin_amdgcn_ballot_w64(any) == 0) return;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
+      grow[cb] = grow[cb] && top[cb] != -INFINITY;  // (nothing attended here: a bound that is NaN stays)
       const float to = grow[cb] ? top[cb] + 8.f : m[cb];
       const float f = grow[cb] ? weight_of(m[cb], to) : 1.f;
       m[cb] = to;
@@ -1024,6 +1044,7 @@ struct NarrowCodes {
       for (int k = 0; k < 2; ++k) {
         const int t = t0 + 32 * k;
         const uint32_t now = (uint32_t)(live >> (32 * k));
+        if (now != 0xffffffffu) values_only(raw[k], now, lane);
         stage_v(raw[k], s_room, lane);
         n.scores(raw[k]);
         if (t0 + 64 < end) ask(raw[k], x.c, K, V, page, t0 + 64, 32 * k, lane);
@@ -1112,6 +1133,7 @@ template <typename T, int D, bool FP4, int NW, int CB, int STEP, bool ANY, bool 
 __global__ __launch_bounds__(64 * NW, FP4 && NW == 1 ? 3 - CB + 1 : NW == 1 || sizeof(T) == 4 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
   constexpr bool CODES = FP4 && NW == 1;  // NarrowCodes
   constexpr int COLS = CODES ? 16 * CB : NW * 32 * CB;
+  constexpr int ALIGN = CODES ? 32 : 16;  // a tile's first token is a multiple of it
   extern __shared__ __align__(1024) char s_dynamic[];  // (static, the compiler would wait for staging loads at every read)
   T(*const s_kv)[2][STEP * D] = reinterpret_cast<T(*)[2][STEP * D]>(s_dynamic);
   __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS];
@@ -1135,7 +1157,7 @@ __global__ __launch_bounds__(64 * NW, FP4 && NW == 1 ? 3 - CB + 1 : NW == 1 || s
     seq = __builtin_amdgcn_readfirstlane(seq);
     begin = __builtin_amdgcn_readfirstlane(begin);
     end = __builtin_amdgcn_readfirstlane(end);
-    if (begin < end) page = look_up(begin / 16 * 16);
+    if (begin < end) page = look_up(begin / ALIGN * ALIGN);
   };
   // columns
   if (window) {
@@ -1255,7 +1277,7 @@ __global__ __launch_bounds__(64 * NW, FP4 && NW == 1 ? 3 - CB + 1 : NW == 1 || s
   any_last = __builtin_amdgcn_readfirstlane(any_last);
   all_lo = __builtin_amdgcn_readfirstlane(all_lo);
   all_last = __builtin_amdgcn_readfirstlane(all_last);
-  begin = begin / 16 * 16;
+  begin = begin / ALIGN * ALIGN;
   head = __builtin_amdgcn_readfirstlane(head);
   const int64_t base = x.b.layer * x.c.layer + head * x.c.head;
   if constexpr (CODES) {

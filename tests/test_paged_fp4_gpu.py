@@ -325,6 +325,30 @@ def test_blocks_that_are_not_finite_where_some_rows_attend(tensor, dtype, n, ps,
         assert float((x - w).abs().max()) <= (2.0 ** -7 * 6 if dtype == BF16 else 1e-4)
 
 
+@pytest.mark.parametrize("held", ["4 bits", "rows"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,topk", [(1, 0), (3, 0), (160, 0), (3, 2), (160, 2)])
+def test_a_key_that_is_nan_before_tokens_that_a_row_does_not_attend(n, topk, dtype, held):
+    """The last tokens that a row attends are NaN, what its tile goes on with is masked for it: the row is NaN all the same."""
+    from tests.test_paged_gpu import make_cache as make_rows
+    g = torch.Generator().manual_seed(n)
+    L, ps = 2000, 32
+    cache = make_cache(g, [L], ps, 1, 64, dtype) if held == "4 bits" else make_rows(g, [L], ps, 1, 64, dtype)
+    bad = L - n  # the first new token: every row attends it, the first one as its last
+    if held == "4 bits":
+        cache.K[0, int(cache.tables[0, bad // ps]), :, ps * 32 + bad % ps * 2] = 255
+    else:
+        cache.K[0, int(cache.tables[0, bad // ps]), :, bad % ps, 3] = math.nan
+    Q = torch.randn((2, n, 64), generator=g).to(dtype).to(DEV)
+    idx = torch.tensor([0, 3], dtype=torch.int32, device=DEV).expand(2, n, 2).contiguous() if topk else None
+    S = 500 if topk else 4000
+    O, LSE = B.sl_paged_span_attention(cache, i32([0]), i32([0, n]), Q, idx, S)
+    assert bool(torch.isnan(O).all()) and bool(torch.isnan(LSE).all())
+    if topk:
+        O = B.sl_paged_span_attention_combined(cache, i32([0]), i32([0, n]), Q, idx, torch.zeros(idx.shape, device=DEV), S)
+        assert bool(torch.isnan(O).all())
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_results_do_not_change_from_run_to_run(dtype):
     g = torch.Generator().manual_seed(23)
