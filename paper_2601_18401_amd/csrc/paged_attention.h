@@ -852,7 +852,8 @@ __device__ __forceinline__ void wait_loads() {
 // (Lane l of a 16x16 result holds column l % 16 and rows 4 (l / 16) + r.  Row m of the token block tb of two is token 8 (m / 4) + 4 tb +
 // m % 4, so that a lane's eight accumulators are eight consecutive tokens, 8 (l / 16) on.)  A lane's codes of K and V are of the same tokens
 // and channels, D / 4 of them: one address for both.  Codes are asked for 64 tokens ahead.
-template <int D, int CB>
+// EASY: no 32 tokens that begin at a multiple of 32 lie in two pages.
+template <int D, int CB, bool EASY>
 struct NarrowCodes {
   static constexpr int KK = D / 32, DB = D / 16, WORDS = D / 32;  // products of a token block; blocks of 16 channels; words of a lane's codes
   typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -863,8 +864,13 @@ struct NarrowCodes {
   // the codes of K and V of 32 tokens
   struct Raw {
     uint32_t k[2][WORDS], v[2][WORDS];
-    int ks[2], vs[2];
+    uint32_t ks[2], vs[2];  // four bytes with their scale, `shift` bits up
+    int shift[2];
+    __device__ __forceinline__ uint32_t k_scale(int tb) const { return ks[tb] >> shift[tb] & 255; }
+    __device__ __forceinline__ uint32_t v_scale(int tb) const { return vs[tb] >> shift[tb] & 255; }
   };
+  // scales from `at` on, which are D / 32 bytes, and what shares their four
+  __device__ __forceinline__ static uint32_t read_scales(const uint8_t* at) { return *reinterpret_cast<const uint32_t*>(at); }
   __device__ __forceinline__ static int token_of(int tb, int lane) { return 8 * ((lane & 15) >> 2) + 4 * tb + (lane & 3); }
   __device__ __forceinline__ static void read_words(const uint8_t* from, uint32_t (&w)[WORDS]) {
     typedef uint32_t Words __attribute__((ext_vector_type(WORDS)));
@@ -878,18 +884,19 @@ struct NarrowCodes {
   __device__ __forceinline__ static void ask(Raw& raw, const PageCache& c, const uint8_t* K, const uint8_t* V, int page, int t0, int first,
                                              int lane) {
     const int part = lane >> 4;
-    if (c.ps % 32 == 0) {
+    if constexpr (EASY) {
       const uint32_t p = __builtin_amdgcn_readlane(page, first), t = __builtin_amdgcn_readfirstlane(t0 + first);
       const uint32_t row = __builtin_amdgcn_readfirstlane(t - t / c.by_ps * c.ps);
       const int64_t at = uniform64((int64_t)(p < (uint32_t)c.n_pages ? p : 0) * c.page);
       const int64_t codes = at + (int64_t)row * (D / 2), scales = at + (int64_t)c.ps * (D / 2) + (int64_t)row * (D / 32);
-      const uint32_t mine = token_of(0, lane) * (D / 2) + part * (D / 8), my_scale = token_of(0, lane) * (D / 32) + part * (D / 4) / 32;
+      const uint32_t mine = token_of(0, lane) * (D / 2) + part * (D / 8), my_scale = token_of(0, lane) * (D / 32);
 #pragma unroll
       for (int tb = 0; tb < 2; ++tb) {
         read_words(K + codes + (mine + 4 * tb * (D / 2)), raw.k[tb]);
         read_words(V + codes + (mine + 4 * tb * (D / 2)), raw.v[tb]);
-        raw.ks[tb] = (K + scales)[my_scale + 4 * tb * (D / 32)];
-        raw.vs[tb] = (V + scales)[my_scale + 4 * tb * (D / 32)];
+        raw.ks[tb] = read_scales(K + scales + ((my_scale & ~3u) + 4 * tb * (D / 32)));
+        raw.vs[tb] = read_scales(V + scales + ((my_scale & ~3u) + 4 * tb * (D / 32)));
+        raw.shift[tb] = 8 * ((my_scale & 3) + part * (D / 4) / 32);
       }
       return;
     }
@@ -898,11 +905,12 @@ struct NarrowCodes {
       const int ahead = first + token_of(tb, lane);
       const uint32_t p = __shfl(page, ahead, 64), t = (uint32_t)(t0 + ahead), row = t - t / c.by_ps * c.ps;
       const int64_t at = (int64_t)(p < (uint32_t)c.n_pages ? p : 0) * c.page, codes = at + (int64_t)row * (D / 2) + part * (D / 8);
-      const int64_t scales = at + (int64_t)c.ps * (D / 2) + (int64_t)row * (D / 32) + part * (D / 4) / 32;
+      const int64_t scales = at + (int64_t)c.ps * (D / 2) + (int64_t)row * (D / 32);
       read_words(K + codes, raw.k[tb]);
       read_words(V + codes, raw.v[tb]);
-      raw.ks[tb] = K[scales];
-      raw.vs[tb] = V[scales];
+      raw.ks[tb] = read_scales(K + (scales & ~(int64_t)3));
+      raw.vs[tb] = read_scales(V + (scales & ~(int64_t)3));
+      raw.shift[tb] = 8 * (((int)scales & 3) + part * (D / 4) / 32);
     }
   }
   // Values of tokens that there are, of 32: what else lies there may be NaN, and zero times that need not be zero.
@@ -918,7 +926,7 @@ struct NarrowCodes {
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
       const int row = token_of(tb, lane);
-      const float by = fp4_power(raw.vs[tb]);
+      const float by = fp4_power(raw.v_scale(tb));
 #pragma unroll
       for (int i = 0; i < WORDS; ++i)
         *reinterpret_cast<uint4*>(vt + row * (2 * D) + (((lane >> 4) * WORDS + i) ^ swizzle(row)) * 16) = fp4_to_bf16(raw.v[tb][i], by);
@@ -926,15 +934,23 @@ struct NarrowCodes {
   }
   __device__ __forceinline__ void scores(const Raw& raw) {
 #pragma unroll
-    for (int tb = 0; tb < 2; ++tb) {
-      const float by = fp4_power(raw.ks[tb]);
+    for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        const bf16x8 a = __builtin_bit_cast(bf16x8, fp4_to_bf16(raw.k[tb][kk], by));
+      for (int tb = 0; tb < 2; ++tb) {
+        const bf16x8 a = __builtin_bit_cast(bf16x8, fp4_to_bf16(raw.k[tb][kk], fp4_power(raw.k_scale(tb))));
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb)
           s[cb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[cb][kk], kk ? s[cb][tb] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
       }
+  }
+  // What has been asked for is here from this point on, and nothing is made of it before: the compiler would work on it, or move it to other
+  // registers, as soon as it had been asked for, and wait there.
+  __device__ __forceinline__ static void arrive(Raw& raw) {
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) asm volatile("" : "+v"(raw.v[tb][i]), "+v"(raw.k[tb][i]));
+      asm volatile("" : "+v"(raw.vs[tb]), "+v"(raw.ks[tb]));
     }
   }
   // live: a bit for each token that has a page
@@ -999,12 +1015,22 @@ struct NarrowCodes {
     const int i = lane & 15, row = 8 * (lane >> 4) + (i >> 2);
     const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)vt + row * (2 * D) +
                         ((((i & 3) >> 1) ^ swizzle(row)) << 4) + 8 * (i & 1);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       const bf16x8 a = transposed8<D>((const bf16_t*)(const __attribute__((address_space(3))) bf16_t*)(uintptr_t)(at ^ (db << 5)));
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[cb], o[cb][db], 0, 0, 0);
     }
+    // reads run three products ahead (0x100 = LDS read, 0x008 = MFMA)
+    __builtin_amdgcn_sched_group_barrier(0x100, 6, 2);
+#pragma unroll
+    for (int db = 0; db < DB - 3; ++db) {
+      __builtin_amdgcn_sched_group_barrier(0x008, CB, 2);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 2);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 3 * CB, 2);
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   // A unit of tile_kernel, whose columns lie in s_rh, s_lo, s_last; page: as look_up(begin) gives it; s_room: 32 rows of D values.
@@ -1013,17 +1039,14 @@ struct NarrowCodes {
     const int lane = threadIdx.x & 63;
     const uint8_t *const K = static_cast<const uint8_t*>(x.c.K) + base, *const V = static_cast<const uint8_t*>(x.c.V) + base;
     const int32_t* const table = x.c.tables + (int64_t)seq * x.c.max_pages;
-    auto look_up = [&](int t0) { return t0 + lane < end ? table[(uint32_t)(t0 + lane) / x.c.by_ps] : -1; };
-    auto there = [&](int page) { return (uint64_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages); };
+    // (the last token's page beyond the end, which `there` takes back: a load in a branch may not have been made)
+    auto look_up = [&](int t0) { return table[(uint32_t)min(t0 + lane, end - 1) / x.c.by_ps]; };
+    auto there = [&](int page, int t0) {
+      return (uint64_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages && t0 + lane < end);
+    };
     NarrowCodes n;
     Raw raw[2];
     uint64_t live = 0;
-    if (begin < end) {
-      live = there(page);
-#pragma unroll
-      for (int k = 0; k < 2; ++k) ask(raw[k], x.c, K, V, page, begin, 32 * k, lane);
-      page = look_up(begin + 64);
-    }
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       const int item = s_rh[cb * 16 + (lane & 15)];
@@ -1037,24 +1060,44 @@ struct NarrowCodes {
 #pragma unroll
       for (int db = 0; db < DB; ++db) n.o[cb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-#pragma unroll 1
-    for (int t0 = begin; t0 < end; t0 += 64) {
-      const uint64_t next = there(page);
+    if (begin < end) {
+      live = there(page, begin);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) ask(raw[k], x.c, K, V, page, begin, 32 * k, lane);
+      page = look_up(begin + 64);
+    }
+    // (a query that may not have come yet would be waited for in every turn, and what was asked for later with it)
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(n.q[cb][kk]));
+    // Loads come back in order: pages are asked for before a turn's codes, and the last turn, which asks for none, has code of its own.  (A
+    // wait for a page behind the codes, or for codes that may not have been asked for, is one for all that is on its way: MEASURE.)
+    auto turn = [&](auto more, int t0) {
+      const uint64_t next = decltype(more)::value ? there(page, t0 + 64) : 0;
+      const int after = decltype(more)::value ? look_up(t0 + 128) : -1;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int t = t0 + 32 * k;
         const uint32_t now = (uint32_t)(live >> (32 * k));
+        arrive(raw[k]);
         if (now != 0xffffffffu) values_only(raw[k], now, lane);
         stage_v(raw[k], s_room, lane);
         n.scores(raw[k]);
-        if (t0 + 64 < end) ask(raw[k], x.c, K, V, page, t0 + 64, 32 * k, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(more)::value) ask(raw[k], x.c, K, V, page, t0 + 64, 32 * k, lane);
+        __builtin_amdgcn_sched_barrier(0);
         if (t < all_lo || t + 31 > all_last || now != 0xffffffffu) n.mask(t, now, s_lo, s_last, lane);
         n.move_bounds(x.scale_log2e);
         n.values(s_room, x.scale_log2e, lane);
       }
       live = next;
-      page = look_up(t0 + 128);
-    }
+      page = after;
+    };
+    int t0 = begin;
+#pragma unroll 1
+    for (; t0 + 64 < end; t0 += 64) turn(std::true_type(), t0);
+    if (t0 < end) turn(std::false_type(), t0);
     // Results, as tile_kernel's: a column with a value that is not finite is marked.
     const bool direct = x.p.count == 1;
     constexpr int LPR = D / 8, RPI = 64 / LPR;  // lanes of a row, rows of an instruction
@@ -1150,7 +1193,7 @@ __global__ __launch_bounds__(64 * NW, FP4 && NW == 1 ? 3 - CB + 1 : NW == 1 || s
   // ANY: lane l has the page of row l of the next stage.
   int page = -1;
   auto look_up = [&](int t0) {
-    const int ln = lane_now(), t = t0 + (ANY ? ln % STEP : ln * 16);
+    const int ln = lane_now(), t = t0 + (ANY || FP4 ? ln % STEP : ln * 16);
     return t < end ? x.c.tables[(int64_t)seq * x.c.max_pages + (uint32_t)t / x.c.by_ps] : -1;
   };
   auto ask_pages = [&] {
@@ -1281,7 +1324,7 @@ __global__ __launch_bounds__(64 * NW, FP4 && NW == 1 ? 3 - CB + 1 : NW == 1 || s
   head = __builtin_amdgcn_readfirstlane(head);
   const int64_t base = x.b.layer * x.c.layer + head * x.c.head;
   if constexpr (CODES) {
-    NarrowCodes<D, CB>::run(x, window, part, seq, begin, end, all_lo, all_last, base, page, s_rh, s_lo, s_last, s_dynamic);
+    NarrowCodes<D, CB, !ANY>::run(x, window, part, seq, begin, end, all_lo, all_last, base, page, s_rh, s_lo, s_last, s_dynamic);
     return;
   }
   const T *const K = static_cast<const T*>(x.c.K), *const V = static_cast<const T*>(x.c.V);
@@ -1906,6 +1949,9 @@ bool launch_tiles_as(const PagedArgs& x, const TilePlan& plan, hipStream_t st) {
 template <typename T, int D, bool FP4, int NW, int CB, int STEP>
 bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
   const bool past = NW > 1 && f.o_bytes >= kStreamedRecords;
+  if constexpr (FP4 && NW == 1) {
+    if (x.c.ps % 32 == 0) return launch_tiles_as<T, D, FP4, NW, CB, STEP, false, false>(x, plan, st);
+  }
   if constexpr (!FP4) {
     if (x.c.ps % 16 == 0) {
       if constexpr (NW > 1)
