@@ -857,8 +857,8 @@ template <int D, int CB, bool EASY>
 struct NarrowCodes {
   static constexpr int KK = D / 32, DB = D / 16, WORDS = D / 32;  // products of a token block; blocks of 16 channels; words of a lane's codes
   typedef float f32x4 __attribute__((ext_vector_type(4)));
-  f32x4 o[CB][DB], s[CB][2];
-  bf16x8 q[CB][KK];
+  f32x4 o[CB][DB], s[CB][4];  // s: of 64 tokens, two of each 32
+  bf16x8 q[CB][KK], p[CB][2];
   float m[CB], l[CB];
 
   // the codes of K and V of 32 tokens
@@ -932,7 +932,8 @@ struct NarrowCodes {
         *reinterpret_cast<uint4*>(vt + row * (2 * D) + (((lane >> 4) * WORDS + i) ^ swizzle(row)) * 16) = fp4_to_bf16(raw.v[tb][i], by);
     }
   }
-  __device__ __forceinline__ void scores(const Raw& raw) {
+  // k: first or second 32 tokens of a turn
+  __device__ __forceinline__ void scores(const Raw& raw, int k) {
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
@@ -940,7 +941,7 @@ struct NarrowCodes {
         const bf16x8 a = __builtin_bit_cast(bf16x8, fp4_to_bf16(raw.k[tb][kk], fp4_power(raw.k_scale(tb))));
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb)
-          s[cb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[cb][kk], kk ? s[cb][tb] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          s[cb][2 * k + tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[cb][kk], kk ? s[cb][2 * k + tb] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
       }
   }
   // What has been asked for is here from this point on, and nothing is made of it before: the compiler would work on it, or move it to other
@@ -953,17 +954,21 @@ struct NarrowCodes {
       asm volatile("" : "+v"(raw.vs[tb]), "+v"(raw.ks[tb]));
     }
   }
-  // live: a bit for each token that has a page
-  __device__ __forceinline__ void mask(int t0, uint32_t live, const int* lo, const int* last, int lane) {
+  // live: a bit for each of 64 tokens that has a page
+  __device__ __forceinline__ void mask(int t0, uint64_t live, const int* lo, const int* last, int lane) {
     const int own = 8 * (lane >> 4);
-    const uint32_t bits = live >> own;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       const int from = lo[16 * cb + (lane & 15)], width = last[16 * cb + (lane & 15)] - from;  // (nothing: INT_MAX, and below 0)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int t = t0 + own + e - from;
-        s[cb][e >> 2][e & 3] = t >= 0 && t <= width && (bits >> e & 1) ? s[cb][e >> 2][e & 3] : -INFINITY;
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t bits = (uint32_t)(live >> (32 * k)) >> own;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int t = t0 + 32 * k + own + e - from;
+          f32x4& v = s[cb][2 * k + (e >> 2)];
+          v[e & 3] = t >= 0 && t <= width && (bits >> e & 1) ? v[e & 3] : -INFINITY;
+        }
       }
     }
   }
@@ -983,7 +988,7 @@ struct NarrowCodes {
     for (int cb = 0; cb < CB; ++cb) {
       top[cb] = s[cb][0][0];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) top[cb] = max_of(top[cb], s[cb][e >> 2][e & 3]);
+      for (int e = 1; e < 16; ++e) top[cb] = max_of(top[cb], s[cb][e >> 2][e & 3]);
       top[cb] = across_max(top[cb]) * sc;
       grow[cb] = !(top[cb] <= m[cb]);
       any = any || grow[cb];
@@ -1000,37 +1005,41 @@ struct NarrowCodes {
       for (int db = 0; db < DB; ++db) o[cb][db] *= f;
     }
   }
-  __device__ __forceinline__ void values(char* vt, float sc, int lane) {
-    bf16x8 p[CB];
+  __device__ __forceinline__ void weights(float sc) {
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       const float minus = m[cb] == -INFINITY ? 0.f : -m[cb];
-      f32x8 w;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(s[cb][e >> 2][e & 3], sc, minus));
-      // the unrounded weights' sum; rounded to bf16 for the product with V (as in Tile)
-      l[cb] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-      p[cb] = __builtin_convertvector(w, bf16x8);
+      for (int k = 0; k < 2; ++k) {
+        f32x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = fast_exp2(fmaf(s[cb][2 * k + (e >> 2)][e & 3], sc, minus));
+        // the unrounded weights' sum; rounded to bf16 for the product with V (as in Tile)
+        l[cb] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        p[cb][k] = __builtin_convertvector(w, bf16x8);
+      }
     }
+  }
+  template <int k>
+  __device__ __forceinline__ void values(char* vt, int lane) {
     const int i = lane & 15, row = 8 * (lane >> 4) + (i >> 2);
     const uint32_t at = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)vt + row * (2 * D) +
                         ((((i & 3) >> 1) ^ swizzle(row)) << 4) + 8 * (i & 1);
-    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       const bf16x8 a = transposed8<D>((const bf16_t*)(const __attribute__((address_space(3))) bf16_t*)(uintptr_t)(at ^ (db << 5)));
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb) o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[cb], o[cb][db], 0, 0, 0);
+      for (int cb = 0; cb < CB; ++cb) o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[cb][k], o[cb][db], 0, 0, 0);
     }
-    // reads run three products ahead (0x100 = LDS read, 0x008 = MFMA)
-    __builtin_amdgcn_sched_group_barrier(0x100, 6, 2);
+    // reads run ahead of their products (0x100 = LDS read, 0x008 = MFMA)
+    constexpr int AHEAD = DB < 6 ? DB : 6;
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 2 + k);
 #pragma unroll
-    for (int db = 0; db < DB - 3; ++db) {
-      __builtin_amdgcn_sched_group_barrier(0x008, CB, 2);
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 2);
+    for (int db = 0; db < DB - AHEAD; ++db) {
+      __builtin_amdgcn_sched_group_barrier(0x008, CB, 2 + k);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 2 + k);
     }
-    __builtin_amdgcn_sched_group_barrier(0x008, 3 * CB, 2);
-    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * CB, 2 + k);
   }
 
   // A unit of tile_kernel, whose columns lie in s_rh, s_lo, s_last; page: as look_up(begin) gives it; s_room: 32 rows of D values.
@@ -1076,21 +1085,29 @@ struct NarrowCodes {
     auto turn = [&](auto more, int t0) {
       const uint64_t next = decltype(more)::value ? there(page, t0 + 64) : 0;
       const int after = decltype(more)::value ? look_up(t0 + 128) : -1;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int t = t0 + 32 * k;
-        const uint32_t now = (uint32_t)(live >> (32 * k));
+      const uint64_t now = live;
+      auto come = [&](int k) {
         arrive(raw[k]);
-        if (now != 0xffffffffu) values_only(raw[k], now, lane);
-        stage_v(raw[k], s_room, lane);
-        n.scores(raw[k]);
+        if ((uint32_t)(now >> (32 * k)) != 0xffffffffu) values_only(raw[k], (uint32_t)(now >> (32 * k)), lane);
+      };
+      auto go_on = [&](int k) {
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (decltype(more)::value) ask(raw[k], x.c, K, V, page, t0 + 64, 32 * k, lane);
         __builtin_amdgcn_sched_barrier(0);
-        if (t < all_lo || t + 31 > all_last || now != 0xffffffffu) n.mask(t, now, s_lo, s_last, lane);
-        n.move_bounds(x.scale_log2e);
-        n.values(s_room, x.scale_log2e, lane);
-      }
+      };
+      come(0);
+      stage_v(raw[0], s_room, lane);
+      n.scores(raw[0], 0);
+      go_on(0);
+      come(1);
+      n.scores(raw[1], 1);
+      if (t0 < all_lo || t0 + 63 > all_last || now != ~(uint64_t)0) n.mask(t0, now, s_lo, s_last, lane);
+      n.move_bounds(x.scale_log2e);
+      n.weights(x.scale_log2e);
+      n.template values<0>(s_room, lane);
+      stage_v(raw[1], s_room, lane);
+      go_on(1);
+      n.template values<1>(s_room, lane);
       live = next;
       page = after;
     };
@@ -1275,7 +1292,8 @@ __global__ __launch_bounds__(64 * NW, FP4 && NW == 1 ? 3 - CB + 1 : NW == 1 || s
     const int64_t u = unit - plan.window_units;
     part = (int)(u % x.p.routed);
     const int64_t item = u / x.p.routed;
-    const int slot = (int)(item % x.a.topk), rh = (int)(item / x.a.topk);
+    // (workgroups u = x (mod 8) run on XCD x: by rh, so that no XCD has the first slots of all, which are filled more often than the last)
+    const int rh = (int)(item / x.a.topk), slot = (int)((item + rh) % x.a.topk);
     const int h = rh / x.b.rows, row = rh - h * x.b.rows;
     const int j = x.idx[h * x.a.ish + row * x.a.ist + slot];
     const Entry at = entry_with_row(x, row);
