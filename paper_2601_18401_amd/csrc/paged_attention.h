@@ -6,6 +6,7 @@
 // FP4: the cache is held in 4 bits (fp4.h); T is the rows' type all the same.
 #pragma once
 
+#include <algorithm>
 #include <climits>
 #include <mutex>
 #include <type_traits>
@@ -45,6 +46,7 @@ struct TilePlan {
   int tiles;             // window tiles of a kv head
   int64_t window_units;  // tiles * pieces of a window * Hkv
   int64_t units;         // ... and the spans' pieces: workgroups that have something to do
+  int slots, groups;     // codes_kernel: slots of a unit, units of a row's slots
   int spans, buckets;    // spans of the longest sequence; B * Hkv * spans
   int32_t *counts, *first_tile;  // [buckets]
   int most_tiles;  // of the buckets; a multiple of 8
@@ -845,6 +847,334 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("" ::: "memory");
 }
 
+// NW wavefronts of 32 * CB columns, two stages of STEP tokens.  Measured (bf16, D = 128): four prompts of 2500 to 6000 tokens, 32:8 heads,
+// 770 us = 1.05 PFLOP/s, where a large library product reaches 1.2; 2000 rows behind 64K tokens, 32:4 heads, eight spans of 512, 215 us =
+// 0.66 PFLOP/s (tiles of 8 steps, whose beginnings and ends are a quarter of them); one token behind a million 49 us = 5.2 TB/s, 24 caches
+// of up to 120000 tokens 93 us = 5.6 TB/s, where a pure read reaches 6.4.
+//   4 wavefronts: the matrix cores are what bounds these
+//   1 wavefront: few columns, so that memory does; four workgroups (D = 128) of a compute unit have 16 KB each on the way
+//                (three and four stages leave room for fewer: 24 caches of up to 120000 tokens 119 -> 122, 153 us)
+// Workgroups of the window come first, then, of the spans' pieces,
+//   4 wavefronts: the buckets' tiles
+//   1 wavefront: one for every (row, head, slot).  Other heads and rows of its 32 columns may list the same span: the first one
+//                that does takes it for all, so that a span is read once for the group.
+//   ANY: pages of a size that is no multiple of 16: every row has a page of its own, at twice the instructions for its address
+//   PAST: records go past the caches
+template <typename T, int D, bool FP4, int NW, int CB, int STEP, bool ANY, bool PAST>
+__global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
+  constexpr int COLS = NW * 32 * CB;
+  extern __shared__ __align__(1024) char s_dynamic[];  // (static, the compiler would wait for staging loads at every read)
+  T(*const s_kv)[2][STEP * D] = reinterpret_cast<T(*)[2][STEP * D]>(s_dynamic);
+  __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS];
+  const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t unit = workgroup();
+  if (unit >= plan.units) return;  // (grid_of rounds up)
+  const bool window = unit < plan.window_units;
+  int seq, head, part;         // sequence, kv head, piece
+  int begin, end;              // tokens [begin, end) of the tile
+  int any_lo, any_last;        // ... that any of the wavefront's columns attends
+  int all_lo, all_last;        // ... that all of them attend
+  // The pages of the first rows are asked for as soon as a tile knows its sequence and tokens.
+  // !ANY: lane g has the page of the g-th sixteen tokens from `batch` on; the next 64 pages are looked up while those are in use.
+  // ANY: lane l has the page of row l of the next stage.
+  int page = -1;
+  auto look_up = [&](int t0) {
+    const int ln = lane_now(), t = t0 + (ANY ? ln % STEP : ln * 16);
+    return t < end ? x.c.tables[(int64_t)seq * x.c.max_pages + (uint32_t)t / x.c.by_ps] : -1;
+  };
+  auto ask_pages = [&] {
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    begin = __builtin_amdgcn_readfirstlane(begin);
+    end = __builtin_amdgcn_readfirstlane(end);
+    if (begin < end) page = look_up(begin / 16 * 16);
+  };
+  // columns
+  if (window) {
+    // (tile, piece) of the kv heads in turn; the last tiles first, whose ranges are the longest
+    head = (int)(unit % x.c.Hkv);
+    const int at = (int)(unit / x.c.Hkv);
+    if (at >= plan.tiles * x.p.window) return;
+    const int tile = plan.tiles - 1 - at / x.p.window, piece = at % x.p.window;
+    part = x.a.topk * x.p.routed + piece;
+    const ColumnRun run = columns_of(x, tile, COLS, x.a.G);
+    if (run.n <= 0) return;
+    const int r0 = run.at.r0, u0 = run.u0, len = run.at.len, pos0 = len - (run.at.r1 - r0);
+    seq = run.at.s;
+    const int first = max(pos0 + u0 / x.a.G, 0);  // position of the tile's first row that has a token
+    const int most = min(len, x.b.L) - 1;         // of the last row that has one
+    const int64_t origin = (int64_t)(first / x.a.S) * x.a.S / 16 * 16 + (int64_t)piece * x.p.window_tokens;
+    const int from = (int)min(origin, (int64_t)INT_MAX), upto = (int)min(origin + x.p.window_tokens - 1, (int64_t)INT_MAX);
+    auto lo_of = [&](int pos) { return max(pos / x.a.S * x.a.S, from); };
+    auto last_of = [&](int pos) { return min(pos, upto); };
+    // Later rows begin and end no earlier.
+    const int last = min(pos0 + (u0 + run.n - 1) / x.a.G, most);
+    begin = lo_of(first);
+    end = first > last ? begin : last_of(last) + 1;
+    ask_pages();
+    for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
+      const int u = u0 + c, row = r0 + u / x.a.G, pos = pos0 + u / x.a.G;
+      int rh = -1, clo = INT_MAX, clast = -1;
+      if (c < run.n) {
+        rh = (head * x.a.G + u % x.a.G) * x.b.rows + row;
+        if (pos >= 0 && pos <= most && lo_of(pos) <= last_of(pos)) {
+          clo = lo_of(pos);
+          clast = last_of(pos);
+        }
+      }
+      s_rh[c] = rh;
+      s_lo[c] = clo;
+      s_last[c] = clast;
+    }
+    const int c0 = wave * 32 * CB, c1 = min(c0 + 32 * CB, run.n) - 1;
+    const int p0 = pos0 + (u0 + c0) / x.a.G, p1 = pos0 + (u0 + c1) / x.a.G, q0 = max(p0, 0), q1 = min(p1, most);
+    const bool some = c0 <= c1 && q0 <= q1;
+    any_lo = some ? lo_of(q0) : INT_MAX;
+    any_last = some ? last_of(q1) : -1;
+    all_lo = p0 < 0 || p1 > most ? INT_MAX : lo_of(q1);  // (a row without a token attends nothing)
+    all_last = last_of(q0);
+  } else if (NW > 1) {
+    // eight tiles, one for each XCD, and their pieces in turn
+    const int64_t u = unit - plan.window_units, group8 = u / (8 * x.p.routed);
+    const int in_group = (int)(u - group8 * 8 * x.p.routed);
+    part = in_group >> 3;
+    const int4 rec = plan.records[group8 * 8 + (in_group & 7)];
+    const int count = rec.w, j = rec.x;
+    if (count == 0) return;
+    head = rec.y % x.c.Hkv;
+    seq = x.b.seqs[rec.y / x.c.Hkv];
+    begin = j * x.a.S + part * x.p.routed_tokens;
+    end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
+    ask_pages();
+    for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
+      const int item = c < count ? plan.items[(int64_t)rec.z * COLS + c] : -1;  // (row and head) * 32 + slot
+      // (where cu_rows decreases, some that are counted have no row: their items hold anything)
+      s_rh[c] = item >= 0 && item >> 5 < x.a.Hq * x.b.rows && (item & 31) < x.a.topk ? item : -1;
+      s_lo[c] = c < count ? begin : INT_MAX;
+      s_last[c] = c < count ? end - 1 : -1;
+    }
+    const bool some = wave * 32 * CB < count;
+    all_lo = begin;
+    all_last = end - 1;
+    any_lo = some ? all_lo : INT_MAX;
+    any_last = some ? all_last : -1;
+  } else {
+    const int64_t u = unit - plan.window_units;
+    part = (int)(u % x.p.routed);
+    const int64_t item = u / x.p.routed;
+    const int slot = (int)(item % x.a.topk), rh = (int)(item / x.a.topk);
+    const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+    const int j = x.idx[h * x.a.ish + row * x.a.ist + slot];
+    const Entry at = entry_with_row(x, row);
+    if (row < at.r0 || row >= at.r1) return;
+    head = h / x.a.G;
+    seq = at.s;
+    const int own = (row - at.r0) * x.a.G + h - head * x.a.G, u0 = own & ~31;  // columns u0 .. u0 + 31 of the entry
+    const int pos = position_of(x, at, row);
+    if (pos < 0 || j < 0 || j >= pos / x.a.S) {
+      if (lane == 0) x.part_lse[(int64_t)rh * x.p.count + slot * x.p.routed + part] = -INFINITY;
+      return;
+    }
+    const int cols = min((min(at.r1, x.b.rows) - at.r0) * x.a.G - u0, 32);
+    begin = any_lo = all_lo = j * x.a.S + part * x.p.routed_tokens;
+    end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
+    any_last = all_last = end - 1;
+    ask_pages();  // (before the other columns' lists: a unit is short, and a chain of loads)
+    if (lane < 32) {
+      s_rh[lane] = -1;
+      s_lo[lane] = INT_MAX;
+      s_last[lane] = -1;
+    }
+    bool earlier = false;
+    for (int i = lane; i < cols * x.a.topk; i += 64) {
+      const int c = i / x.a.topk, k = i - c * x.a.topk;
+      const int row2 = at.r0 + (u0 + c) / x.a.G, h2 = head * x.a.G + (u0 + c) % x.a.G;
+      const int pos2 = position_of(x, at, row2);
+      if (pos2 >= 0 && j < pos2 / x.a.S && x.idx[h2 * x.a.ish + row2 * x.a.ist + k] == j) {
+        earlier = earlier || u0 + c < own || (u0 + c == own && k < slot);
+        s_rh[c] = (h2 * x.b.rows + row2) * 32 + k;
+        s_lo[c] = begin;
+        s_last[c] = end - 1;
+      }
+    }
+    if (__builtin_amdgcn_ballot_w64(earlier) != 0) return;
+  }
+  __syncthreads();
+  constexpr int KB = CB == 2 || STEP == 32 || sizeof(T) == 4 ? 1 : 2;
+  Tile<T, D, CB, KB> tile;
+  tile.clear(lane);
+  any_lo = __builtin_amdgcn_readfirstlane(any_lo);
+  any_last = __builtin_amdgcn_readfirstlane(any_last);
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_last = __builtin_amdgcn_readfirstlane(all_last);
+  begin = begin / 16 * 16;
+  head = __builtin_amdgcn_readfirstlane(head);
+  const int64_t base = x.b.layer * x.c.layer + head * x.c.head;
+  const T *const K = static_cast<const T*>(x.c.K), *const V = static_cast<const T*>(x.c.V);
+  CodeStage<T, D, NW, STEP> codes;
+  constexpr int GROUPS = STEP / 16;
+  auto there = [&](int page) { return (uint64_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages); };
+  int batch = begin, next_page = -1;
+  uint64_t alive = 0;       // which of the looked up pages there are
+  uint64_t live[2] = {};    // of the stages: a bit for each sixteen rows (ANY: for each)
+  auto stage = [&](int t0, int b) {
+    const int ln = lane_now();
+    if constexpr (FP4) {
+      live[b] = there(page);
+      codes.load(x.c, base, page, t0, wave, ln);
+      page = look_up(t0 + STEP);
+    } else if constexpr (ANY) {
+      const int t = t0 + ln % STEP;
+      live[b] = there(page);
+      const int64_t at = (uint32_t)page < (uint32_t)x.c.n_pages
+                             ? base + page * x.c.page + (int64_t)((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps) * x.c.tok
+                             : -1;
+#pragma unroll
+      for (int i = 0; i < GROUPS / NW; ++i) {
+        const int r0 = (NW == 1 ? i : wave) * 16;
+        stage_rows_any<T, D, 0, NW == 1>(&s_kv[b][0][r0 * D], r0, K, at, ln);
+        stage_rows_any<T, D, 1, NW == 1>(&s_kv[b][1][r0 * D], r0, V, at, ln);
+      }
+      page = look_up(t0 + STEP);
+    } else {
+      if (t0 - batch >= 1024) {
+        batch += 1024;
+        page = next_page;
+        alive = there(page);
+        next_page = look_up(batch + 1024);
+      }
+      const int first = (t0 - batch) / 16, row_bytes = (int)x.c.tok * (int)sizeof(T);
+      live[b] = alive >> first;
+#pragma unroll
+      for (int i = 0; i < GROUPS / NW; ++i) {
+        const int g = NW == 1 ? i : wave, r0 = g * 16, t = __builtin_amdgcn_readfirstlane(t0 + r0);
+        const bool on = live[b] >> g & 1;
+        const int rows = on ? min(end - t, 16) : 0;
+        const int in_page = __builtin_amdgcn_readfirstlane((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps);
+        const int64_t from = on ? uniform64(base + __builtin_amdgcn_readlane(page, first + g) * x.c.page + in_page * x.c.tok) : 0;
+        stage_rows<T, D, 0, NW == 1>(&s_kv[b][0][r0 * D], r0, K + from, rows, row_bytes, ln);
+        stage_rows<T, D, 1, NW == 1>(&s_kv[b][1][r0 * D], r0, V + from, rows, row_bytes, ln);
+      }
+    }
+  };
+  if (begin < end) {
+    alive = there(page);
+    if (!ANY && end - batch > 1024) next_page = look_up(batch + 1024);
+    stage(begin, 0);
+    if constexpr (FP4) {
+      codes.store(s_kv[0][0], s_kv[0][1], wave, lane_now());
+      if (begin + STEP < end) stage(begin + STEP, 1);
+    }
+  }
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    const int item = s_rh[wave * 32 * CB + cb * 32 + (lane & 31)];
+    const int rh = max(window ? item : item >> 5, 0);  // (a column of nobody reads some row: nothing is made of it)
+    const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+    tile.load_q(cb, static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst, lane);
+  }
+  int b = 0;
+  for (int t0 = begin; t0 < end; t0 += STEP, b ^= 1) {
+    const uint64_t here = live[b];
+    if constexpr (FP4) {
+      // the rows of this step lie in their stage; those of the next one, whose codes are in registers, follow into the other
+      wait_lds();
+      if (NW > 1) {
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+      if (t0 + STEP < end) codes.store(s_kv[b ^ 1][0], s_kv[b ^ 1][1], wave, lane_now());
+      if (t0 + 2 * STEP < end) stage(t0 + 2 * STEP, b);
+    } else {
+      wait_loads();
+      if (NW > 1) {
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+      if (t0 + STEP < end) stage(t0 + STEP, b ^ 1);
+    }
+#pragma unroll 1
+    for (int at = 0; at < STEP; at += 32 * KB) {
+      const int t = t0 + at, upto = t + 32 * KB - 1;
+      if (upto < any_lo || t > any_last) continue;
+      typedef std::conditional_t<ANY, uint64_t, uint32_t> Live;
+      constexpr Live kAll = ANY ? (KB == 2 ? ~(Live)0 : (Live)0xffffffffu) : (Live)((1 << 2 * KB) - 1);
+      const Live now = (Live)(here >> (ANY ? at : at / 16)) & kAll;
+      tile.attend(&s_kv[b][0][at * D], &s_kv[b][1][at * D], t, t < all_lo || upto > all_last || now != kAll, now, x.scale_log2e,
+                  s_lo + wave * 32 * CB, s_last + wave * 32 * CB);
+    }
+  }
+  // Results.  A column with a value that is not finite is marked by an lse that is not a number: it may have come from a
+  // token that the column does not attend, and the merge takes such a piece again, row by row.
+  // Values go out by way of the stages, whose rows are free by now: a lane has four of them of one column, 8 or 16 bytes of a row's 256.
+  if (NW > 1) __syncthreads();
+  const bool direct = x.p.count == 1;
+  typedef typename Record<T>::Value Value;
+  typedef std::conditional_t<sizeof(T) == 2, __bf16, float> Out;
+  constexpr int LPR = D * (int)sizeof(Value) / 16, RPI = 64 / LPR;  // lanes of a row, rows of an instruction
+  char* const s_out = s_dynamic + wave * (32 * D * (int)sizeof(Value));
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    const int ln = lane_now(), own = wave * 32 * CB + cb * 32 + (ln & 31), item = s_rh[own];
+    const float sum = across_halves_sum(tile.l[cb]);
+    const float inv = 1.f / sum;
+    float check = 0.f, top = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        check = fmaf(tile.o[cb][dt][r], 0.f, check);
+        top = max_of(top, fabsf(tile.o[cb][dt][r]));
+      }
+    check = across_halves_sum(check);
+    top = across_halves_max(top);
+    const bool none = tile.m[cb] == -INFINITY;
+    const float lse = none ? -INFINITY : check == 0.f ? tile.m[cb] + __log2f(sum) : NAN;
+    auto record = [&](int item) {
+      return (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
+    };
+    const float scale = direct || sizeof(T) == 4 ? 1.f : scale_above(top * inv);
+    if (item >= 0 && ln < 32) {
+      const int64_t rec = record(item);
+      x.part_lse[rec] = lse;
+      if (direct && x.LSE) x.LSE[rec] = lse * kLn2;
+      if (!direct && sizeof(T) == 2) x.part_scale[rec] = scale;
+    }
+    // d = 32 dt + 8 g + 4 (ln / 32) on: a 16-byte unit, or half of one, swizzled by the row
+    auto put = [&](auto zero, float by) {
+      typedef decltype(zero) V;
+      typedef V Four __attribute__((ext_vector_type(4)));
+      const int row = ln & 31, hf = ln >> 5;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          Four v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (V)(none ? 0.f : tile.o[cb][dt][4 * g + e] * by);
+          const int unit = sizeof(V) == 2 ? 4 * dt + g : 8 * dt + 2 * g + hf;
+          *reinterpret_cast<Four*>(s_out + (row * LPR + (unit ^ row % LPR)) * 16 + (sizeof(V) == 2 ? 8 * hf : 0)) = v;
+        }
+    };
+    if (direct) put(Out(), inv);
+    else put(Value(), inv / scale);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    char* const to = static_cast<char*>(direct ? x.O : x.part_o);
+    const uint64_t write = __builtin_amdgcn_ballot_w64(item >= 0 && (direct || !none));
+#pragma unroll
+    for (int i = 0; i < 32 / RPI; ++i) {
+      const int row = i * RPI + ln / LPR, piece = ln % LPR;
+      if (!(write >> row & 1)) continue;
+      const uint4 v = *reinterpret_cast<const uint4*>(s_out + (row * LPR + (piece ^ row % LPR)) * 16);
+      char* const at = to + record(s_rh[wave * 32 * CB + cb * 32 + row]) * (D * (int)sizeof(Value)) + piece * 16;
+      if (PAST) store16_stream(at, v);
+      else *reinterpret_cast<uint4*>(at) = v;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // What few columns attend of a cache in 4 bits, by one wavefront: CB blocks of 16 columns, 32 tokens at a time, in products of 16x16x32.
 //   S^T[token][column] = K . Q^T      A: lane l has token row l % 16 and the channels of quarter l / 16 of a row, which come from its codes
 //                                     in registers: neither K's codes nor its values pass LDS
@@ -1042,104 +1372,49 @@ struct NarrowCodes {
     __builtin_amdgcn_sched_group_barrier(0x008, AHEAD * CB, 2 + k);
   }
 
-  // A unit of tile_kernel, whose columns lie in s_rh, s_lo, s_last; page: as look_up(begin) gives it; s_room: 32 rows of D values.
-  __device__ static __forceinline__ void run(const PagedArgs& x, bool window, int part, int seq, int begin, int end, int all_lo, int all_last,
-                                             int64_t base, int page, const int* s_rh, const int* s_lo, const int* s_last, char* s_room) {
-    const int lane = threadIdx.x & 63;
-    const uint8_t *const K = static_cast<const uint8_t*>(x.c.K) + base, *const V = static_cast<const uint8_t*>(x.c.V) + base;
-    const int32_t* const table = x.c.tables + (int64_t)seq * x.c.max_pages;
-    // (the last token's page beyond the end, which `there` takes back: a load in a branch may not have been made)
-    auto look_up = [&](int t0) { return table[(uint32_t)min(t0 + lane, end - 1) / x.c.by_ps]; };
-    auto there = [&](int page, int t0) {
-      return (uint64_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages && t0 + lane < end);
-    };
-    NarrowCodes n;
-    Raw raw[2];
-    uint64_t live = 0;
+  __device__ __forceinline__ void load_q(int cb, const bf16_t* row, int lane) {
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-      const int item = s_rh[cb * 16 + (lane & 15)];
-      const int rh = max(window ? item : item >> 5, 0);  // (a column of nobody reads some row: nothing is made of it)
-      const int h = rh / x.b.rows, row = rh - h * x.b.rows;
-      const bf16_t* const from = static_cast<const bf16_t*>(x.Q) + h * x.a.qsh + row * x.a.qst + (lane >> 4) * (D / 4);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) n.q[cb][kk] = *reinterpret_cast<const bf16x8*>(from + 8 * kk);
-      n.m[cb] = -INFINITY;
-      n.l[cb] = 0.f;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) n.o[cb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    if (begin < end) {
-      live = there(page, begin);
-#pragma unroll
-      for (int k = 0; k < 2; ++k) ask(raw[k], x.c, K, V, page, begin, 32 * k, lane);
-      page = look_up(begin + 64);
-    }
-    // (a query that may not have come yet would be waited for in every turn, and what was asked for later with it)
+    for (int kk = 0; kk < KK; ++kk) q[cb][kk] = *reinterpret_cast<const bf16x8*>(row + (lane >> 4) * (D / 4) + 8 * kk);
+  }
+  __device__ __forceinline__ void have_q() {
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(n.q[cb][kk]));
-    // Loads come back in order: pages are asked for before a turn's codes, and the last turn, which asks for none, has code of its own.  (A
-    // wait for a page behind the codes, or for codes that may not have been asked for, is one for all that is on its way: MEASURE.)
-    auto turn = [&](auto more, int t0) {
-      const uint64_t next = decltype(more)::value ? there(page, t0 + 64) : 0;
-      const int after = decltype(more)::value ? look_up(t0 + 128) : -1;
-      const uint64_t now = live;
-      auto come = [&](int k) {
-        arrive(raw[k]);
-        if ((uint32_t)(now >> (32 * k)) != 0xffffffffu) values_only(raw[k], (uint32_t)(now >> (32 * k)), lane);
-      };
-      auto go_on = [&](int k) {
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (decltype(more)::value) ask(raw[k], x.c, K, V, page, t0 + 64, 32 * k, lane);
-        __builtin_amdgcn_sched_barrier(0);
-      };
-      come(0);
-      stage_v(raw[0], s_room, lane);
-      n.scores(raw[0], 0);
-      go_on(0);
-      come(1);
-      n.scores(raw[1], 1);
-      if (t0 < all_lo || t0 + 63 > all_last || now != ~(uint64_t)0) n.mask(t0, now, s_lo, s_last, lane);
-      n.move_bounds(x.scale_log2e);
-      n.weights(x.scale_log2e);
-      n.template values<0>(s_room, lane);
-      stage_v(raw[1], s_room, lane);
-      go_on(1);
-      n.template values<1>(s_room, lane);
-      live = next;
-      page = after;
-    };
-    int t0 = begin;
-#pragma unroll 1
-    for (; t0 + 64 < end; t0 += 64) turn(std::true_type(), t0);
-    if (t0 < end) turn(std::false_type(), t0);
-    // Results, as tile_kernel's: a column with a value that is not finite is marked.
+      for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(q[cb][kk]));
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      m[cb] = -INFINITY;
+      l[cb] = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[cb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  // The records of piece `part` (of a span's; or of the window) of the columns in s_rh, as tile_kernel's: a column with a value that is not
+  // finite is marked.
+  __device__ __forceinline__ void results(const PagedArgs& x, bool window, int part, const int* s_rh, char* s_room, int lane) const {
     const bool direct = x.p.count == 1;
     constexpr int LPR = D / 8, RPI = 64 / LPR;  // lanes of a row, rows of an instruction
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       const int item = s_rh[cb * 16 + (lane & 15)];
-      const float sum = across_sum(n.l[cb]), inv = 1.f / sum;
+      const float sum = across_sum(l[cb]), inv = 1.f / sum;
       float check = 0.f, top = 0.f;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          check = fmaf(n.o[cb][db][r], 0.f, check);
-          top = max_of(top, fabsf(n.o[cb][db][r]));
+          check = fmaf(o[cb][db][r], 0.f, check);
+          top = max_of(top, fabsf(o[cb][db][r]));
         }
       check = across_sum(check);
       top = across_max(top);
-      const bool none = n.m[cb] == -INFINITY;
-      const float lse = none ? -INFINITY : check == 0.f ? n.m[cb] + __log2f(sum) : NAN;
-      auto record = [&](int item) {
-        return (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
-      };
+      const bool none = m[cb] == -INFINITY;
+      const float lse = none ? -INFINITY : check == 0.f ? m[cb] + __log2f(sum) : NAN;
+      const int64_t rec = (int64_t)(window ? item : item >> 5) * x.p.count + (window ? x.a.topk : item & 31) * x.p.routed + part;
       const float scale = direct ? 1.f : scale_above(top * inv);
       if (item >= 0 && lane < 16) {
-        const int64_t rec = record(item);
         x.part_lse[rec] = lse;
         if (direct && x.LSE) x.LSE[rec] = lse * kLn2;
         if (!direct) x.part_scale[rec] = scale;
@@ -1148,27 +1423,31 @@ struct NarrowCodes {
       auto put = [&](auto zero, float by) {
         typedef decltype(zero) Out;
         typedef Out Four __attribute__((ext_vector_type(4)));
-        const int row = lane & 15, part = lane >> 4;
+        const int row = lane & 15, quarter = lane >> 4;
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           Four v;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = (Out)(none ? 0.f : n.o[cb][db][e] * by);
-          *reinterpret_cast<Four*>(s_room + (row * LPR + ((2 * db + (part >> 1)) ^ row % LPR)) * 16 + 8 * (part & 1)) = v;
+          for (int e = 0; e < 4; ++e) v[e] = (Out)(none ? 0.f : o[cb][db][e] * by);
+          *reinterpret_cast<Four*>(s_room + (row * LPR + ((2 * db + (quarter >> 1)) ^ row % LPR)) * 16 + 8 * (quarter & 1)) = v;
         }
       };
       if (direct) put(__bf16(), inv);
       else put((_Float16)0, inv / scale);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      char* const to = static_cast<char*>(direct ? x.O : x.part_o);
+      // (a choice between two pointers of the arguments would be made in scratch memory)
+      const uint64_t part_o = (uint64_t)x.part_o, other = (uint64_t)x.O - part_o;
+      char* const to = reinterpret_cast<char*>(part_o + (direct ? other : 0));
       const uint64_t write = __builtin_amdgcn_ballot_w64(item >= 0 && (direct || !none));
 #pragma unroll
       for (int i = 0; i < 16 / RPI; ++i) {
         const int row = i * RPI + lane / LPR, piece = lane % LPR;
+        const int lo = __shfl((int)(uint32_t)rec, row, 64), hi = __shfl((int)(rec >> 32), row, 64);
+        const int64_t at = ((int64_t)hi << 32) | (uint32_t)lo;
         if (!(write >> row & 1)) continue;
         const uint4 v = *reinterpret_cast<const uint4*>(s_room + (row * LPR + (piece ^ row % LPR)) * 16);
-        *reinterpret_cast<uint4*>(to + record(s_rh[cb * 16 + row]) * (2 * D) + piece * 16) = v;
+        *reinterpret_cast<uint4*>(to + at * (2 * D) + piece * 16) = v;
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -1176,339 +1455,231 @@ struct NarrowCodes {
   }
 };
 
-// NW wavefronts of 32 * CB columns, two stages of STEP tokens.  Measured (bf16, D = 128): four prompts of 2500 to 6000 tokens, 32:8 heads,
-// 770 us = 1.05 PFLOP/s, where a large library product reaches 1.2; 2000 rows behind 64K tokens, 32:4 heads, eight spans of 512, 215 us =
-// 0.66 PFLOP/s (tiles of 8 steps, whose beginnings and ends are a quarter of them); one token behind a million 49 us = 5.2 TB/s, 24 caches
-// of up to 120000 tokens 93 us = 5.6 TB/s, where a pure read reaches 6.4.
-//   4 wavefronts: the matrix cores are what bounds these
-//   1 wavefront: few columns, so that memory does; four workgroups (D = 128) of a compute unit have 16 KB each on the way
-//                (three and four stages leave room for fewer: 24 caches of up to 120000 tokens 119 -> 122, 153 us)
-// Workgroups of the window come first, then, of the spans' pieces,
-//   4 wavefronts: the buckets' tiles
-//   1 wavefront: one for every (row, head, slot).  Other heads and rows of its 32 columns may list the same span: the first one
-//                that does takes it for all, so that a span is read once for the group.
-//   ANY: pages of a size that is no multiple of 16: every row has a page of its own, at twice the instructions for its address
-//   PAST: records go past the caches
-template <typename T, int D, bool FP4, int NW, int CB, int STEP, bool ANY, bool PAST>
-__global__ __launch_bounds__(64 * NW, FP4 && NW == 1 ? 3 - CB + 1 : NW == 1 || sizeof(T) == 4 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
-  constexpr bool CODES = FP4 && NW == 1;  // NarrowCodes
-  constexpr int COLS = CODES ? 16 * CB : NW * 32 * CB;
-  constexpr int ALIGN = CODES ? 32 : 16;  // a tile's first token is a multiple of it
-  extern __shared__ __align__(1024) char s_dynamic[];  // (static, the compiler would wait for staging loads at every read)
-  T(*const s_kv)[2][STEP * D] = reinterpret_cast<T(*)[2][STEP * D]>(s_dynamic);
-  __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS];
-  const int lane = threadIdx.x & 63, wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// Workgroups of the window come first, as tile_kernel's; then, of the spans' pieces, one for every (row, head, group of slots, piece): it takes
+// the piece of each of its slots' spans, one after the other.  Other heads and rows of its columns may list the same span: the first one
+// that does takes it for all.  What a unit has to find out before it can ask for codes is a chain of five loads, 9 to 12 us of them where
+// memory is busy, as long as 200 to 300 tokens take: hence several spans a unit, and codes and pages of the next one asked for while one is
+// attended.
+template <int D, int CB, bool EASY>
+__global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedArgs x, const TilePlan plan) {
+  constexpr int COLS = 16 * CB;
+  extern __shared__ __align__(1024) char s_dynamic[];
+  __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS], s_list[COLS * SL_MAX_TOPK];
+  const int lane = threadIdx.x;
   const int64_t unit = workgroup();
   if (unit >= plan.units) return;  // (grid_of rounds up)
   const bool window = unit < plan.window_units;
-  int seq, head, part;         // sequence, kv head, piece
-  int begin, end;              // tokens [begin, end) of the tile
-  int any_lo, any_last;        // ... that any of the wavefront's columns attends
-  int all_lo, all_last;        // ... that all of them attend
-  // The pages of the first rows are asked for as soon as a tile knows its sequence and tokens.
-  // !ANY: lane g has the page of the g-th sixteen tokens from `batch` on; the next 64 pages are looked up while those are in use.
-  // ANY: lane l has the page of row l of the next stage.
-  int page = -1;
-  auto look_up = [&](int t0) {
-    const int ln = lane_now(), t = t0 + (ANY || FP4 ? ln % STEP : ln * 16);
-    return t < end ? x.c.tables[(int64_t)seq * x.c.max_pages + (uint32_t)t / x.c.by_ps] : -1;
-  };
-  auto ask_pages = [&] {
-    seq = __builtin_amdgcn_readfirstlane(seq);
-    begin = __builtin_amdgcn_readfirstlane(begin);
-    end = __builtin_amdgcn_readfirstlane(end);
-    if (begin < end) page = look_up(begin / ALIGN * ALIGN);
-  };
-  // columns
+  Entry at;
+  int head, part, u0, cols, begin = 0, end = 0, all_lo, all_last;
+  int mine = -1;      // lane k: span of slot k of the unit's own row, -1: none, or none of its slots
+  uint32_t todo = 0;  // slots to come
   if (window) {
-    // (tile, piece) of the kv heads in turn; the last tiles first, whose ranges are the longest
     head = (int)(unit % x.c.Hkv);
-    const int at = (int)(unit / x.c.Hkv);
-    if (at >= plan.tiles * x.p.window) return;
-    const int tile = plan.tiles - 1 - at / x.p.window, piece = at % x.p.window;
-    part = x.a.topk * x.p.routed + piece;
+    const int turn = (int)(unit / x.c.Hkv);
+    if (turn >= plan.tiles * x.p.window) return;
+    const int tile = plan.tiles - 1 - turn / x.p.window;
+    part = turn % x.p.window;
     const ColumnRun run = columns_of(x, tile, COLS, x.a.G);
     if (run.n <= 0) return;
-    const int r0 = run.at.r0, u0 = run.u0, len = run.at.len, pos0 = len - (run.at.r1 - r0);
-    seq = run.at.s;
-    const int first = max(pos0 + u0 / x.a.G, 0);  // position of the tile's first row that has a token
-    const int most = min(len, x.b.L) - 1;         // of the last row that has one
-    const int64_t origin = (int64_t)(first / x.a.S) * x.a.S / 16 * 16 + (int64_t)piece * x.p.window_tokens;
+    at = run.at;
+    u0 = run.u0;
+    cols = run.n;
+  } else {
+    const int64_t u = unit - plan.window_units;
+    part = (int)(u % x.p.routed);
+    const int64_t v = u / x.p.routed;
+    const int rh = (int)(v / plan.groups), group = (int)(v - (int64_t)rh * plan.groups);
+    const int h = rh / x.b.rows, row = rh - h * x.b.rows;
+    at = entry_with_row(x, row);
+    if (row < at.r0 || row >= at.r1) return;
+    head = h / x.a.G;
+    const int own = (row - at.r0) * x.a.G + h - head * x.a.G;  // column of the entry
+    u0 = own & ~(COLS - 1);
+    cols = min((min(at.r1, x.b.rows) - at.r0) * x.a.G - u0, COLS);
+    // the columns' lists, without what is no candidate
+    const uint32_t topk = x.a.topk, by_topk = (65536 + topk - 1) / topk;  // (exact below 2^11 / 2)
+    for (int i = lane; i < cols * (int)topk; i += 64) {
+      const int c = i * by_topk >> 16, k = i - c * topk;
+      const int row2 = at.r0 + (u0 + c) / x.a.G, h2 = head * x.a.G + (u0 + c) % x.a.G;
+      const int pos = position_of(x, at, row2), j = x.idx[h2 * x.a.ish + row2 * x.a.ist + k];
+      s_list[i] = pos >= 0 && j >= 0 && j < pos / x.a.S ? j : -1;
+    }
+    const int k0 = group * plan.slots, k1 = min(k0 + plan.slots, (int)topk);
+    if (lane >= k0 && lane < k1) {
+      mine = s_list[(own - u0) * topk + lane];
+      if (mine < 0) x.part_lse[(int64_t)rh * x.p.count + lane * x.p.routed + part] = -INFINITY;
+    }
+    const int before = (own - u0) * topk;
+    for (int k = k0; k < k1; ++k) {
+      const int j = __builtin_amdgcn_readlane(mine, k);
+      if (j < 0) continue;
+      bool earlier = false;
+      for (int i = lane; i < before + k; i += 64) earlier = earlier || s_list[i] == j;
+      if (__builtin_amdgcn_ballot_w64(earlier) == 0) todo |= 1u << k;
+    }
+    if (todo == 0) return;
+  }
+  const int seq = __builtin_amdgcn_readfirstlane(at.s);
+  head = __builtin_amdgcn_readfirstlane(head);
+  part = __builtin_amdgcn_readfirstlane(part);
+  todo = __builtin_amdgcn_readfirstlane(todo);
+  typedef NarrowCodes<D, CB, EASY> Codes;
+  Codes n;
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    const int u = u0 + min(cb * 16 + (lane & 15), cols - 1);  // (a column of nobody reads some row: nothing is made of it)
+    n.load_q(cb, static_cast<const bf16_t*>(x.Q) + (int64_t)(head * x.a.G + u % x.a.G) * x.a.qsh + (at.r0 + u / x.a.G) * x.a.qst, lane);
+  }
+  // ---- what a unit attends: of the window, its columns' ranges at once; else the next slot's span
+  auto take_window = [&] {
+    const int r0 = at.r0, pos0 = at.len - (at.r1 - r0);
+    const int first = max(pos0 + u0 / x.a.G, 0);     // position of the tile's first row that has a token
+    const int most = min(at.len, x.b.L) - 1;         // of the last row that has one
+    const int64_t origin = (int64_t)(first / x.a.S) * x.a.S / 16 * 16 + (int64_t)part * x.p.window_tokens;
     const int from = (int)min(origin, (int64_t)INT_MAX), upto = (int)min(origin + x.p.window_tokens - 1, (int64_t)INT_MAX);
     auto lo_of = [&](int pos) { return max(pos / x.a.S * x.a.S, from); };
     auto last_of = [&](int pos) { return min(pos, upto); };
     // Later rows begin and end no earlier.
-    const int last = min(pos0 + (u0 + run.n - 1) / x.a.G, most);
+    const int end_pos = pos0 + (u0 + cols - 1) / x.a.G, last = min(end_pos, most), start_pos = pos0 + u0 / x.a.G;
     begin = lo_of(first);
     end = first > last ? begin : last_of(last) + 1;
-    ask_pages();
-    for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
-      const int u = u0 + c, row = r0 + u / x.a.G, pos = pos0 + u / x.a.G;
+    all_lo = start_pos < 0 || end_pos > most ? INT_MAX : lo_of(last);  // (a row without a token attends nothing)
+    all_last = last_of(first);
+    if (lane < COLS) {
+      const int u = u0 + lane, pos = pos0 + u / x.a.G;
       int rh = -1, clo = INT_MAX, clast = -1;
-      if (c < run.n) {
-        rh = (head * x.a.G + u % x.a.G) * x.b.rows + row;
+      if (lane < cols) {
+        rh = (head * x.a.G + u % x.a.G) * x.b.rows + r0 + u / x.a.G;
         if (pos >= 0 && pos <= most && lo_of(pos) <= last_of(pos)) {
           clo = lo_of(pos);
           clast = last_of(pos);
         }
       }
-      s_rh[c] = rh;
-      s_lo[c] = clo;
-      s_last[c] = clast;
+      s_rh[lane] = rh;
+      s_lo[lane] = clo;
+      s_last[lane] = clast;
     }
-    const int c0 = wave * 32 * CB, c1 = min(c0 + 32 * CB, run.n) - 1;
-    const int p0 = pos0 + (u0 + c0) / x.a.G, p1 = pos0 + (u0 + c1) / x.a.G, q0 = max(p0, 0), q1 = min(p1, most);
-    const bool some = c0 <= c1 && q0 <= q1;
-    any_lo = some ? lo_of(q0) : INT_MAX;
-    any_last = some ? last_of(q1) : -1;
-    all_lo = p0 < 0 || p1 > most ? INT_MAX : lo_of(q1);  // (a row without a token attends nothing)
-    all_last = last_of(q0);
-  } else if (NW > 1) {
-    // eight tiles, one for each XCD, and their pieces in turn
-    const int64_t u = unit - plan.window_units, group8 = u / (8 * x.p.routed);
-    const int in_group = (int)(u - group8 * 8 * x.p.routed);
-    part = in_group >> 3;
-    const int4 rec = plan.records[group8 * 8 + (in_group & 7)];
-    const int count = rec.w, j = rec.x;
-    if (count == 0) return;
-    head = rec.y % x.c.Hkv;
-    seq = x.b.seqs[rec.y / x.c.Hkv];
-    begin = j * x.a.S + part * x.p.routed_tokens;
-    end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
-    ask_pages();
-    for (int c = threadIdx.x; c < COLS; c += 64 * NW) {
-      const int item = c < count ? plan.items[(int64_t)rec.z * COLS + c] : -1;  // (row and head) * 32 + slot
-      // (where cu_rows decreases, some that are counted have no row: their items hold anything)
-      s_rh[c] = item >= 0 && item >> 5 < x.a.Hq * x.b.rows && (item & 31) < x.a.topk ? item : -1;
-      s_lo[c] = c < count ? begin : INT_MAX;
-      s_last[c] = c < count ? end - 1 : -1;
-    }
-    const bool some = wave * 32 * CB < count;
+  };
+  // tokens of slot k's piece
+  auto piece_of = [&](int k, int* from, int* to) {
+    const int j = __builtin_amdgcn_readlane(mine, k);
+    *from = j * x.a.S + part * x.p.routed_tokens;
+    *to = min(*from + x.p.routed_tokens, (j + 1) * x.a.S);
+  };
+  auto take_span = [&](int k) {
+    const int j = __builtin_amdgcn_readlane(mine, k);
+    piece_of(k, &begin, &end);
     all_lo = begin;
     all_last = end - 1;
-    any_lo = some ? all_lo : INT_MAX;
-    any_last = some ? all_last : -1;
-  } else {
-    const int64_t u = unit - plan.window_units;
-    part = (int)(u % x.p.routed);
-    const int64_t item = u / x.p.routed;
-    // (workgroups u = x (mod 8) run on XCD x: by rh, so that no XCD has the first slots of all, which are filled more often than the last)
-    const int rh = (int)(item / x.a.topk), slot = (int)((item + rh) % x.a.topk);
-    const int h = rh / x.b.rows, row = rh - h * x.b.rows;
-    const int j = x.idx[h * x.a.ish + row * x.a.ist + slot];
-    const Entry at = entry_with_row(x, row);
-    if (row < at.r0 || row >= at.r1) return;
-    head = h / x.a.G;
-    seq = at.s;
-    const int own = (row - at.r0) * x.a.G + h - head * x.a.G, u0 = own & ~(COLS - 1);  // columns u0 .. of the entry
-    const int pos = position_of(x, at, row);
-    if (pos < 0 || j < 0 || j >= pos / x.a.S) {
-      if (lane == 0) x.part_lse[(int64_t)rh * x.p.count + slot * x.p.routed + part] = -INFINITY;
-      return;
-    }
-    const int cols = min((min(at.r1, x.b.rows) - at.r0) * x.a.G - u0, COLS);
-    begin = any_lo = all_lo = j * x.a.S + part * x.p.routed_tokens;
-    end = min(begin + x.p.routed_tokens, (j + 1) * x.a.S);
-    any_last = all_last = end - 1;
-    ask_pages();  // (before the other columns' lists: a unit is short, and a chain of loads)
     if (lane < COLS) {
       s_rh[lane] = -1;
       s_lo[lane] = INT_MAX;
       s_last[lane] = -1;
     }
-    bool earlier = false;
-    for (int i = lane; i < cols * x.a.topk; i += 64) {
-      const int c = i / x.a.topk, k = i - c * x.a.topk;
-      const int row2 = at.r0 + (u0 + c) / x.a.G, h2 = head * x.a.G + (u0 + c) % x.a.G;
-      const int pos2 = position_of(x, at, row2);
-      if (pos2 >= 0 && j < pos2 / x.a.S && x.idx[h2 * x.a.ish + row2 * x.a.ist + k] == j) {
-        earlier = earlier || u0 + c < own || (u0 + c == own && k < slot);
-        s_rh[c] = (h2 * x.b.rows + row2) * 32 + k;
-        s_lo[c] = begin;
-        s_last[c] = end - 1;
-      }
-    }
-    if (__builtin_amdgcn_ballot_w64(earlier) != 0) return;
-  }
-  __syncthreads();
-  constexpr int KB = CB == 2 || STEP == 32 || sizeof(T) == 4 ? 1 : 2;
-  Tile<T, D, CB, KB> tile;
-  tile.clear(lane);
-  any_lo = __builtin_amdgcn_readfirstlane(any_lo);
-  any_last = __builtin_amdgcn_readfirstlane(any_last);
-  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-  all_last = __builtin_amdgcn_readfirstlane(all_last);
-  begin = begin / ALIGN * ALIGN;
-  head = __builtin_amdgcn_readfirstlane(head);
-  const int64_t base = x.b.layer * x.c.layer + head * x.c.head;
-  if constexpr (CODES) {
-    NarrowCodes<D, CB, !ANY>::run(x, window, part, seq, begin, end, all_lo, all_last, base, page, s_rh, s_lo, s_last, s_dynamic);
-    return;
-  }
-  const T *const K = static_cast<const T*>(x.c.K), *const V = static_cast<const T*>(x.c.V);
-  CodeStage<T, D, NW, STEP> codes;
-  constexpr int GROUPS = STEP / 16;
-  auto there = [&](int page) { return (uint64_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages); };
-  int batch = begin, next_page = -1;
-  uint64_t alive = 0;       // which of the looked up pages there are
-  uint64_t live[2] = {};    // of the stages: a bit for each sixteen rows (ANY: for each)
-  auto stage = [&](int t0, int b) {
-    const int ln = lane_now();
-    if constexpr (FP4) {
-      live[b] = there(page);
-      codes.load(x.c, base, page, t0, wave, ln);
-      page = look_up(t0 + STEP);
-    } else if constexpr (ANY) {
-      const int t = t0 + ln % STEP;
-      live[b] = there(page);
-      const int64_t at = (uint32_t)page < (uint32_t)x.c.n_pages
-                             ? base + page * x.c.page + (int64_t)((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps) * x.c.tok
-                             : -1;
-#pragma unroll
-      for (int i = 0; i < GROUPS / NW; ++i) {
-        const int r0 = (NW == 1 ? i : wave) * 16;
-        stage_rows_any<T, D, 0, NW == 1>(&s_kv[b][0][r0 * D], r0, K, at, ln);
-        stage_rows_any<T, D, 1, NW == 1>(&s_kv[b][1][r0 * D], r0, V, at, ln);
-      }
-      page = look_up(t0 + STEP);
-    } else {
-      if (t0 - batch >= 1024) {
-        batch += 1024;
-        page = next_page;
-        alive = there(page);
-        next_page = look_up(batch + 1024);
-      }
-      const int first = (t0 - batch) / 16, row_bytes = (int)x.c.tok * (int)sizeof(T);
-      live[b] = alive >> first;
-#pragma unroll
-      for (int i = 0; i < GROUPS / NW; ++i) {
-        const int g = NW == 1 ? i : wave, r0 = g * 16, t = __builtin_amdgcn_readfirstlane(t0 + r0);
-        const bool on = live[b] >> g & 1;
-        const int rows = on ? min(end - t, 16) : 0;
-        const int in_page = __builtin_amdgcn_readfirstlane((uint32_t)t - (uint32_t)t / x.c.by_ps * x.c.ps);
-        const int64_t from = on ? uniform64(base + __builtin_amdgcn_readlane(page, first + g) * x.c.page + in_page * x.c.tok) : 0;
-        stage_rows<T, D, 0, NW == 1>(&s_kv[b][0][r0 * D], r0, K + from, rows, row_bytes, ln);
-        stage_rows<T, D, 1, NW == 1>(&s_kv[b][1][r0 * D], r0, V + from, rows, row_bytes, ln);
-      }
+    const uint32_t topk = x.a.topk, by_topk = (65536 + topk - 1) / topk;
+    for (int i = lane; i < cols * (int)topk; i += 64) {
+      if (s_list[i] != j) continue;
+      const int c = i * by_topk >> 16, u = u0 + c;
+      s_rh[c] = ((head * x.a.G + u % x.a.G) * x.b.rows + at.r0 + u / x.a.G) * 32 + i - c * topk;
+      s_lo[c] = begin;
+      s_last[c] = end - 1;
     }
   };
+  if (window) {
+    take_window();
+  } else {
+    take_span(__builtin_ctz(todo));
+    todo &= todo - 1;
+  }
+  begin = __builtin_amdgcn_readfirstlane(begin);
+  end = __builtin_amdgcn_readfirstlane(end);
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_last = __builtin_amdgcn_readfirstlane(all_last);
+  const int64_t base = x.b.layer * x.c.layer + head * x.c.head;
+  const uint8_t *const K = static_cast<const uint8_t*>(x.c.K) + base, *const V = static_cast<const uint8_t*>(x.c.V) + base;
+  const int32_t* const table = x.c.tables + (int64_t)seq * x.c.max_pages;
+  // A turn: 64 tokens from t on, of those below `end`; t < 0: none.
+  struct Turn {
+    int t, end;
+  };
+  uint32_t ahead = todo;  // slots whose turns have not been planned
+  auto turn_after = [&](Turn v) {
+    v.t += 64;
+    if (v.t < v.end) return v;
+    if (ahead == 0) return Turn{-1, 1};
+    int from;
+    piece_of(__builtin_ctz(ahead), &from, &v.end);
+    ahead &= ahead - 1;
+    v.t = from / 32 * 32;
+    return v;
+  };
+  // (the last token's page beyond the end, which `there` takes back: a load in a branch may not have been made)
+  auto look_up = [&](Turn v) { return table[(uint32_t)min(max(v.t, 0) + lane, v.end - 1) / x.c.by_ps]; };
+  auto there = [&](int page, Turn v) {
+    return (uint64_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages && v.t >= 0 && v.t + lane < v.end);
+  };
+  typename Codes::Raw raw[2];
+  n.clear();
   if (begin < end) {
-    alive = there(page);
-    if (!ANY && end - batch > 1024) next_page = look_up(batch + 1024);
-    stage(begin, 0);
-    if constexpr (FP4) {
-      codes.store(s_kv[0][0], s_kv[0][1], wave, lane_now());
-      if (begin + STEP < end) stage(begin + STEP, 1);
-    }
-  }
+    Turn now = {begin / 32 * 32, end}, next = turn_after(now);
+    int page = look_up(now);
+    uint64_t live = there(page, now);
 #pragma unroll
-  for (int cb = 0; cb < CB; ++cb) {
-    const int item = s_rh[wave * 32 * CB + cb * 32 + (lane & 31)];
-    const int rh = max(window ? item : item >> 5, 0);  // (a column of nobody reads some row: nothing is made of it)
-    const int h = rh / x.b.rows, row = rh - h * x.b.rows;
-    tile.load_q(cb, static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst, lane);
-  }
-  int b = 0;
-  for (int t0 = begin; t0 < end; t0 += STEP, b ^= 1) {
-    const uint64_t here = live[b];
-    if constexpr (FP4) {
-      // the rows of this step lie in their stage; those of the next one, whose codes are in registers, follow into the other
-      wait_lds();
-      if (NW > 1) {
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-      }
-      if (t0 + STEP < end) codes.store(s_kv[b ^ 1][0], s_kv[b ^ 1][1], wave, lane_now());
-      if (t0 + 2 * STEP < end) stage(t0 + 2 * STEP, b);
-    } else {
-      wait_loads();
-      if (NW > 1) {
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-      }
-      if (t0 + STEP < end) stage(t0 + STEP, b ^ 1);
-    }
+    for (int k = 0; k < 2; ++k) Codes::ask(raw[k], x.c, K, V, page, now.t, 32 * k, lane);
+    page = look_up(next);
+    // (a query that may not have come yet would be waited for in every turn, and what was asked for later with it)
+    n.have_q();
+    // Loads come back in order: pages are asked for before a turn's codes, and the last turn, which asks for none, has code of its own.  (A
+    // wait for a page behind the codes, or for codes that may not have been asked for, is one for all that is on its way.)
+    auto take = [&](auto more) {
+      constexpr bool MORE = decltype(more)::value;
+      const Turn after = MORE ? turn_after(next) : Turn{-1, 1};
+      const uint64_t to_come = MORE ? there(page, next) : 0;
+      const int page_after = MORE ? look_up(after) : -1;
+      auto go_on = [&](int k) {
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (MORE) Codes::ask(raw[k], x.c, K, V, page, next.t, 32 * k, lane);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto come = [&](int k) {
+        Codes::arrive(raw[k]);
+        if ((uint32_t)(live >> (32 * k)) != 0xffffffffu) Codes::values_only(raw[k], (uint32_t)(live >> (32 * k)), lane);
+      };
+      come(0);
+      Codes::stage_v(raw[0], s_dynamic, lane);
+      n.scores(raw[0], 0);
+      go_on(0);
+      come(1);
+      n.scores(raw[1], 1);
+      if (now.t < all_lo || now.t + 63 > all_last || live != ~(uint64_t)0) n.mask(now.t, live, s_lo, s_last, lane);
+      n.move_bounds(x.scale_log2e);
+      n.weights(x.scale_log2e);
+      n.template values<0>(s_dynamic, lane);
+      Codes::stage_v(raw[1], s_dynamic, lane);
+      go_on(1);
+      n.template values<1>(s_dynamic, lane);
+      const bool over = now.t + 64 >= now.end;
+      now = next;
+      next = after;
+      live = to_come;
+      page = page_after;
+      return over;
+    };
 #pragma unroll 1
-    for (int at = 0; at < STEP; at += 32 * KB) {
-      const int t = t0 + at, upto = t + 32 * KB - 1;
-      if (upto < any_lo || t > any_last) continue;
-      typedef std::conditional_t<ANY, uint64_t, uint32_t> Live;
-      constexpr Live kAll = ANY ? (KB == 2 ? ~(Live)0 : (Live)0xffffffffu) : (Live)((1 << 2 * KB) - 1);
-      const Live now = (Live)(here >> (ANY ? at : at / 16)) & kAll;
-      tile.attend(&s_kv[b][0][at * D], &s_kv[b][1][at * D], t, t < all_lo || upto > all_last || now != kAll, now, x.scale_log2e,
-                  s_lo + wave * 32 * CB, s_last + wave * 32 * CB);
-    }
-  }
-  // Results.  A column with a value that is not finite is marked by an lse that is not a number: it may have come from a
-  // token that the column does not attend, and the merge takes such a piece again, row by row.
-  // Values go out by way of the stages, whose rows are free by now: a lane has four of them of one column, 8 or 16 bytes of a row's 256.
-  if (NW > 1) __syncthreads();
-  const bool direct = x.p.count == 1;
-  typedef typename Record<T>::Value Value;
-  typedef std::conditional_t<sizeof(T) == 2, __bf16, float> Out;
-  constexpr int LPR = D * (int)sizeof(Value) / 16, RPI = 64 / LPR;  // lanes of a row, rows of an instruction
-  char* const s_out = s_dynamic + wave * (32 * D * (int)sizeof(Value));
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb) {
-    const int ln = lane_now(), own = wave * 32 * CB + cb * 32 + (ln & 31), item = s_rh[own];
-    const float sum = across_halves_sum(tile.l[cb]);
-    const float inv = 1.f / sum;
-    float check = 0.f, top = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        check = fmaf(tile.o[cb][dt][r], 0.f, check);
-        top = max_of(top, fabsf(tile.o[cb][dt][r]));
+    while (next.t >= 0)
+      if (take(std::true_type())) {  // (turns are left: so are spans)
+        n.results(x, window, part, s_rh, s_dynamic, lane);
+        n.clear();
+        take_span(__builtin_ctz(todo));
+        todo &= todo - 1;
+        begin = __builtin_amdgcn_readfirstlane(begin);
+        end = __builtin_amdgcn_readfirstlane(end);
+        all_lo = begin;
+        all_last = end - 1;
       }
-    check = across_halves_sum(check);
-    top = across_halves_max(top);
-    const bool none = tile.m[cb] == -INFINITY;
-    const float lse = none ? -INFINITY : check == 0.f ? tile.m[cb] + __log2f(sum) : NAN;
-    auto record = [&](int item) {
-      return (int64_t)(window ? item : item >> 5) * x.p.count + (window ? part : (item & 31) * x.p.routed + part);
-    };
-    const float scale = direct || sizeof(T) == 4 ? 1.f : scale_above(top * inv);
-    if (item >= 0 && ln < 32) {
-      const int64_t rec = record(item);
-      x.part_lse[rec] = lse;
-      if (direct && x.LSE) x.LSE[rec] = lse * kLn2;
-      if (!direct && sizeof(T) == 2) x.part_scale[rec] = scale;
-    }
-    // d = 32 dt + 8 g + 4 (ln / 32) on: a 16-byte unit, or half of one, swizzled by the row
-    auto put = [&](auto zero, float by) {
-      typedef decltype(zero) V;
-      typedef V Four __attribute__((ext_vector_type(4)));
-      const int row = ln & 31, hf = ln >> 5;
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          Four v;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = (V)(none ? 0.f : tile.o[cb][dt][4 * g + e] * by);
-          const int unit = sizeof(V) == 2 ? 4 * dt + g : 8 * dt + 2 * g + hf;
-          *reinterpret_cast<Four*>(s_out + (row * LPR + (unit ^ row % LPR)) * 16 + (sizeof(V) == 2 ? 8 * hf : 0)) = v;
-        }
-    };
-    if (direct) put(Out(), inv);
-    else put(Value(), inv / scale);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    char* const to = static_cast<char*>(direct ? x.O : x.part_o);
-    const uint64_t write = __builtin_amdgcn_ballot_w64(item >= 0 && (direct || !none));
-#pragma unroll
-    for (int i = 0; i < 32 / RPI; ++i) {
-      const int row = i * RPI + ln / LPR, piece = ln % LPR;
-      if (!(write >> row & 1)) continue;
-      const uint4 v = *reinterpret_cast<const uint4*>(s_out + (row * LPR + (piece ^ row % LPR)) * 16);
-      char* const at = to + record(s_rh[wave * 32 * CB + cb * 32 + row]) * (D * (int)sizeof(Value)) + piece * 16;
-      if (PAST) store16_stream(at, v);
-      else *reinterpret_cast<uint4*>(at) = v;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    take(std::false_type());
   }
+  n.results(x, window, part, s_rh, s_dynamic, lane);
 }
 
 // ---- the rows that list a span: buckets (entry, kv head, span), each cut into tiles of `cols` items
@@ -1874,10 +2045,12 @@ struct Form {
   size_t o_bytes, lse_bytes, plan_bytes;
 };
 
-#ifndef CODE_UNITS
-#define CODE_UNITS 4096
+#ifndef ROUNDS
+#define ROUNDS 1
 #endif
-constexpr int kCodeUnits = CODE_UNITS;
+#ifndef WROUNDS
+#define WROUNDS 2
+#endif
 Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   const int64_t rh = (int64_t)a.Hq * b.rows, window = a.S < b.L ? a.S : b.L;
   Form f = {};
@@ -1907,11 +2080,18 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
     if (n > div_up(tokens, 64)) n = div_up(tokens, 64);
     return n < 1 ? 1 : n;
   };
+  const int64_t resident = 256 * (cols == 16 ? (c.D == 64 ? 16 : 12) : c.D == 64 ? 12 : 8);  // workgroups of codes_kernel
+  int64_t share = 0;
   Pieces& p = f.p;
+  f.plan.slots = 1;
   p = {1, a.S, 1, (int)window, 0};
   if (a.topk > 0 && a.S <= b.L) {  // (no row has a longer span among its candidates)
     const int64_t units = f.buckets ? items / cols + 1 : items;
-    p.routed_tokens = (int)div_up(div_up(a.S, cut(a.S, units, codes ? kCodeUnits : 1024, 64)), 16) * 16;
+    // codes_kernel: a share of all tokens for every workgroup that the chip holds at once, of one span or several
+    if (codes) share = std::max<int64_t>(items * a.S / (ROUNDS * resident), 64);
+    f.plan.slots = codes ? (int)std::min<int64_t>(std::max<int64_t>(share / a.S, 1), a.topk) : 1;
+    const int64_t pieces = codes ? std::min<int64_t>(div_up(a.S, share), 64) : cut(a.S, units, 1024, 64);
+    p.routed_tokens = (int)div_up(div_up(a.S, pieces), codes ? 32 : 16) * (codes ? 32 : 16);
     p.routed = (int)div_up(a.S, p.routed_tokens);
   }
   if (f.tiles) {
@@ -1919,7 +2099,8 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
     const int64_t longest = window + cols / a.G + 17;  // a tile's rows may lie in two windows; it begins at a multiple of 16
     // Enough workgroups of the narrow form for what fits the chip at once, four or (D = 64) nine to a compute unit: 32 caches of 1000
     // tokens, 32:8 heads, 39 us with four times as many, 33 so; of the wide one, twice.
-    const int64_t n = cut(longest, (int64_t)f.plan.tiles * c.Hkv, codes ? kCodeUnits : cols == 32 && c.D == 64 ? 2048 : 1024, 256);
+    const int64_t n = codes && share ? std::min<int64_t>(div_up(longest, std::max<int64_t>(share, 64)), 256)
+                      : cut(longest, (int64_t)f.plan.tiles * c.Hkv, codes ? WROUNDS * resident : cols == 32 && c.D == 64 ? 2048 : 1024, 256);
     p.window_tokens = (int)div_up(div_up(longest, n), 64) * 64;
     p.window = (int)div_up(longest, p.window_tokens);
     f.plan.window_units = div_up((int64_t)f.plan.tiles * p.window * c.Hkv, 8) * 8;
@@ -1941,7 +2122,8 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
     f.plan.units += f.most_tiles * p.routed;
     f.plan_bytes = align_up(sizeof(int32_t) * (align_up(2 * (size_t)buckets, 64) + 4 * (size_t)f.most_tiles + (size_t)items + (size_t)f.most_tiles * cols), 256);
   } else {
-    f.plan.units += items * p.routed;
+    f.plan.groups = a.topk > 0 ? (int)div_up(a.topk, f.plan.slots) : 0;
+    f.plan.units += rh * f.plan.groups * p.routed;
   }
   return f;
 }
@@ -1949,7 +2131,7 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
 // The stages fill up to 128 KB of dynamic LDS beside the static arrays: more than a kernel has without asking.
 template <typename T, int D, bool FP4, int NW, int CB, int STEP, bool ANY, bool PAST>
 bool launch_tiles_as(const PagedArgs& x, const TilePlan& plan, hipStream_t st) {
-  constexpr int kBytes = FP4 && NW == 1 ? 32 * D * (int)sizeof(T) : 2 * 2 * STEP * D * (int)sizeof(T);
+  constexpr int kBytes = 2 * 2 * STEP * D * (int)sizeof(T);
   static std::mutex mu;
   static bool asked[64];
   int dev = -1;
@@ -1967,9 +2149,6 @@ bool launch_tiles_as(const PagedArgs& x, const TilePlan& plan, hipStream_t st) {
 template <typename T, int D, bool FP4, int NW, int CB, int STEP>
 bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
   const bool past = NW > 1 && f.o_bytes >= kStreamedRecords;
-  if constexpr (FP4 && NW == 1) {
-    if (x.c.ps % 32 == 0) return launch_tiles_as<T, D, FP4, NW, CB, STEP, false, false>(x, plan, st);
-  }
   if constexpr (!FP4) {
     if (x.c.ps % 16 == 0) {
       if constexpr (NW > 1)
@@ -1980,6 +2159,19 @@ bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipSt
   if constexpr (NW > 1)
     if (past) return launch_tiles_as<T, D, FP4, NW, CB, STEP, true, true>(x, plan, st);
   return launch_tiles_as<T, D, FP4, NW, CB, STEP, true, false>(x, plan, st);
+}
+
+template <int D, int CB>
+bool launch_codes(const PagedArgs& x, const TilePlan& plan, hipStream_t st) {
+  constexpr int kBytes = 32 * D * 2;  // V's values of 32 tokens
+  if (x.c.ps % 32 == 0) codes_kernel<D, CB, true><<<grid_of(plan.units), 64, kBytes, st>>>(x, plan);
+  else codes_kernel<D, CB, false><<<grid_of(plan.units), 64, kBytes, st>>>(x, plan);
+  return true;
+}
+template <typename T, int D, bool FP4>
+bool launch_few_columns(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
+  if constexpr (FP4) return f.cols_log2 == 4 ? launch_codes<D, 1>(x, plan, st) : launch_codes<D, 2>(x, plan, st);
+  else return launch_tiles<T, D, FP4, 1, 1, 32>(x, f, plan, st);
 }
 
 template <typename T, int D, bool FP4>
@@ -2003,8 +2195,7 @@ sl_status launch(const PagedArgs& x, const Form& f, char* ws, hipStream_t st) {
     }
     bool done;
     if constexpr (sizeof(T) == 2)
-      done = f.cols_log2 == 4   ? launch_tiles<T, D, FP4, 1, 1, FP4 ? 64 : 32>(x, f, plan, st)
-             : f.cols_log2 == 5 ? launch_tiles<T, D, FP4, 1, FP4 ? 2 : 1, FP4 ? 64 : 32>(x, f, plan, st)
+      done = f.cols_log2 <= 5   ? launch_few_columns<T, D, FP4>(x, f, plan, st)
              : f.cols_log2 == 7 ? launch_tiles<T, D, FP4, 4, 1, 64>(x, f, plan, st)
                                 : launch_tiles<T, D, FP4, 4, 2, 64>(x, f, plan, st);
     else
