@@ -47,6 +47,7 @@ struct TilePlan {
   int64_t window_units;  // tiles * pieces of a window * Hkv
   int64_t units;         // ... and the spans' pieces: workgroups that have something to do
   int slots, groups;     // codes_kernel: slots of a unit, units of a row's slots
+  FastDiv by_rows, by_G, by_S, by_Hkv, by_window, by_routed, by_groups;
   int spans, buckets;    // spans of the longest sequence; B * Hkv * spans
   int32_t *counts, *first_tile;  // [buckets]
   int most_tiles;  // of the buckets; a multiple of 8
@@ -90,7 +91,8 @@ struct Entry {
 };
 // The last entry e with before(cu[e], e), which holds for entry 0 and up to some entry: 64 of them are looked at at once, with all that
 // is asked of the one that is found.  (A binary search is a chain of loads: a piece of 64 tokens took as long to find as to attend.)
-template <typename F>
+// (READ_LEN: else its length is left at 0.)
+template <bool READ_LEN = true, typename F>
 __device__ __forceinline__ Entry find_entry(const PagedArgs& x, F&& before) {
   const int lane = threadIdx.x & 63;
   int lo = 0, n = x.b.B;
@@ -102,7 +104,7 @@ __device__ __forceinline__ Entry find_entry(const PagedArgs& x, F&& before) {
     lo += k * step;
   }
   const int at = min(lo + lane, x.b.B - 1);
-  const int cu = x.b.cu[at], r0 = max(cu, 0), r1 = x.b.cu[at + 1], s = x.b.seqs[at], len = length_of(x.c, s);
+  const int cu = x.b.cu[at], r0 = max(cu, 0), r1 = x.b.cu[at + 1], s = x.b.seqs[at], len = READ_LEN ? length_of(x.c, s) : 0;
   const int k = max(__popcll(__builtin_amdgcn_ballot_w64(lane < n && before(cu, at))) - 1, 0);
   return {lo + k, __builtin_amdgcn_readlane(s, k), __builtin_amdgcn_readlane(len, k), __builtin_amdgcn_readlane(r0, k),
           __builtin_amdgcn_readlane(r1, k)};
@@ -1357,12 +1359,12 @@ struct NarrowCodes {
                         ((((i & 3) >> 1) ^ swizzle(row)) << 4) + 8 * (i & 1);
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-      const bf16x8 a = transposed8<D>((const bf16_t*)(const __attribute__((address_space(3))) bf16_t*)(uintptr_t)(at ^ (db << 5)));
+      const bf16x8 a = transposed8<D>((const bf16_t*)(const __attribute__((address_space(3))) bf16_t*)(uintptr_t)((at ^ ((db & 3) << 5)) + (db >> 2) * 128));
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[cb][k], o[cb][db], 0, 0, 0);
     }
     // reads run ahead of their products (0x100 = LDS read, 0x008 = MFMA)
-    constexpr int AHEAD = DB < 6 ? DB : 6;
+    constexpr int AHEAD = 4;
     __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 2 + k);
 #pragma unroll
     for (int db = 0; db < DB - AHEAD; ++db) {
@@ -1393,7 +1395,8 @@ struct NarrowCodes {
   }
   // The records of piece `part` (of a span's; or of the window) of the columns in s_rh, as tile_kernel's: a column with a value that is not
   // finite is marked.
-  __device__ __forceinline__ void results(const PagedArgs& x, bool window, int part, const int* s_rh, char* s_room, int lane) const {
+  __device__ __forceinline__ void results(const PagedArgs& x, bool window, int part, const int* s_rh, char* s_room) const {
+    const int lane = lane_now();  // (what could be derived from the lane ahead of all turns would take their registers)
     const bool direct = x.p.count == 1;
     constexpr int LPR = D / 8, RPI = 64 / LPR;  // lanes of a row, rows of an instruction
 #pragma unroll
@@ -1468,44 +1471,70 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
   const int lane = threadIdx.x;
   const int64_t unit = workgroup();
   if (unit >= plan.units) return;  // (grid_of rounds up)
-  const bool window = unit < plan.window_units;
+  const bool window = unit < plan.window_units;  // (there are fewer than 2^31 units)
   Entry at;
   int head, part, u0, cols, begin = 0, end = 0, all_lo, all_last;
   int mine = -1;      // lane k: span of slot k of the unit's own row, -1: none, or none of its slots
   uint32_t todo = 0;  // slots to come
+  int page = -1, asked = -1;  // pages of the first turn, of slot `asked`
+  typedef NarrowCodes<D, CB, EASY> Codes;
+  Codes n;
+  auto load_queries = [&](auto&& head_of, auto&& row_of) {
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const int u = u0 + min(cb * 16 + (lane & 15), cols - 1);  // (a column of nobody reads some row: nothing is made of it)
+      n.load_q(cb, static_cast<const bf16_t*>(x.Q) + head_of(u) * x.a.qsh + row_of(u) * x.a.qst, lane);
+    }
+  };
+  const uint32_t topk = x.a.topk, by_topk = (65536 + topk - 1) / max(topk, 1u);  // (exact below 2^10, as lists are)
+  // column c: row and query head
+  auto row_of = [&](uint32_t c) { return at.r0 + (int)(c / plan.by_G); };
+  auto head_of = [&](uint32_t c) { return head * x.a.G + (int)(c - c / plan.by_G * x.a.G); };
   if (window) {
-    head = (int)(unit % x.c.Hkv);
-    const int turn = (int)(unit / x.c.Hkv);
-    if (turn >= plan.tiles * x.p.window) return;
-    const int tile = plan.tiles - 1 - turn / x.p.window;
-    part = turn % x.p.window;
-    const ColumnRun run = columns_of(x, tile, COLS, x.a.G);
+    const uint32_t turn = (uint32_t)unit / plan.by_Hkv;
+    head = (int)((uint32_t)unit - turn * x.c.Hkv);
+    const uint32_t back = turn / plan.by_window;
+    part = (int)(turn - back * x.p.window);
+    if ((int)back >= plan.tiles) return;
+    const ColumnRun run = columns_of(x, plan.tiles - 1 - (int)back, COLS, x.a.G);
     if (run.n <= 0) return;
     at = run.at;
     u0 = run.u0;
     cols = run.n;
+    load_queries(head_of, row_of);
   } else {
-    const int64_t u = unit - plan.window_units;
-    part = (int)(u % x.p.routed);
-    const int64_t v = u / x.p.routed;
-    const int rh = (int)(v / plan.groups), group = (int)(v - (int64_t)rh * plan.groups);
-    const int h = rh / x.b.rows, row = rh - h * x.b.rows;
-    at = entry_with_row(x, row);
+    const uint32_t u = (uint32_t)(unit - plan.window_units), v = u / plan.by_routed;
+    part = (int)(u - v * x.p.routed);
+    const uint32_t rh = v / plan.by_groups, h = rh / plan.by_rows;
+    const int group = (int)(v - rh * plan.groups), row = (int)(rh - h * x.b.rows);
+    // Three rounds of loads: the row's own slots and its entry; its length, the pages of the first slot, the queries, and the lists of all
+    // columns; codes.  (With the lists before the pages and the queries behind them, one token behind a million took MEASURE.)
+    const int k0 = group * plan.slots, k1 = min(k0 + plan.slots, (int)topk);
+    const bool my_slot = lane >= k0 && lane < k1;
+    if (my_slot) mine = x.idx[h * x.a.ish + row * x.a.ist + lane];
+    at = find_entry<false>(x, [=](int r0, int) { return r0 <= row; });
     if (row < at.r0 || row >= at.r1) return;
-    head = h / x.a.G;
-    const int own = (row - at.r0) * x.a.G + h - head * x.a.G;  // column of the entry
+    at.len = length_of(x.c, at.s);
+    head = (int)(h / plan.by_G);
+    const int own = (row - at.r0) * x.a.G + (int)h - head * x.a.G;  // column of the entry
     u0 = own & ~(COLS - 1);
     cols = min((min(at.r1, x.b.rows) - at.r0) * x.a.G - u0, COLS);
-    // the columns' lists, without what is no candidate
-    const uint32_t topk = x.a.topk, by_topk = (65536 + topk - 1) / topk;  // (exact below 2^11 / 2)
-    for (int i = lane; i < cols * (int)topk; i += 64) {
-      const int c = i * by_topk >> 16, k = i - c * topk;
-      const int row2 = at.r0 + (u0 + c) / x.a.G, h2 = head * x.a.G + (u0 + c) % x.a.G;
-      const int pos = position_of(x, at, row2), j = x.idx[h2 * x.a.ish + row2 * x.a.ist + k];
-      s_list[i] = pos >= 0 && j >= 0 && j < pos / x.a.S ? j : -1;
+    {
+      asked = k0;
+      const int j = __builtin_amdgcn_readlane(mine, k0);
+      const int64_t t = ((int64_t)j * x.a.S + part * x.p.routed_tokens) / 32 * 32 + lane;
+      const uint32_t k = (uint32_t)t / x.c.by_ps;
+      if (j >= 0 && t <= INT_MAX && (int)k < x.c.max_pages && (uint32_t)at.s < (uint32_t)x.c.n_seqs)
+        page = x.c.tables[(int64_t)at.s * x.c.max_pages + k];
     }
-    const int k0 = group * plan.slots, k1 = min(k0 + plan.slots, (int)topk);
-    if (lane >= k0 && lane < k1) {
+    load_queries(head_of, row_of);
+    // the columns' lists, without what is no candidate
+    for (int i = lane; i < cols * (int)topk; i += 64) {
+      const int c = i * by_topk >> 16, k = i - c * topk, row2 = row_of(u0 + c);
+      const int pos = position_of(x, at, row2), j = x.idx[head_of(u0 + c) * x.a.ish + row2 * x.a.ist + k];
+      s_list[i] = pos >= 0 && j >= 0 && j < (int)((uint32_t)pos / plan.by_S) ? j : -1;
+    }
+    if (my_slot) {
       mine = s_list[(own - u0) * topk + lane];
       if (mine < 0) x.part_lse[(int64_t)rh * x.p.count + lane * x.p.routed + part] = -INFINITY;
     }
@@ -1523,33 +1552,27 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
   head = __builtin_amdgcn_readfirstlane(head);
   part = __builtin_amdgcn_readfirstlane(part);
   todo = __builtin_amdgcn_readfirstlane(todo);
-  typedef NarrowCodes<D, CB, EASY> Codes;
-  Codes n;
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb) {
-    const int u = u0 + min(cb * 16 + (lane & 15), cols - 1);  // (a column of nobody reads some row: nothing is made of it)
-    n.load_q(cb, static_cast<const bf16_t*>(x.Q) + (int64_t)(head * x.a.G + u % x.a.G) * x.a.qsh + (at.r0 + u / x.a.G) * x.a.qst, lane);
-  }
   // ---- what a unit attends: of the window, its columns' ranges at once; else the next slot's span
   auto take_window = [&] {
-    const int r0 = at.r0, pos0 = at.len - (at.r1 - r0);
-    const int first = max(pos0 + u0 / x.a.G, 0);     // position of the tile's first row that has a token
+    const int pos0 = at.len - (at.r1 - at.r0), start_pos = pos0 + row_of(u0) - at.r0, end_pos = pos0 + row_of(u0 + cols - 1) - at.r0;
+    const int first = max(start_pos, 0);             // position of the tile's first row that has a token
     const int most = min(at.len, x.b.L) - 1;         // of the last row that has one
-    const int64_t origin = (int64_t)(first / x.a.S) * x.a.S / 16 * 16 + (int64_t)part * x.p.window_tokens;
+    auto window_of = [&](int pos) { return (int)((uint32_t)max(pos, 0) / plan.by_S) * x.a.S; };
+    const int64_t origin = (int64_t)window_of(first) / 16 * 16 + (int64_t)part * x.p.window_tokens;
     const int from = (int)min(origin, (int64_t)INT_MAX), upto = (int)min(origin + x.p.window_tokens - 1, (int64_t)INT_MAX);
-    auto lo_of = [&](int pos) { return max(pos / x.a.S * x.a.S, from); };
+    auto lo_of = [&](int pos) { return max(window_of(pos), from); };
     auto last_of = [&](int pos) { return min(pos, upto); };
     // Later rows begin and end no earlier.
-    const int end_pos = pos0 + (u0 + cols - 1) / x.a.G, last = min(end_pos, most), start_pos = pos0 + u0 / x.a.G;
+    const int last = min(end_pos, most);
     begin = lo_of(first);
     end = first > last ? begin : last_of(last) + 1;
     all_lo = start_pos < 0 || end_pos > most ? INT_MAX : lo_of(last);  // (a row without a token attends nothing)
     all_last = last_of(first);
     if (lane < COLS) {
-      const int u = u0 + lane, pos = pos0 + u / x.a.G;
+      const int u = u0 + lane, row = row_of(u), pos = pos0 + row - at.r0;
       int rh = -1, clo = INT_MAX, clast = -1;
       if (lane < cols) {
-        rh = (head * x.a.G + u % x.a.G) * x.b.rows + r0 + u / x.a.G;
+        rh = head_of(u) * x.b.rows + row;
         if (pos >= 0 && pos <= most && lo_of(pos) <= last_of(pos)) {
           clo = lo_of(pos);
           clast = last_of(pos);
@@ -1567,6 +1590,7 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
     *to = min(*from + x.p.routed_tokens, (j + 1) * x.a.S);
   };
   auto take_span = [&](int k) {
+    const int lane = lane_now();
     const int j = __builtin_amdgcn_readlane(mine, k);
     piece_of(k, &begin, &end);
     all_lo = begin;
@@ -1576,11 +1600,10 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
       s_lo[lane] = INT_MAX;
       s_last[lane] = -1;
     }
-    const uint32_t topk = x.a.topk, by_topk = (65536 + topk - 1) / topk;
     for (int i = lane; i < cols * (int)topk; i += 64) {
       if (s_list[i] != j) continue;
       const int c = i * by_topk >> 16, u = u0 + c;
-      s_rh[c] = ((head * x.a.G + u % x.a.G) * x.b.rows + at.r0 + u / x.a.G) * 32 + i - c * topk;
+      s_rh[c] = (head_of(u) * x.b.rows + row_of(u)) * 32 + i - c * topk;
       s_lo[c] = begin;
       s_last[c] = end - 1;
     }
@@ -1588,7 +1611,9 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
   if (window) {
     take_window();
   } else {
-    take_span(__builtin_ctz(todo));
+    const int k = __builtin_ctz(todo);
+    if (k != asked) asked = -1;
+    take_span(k);
     todo &= todo - 1;
   }
   begin = __builtin_amdgcn_readfirstlane(begin);
@@ -1622,7 +1647,7 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
   n.clear();
   if (begin < end) {
     Turn now = {begin / 32 * 32, end}, next = turn_after(now);
-    int page = look_up(now);
+    if (window || asked < 0) page = look_up(now);
     uint64_t live = there(page, now);
 #pragma unroll
     for (int k = 0; k < 2; ++k) Codes::ask(raw[k], x.c, K, V, page, now.t, 32 * k, lane);
@@ -1668,7 +1693,7 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
 #pragma unroll 1
     while (next.t >= 0)
       if (take(std::true_type())) {  // (turns are left: so are spans)
-        n.results(x, window, part, s_rh, s_dynamic, lane);
+        n.results(x, window, part, s_rh, s_dynamic);
         n.clear();
         take_span(__builtin_ctz(todo));
         todo &= todo - 1;
@@ -1679,7 +1704,7 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
       }
     take(std::false_type());
   }
-  n.results(x, window, part, s_rh, s_dynamic, lane);
+  n.results(x, window, part, s_rh, s_dynamic);
 }
 
 // ---- the rows that list a span: buckets (entry, kv head, span), each cut into tiles of `cols` items
@@ -2045,11 +2070,8 @@ struct Form {
   size_t o_bytes, lse_bytes, plan_bytes;
 };
 
-#ifndef ROUNDS
-#define ROUNDS 1
-#endif
 #ifndef WROUNDS
-#define WROUNDS 2
+#define WROUNDS 3
 #endif
 Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   const int64_t rh = (int64_t)a.Hq * b.rows, window = a.S < b.L ? a.S : b.L;
@@ -2088,7 +2110,10 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   if (a.topk > 0 && a.S <= b.L) {  // (no row has a longer span among its candidates)
     const int64_t units = f.buckets ? items / cols + 1 : items;
     // codes_kernel: a share of all tokens for every workgroup that the chip holds at once, of one span or several
-    if (codes) share = std::max<int64_t>(items * a.S / (ROUNDS * resident), 64);
+    if (codes) {
+      const int64_t even = items * a.S / resident;
+      share = std::max<int64_t>({(int64_t)64, even / 2, std::min<int64_t>(256, even * 3 / 2)});
+    }
     f.plan.slots = codes ? (int)std::min<int64_t>(std::max<int64_t>(share / a.S, 1), a.topk) : 1;
     const int64_t pieces = codes ? std::min<int64_t>(div_up(a.S, share), 64) : cut(a.S, units, 1024, 64);
     p.routed_tokens = (int)div_up(div_up(a.S, pieces), codes ? 32 : 16) * (codes ? 32 : 16);
@@ -2162,8 +2187,15 @@ bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipSt
 }
 
 template <int D, int CB>
-bool launch_codes(const PagedArgs& x, const TilePlan& plan, hipStream_t st) {
+bool launch_codes(const PagedArgs& x, TilePlan plan, hipStream_t st) {
   constexpr int kBytes = 32 * D * 2;  // V's values of 32 tokens
+  plan.by_rows = fast_div(x.b.rows);
+  plan.by_G = fast_div(x.a.G);
+  plan.by_S = fast_div(x.a.S);
+  plan.by_Hkv = fast_div(x.c.Hkv);
+  plan.by_window = fast_div(x.p.window);
+  plan.by_routed = fast_div(x.p.routed);
+  plan.by_groups = fast_div(std::max(plan.groups, 1));
   if (x.c.ps % 32 == 0) codes_kernel<D, CB, true><<<grid_of(plan.units), 64, kBytes, st>>>(x, plan);
   else codes_kernel<D, CB, false><<<grid_of(plan.units), 64, kBytes, st>>>(x, plan);
   return true;
