@@ -1648,10 +1648,15 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
   if (begin < end) {
     Turn now = {begin / 32 * 32, end}, next = turn_after(now);
     if (window || asked < 0) page = look_up(now);
+    const int page_next = look_up(next);
     uint64_t live = there(page, now);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) Codes::ask(raw[k], x.c, K, V, page, now.t, 32 * k, lane);
-    page = look_up(next);
+    for (int k = 0; k < 2; ++k) {
+      __builtin_amdgcn_sched_barrier(0);  // (in the turns' order)
+      Codes::ask(raw[k], x.c, K, V, page, now.t, 32 * k, lane);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    page = page_next;
     // (a query that may not have come yet would be waited for in every turn, and what was asked for later with it)
     n.have_q();
     // Loads come back in order: pages are asked for before a turn's codes, and the last turn, which asks for none, has code of its own.  (A
