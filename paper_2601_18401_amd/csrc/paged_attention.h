@@ -533,8 +533,10 @@ __device__ __forceinline__ void stage_rows_any(T* to, int first_row, const T* ba
 }
 
 // A stage of a cache in 4 bits, 16 bytes of codes and their scale a lane and piece: global -> registers, and, a step later, the values
-// they stand for, which T holds exactly, -> LDS, where they lie as stage_rows leaves rows.
-template <typename T, int D, int NW, int STEP>
+// they stand for, which T holds exactly, -> LDS, where K lies as stage_rows leaves it.  V's 16-byte pieces lie in another order (bf16), piece
+// 4 a + j of a row's blocks a at PIECES j + a: four lanes that write together hold the same j of a row's blocks.
+// EASY: a wavefront's rows lie in one page, and next to each other.
+template <typename T, int D, int NW, int STEP, bool EASY>
 struct CodeStage {
   static constexpr int PIECES = D / 32, ROWS = STEP / NW;     // pieces of a row; rows of a wavefront
   static constexpr int EACH = ROWS * PIECES, N = 2 * EACH / 64;  // pieces of K or V, and a lane's of both
@@ -543,38 +545,60 @@ struct CodeStage {
   int scale[N];
 
   // row of the stage, piece of the row, K (0) or V (1)
-  __device__ __forceinline__ static int row_of(int i, int wave, int lane) { return (NW == 1 ? 0 : wave * ROWS) + (i * 64 + lane) % EACH / PIECES; }
+  __device__ __forceinline__ static int row_of(int i, int wave, int lane) { return wave * ROWS + (i * 64 + lane) % EACH / PIECES; }
   __device__ __forceinline__ static int piece_of(int lane) { return lane % PIECES; }
   __device__ __forceinline__ static int tensor_of(int i, int lane) { return (i * 64 + lane) / EACH; }
+  __device__ __forceinline__ static int piece_at(int place) { return 4 * (place % PIECES) + place / PIECES; }
 
-  // base: of the layer and head; page of lane l: of row l of the stage
+  // base: of the layer and head; page of lane l: of row l of the stage.  (A row without a page gets what lies in page 0; `store` knows.)
   __device__ __forceinline__ void load(const PageCache& c, int64_t base, int page, int t0, int wave, int lane) {
+    if constexpr (EASY) {
+      const uint32_t p = __builtin_amdgcn_readlane(page, wave * ROWS), t = __builtin_amdgcn_readfirstlane(t0 + wave * ROWS);
+      const uint32_t row = __builtin_amdgcn_readfirstlane(t - t / c.by_ps * c.ps);
+      const int64_t at = uniform64(base + (int64_t)(p < (uint32_t)c.n_pages ? p : 0) * c.page);
+      const int64_t codes = at + (int64_t)row * (D / 2), scales = at + (int64_t)c.ps * (D / 2) + (int64_t)row * PIECES;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint8_t* const from = static_cast<const uint8_t*>(tensor_of(i, lane) ? c.V : c.K);
+        const uint32_t mine = (uint32_t)((i * 64 + lane) % EACH);
+        code[i] = load16(from + codes + mine * 16);
+        scale[i] = (from + scales)[mine];
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int row = row_of(i, wave, lane), p = __shfl(page, row, 64);
-      const uint32_t t = (uint32_t)(t0 + row);
-      code[i] = make_uint4(0, 0, 0, 0);
-      scale[i] = 0;
-      if ((uint32_t)p < (uint32_t)c.n_pages) {
-        const uint8_t* const from = static_cast<const uint8_t*>(tensor_of(i, lane) ? c.V : c.K) + base + p * c.page;
-        const uint32_t in_page = t - t / c.by_ps * c.ps;
-        const int64_t at = (int64_t)in_page * PIECES + piece_of(lane);  // of the head's pieces, and its scales
-        code[i] = NW == 1 ? load16_stream(from + at * 16) : load16(from + at * 16);
-        scale[i] = from[(int64_t)c.ps * (D / 2) + at];
-      }
+      const int row = row_of(i, wave, lane);
+      const uint32_t p = __shfl(page, row, 64), t = (uint32_t)(t0 + row), in_page = t - t / c.by_ps * c.ps;
+      const uint8_t* const from = static_cast<const uint8_t*>(tensor_of(i, lane) ? c.V : c.K) + base + (int64_t)(p < (uint32_t)c.n_pages ? p : 0) * c.page;
+      const int64_t at = (int64_t)in_page * PIECES + piece_of(lane);  // of the head's pieces, and its scales
+      code[i] = load16(from + at * 16);
+      scale[i] = from[(int64_t)c.ps * (D / 2) + at];
     }
   }
-  __device__ __forceinline__ void store(T* kt, T* vt, int wave, int lane) const {
+  // live: a bit for each row of the stage that there is: others become zeros (what lies there may be NaN, and zero times that need not be zero)
+  __device__ __forceinline__ void store(T* kt, T* vt, uint64_t live, int wave, int lane) {
+    if ((uint32_t)(live >> (wave * ROWS) & ((1u << ROWS) - 1)) != (1u << ROWS) - 1) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (!(live >> row_of(i, wave, lane) & 1)) {
+          code[i] = make_uint4(0, 0, 0, 0);
+          scale[i] = 0;
+        }
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int row = row_of(i, wave, lane), v = tensor_of(i, lane);
+      const int row = row_of(i, wave, lane), v = tensor_of(i, lane), piece = piece_of(lane);
       const int swizzle = v ? v_swizzle<T, D>(row) : k_swizzle<T, D>(row);
       char* const to = reinterpret_cast<char*>((v ? vt : kt) + row * D);
       constexpr int PER = 32 * (int)sizeof(T) / 16;  // 16-byte pieces of 32 values
       uint4 w[PER];
       fp4_to_rows<T>(code[i], scale[i], w);
 #pragma unroll
-      for (int j = 0; j < PER; ++j) *reinterpret_cast<uint4*>(to + ((piece_of(lane) * PER + j) ^ swizzle) * 16) = w[j];
+      for (int j = 0; j < PER; ++j) {
+        const int place = v && sizeof(T) == 2 ? PIECES * j + piece : piece * PER + j;
+        *reinterpret_cast<uint4*>(to + (place ^ swizzle) * 16) = w[j];
+      }
     }
   }
 };
@@ -865,6 +889,7 @@ __device__ __forceinline__ void wait_loads() {
 template <typename T, int D, bool FP4, int NW, int CB, int STEP, bool ANY, bool PAST>
 __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
   constexpr int COLS = NW * 32 * CB;
+  constexpr bool EACH_ROW = ANY || FP4;  // pages are looked up row by row
   extern __shared__ __align__(1024) char s_dynamic[];  // (static, the compiler would wait for staging loads at every read)
   T(*const s_kv)[2][STEP * D] = reinterpret_cast<T(*)[2][STEP * D]>(s_dynamic);
   __shared__ int s_rh[COLS], s_lo[COLS], s_last[COLS];
@@ -881,7 +906,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
   // ANY: lane l has the page of row l of the next stage.
   int page = -1;
   auto look_up = [&](int t0) {
-    const int ln = lane_now(), t = t0 + (ANY ? ln % STEP : ln * 16);
+    const int ln = lane_now(), t = t0 + (EACH_ROW ? ln % STEP : ln * 16);
     return t < end ? x.c.tables[(int64_t)seq * x.c.max_pages + (uint32_t)t / x.c.by_ps] : -1;
   };
   auto ask_pages = [&] {
@@ -1012,7 +1037,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
   head = __builtin_amdgcn_readfirstlane(head);
   const int64_t base = x.b.layer * x.c.layer + head * x.c.head;
   const T *const K = static_cast<const T*>(x.c.K), *const V = static_cast<const T*>(x.c.V);
-  CodeStage<T, D, NW, STEP> codes;
+  typedef CodeStage<T, D, NW, STEP, !ANY> Codes;
+  Codes codes;
   constexpr int GROUPS = STEP / 16;
   auto there = [&](int page) { return (uint64_t)__builtin_amdgcn_ballot_w64((uint32_t)page < (uint32_t)x.c.n_pages); };
   int batch = begin, next_page = -1;
@@ -1060,10 +1086,10 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
   };
   if (begin < end) {
     alive = there(page);
-    if (!ANY && end - batch > 1024) next_page = look_up(batch + 1024);
+    if (!EACH_ROW && end - batch > 1024) next_page = look_up(batch + 1024);
     stage(begin, 0);
     if constexpr (FP4) {
-      codes.store(s_kv[0][0], s_kv[0][1], wave, lane_now());
+      codes.store(s_kv[0][0], s_kv[0][1], live[0], wave, lane_now());
       if (begin + STEP < end) stage(begin + STEP, 1);
     }
   }
@@ -1084,7 +1110,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       }
-      if (t0 + STEP < end) codes.store(s_kv[b ^ 1][0], s_kv[b ^ 1][1], wave, lane_now());
+      if (t0 + STEP < end) codes.store(s_kv[b ^ 1][0], s_kv[b ^ 1][1], live[b ^ 1], wave, lane_now());
       if (t0 + 2 * STEP < end) stage(t0 + 2 * STEP, b);
     } else {
       wait_loads();
@@ -1098,9 +1124,9 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
     for (int at = 0; at < STEP; at += 32 * KB) {
       const int t = t0 + at, upto = t + 32 * KB - 1;
       if (upto < any_lo || t > any_last) continue;
-      typedef std::conditional_t<ANY, uint64_t, uint32_t> Live;
-      constexpr Live kAll = ANY ? (KB == 2 ? ~(Live)0 : (Live)0xffffffffu) : (Live)((1 << 2 * KB) - 1);
-      const Live now = (Live)(here >> (ANY ? at : at / 16)) & kAll;
+      typedef std::conditional_t<EACH_ROW, uint64_t, uint32_t> Live;
+      constexpr Live kAll = EACH_ROW ? (KB == 2 ? ~(Live)0 : (Live)0xffffffffu) : (Live)((1 << 2 * KB) - 1);
+      const Live now = (Live)(here >> (EACH_ROW ? at : at / 16)) & kAll;
       tile.attend(&s_kv[b][0][at * D], &s_kv[b][1][at * D], t, t < all_lo || upto > all_last || now != kAll, now, x.scale_log2e,
                   s_lo + wave * 32 * CB, s_last + wave * 32 * CB);
     }
@@ -1168,7 +1194,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
       const int row = i * RPI + ln / LPR, piece = ln % LPR;
       if (!(write >> row & 1)) continue;
       const uint4 v = *reinterpret_cast<const uint4*>(s_out + (row * LPR + (piece ^ row % LPR)) * 16);
-      char* const at = to + record(s_rh[wave * 32 * CB + cb * 32 + row]) * (D * (int)sizeof(Value)) + piece * 16;
+      const int unit = FP4 && sizeof(T) == 2 ? Codes::piece_at(piece) : piece;  // (V's pieces in a row's order)
+      char* const at = to + record(s_rh[wave * 32 * CB + cb * 32 + row]) * (D * (int)sizeof(Value)) + unit * 16;
       if (PAST) store16_stream(at, v);
       else *reinterpret_cast<uint4*>(at) = v;
     }
@@ -2179,12 +2206,10 @@ bool launch_tiles_as(const PagedArgs& x, const TilePlan& plan, hipStream_t st) {
 template <typename T, int D, bool FP4, int NW, int CB, int STEP>
 bool launch_tiles(const PagedArgs& x, const Form& f, const TilePlan& plan, hipStream_t st) {
   const bool past = NW > 1 && f.o_bytes >= kStreamedRecords;
-  if constexpr (!FP4) {
-    if (x.c.ps % 16 == 0) {
-      if constexpr (NW > 1)
-        if (past) return launch_tiles_as<T, D, FP4, NW, CB, STEP, false, true>(x, plan, st);
-      return launch_tiles_as<T, D, FP4, NW, CB, STEP, false, false>(x, plan, st);
-    }
+  if (x.c.ps % 16 == 0) {
+    if constexpr (NW > 1)
+      if (past) return launch_tiles_as<T, D, FP4, NW, CB, STEP, false, true>(x, plan, st);
+    return launch_tiles_as<T, D, FP4, NW, CB, STEP, false, false>(x, plan, st);
   }
   if constexpr (NW > 1)
     if (past) return launch_tiles_as<T, D, FP4, NW, CB, STEP, true, true>(x, plan, st);
