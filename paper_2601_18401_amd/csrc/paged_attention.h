@@ -603,13 +603,6 @@ struct CodeStage {
   }
 };
 
-// Waits for the wavefront's LDS operations.
-__device__ __forceinline__ void wait_lds() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-  asm volatile("" ::: "memory");
-}
-
 // An LDS address that the compiler knows nothing of: where it sees that staged rows are read, it waits for every staging load
 // in flight, the next step's among them.
 template <typename T>
@@ -1105,7 +1098,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
     const uint64_t here = live[b];
     if constexpr (FP4) {
       // the rows of this step lie in their stage; those of the next one, whose codes are in registers, follow into the other
-      wait_lds();
+      // (the wait is for the compiler, too, which would wait for queries, and the codes asked for behind them, in every step)
+      wait_loads();
       if (NW > 1) {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
