@@ -1508,6 +1508,11 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
     }
   };
   const uint32_t topk = x.a.topk, by_topk = (65536 + topk - 1) / max(topk, 1u);  // (exact below 2^10, as lists are)
+  // (what other lanes wrote to LDS is read behind it)
+  auto settle = [] {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
   // column c: row and query head
   auto row_of = [&](uint32_t c) { return at.r0 + (int)(c / plan.by_G); };
   auto head_of = [&](uint32_t c) { return head * x.a.G + (int)(c - c / plan.by_G * x.a.G); };
@@ -1555,6 +1560,7 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
       const int pos = position_of(x, at, row2), j = x.idx[head_of(u0 + c) * x.a.ish + row2 * x.a.ist + k];
       s_list[i] = pos >= 0 && j >= 0 && j < (int)((uint32_t)pos / plan.by_S) ? j : -1;
     }
+    settle();
     if (my_slot) {
       mine = s_list[(own - u0) * topk + lane];
       if (mine < 0) x.part_lse[(int64_t)rh * x.p.count + lane * x.p.routed + part] = -INFINITY;
@@ -1616,11 +1622,13 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
     piece_of(k, &begin, &end);
     all_lo = begin;
     all_last = end - 1;
+    settle();
     if (lane < COLS) {
       s_rh[lane] = -1;
       s_lo[lane] = INT_MAX;
       s_last[lane] = -1;
     }
+    settle();
     for (int i = lane; i < cols * (int)topk; i += 64) {
       if (s_list[i] != j) continue;
       const int c = i * by_topk >> 16, u = u0 + c;
@@ -1628,9 +1636,11 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
       s_lo[c] = begin;
       s_last[c] = end - 1;
     }
+    settle();
   };
   if (window) {
     take_window();
+    settle();
   } else {
     const int k = __builtin_ctz(todo);
     if (k != asked) asked = -1;
@@ -2096,9 +2106,6 @@ struct Form {
   size_t o_bytes, lse_bytes, plan_bytes;
 };
 
-#ifndef WROUNDS
-#define WROUNDS 3
-#endif
 Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   const int64_t rh = (int64_t)a.Hq * b.rows, window = a.S < b.L ? a.S : b.L;
   Form f = {};
@@ -2135,7 +2142,10 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   p = {1, a.S, 1, (int)window, 0};
   if (a.topk > 0 && a.S <= b.L) {  // (no row has a longer span among its candidates)
     const int64_t units = f.buckets ? items / cols + 1 : items;
-    // codes_kernel: a share of all tokens for every workgroup that the chip holds at once, of one span or several
+    // codes_kernel: half of an even share of all tokens, so that there are two workgroups for each that the chip holds at once (some have
+    // nothing to do, where heads list the same spans), but no fewer than 256 while there is one for each.  One token behind a million,
+    // 512 spans of 1024: 26 us with pieces of 256 tokens, 33 and 37 with 192 and 96; 40 caches, 10240 spans of 512: 104 us with one
+    // workgroup for each, 96 with two.
     if (codes) {
       const int64_t even = items * a.S / resident;
       share = std::max<int64_t>({(int64_t)64, even / 2, std::min<int64_t>(256, even * 3 / 2)});
@@ -2150,8 +2160,11 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
     const int64_t longest = window + cols / a.G + 17;  // a tile's rows may lie in two windows; it begins at a multiple of 16
     // Enough workgroups of the narrow form for what fits the chip at once, four or (D = 64) nine to a compute unit: 32 caches of 1000
     // tokens, 32:8 heads, 39 us with four times as many, 33 so; of the wide one, twice.
-    const int64_t n = codes && share ? std::min<int64_t>(div_up(longest, std::max<int64_t>(share, 64)), 256)
-                      : cut(longest, (int64_t)f.plan.tiles * c.Hkv, codes ? WROUNDS * resident : cols == 32 && c.D == 64 ? 2048 : 1024, 256);
+    // codes_kernel: pieces as long as the spans' units (which count in 31 bits); without spans three for each that the chip holds, since the
+    // sequences of a batch may be much shorter than the longest: drafts of 12 sequences of 3000 to 40000 tokens 83 us with one, 71 with two, 69.
+    const int64_t of_piece = (int64_t)f.plan.tiles * c.Hkv;
+    const int64_t n = codes && share ? std::min<int64_t>({div_up(longest, share), (int64_t)256, std::max<int64_t>((1 << 30) / of_piece, 1)})
+                      : cut(longest, of_piece, codes ? 3 * resident : cols == 32 && c.D == 64 ? 2048 : 1024, 256);
     p.window_tokens = (int)div_up(div_up(longest, n), 64) * 64;
     p.window = (int)div_up(longest, p.window_tokens);
     f.plan.window_units = div_up((int64_t)f.plan.tiles * p.window * c.Hkv, 8) * 8;

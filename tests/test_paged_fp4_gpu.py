@@ -242,6 +242,28 @@ def test_attention(case, form):
         check(cache, seqs, cu, Q, idx, scores, S, O)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,ps,S,topk,ns,Ls", [
+    (32, 4, 128, 32, 4, 32, [1] * 20, list(range(380, 420, 2))),       # two spans and three a workgroup, pages of many spans
+    (32, 4, 64, 24, 3, 32, [1] * 32, list(range(300, 364, 2))),        # pages that end anywhere
+    (16, 2, 128, 16, 70, 16, [1] * 64, [9 * 70 + k for k in range(64)]),   # spans that begin and end inside 32 tokens
+    (32, 4, 64, 64, 1, 32, [5] * 8, [500, 430, 480, 9, 5, 511, 450, 500]),   # spans of one token, columns of several rows
+])
+def test_several_spans_a_workgroup(Hq, Hkv, D, ps, S, topk, ns, Ls):
+    """More lists than workgroups that the chip holds: one takes several slots of a row, with the codes of the next one on their way."""
+    g = torch.Generator().manual_seed(S)
+    cache = make_cache(g, Ls, ps, Hkv, D, BF16)
+    cu = [sum(ns[:b]) for b in range(len(ns) + 1)]
+    Q = torch.randn((Hq, cu[-1], D), generator=g).to(BF16).to(DEV)
+    idx = choose(g, Hq, cu[-1], topk, max(Ls) // S + 1)
+    idx[:, ::3] = idx[:1, ::3]      # heads that share their spans
+    scores = torch.randn(idx.shape, generator=g).to(DEV)
+    seqs = list(range(len(Ls)))
+    O, LSE = B.sl_paged_span_attention(cache, i32(seqs), i32(cu), Q, idx, S, L=max(Ls))
+    check(cache, seqs, cu, Q, idx, None, S, O, LSE)
+    O = B.sl_paged_span_attention_combined(cache, i32(seqs), i32(cu), Q, idx, scores, S, L=max(Ls))
+    check(cache, seqs, cu, Q, idx, scores, S, O)
+
+
 @pytest.mark.parametrize("dtype,Hq,Hkv,D,ps,ns,Ls", [
     (BF16, 8, 2, 128, 64, [1, 1], [1500, 3]), (BF16, 8, 1, 64, 20, [4, 1, 7], [900, 513, 7]), (BF16, 4, 4, 128, 32, [200], [200]),
     (BF16, 12, 4, 128, 64, [150, 1, 64], [900, 64, 65]), (F32, 4, 2, 64, 16, [100, 3], [100, 600]), (BF16, 2, 1, 64, 64, [300, 129], [300, 640]),
