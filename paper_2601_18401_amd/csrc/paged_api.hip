@@ -209,8 +209,9 @@ sl_status sl_paged_read(const sl_page_cache* pc, const sl_paged_batch* pb, void*
   sl::PagedBatch b;
   const sl_status s = sl::rows_of(pc, pb, K, V, &stride_h, &stride_t, &c, &b);
   if (s != SL_OK || b.B == 0 || b.rows == 0) return s;
-  // (heads of one row may lie in any order; rows that share elements would be written twice)
-  if (c.Hkv > 1 && stride_h < c.D) return SL_ERR_INVALID_ARG;
+  // (heads first or tokens first: rows that share elements would be written by several)
+  if (c.Hkv > 1 && stride_h < (b.rows - 1) * stride_t + c.D && (stride_h < c.D || (b.rows > 1 && stride_t < (c.Hkv - 1) * stride_h + c.D)))
+    return SL_ERR_INVALID_ARG;
   return sl::paged_read(c, b, K, V, stride_h, stride_t, static_cast<hipStream_t>(hip_stream));
 }
 

@@ -879,6 +879,8 @@ __device__ __forceinline__ void wait_loads() {
 //                that does takes it for all, so that a span is read once for the group.
 //   ANY: pages of a size that is no multiple of 16: every row has a page of its own, at twice the instructions for its address
 //   PAST: records go past the caches
+//   FP4: a cache in 4 bits, whose values are staged where bf16 or fp32 rows would be (CodeStage): three prompts of 2000 to 5500 tokens, 32:8 heads,
+//   374 Gflop in 410 us = 0.91 PFLOP/s, where bf16 rows, which no vector instruction touches, reach 1.05
 template <typename T, int D, bool FP4, int NW, int CB, int STEP, bool ANY, bool PAST>
 __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void tile_kernel(const PagedArgs x, const TilePlan plan) {
   constexpr int COLS = NW * 32 * CB;
@@ -1198,13 +1200,18 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
   }
 }
 
-// What few columns attend of a cache in 4 bits, by one wavefront: CB blocks of 16 columns, 32 tokens at a time, in products of 16x16x32.
+// What few columns attend of a cache in 4 bits, by one wavefront: CB blocks of 16 columns, 64 tokens a turn, in products of 16x16x32.
 //   S^T[token][column] = K . Q^T      A: lane l has token row l % 16 and the channels of quarter l / 16 of a row, which come from its codes
 //                                     in registers: neither K's codes nor its values pass LDS
 //   O^T[d][column] += V^T . P^T       A: V's values through transposing LDS reads, B = P^T straight from the accumulators
 // (Lane l of a 16x16 result holds column l % 16 and rows 4 (l / 16) + r.  Row m of the token block tb of two is token 8 (m / 4) + 4 tb +
 // m % 4, so that a lane's eight accumulators are eight consecutive tokens, 8 (l / 16) on.)  A lane's codes of K and V are of the same tokens
 // and channels, D / 4 of them: one address for both.  Codes are asked for 64 tokens ahead.
+// Measured (D = 128, 32:4 heads): 40 caches of up to 200000 tokens, eight spans of 512 each, 371 MB in 75 us = 4.9 TB/s, where a pure read reaches
+// 6.4; one token behind a million, sixteen spans of 1024, 76 MB in 20.5 us, of which 5 pass before a unit's first codes are asked for
+// and 2 are the launch.  A turn has 280 vector instructions, 128 of them conversions, in some 1700 cycles of a SIMD.  The matrix form of
+// bf16 tiles, values staged in LDS for 32 columns, took 56 us for the million; codes that come row after row and pass LDS on their way
+// to the lanes that multiply them, 81 us for 75: more LDS traffic, and no fewer bytes.
 // EASY: no 32 tokens that begin at a multiple of 32 lie in two pages.
 template <int D, int CB, bool EASY>
 struct NarrowCodes {
@@ -1232,8 +1239,8 @@ struct NarrowCodes {
     for (int i = 0; i < WORDS; ++i) w[i] = x[i];
   }
   // page: of lane l, of token t0 + l; the block begins at t0 + first.  A token without a page gets what lies in page 0: its score is masked,
-  // and `values_only` takes its V.  Where no 32 tokens lie in two pages their address is the wavefront's: no vector instruction is spent on
-  // it (a block has 130 without, and 200 with each lane's own; 40 caches of up to 200000 tokens MEASURE).
+  // and `values_only` takes its V.  Where no 32 tokens lie in two pages their address is the wavefront's, and no vector instruction is spent on
+  // it: a turn has 280 without, and some 420 with each lane's own.
   __device__ __forceinline__ static void ask(Raw& raw, const PageCache& c, const uint8_t* K, const uint8_t* V, int page, int t0, int first,
                                              int lane) {
     const int part = lane >> 4;
@@ -1384,7 +1391,7 @@ struct NarrowCodes {
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) o[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p[cb][k], o[cb][db], 0, 0, 0);
     }
-    // reads run ahead of their products (0x100 = LDS read, 0x008 = MFMA)
+    // reads run four products ahead (0x100 = LDS read, 0x008 = MFMA); one by one, 40 caches take 95 us for 84, and six, registers that spill
     constexpr int AHEAD = 4;
     __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 2 + k);
 #pragma unroll
@@ -1480,10 +1487,8 @@ struct NarrowCodes {
 };
 
 // Workgroups of the window come first, as tile_kernel's; then, of the spans' pieces, one for every (row, head, group of slots, piece): it takes
-// the piece of each of its slots' spans, one after the other.  Other heads and rows of its columns may list the same span: the first one
-// that does takes it for all.  What a unit has to find out before it can ask for codes is a chain of five loads, 9 to 12 us of them where
-// memory is busy, as long as 200 to 300 tokens take: hence several spans a unit, and codes and pages of the next one asked for while one is
-// attended.
+// the piece of each of its slots' spans, one after the other, with codes and pages of the next one asked for while one is attended.  Other
+// heads and rows of its columns may list the same span: the first one that does takes it for all.
 template <int D, int CB, bool EASY>
 __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedArgs x, const TilePlan plan) {
   constexpr int COLS = 16 * CB;
@@ -1534,7 +1539,7 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
     const uint32_t rh = v / plan.by_groups, h = rh / plan.by_rows;
     const int group = (int)(v - rh * plan.groups), row = (int)(rh - h * x.b.rows);
     // Three rounds of loads: the row's own slots and its entry; its length, the pages of the first slot, the queries, and the lists of all
-    // columns; codes.  (With the lists before the pages and the queries behind them, one token behind a million took MEASURE.)
+    // columns; codes.  (Five, of 9 to 12 us where memory is busy, with the lists before the pages and the queries behind them; 5 to 6 so.)
     const int k0 = group * plan.slots, k1 = min(k0 + plan.slots, (int)topk);
     const bool my_slot = lane >= k0 && lane < k1;
     if (my_slot) mine = x.idx[h * x.a.ish + row * x.a.ist + lane];
@@ -1691,7 +1696,8 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
     // (a query that may not have come yet would be waited for in every turn, and what was asked for later with it)
     n.have_q();
     // Loads come back in order: pages are asked for before a turn's codes, and the last turn, which asks for none, has code of its own.  (A
-    // wait for a page behind the codes, or for codes that may not have been asked for, is one for all that is on its way.)
+    // wait for a page behind the codes, or for codes that may not have been asked for, is one for all that is on its way: 40 caches
+    // 109 us with such waits, 100 without.)
     auto take = [&](auto more) {
       constexpr bool MORE = decltype(more)::value;
       const Turn after = MORE ? turn_after(next) : Turn{-1, 1};
@@ -2120,9 +2126,13 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   f.tiles = c.dtype == SL_BF16 || f.buckets || (a.topk == 0 && columns > 32 * (int64_t)b.B);
   const bool narrow = (columns <= 32 * (int64_t)b.B || a.topk > 0) && !f.buckets;
   const bool codes = narrow && c.fp4 && c.dtype == SL_BF16;
-  f.cols_log2 = narrow                                                              ? (codes && columns <= 16 * (int64_t)b.B ? 4 : 5)
-                : c.dtype == SL_BF16 && columns * c.Hkv + items >= 256 * 1024 ? 8
-                                                                             : 7;
+  // Of a cache in 4 bits, tiles of 128 columns also where those of 256 would stand a third emptier (32:4 heads, top-8, us with 256 and with 128:
+  // 300 items a bucket, spans of 256 170 and 153, of 128 235 and 218; 600, 240 and 245, 361 and 353; 1200, 411 and 428; spans of 512 297 and 333).
+  const int64_t in_bucket = f.buckets ? items / buckets : 0;
+  const bool emptier = c.fp4 && f.buckets && div_up(in_bucket, 256) * 256 * 3 >= div_up(in_bucket, 128) * 128 * 4;
+  f.cols_log2 = narrow ? (codes && columns <= 16 * (int64_t)b.B ? 4 : 5)
+                : c.dtype == SL_BF16 && columns * c.Hkv + items >= 256 * 1024 && !emptier ? 8
+                                                                                         : 7;
   const int cols = 1 << f.cols_log2;
   f.whole = !f.tiles && rh >= 1024;
   if (f.whole) {

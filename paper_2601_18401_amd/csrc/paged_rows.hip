@@ -14,7 +14,6 @@ namespace {
 // 218; with plain stores 240), where a large copy reaches 5.0.
 constexpr int kRows = 64;
 
-// 0: bf16, 16 bytes a lane; fp32: 32
 template <typename T>
 __device__ __forceinline__ void load_row8(const T* from, uint4* to) {
   to[0] = load16_stream(from);

@@ -251,12 +251,12 @@ __device__ __forceinline__ void copy_part(const PageCache& c, int from, int to, 
   const int64_t at = (int64_t)c.ps * c.tok;
   const char* const s = base + from * c.page + at;
   char* const d = base + to * c.page + at;
-  const int n = rows * (c.D / 32);
+  const int64_t n = (int64_t)rows * (c.D / 32);
 #pragma unroll 1
-  for (int p = thread; p < n >> 4; p += threads) *reinterpret_cast<uint4*>(d + (int64_t)p * 16) = load16(s + (int64_t)p * 16);
+  for (int64_t p = thread; p < n >> 4; p += threads) *reinterpret_cast<uint4*>(d + p * 16) = load16(s + p * 16);
 #pragma unroll 1
-  for (int p = (n >> 4 << 3) + thread; p < n >> 1; p += threads)
-    *reinterpret_cast<uint16_t*>(d + (int64_t)p * 2) = *reinterpret_cast<const uint16_t*>(s + (int64_t)p * 2);
+  for (int64_t p = (n >> 4 << 3) + thread; p < n >> 1; p += threads)
+    *reinterpret_cast<uint16_t*>(d + p * 2) = *reinterpret_cast<const uint16_t*>(s + p * 2);
 }
 
 constexpr int kForkEntries = 1024;  // table entries of a workgroup

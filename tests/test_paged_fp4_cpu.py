@@ -53,7 +53,8 @@ def test_reads_are_refused(dtype):
         assert lib.sl_paged_read(c, b, P, P, 0, 0, None) == status
     c, b, _ = (ctypes.byref(x) for x in records(dtype=dtype))
     for args, status in (((None, P, 0, 0), 1), ((P, None, 0, 0), 1), ((P + 8, P, 0, 0), 1), ((P, P + 4, 0, 0), 1), ((P, P, -8, 0), 1),
-                         ((P, P, 0, -8), 1), ((P, P, 0, 120), 1), ((P, P, 0, 130), 1), ((P, P, 4 * 128 + 2, 128), 1), ((P, P, 64, 512), 1),
+                         ((P, P, 0, -8), 1), ((P, P, 0, 120), 1), ((P, P, 0, 130), 1), ((P, P, 4 * 128 + 2, 128), 1), ((P, P, 64, 512), 1), ((P, P, 128, 128), 1),
+                         ((P, P, 39 * 128, 128), 1), ((P, P, 128, 3 * 128), 1),
                          ((P, P, 1 << 50, 0), 2), ((P, P, 0, 1 << 40), 2)):
         assert lib.sl_paged_read(c, b, *args, None) == status
     for kw in (dict(B=0, seqs=None, cu_rows=None), dict(rows=0)):
