@@ -29,22 +29,19 @@ __device__ __forceinline__ uint32_t fp4_scale(uint32_t top) {
 // bits of 2^(scale - 127) as the conversions take them
 __device__ __forceinline__ float fp4_power(uint32_t scale) { return __uint_as_float(scale << 23); }
 
-// N (4 or 8) codes from the low end of w on
-template <int N>
+// eight codes
 __device__ __forceinline__ void fp4_to_f32(uint32_t w, uint32_t scale, float* f) {
   const float by = fp4_power(scale);
   const fp4_f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, by, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, by, 1);
+  const fp4_f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, by, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, by, 3);
   f[0] = a[0];
   f[1] = a[1];
   f[2] = b[0];
   f[3] = b[1];
-  if constexpr (N == 8) {
-    const fp4_f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, by, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, by, 3);
-    f[4] = c[0];
-    f[5] = c[1];
-    f[6] = d[0];
-    f[7] = d[1];
-  }
+  f[4] = c[0];
+  f[5] = c[1];
+  f[6] = d[0];
+  f[7] = d[1];
 }
 
 // eight codes as 16 bytes of bf16
@@ -62,7 +59,7 @@ __device__ __forceinline__ void fp4_to_row8(uint32_t w, uint32_t scale, uint4* t
     to[0] = fp4_to_bf16(w, fp4_power(scale));
   } else {
     float f[8];
-    fp4_to_f32<8>(w, scale, f);
+    fp4_to_f32(w, scale, f);
     to[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
     to[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
   }

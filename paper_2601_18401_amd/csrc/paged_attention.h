@@ -123,7 +123,9 @@ __device__ __forceinline__ int position_of(const PagedArgs& x, const Entry& e, i
 // row group with its own running maximum and sum.
 template <typename T, int D, bool FP4>
 struct RowState {
-  static constexpr int EPL = RowLayout<T, D>::EPL, LPR = RowLayout<T, D>::LPR, RPW = RowLayout<T, D>::RPW;
+  // (a lane of 16 bytes of fp32 values would read two bytes of codes: eight lanes a row instead, and two loads of them at once for four)
+  static constexpr int EPL = FP4 && sizeof(T) == 4 ? D / 8 : RowLayout<T, D>::EPL, LPR = D / EPL, RPW = 64 / LPR;
+  static constexpr int AT_ONCE = FP4 && sizeof(T) == 4 ? 2 : 4;
   typedef std::conditional_t<FP4, uint8_t, T> Held;
   float m, l, o[EPL];
   __device__ __forceinline__ void clear() {
@@ -141,14 +143,17 @@ struct RowState {
     __device__ __forceinline__ void unpack(float* f) const { Elem<T>::unpack(r, f); }
   };
   struct Codes {
-    uint32_t r = 0;
+    typedef uint32_t Words __attribute__((ext_vector_type(EPL < 8 ? 1 : EPL / 8)));
+    Words r = {};
     int scale = 0;
     __device__ __forceinline__ void load(const PageCache& c, const uint8_t* page, int row, int lr) {
-      const uint8_t* const at = page + (int64_t)row * (D / 2) + lr * (EPL / 2);
-      r = EPL == 8 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
+      r = *reinterpret_cast<const Words*>(page + (int64_t)row * (D / 2) + lr * (EPL / 2));
       scale = page[(int64_t)c.ps * (D / 2) + (int64_t)row * (D / 32) + lr * EPL / 32];
     }
-    __device__ __forceinline__ void unpack(float* f) const { fp4_to_f32<EPL>(r, scale, f); }
+    __device__ __forceinline__ void unpack(float* f) const {
+#pragma unroll
+      for (int i = 0; i < EPL / 8; ++i) fp4_to_f32(r[i], scale, f + 8 * i);
+    }
   };
   typedef std::conditional_t<FP4, Codes, Sixteen> Piece;
   __device__ __forceinline__ void scale_to(float to) {
@@ -157,6 +162,11 @@ struct RowState {
 #pragma unroll
     for (int e = 0; e < EPL; ++e) o[e] *= f;
     m = to;
+  }
+  __device__ __forceinline__ static void load_query(const T* row, int lr, float (&q)[EPL]) {
+    constexpr int PER = Elem<T>::EPL;
+#pragma unroll
+    for (int i = 0; i < EPL / PER; ++i) Elem<T>::unpack(load16(row + lr * EPL + i * PER), q + i * PER);
   }
   // tokens [t0, t1) of the sequence whose table is given
   template <int U>
@@ -251,18 +261,18 @@ __device__ __forceinline__ void take_piece(const PagedArgs& x, int s, int rh, co
   typedef typename RS::Held Held;
   const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
   const int h = rh / x.b.rows, row = rh - h * x.b.rows;
-  constexpr int RUN = 4 * RS::RPW;
+  constexpr int RUN = RS::AT_ONCE * RS::RPW;
   const int run = ((r.t1 - r.t0 + WAVES - 1) / WAVES + RUN - 1) / RUN * RUN;
   const int t0 = r.t0 + wave * run, t1 = min(t0 + run, r.t1);
   RS st;
   st.clear();
   if (t0 < t1) {
     float q[RS::EPL];
-    Elem<T>::unpack(load16(static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst + lane % RS::LPR * RS::EPL), q);
+    RS::load_query(static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst, lane % RS::LPR, q);
 #pragma unroll
     for (int e = 0; e < RS::EPL; ++e) q[e] *= x.scale_log2e;
     const int64_t base = x.b.layer * x.c.layer + h / x.a.G * x.c.head;
-    st.template attend<4>(x.c, static_cast<const Held*>(x.c.K) + base, static_cast<const Held*>(x.c.V) + base,
+    st.template attend<RS::AT_ONCE>(x.c, static_cast<const Held*>(x.c.K) + base, static_cast<const Held*>(x.c.V) + base,
                           x.c.tables + (int64_t)s * x.c.max_pages, q, t0, t1, lane);
     st.join_groups();
   }
@@ -346,14 +356,14 @@ template <typename T, int D, bool FP4>
 __global__ __launch_bounds__(256) void whole_rows_kernel(const PagedArgs x) {
   using RS = RowState<T, D, FP4>;
   typedef typename RS::Held Held;
-  constexpr int RUN = 4 * RS::RPW;
+  constexpr int RUN = RS::AT_ONCE * RS::RPW;
   __shared__ float s_o[4][D], s_ml[4][2];
   if (workgroup() >= (int64_t)x.a.Hq * x.b.rows) return;
   const int rh = (int)workgroup(), lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane % RS::LPR;
   const int h = rh / x.b.rows, row = rh - h * x.b.rows;
   // asked for at once: the query, the slots and their scores, the row's entry
   float q[RS::EPL];
-  Elem<T>::unpack(load16(static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst + lr * RS::EPL), q);
+  RS::load_query(static_cast<const T*>(x.Q) + h * x.a.qsh + row * x.a.qst, lr, q);
   const int64_t at_slots = h * x.a.ish + row * x.a.ist;
   int slot = lane < x.a.topk ? x.idx[at_slots + lane] : -1;
   float score = x.a.combined && lane < x.a.topk ? x.scores[at_slots + lane] : -INFINITY;
@@ -370,13 +380,13 @@ __global__ __launch_bounds__(256) void whole_rows_kernel(const PagedArgs x) {
   st.clear();
   auto spans = [&](int k) {  // slot k's span, by this wavefront
     const int j = __builtin_amdgcn_readlane(slot, k);
-    if (j >= 0) st.template attend<4>(x.c, K, V, table, q, j * x.a.S, (j + 1) * x.a.S, lane);
+    if (j >= 0) st.template attend<RS::AT_ONCE>(x.c, K, V, table, q, j * x.a.S, (j + 1) * x.a.S, lane);
   };
   if (!x.a.combined)
     for (int k = wave; k < x.a.topk; k += 4) spans(k);
   if (pos >= 0) {
     const int t0 = c * x.a.S, run = ((pos + 1 - t0 + 3) / 4 + RUN - 1) / RUN * RUN, from = t0 + wave * run;
-    st.template attend<4>(x.c, K, V, table, q, from, min(from + run, pos + 1), lane);
+    st.template attend<RS::AT_ONCE>(x.c, K, V, table, q, from, min(from + run, pos + 1), lane);
   }
   st.join_groups();
   // the wavefronts' states into one, in every wavefront
