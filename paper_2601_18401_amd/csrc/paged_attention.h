@@ -1220,10 +1220,10 @@ __global__ __launch_bounds__(64 * NW, NW == 1 || sizeof(T) == 4 ? 1 : 2) void ti
 // Measured (D = 128, 32:4 heads): 40 caches of up to 200000 tokens, eight spans of 512 each, 371 MB in 75 us = 4.9 TB/s, where a pure read reaches
 // 6.4; one token behind a million, sixteen spans of 1024, 76 MB in 20.5 us, of which 5 pass before a unit's first codes are asked for
 // and 2 are the launch.  A turn has 280 vector instructions, 128 of them conversions, in some 1700 cycles of a SIMD.  The matrix form of
-// bf16 tiles, values staged in LDS for 32 columns, took 56 us for the million; codes that come row after row and pass LDS on their way
-// to the lanes that multiply them, 81 us for 75: more LDS traffic, and no fewer bytes.
-// EASY: no 32 tokens that begin at a multiple of 32 lie in two pages.
-template <int D, int CB, bool EASY>
+// bf16 tiles, values staged in LDS for 32 columns, took 50 us for the million; codes that come row after row and pass LDS on their way
+// to the lanes that multiply them, 95 us for the 40 caches where this order took 86: more LDS traffic, and no fewer bytes.
+// RUN: no that many tokens that begin at a multiple of it lie in two pages: 32, 8 or 1.
+template <int D, int CB, int RUN>
 struct NarrowCodes {
   static constexpr int KK = D / 32, DB = D / 16, WORDS = D / 32;  // products of a token block; blocks of 16 channels; words of a lane's codes
   typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -1250,11 +1250,11 @@ struct NarrowCodes {
   }
   // page: of lane l, of token t0 + l; the block begins at t0 + first.  A token without a page gets what lies in page 0: its score is masked,
   // and `values_only` takes its V.  Where no 32 tokens lie in two pages their address is the wavefront's, and no vector instruction is spent on
-  // it: a turn has 280 without, and some 420 with each lane's own.
+  // it: a turn has 280 without, and some 420 with each lane's own (drafts over pages of 40 tokens 52.5 us, 51.3 with one address for a lane's two rows).
   __device__ __forceinline__ static void ask(Raw& raw, const PageCache& c, const uint8_t* K, const uint8_t* V, int page, int t0, int first,
                                              int lane) {
     const int part = lane >> 4;
-    if constexpr (EASY) {
+    if constexpr (RUN == 32) {
       const uint32_t p = __builtin_amdgcn_readlane(page, first), t = __builtin_amdgcn_readfirstlane(t0 + first);
       const uint32_t row = __builtin_amdgcn_readfirstlane(t - t / c.by_ps * c.ps);
       const int64_t at = uniform64((int64_t)(p < (uint32_t)c.n_pages ? p : 0) * c.page);
@@ -1270,16 +1270,21 @@ struct NarrowCodes {
       }
       return;
     }
+    int64_t codes, scales;
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
-      const int ahead = first + token_of(tb, lane);
-      const uint32_t p = __shfl(page, ahead, 64), t = (uint32_t)(t0 + ahead), row = t - t / c.by_ps * c.ps;
-      const int64_t at = (int64_t)(p < (uint32_t)c.n_pages ? p : 0) * c.page, codes = at + (int64_t)row * (D / 2) + part * (D / 8);
-      const int64_t scales = at + (int64_t)c.ps * (D / 2) + (int64_t)row * (D / 32);
-      read_words(K + codes, raw.k[tb]);
-      read_words(V + codes, raw.v[tb]);
-      raw.ks[tb] = read_scales(K + (scales & ~(int64_t)3));
-      raw.vs[tb] = read_scales(V + (scales & ~(int64_t)3));
+      if (RUN == 1 || tb == 0) {
+        const int ahead = first + token_of(tb, lane);
+        const uint32_t p = __shfl(page, ahead, 64), t = (uint32_t)(t0 + ahead), row = t - t / c.by_ps * c.ps;
+        const int64_t at = (int64_t)(p < (uint32_t)c.n_pages ? p : 0) * c.page;
+        codes = at + (int64_t)row * (D / 2) + part * (D / 8);
+        scales = at + (int64_t)c.ps * (D / 2) + (int64_t)row * (D / 32);
+      }
+      const int on = RUN == 1 ? 0 : tb * 4;  // (rows of the first block's page)
+      read_words(K + codes + on * (D / 2), raw.k[tb]);
+      read_words(V + codes + on * (D / 2), raw.v[tb]);
+      raw.ks[tb] = read_scales(K + (scales & ~(int64_t)3) + on * (D / 32));
+      raw.vs[tb] = read_scales(V + (scales & ~(int64_t)3) + on * (D / 32));
       raw.shift[tb] = 8 * (((int)scales & 3) + part * (D / 4) / 32);
     }
   }
@@ -1499,7 +1504,7 @@ struct NarrowCodes {
 // Workgroups of the window come first, as tile_kernel's; then, of the spans' pieces, one for every (row, head, group of slots, piece): it takes
 // the piece of each of its slots' spans, one after the other, with codes and pages of the next one asked for while one is attended.  Other
 // heads and rows of its columns may list the same span: the first one that does takes it for all.
-template <int D, int CB, bool EASY>
+template <int D, int CB, int RUN>
 __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedArgs x, const TilePlan plan) {
   constexpr int COLS = 16 * CB;
   extern __shared__ __align__(1024) char s_dynamic[];
@@ -1513,7 +1518,7 @@ __global__ __launch_bounds__(64, CB == 1 ? 3 : 2) void codes_kernel(const PagedA
   int mine = -1;      // lane k: span of slot k of the unit's own row, -1: none, or none of its slots
   uint32_t todo = 0;  // slots to come
   int page = -1, asked = -1;  // pages of the first turn, of slot `asked`
-  typedef NarrowCodes<D, CB, EASY> Codes;
+  typedef NarrowCodes<D, CB, RUN> Codes;
   Codes n;
   auto load_queries = [&](auto&& head_of, auto&& row_of) {
 #pragma unroll
@@ -2253,8 +2258,9 @@ bool launch_codes(const PagedArgs& x, TilePlan plan, hipStream_t st) {
   plan.by_window = fast_div(x.p.window);
   plan.by_routed = fast_div(x.p.routed);
   plan.by_groups = fast_div(std::max(plan.groups, 1));
-  if (x.c.ps % 32 == 0) codes_kernel<D, CB, true><<<grid_of(plan.units), 64, kBytes, st>>>(x, plan);
-  else codes_kernel<D, CB, false><<<grid_of(plan.units), 64, kBytes, st>>>(x, plan);
+  if (x.c.ps % 32 == 0) codes_kernel<D, CB, 32><<<grid_of(plan.units), 64, kBytes, st>>>(x, plan);
+  else if (x.c.ps % 8 == 0) codes_kernel<D, CB, 8><<<grid_of(plan.units), 64, kBytes, st>>>(x, plan);
+  else codes_kernel<D, CB, 1><<<grid_of(plan.units), 64, kBytes, st>>>(x, plan);
   return true;
 }
 template <typename T, int D, bool FP4>

@@ -10,7 +10,7 @@ namespace sl {
 namespace {
 
 // Rows of a workgroup: 64 hold 2 or 4 loads of a lane in flight.  Both kernels are bound by memory, at 4.9 (rounded, 99000 rows of 8 heads,
-// 128 channels, and read back: 920 MB in 187 us; with 32 rows 194, 256 216) and 4.2 TB/s (160000 rows of 8 heads read, 835 MB in 200 us; 32 rows
+// 128 channels, and read back: 920 MB in 187 us; with 32 rows 194, 256 216) and 4.2 TB/s (162000 rows of 8 heads read, 835 MB in 200 us; 32 rows
 // 218; with plain stores 240), where a large copy reaches 5.0.
 constexpr int kRows = 64;
 
