@@ -430,7 +430,7 @@ sl_status sl_paged_append(const sl_page_cache* c, const sl_paged_batch* b, const
 /* The batch's tokens as rows again: K, V [Hkv][rows][D] of the rows' type, element strides (stride_h, stride_t, 1), 0 = packed; a chunk
  * that is a whole sequence reads all of it.  Rows without a token, or whose token has no page, become zeros; rows of no entry are left as
  * they were.  What a cache in 4 bits hands back is what its codes stand for, exactly.  Any dtype.  No two rows may share elements: stride_h is
- * at least (rows - 1) * stride_t + D, or stride_t at least (Hkv - 1) * stride_h + D. */
+ * at least (rows - 1) * stride_t + D, or stride_t at least (Hkv - 1) * stride_h + D, and no row of K meets one of V. */
 sl_status sl_paged_read(const sl_page_cache* c, const sl_paged_batch* b, void* K, void* V, int64_t stride_h, int64_t stride_t,
                         void* hip_stream);
 

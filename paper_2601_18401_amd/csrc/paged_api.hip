@@ -1,6 +1,7 @@
 // C-ABI layer of the paged cache: argument validation on the host, then dispatch to the launchers.
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "paged.h"
 
@@ -119,6 +120,19 @@ sl_status rows_of(const sl_page_cache* pc, const sl_paged_batch* pb, const void*
   return *stride_t < c->D || *stride_t % epl || *stride_h % epl ? SL_ERR_INVALID_ARG : SL_OK;
 }
 
+// Whether some row [D] of K and some row of V share elements, byte strides sh >= 0 and st >= D * es.
+bool rows_meet(const void* K, const void* V, int64_t heads, int64_t rows, int64_t sh, int64_t st, int64_t row_bytes) {
+  const int64_t ahead = (int64_t)(reinterpret_cast<uintptr_t>(V) - reinterpret_cast<uintptr_t>(K));
+  const int64_t extent = (heads - 1) * sh + (rows - 1) * st + row_bytes;
+  if (ahead >= extent || ahead <= -extent) return false;
+  for (int64_t h = 1 - heads; h < heads; ++h) {
+    const int64_t left = ahead - h * sh;  // (heads that far apart: within less than a row of a multiple of st?)
+    for (int64_t t = left / st - 1; t <= left / st + 1; ++t)
+      if (t > -rows && t < rows && std::abs(left - t * st) < row_bytes) return true;
+  }
+  return false;
+}
+
 sl_status attention_entry(const sl_page_cache* pc, const sl_paged_batch* pb, const sl_paged_attention* pa, const void* Q,
                           const int32_t* idx, const float* scores, bool combined, void* O, float* LSE, void* ws, size_t ws_bytes,
                           void* stream) {
@@ -212,6 +226,8 @@ sl_status sl_paged_read(const sl_page_cache* pc, const sl_paged_batch* pb, void*
   // (heads first or tokens first: rows that share elements would be written by several)
   if (c.Hkv > 1 && stride_h < (b.rows - 1) * stride_t + c.D && (stride_h < c.D || (b.rows > 1 && stride_t < (c.Hkv - 1) * stride_h + c.D)))
     return SL_ERR_INVALID_ARG;
+  const int64_t es = c.dtype == SL_BF16 ? 2 : 4;
+  if (sl::rows_meet(K, V, c.Hkv, b.rows, c.Hkv > 1 ? stride_h * es : 0, stride_t * es, c.D * es)) return SL_ERR_INVALID_ARG;
   return sl::paged_read(c, b, K, V, stride_h, stride_t, static_cast<hipStream_t>(hip_stream));
 }
 

@@ -139,3 +139,17 @@ def test_the_plain_format():
     assert fp4.block_scale(row) == 255 and np.isnan(fp4.hold(row[None])).all()
     codes = np.arange(64, dtype=np.uint8).reshape(2, 32) % 16
     assert np.array_equal(fp4.unpack(fp4.pack(codes)), codes)
+
+
+@pytest.mark.parametrize("dtype", [B.SL_F32, B.SL_BF16, B.SL_MXFP4 + B.SL_F32, B.SL_MXFP4 + B.SL_BF16])
+def test_reads_into_rows_of_k_that_are_rows_of_v_are_refused(dtype):
+    """40 rows of 4 heads, 128 channels; V begins so many elements behind K, or before it."""
+    lib = B.load()
+    es = 2 if dtype % 16 == B.SL_BF16 else 4
+    c, b, _ = (ctypes.byref(x) for x in records(dtype=dtype))
+    for behind, sh, st in ((0, 0, 0), (120, 0, 0), (128, 0, 0), (4 * 40 * 128 - 8, 0, 0), (128, 40 * 256, 256 - 16), (8, 128, 4 * 128),
+                           (3 * 40 * 256 + 39 * 256, 0, 256), (40 * 128 + 8, 2 * 40 * 128, 128)):
+        meets = any(abs(behind - h * (sh or 40 * (st or 128)) - t * (st or 128)) < 128 for h in range(-3, 4) for t in range(-39, 40))
+        assert meets
+        for k, v in ((P, P + behind * es), (P + behind * es, P)):
+            assert lib.sl_paged_read(c, b, k, v, sh, st, None) == 1
