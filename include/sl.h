@@ -347,8 +347,10 @@ sl_status sl_anchor_attention_decode_batched(const sl_params* p, const sl_anchor
  * synchronises or records profile events.
  * A cache in 4 bits (dtype SL_MXFP4_*).  A row of D channels is D / 32 blocks of 32: codes of 4 bits (e2m1: bit 3 the sign, the others 0, 0.5,
  * 1, 1.5, 2, 3, 4 or 6) and a scale of 8 bits; a channel is its code's value times 2^(scale - 127), and a scale of 255 makes all of its
- * block NaN.  The part of a page that holds one head is SL_MXFP4_PAGE_BYTES(page_size, D) bytes: page_size rows of D / 2 bytes of codes
- * (channel 2 i in the low half of byte i), then page_size rows of D / 32 scales; what is left of the last 16 bytes is not used.  K and V are
+ * block NaN.  (Scales 0, 1, 253 and 254 come from no append, but from who fills pages otherwise: the first two give values below the normal
+ * range, too, exactly; of the others those from 2^128 on, codes 4 and 6, and with 254 also 2 and 3, are infinite.)  The part of a page
+ * that holds one head is SL_MXFP4_PAGE_BYTES(page_size, D) bytes: page_size rows of D / 2 bytes of codes (channel 2 i in the low half of
+ * byte i), then page_size rows of D / 32 scales; what is left of the last 16 bytes is not used.  K and V are
  * [layers][n_pages][Hkv] of such parts; the strides count bytes, are multiples of 16 and not below a part; kv_stride_t is 0 or D / 2.
  * sl_paged_append rounds: a block with the largest value x gets the smallest power of two that leaves x / 2^e below 7 (scale e + 127, kept
  * within 2 .. 252), and each value the code nearest to value / 2^e, half way the even one, at most 6.  A value that is not finite
@@ -429,8 +431,9 @@ sl_status sl_paged_append(const sl_page_cache* c, const sl_paged_batch* b, const
 
 /* The batch's tokens as rows again: K, V [Hkv][rows][D] of the rows' type, element strides (stride_h, stride_t, 1), 0 = packed; a chunk
  * that is a whole sequence reads all of it.  Rows without a token, or whose token has no page, become zeros; rows of no entry are left as
- * they were.  What a cache in 4 bits hands back is what its codes stand for, exactly.  Any dtype.  No two rows may share elements: stride_h is
- * at least (rows - 1) * stride_t + D, or stride_t at least (Hkv - 1) * stride_h + D, and no row of K meets one of V. */
+ * they were.  What a cache in 4 bits hands back is what its codes stand for, exactly (infinity for 2^128 and more).  Any dtype.  No two
+ * rows may share elements: stride_h is at least (rows - 1) * stride_t + D, or stride_t at least (Hkv - 1) * stride_h + D, and no row of K
+ * meets one of V. */
 sl_status sl_paged_read(const sl_page_cache* c, const sl_paged_batch* b, void* K, void* V, int64_t stride_h, int64_t stride_t,
                         void* hip_stream);
 

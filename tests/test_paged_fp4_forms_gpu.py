@@ -234,3 +234,28 @@ def test_more_tiles_of_windows_than_a_grid_dimension_takes(dtype, B_, Hkv, n):
     rows = torch.cat([torch.arange(e * n, (e + 1) * n, device=DEV) for e in few])
     want = whole.attention(some, [0, 1, 2, 3], [k * n for k in range(5)], Q[:, rows], None, None, 1000)
     check(some, want, O[:, rows], LSE[:, rows])
+
+
+@pytest.mark.parametrize("dtype,n,ps,Hq", [(BF16, 3, 32, 4), (BF16, 3, 27, 40), (BF16, 130, 32, 4), (BF16, 130, 27, 4), (F32, 3, 32, 4), (F32, 300, 27, 4),
+                                           (F32, 200, 16, 32)])
+@pytest.mark.parametrize("tensor", ["K", "V"])
+def test_infinite_blocks_where_some_rows_attend(tensor, dtype, n, ps, Hq):
+    """Scales 253 and 254, which no append writes: rows that attend such a token are not finite (in its 32 channels, or, of a key, all), and no
+    other is."""
+    g = torch.Generator(device=DEV).manual_seed(n)
+    L, S = 400, 50
+    cache, marked = (make_cache(torch.Generator(device=DEV).manual_seed(n), [L], ps, 2, 128, dtype) for _ in range(2))
+    for t, scale in ((L - 2, 253), (120, 254)):
+        page, at = int(cache.tables[0, t // ps]), ps * 64 + t % ps * 4 + 1
+        x = getattr(cache, tensor)[0, page]
+        x[:, t % ps * 64 + 16:t % ps * 64 + 32] = 0x77      # sixes
+        x[:, at] = scale
+        spoil(marked, tensor, 0, t)
+    Q = torch.randn((Hq, n, 128), generator=g, device=DEV).to(dtype)
+    idx = torch.tensor([[[0, 2], [0, 1]][(h + r) % 2] for h in range(Hq) for r in range(n)], dtype=torch.int32, device=DEV).view(Hq, n, 2)
+    scores = torch.randn(idx.shape, generator=g, device=DEV)
+    seqs, cu = i32([0]), i32([0, n])
+    for got, want in ((B.sl_paged_span_attention(cache, seqs, cu, Q, idx, S)[0], whole.attention(marked, [0], [0, n], Q, idx, None, S)),
+                      (B.sl_paged_span_attention_combined(cache, seqs, cu, Q, idx, scores, S), whole.attention(marked, [0], [0, n], Q, idx, scores, S)),
+                      (B.sl_paged_span_attention(cache, seqs, cu, Q, None, 4000)[0], whole.attention(marked, [0], [0, n], Q, None, None, 4000))):
+        check(cache, want, torch.where(torch.isfinite(got), got, torch.nan))

@@ -60,3 +60,24 @@ def test_rows_of_k_and_v_in_turn_from_4_bits(dtype):
             B.sl_paged_read(cache, i32([0]), i32([0, 100]), 100, out=out)
     torch.cuda.synchronize()
     assert torch.equal(turns, before)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_code_under_every_scale(dtype, D):
+    """A code's value times 2^(scale - 127) in rows of either type, below the normal range too; 2^128 and more, of scales that no append writes,
+    is infinite; scale 255: NaN."""
+    ps = 256
+    cache = B.PageCache.empty(1, ps, 1, D, n_seqs=1, max_pages=1, dtype=dtype, fp4=True)
+    cache.tables.zero_(), cache.refs.fill_(1), cache.lens.fill_(ps)
+    codes = torch.arange(D, device=DEV) % 16
+    for x in (cache.K, cache.V):
+        x[0, 0, 0, :ps * D // 2] = (codes[0::2] | codes[1::2] << 4).to(torch.uint8).repeat(ps)
+        x[0, 0, 0, ps * D // 2:] = torch.arange(ps, device=DEV).repeat_interleave(D // 32).to(torch.uint8)
+    want = whole.values(cache, "K")[0]
+    want = torch.where(want.abs() >= 2.0 ** 128, want.sign() * torch.inf, want)
+    for x in B.sl_paged_read(cache, i32([0]), i32([0, ps]), ps):
+        assert same(x, want)
+    Ks = torch.zeros((1, 1, ps, D), dtype=dtype, device=DEV)
+    B.sl_paged_span_keys(cache, i32([0]), i32([0, ps]), Ks, 1)
+    assert same(Ks[0], want)
