@@ -226,6 +226,7 @@ sl_status sl_paged_read(const sl_page_cache* pc, const sl_paged_batch* pb, void*
   // (heads first or tokens first: rows that share elements would be written by several)
   if (c.Hkv > 1 && stride_h < (b.rows - 1) * stride_t + c.D && (stride_h < c.D || (b.rows > 1 && stride_t < (c.Hkv - 1) * stride_h + c.D)))
     return SL_ERR_INVALID_ARG;
+  if (c.Hkv > 1 && stride_h > sl::kMaxExtent / c.Hkv) return SL_ERR_UNSUPPORTED;
   const int64_t es = c.dtype == SL_BF16 ? 2 : 4;
   if (sl::rows_meet(K, V, c.Hkv, b.rows, c.Hkv > 1 ? stride_h * es : 0, stride_t * es, c.D * es)) return SL_ERR_INVALID_ARG;
   return sl::paged_read(c, b, K, V, stride_h, stride_t, static_cast<hipStream_t>(hip_stream));

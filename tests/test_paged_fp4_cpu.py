@@ -153,3 +153,27 @@ def test_reads_into_rows_of_k_that_are_rows_of_v_are_refused(dtype):
         assert meets
         for k, v in ((P, P + behind * es), (P + behind * es, P)):
             assert lib.sl_paged_read(c, b, k, v, sh, st, None) == 1
+
+
+def test_limits_under_address_and_undefined_sanitizers(tmp_path):
+    """Validation, size arithmetic, and whether rows meet, of records at and beyond every limit, in a build of the host side with ASan + UBSan."""
+    import glob
+    import os
+    import shutil
+    import subprocess
+    from paper_2601_18401_amd import build as _build
+    clang = "/opt/rocm/lib/llvm/bin/clang"
+    if not os.path.exists(clang) or not shutil.which("hipcc"):
+        pytest.skip("no ROCm clang")
+    sources = _build.sources() + glob.glob(os.path.join(_build.CSRC, "*.h")) + [os.path.join(_build.ROOT, "include", "sl.h")]
+    built = os.path.exists(_build.SAN_LIB) and os.path.getmtime(_build.SAN_LIB) > max(os.path.getmtime(s) for s in sources)
+    lib = _build.SAN_LIB if built else _build.build(sanitize=True)
+    exe = str(tmp_path / "fp4_limits_from_c")
+    subprocess.run([clang, "-std=c99", "-Wall", "-Wextra", "-Werror", "-g", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=undefined", "-shared-libsan", "-I", os.path.join(_build.ROOT, "include"),
+                    os.path.join(_build.ROOT, "tests", "cabi", "fp4_limits_from_c.c"), "-o", exe, "-ldl"], check=True)
+    rt = os.path.dirname(glob.glob("/opt/rocm*/lib/llvm/lib/clang/*/lib/*/libclang_rt.asan*.so")[0])
+    env = dict(os.environ, LD_LIBRARY_PATH=rt, ASAN_OPTIONS="detect_leaks=0")
+    run = subprocess.run([exe, lib], capture_output=True, text=True, env=env, timeout=300)
+    assert run.returncode == 0 and "wrong=0" in run.stdout, (run.stdout, run.stderr[-3000:])
+    assert "runtime error" not in run.stderr and "AddressSanitizer" not in run.stderr, run.stderr[-3000:]
