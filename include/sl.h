@@ -424,7 +424,8 @@ size_t sl_pages_compact_workspace_bytes(const sl_page_cache* c);
 sl_status sl_pages_compact(const sl_page_cache* c, int32_t* map, void* ws, size_t ws_bytes, void* hip_stream);
 
 /* Writes the batch's new tokens into their pages (a sequence's tokens by one entry: of entries that
- * list it twice, which one's rows stay is unspecified), rounded to 4 bits where the cache holds those.  Entries that sl_pages_extend did not serve are to be -1 in seqs.  K, V: [Hkv][rows][D] with element strides
+ * list it twice, which one's values stay is unspecified, and codes of one may stay with scales of the other), rounded to 4 bits where the
+ * cache holds those.  Entries that sl_pages_extend did not serve are to be -1 in seqs.  K, V: [Hkv][rows][D] with element strides
  * (stride_h, stride_t, 1), 0 = packed. */
 sl_status sl_paged_append(const sl_page_cache* c, const sl_paged_batch* b, const void* K, const void* V,
                           int64_t stride_h, int64_t stride_t, void* hip_stream);

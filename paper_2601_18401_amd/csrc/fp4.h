@@ -3,7 +3,7 @@
 //
 // A block whose largest value is x has the smallest power of two that leaves x / 2^e below 7, which rounds to 6 at most: floor(log2 x) - 2,
 // and one more from 1.75 * 2^floor(log2 x) on.  Division by 2^e is exact, so that a code is the value's one rounding, half way to even: off
-// by half a step of e2m1 at most, 1/4 of the block's smallest step up to 1 of its largest (x in (6, 7)).  Scales stay in
+// by half a step of e2m1, which is 2^e / 4 for values below 2 * 2^e, 2^e / 2 up to 4 * 2^e, and 2^e from there to 7 * 2^e.  Scales stay in
 // 2 .. 252, where every value that they give is a normal number of bf16 and fp32: smaller blocks lose what lies below 2^-127, and the last
 // eighth below 2^128 becomes 6 * 2^125.
 #pragma once

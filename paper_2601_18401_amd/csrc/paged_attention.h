@@ -1250,7 +1250,8 @@ struct NarrowCodes {
   }
   // page: of lane l, of token t0 + l; the block begins at t0 + first.  A token without a page gets what lies in page 0: its score is masked,
   // and `values_only` takes its V.  Where no 32 tokens lie in two pages their address is the wavefront's, and no vector instruction is spent on
-  // it: a turn has 280 without, and some 420 with each lane's own (drafts over pages of 40 tokens 52.5 us, 51.3 with one address for a lane's two rows).
+  // it: a turn has 281 without, 313 with one address for a lane's two rows (RUN 8) and 355 with one for each (D = 128, 16 columns; drafts over
+  // pages of 40 tokens 51.3 us with one address, 52.5 with two).
   __device__ __forceinline__ static void ask(Raw& raw, const PageCache& c, const uint8_t* K, const uint8_t* V, int page, int t0, int first,
                                              int lane) {
     const int part = lane >> 4;
@@ -2136,6 +2137,9 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
   // without: bf16, 2.2 items a bucket 56 and 51, 4.4 65 and 91, 17 77 and 321; fp32, where a tile costs as much as 128 items however
   // few it has, 4.4 222 and 159, 8.7 228 and 312, 17 234 and 633.
   // (fp32 calls below 2^19 keys: 250 rows of 4 heads, top-4 of spans of 64, 33 and 25)
+  // Caches in 4 bits go by the same number, although codes_kernel takes half as long as the tiles of 32 columns that it was measured against:
+  // the two meet at eight items.  us, 32:4 heads, top-8 behind 64K, buckets and without: spans of 128, 2 items 67 and 35, 4 77 and 53, 8 88
+  // and 86, 16 89 and 151; of 512, 4 71 and 38, 8 74 and 60, 16 81 and 103; of 64, 4 82 and 67, 8 89 and 115.
   f.buckets = a.topk > 0 && (c.dtype == SL_BF16 ? items >= 3 * buckets : items >= 6 * buckets && items * a.S >= 1 << 19);
   // fp32: row by row where tiles of 128 columns would be all but empty.
   f.tiles = c.dtype == SL_BF16 || f.buckets || (a.topk == 0 && columns > 32 * (int64_t)b.B);
@@ -2160,7 +2164,10 @@ Form form_of(const PageCache& c, const PagedBatch& b, const PagedAttention& a) {
     if (n > div_up(tokens, 64)) n = div_up(tokens, 64);
     return n < 1 ? 1 : n;
   };
-  const int64_t resident = 256 * (cols == 16 ? (c.D == 64 ? 16 : 12) : c.D == 64 ? 12 : 8);  // workgroups of codes_kernel
+  // Workgroups of codes_kernel that the chip holds, by a lane's registers: at D = 64 up to 120 and 166 (16 and 32 columns), at 128 up to 168
+  // and 241.  At D = 64 on pages of no multiple of eight tokens it has 130 and 171, and 12 and 8 fit a compute unit: with those numbers dense
+  // drafts of 12 sequences take 40 us for 43.5, and drafts of 40 sequences with spans of 300 tokens 127 for 97.
+  const int64_t resident = 256 * (cols == 16 ? (c.D == 64 ? 16 : 12) : c.D == 64 ? 12 : 8);
   int64_t share = 0;
   Pieces& p = f.p;
   f.plan.slots = 1;
