@@ -177,3 +177,10 @@ def test_limits_under_address_and_undefined_sanitizers(tmp_path):
     run = subprocess.run([exe, lib], capture_output=True, text=True, env=env, timeout=300)
     assert run.returncode == 0 and "wrong=0" in run.stdout, (run.stdout, run.stderr[-3000:])
     assert "runtime error" not in run.stderr and "AddressSanitizer" not in run.stderr, run.stderr[-3000:]
+
+
+def test_reads_into_heads_beyond_what_64_bits_address_are_refused():
+    c, b, _ = (ctypes.byref(x) for x in records(**GOOD, rows=1 << 25))
+    assert B.load().sl_paged_read(c, b, P, P, 0, 1 << 32, None) == 2
+    c, b, _ = (ctypes.byref(x) for x in records(**GOOD, rows=1 << 25, Hkv=1024))
+    assert B.load().sl_paged_read(c, b, P, P, 0, 1 << 25, None) == 2

@@ -139,8 +139,7 @@ def test_records_beyond_the_caches(dtype, n, D, ps, S, L, width):
 
 
 # ---- few columns
-@pytest.mark.parametrize("ps", [64, 32, 40, 8, 20, 7])
-@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("D,ps", [(64, 64), (128, 32), (64, 8), (128, 40), (64, 20), (128, 7)])
 @pytest.mark.parametrize("Hq,Hkv,ns", [
     (8, 2, [1, 1, 1]), (3, 1, [1, 5, 4]), (15, 3, [2, 3, 0]), (16, 1, [1, 1, 1]),      # up to 16 columns
     (24, 1, [1, 1, 1]), (9, 3, [10, 7, 9]), (64, 2, [1, 1, 0]), (20, 4, [6, 5, 6]),    # up to 32
