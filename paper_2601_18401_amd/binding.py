@@ -767,8 +767,8 @@ def sl_paged_append(cache: PageCache, seqs, cu_rows, K, V, layer=0):
 
 def sl_paged_read(cache: PageCache, seqs, cu_rows, rows, layer=0, out=None):
     """The batch's tokens as rows again: K, V [Hkv, rows, D] of the cache's dtype, from a cache in 4 bits what its codes stand for.  rows:
-    how many rows the tensors have (cu_rows ends at it, or before).  Rows without a token or a page become zeros, rows of no entry
-    stay as they were (with out) or undefined."""
+    how many rows the tensors have (cu_rows ends at it, or before); out: two such tensors, no row of which meets another.  Rows
+    without a token or a page become zeros, rows of no entry stay as they were (with out) or undefined."""
     if out is None:
         out = tuple(torch.empty((cache.Hkv, rows, cache.D), dtype=cache.dtype, device=cache.device) for _ in range(2))
     K, V = out
